@@ -327,6 +327,66 @@ ROM_API int rom_mamba2_layer_forward(const rom_config *cfg, int32_t headdim, con
                              void *out, int32_t *topk_idx_out, float *gates_out, int32_t *counts_out,
                              void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------------------
+ * Serving: prompts and generated tokens of many sequences in one call.  Every live sequence has a slot in pools that the caller
+ * owns: conv windows [n_slots, d_conv-1, d_inner] fp32 (oldest first) and scan states [n_slots, d_inner, d_state] fp32, the
+ * layouts that rom_layer_step carries.  The recurrence and the short conv are those of Section 3.1; a prompt run by the ragged calls and
+ * continued token by token gives what one call over the whole sequence gives, up to the rounding of the storage dtype.
+ * Pools: a call reads the slots it names in the *_in pool and writes them in the *_out pool; the two may be one buffer (updated
+ * in place) or two that do not overlap.  Slots that no sequence names are not touched.  Two sequences of a call must not name the same
+ * slot: nothing is read or written out of bounds if they do, but what both yield is unspecified.  Pools, activations and weights are
+ * 16-byte aligned; seq_start, slot, resume, Bm, Cm, D and b_conv need the alignment of their elements.  Rows of activations may lie ld
+ * elements apart (ldx, ldz: at least d_inner, a multiple of 16 bytes; ld_bc: at least d_state). */
+typedef struct {               /* sequences packed one behind the other in buffers of `rows` rows */
+  int32_t n_seq;               /* sequences (0: nothing is done), at most 2^20                                    */
+  int32_t rows;                /* rows of the packed buffers                                                      */
+  int32_t n_slots;             /* states in each pool                                                             */
+  const int32_t *seq_start;    /* device [n_seq+1], ascending: sequence i is rows [seq_start[i], seq_start[i+1]), none of them when the two
+                                  are equal.  Outputs of the rows before the first and behind the last sequence are left as they are (their inputs
+                                  may hold anything).  Offsets are cut to [0, rows]; what descending ones yield is unspecified, but in bounds.  */
+  const int32_t *slot;         /* device [n_seq] or NULL (sequence i has slot i).  Outside [0, n_slots): the sequence starts
+                                  from zeros and its state is not kept                                            */
+  const int32_t *resume;       /* device [n_seq] or NULL.  0 (NULL: all): the sequence starts from zeros; else from its slot */
+} rom_ragged;
+
+/* Causal depthwise conv + SiLU over packed sequences: y_t = SiLU(b_conv + sum_j w_conv[j] x_{t-(d_conv-1)+j}), the rows before a sequence's first
+ * one taken from its window (or zeros); afterwards the slot holds the sequence's last d_conv-1 rows.
+ *   x : [rows, d_inner] dtype, pitch ldx;  w_conv : [d_conv, d_inner] dtype, tap d_conv-1 = current row;  b_conv : [d_inner] fp32 or NULL;
+ *   win_in (NULL: every sequence starts from zeros), win_out (NULL: not kept);  y : [rows, d_inner] dtype, contiguous, not x.
+ * Uses cfg->d_inner, d_conv, dtype (B and L are not used).                                                        */
+ROM_API int rom_conv_ragged(const rom_config *cfg, const rom_ragged *seqs, const void *x, int64_t ldx, const void *w_conv,
+                    const float *b_conv, const float *win_in, float *win_out, void *y, void *stream);
+
+/* Selective scan over packed sequences: rom_scan's recurrence, skip and gate for each of them, states in slots.
+ *   u, y : [rows, d_inner] dtype, contiguous;  delta : [rows, d_inner] fp32, contiguous;  Bm, Cm : [rows, d_state] fp32, pitch ld_bc;
+ *   A, D as in rom_scan;  z : [rows, d_inner] dtype, pitch ldz, or NULL (no gate);
+ *   h_in (NULL: every sequence starts from zeros), h_out (NULL: not kept).  y is none of the inputs.
+ *   ws : rom_scan_ragged_workspace_size(cfg, n_seq, rows) bytes (host out); scratch of this call alone: overlapping calls, captured graphs
+ *        that may run at the same time among them, need one each.
+ * State and arithmetic are fp32.  Uses cfg->d_inner, d_state, dtype, disc_mode (B and L are not used).             */
+ROM_API int rom_scan_ragged_workspace_size(const rom_config *cfg, int32_t n_seq, int32_t rows, size_t *bytes);
+ROM_API int rom_scan_ragged(const rom_config *cfg, const rom_ragged *seqs, const void *u, const float *delta, const float *A,
+                    const float *Bm, const float *Cm, int64_t ld_bc, const float *D, const void *z, int64_t ldz, const float *h_in,
+                    float *h_out, void *y, void *ws, size_t ws_bytes, void *stream);
+
+/* The same for one token of cfg->B sequences (cfg->L must be 1): row b continues the sequence of slot[b] (NULL: slot b).  A row whose slot
+ * is outside [0, n_slots) is padding: its output and all slots are left as they are.  Both pools are required.     */
+ROM_API int rom_conv_step(const rom_config *cfg, const void *x, int64_t ldx, const void *w_conv, const float *b_conv, const int32_t *slot,
+                  int32_t n_slots, const float *win_in, float *win_out, void *y, void *stream);
+ROM_API int rom_scan_step(const rom_config *cfg, const void *u, const float *delta, const float *A, const float *Bm, const float *Cm,
+                  int64_t ld_bc, const float *D, const void *z, int64_t ldz, const int32_t *slot, int32_t n_slots, const float *h_in,
+                  float *h_out, void *y, void *stream);
+
+/* rom_ffn_moe_forward for the few tokens of a generation step (B*L <= 64): same equation, inputs and layouts, in two launches that read
+ * each chosen expert's weights once.  An expert index outside [0, E) contributes nothing; negative ones are the padding of a fixed
+ * batch (a token with none but those gets a row of zeros), others are reported by rom_get_status as ROM_ERR_INVALID_ARG.  An expert that a
+ * token names twice counts twice.
+ *   ws : rom_ffn_moe_step_workspace_size(cfg, d_ff) bytes (host out); overlapping calls need one each.
+ * Uses cfg->B, L, d_model, E, K, dtype (flags must be 0).                                                          */
+ROM_API int rom_ffn_moe_step_workspace_size(const rom_config *cfg, int32_t d_ff, size_t *bytes);
+ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_gu, const void *W_down, const void *x,
+                     const int32_t *topk_idx, const float *gates, void *out, void *ws, size_t ws_bytes, void *stream);
+
 /* Profiling aid: the same launch sequence as rom_layer_forward with a CUDA event recorded on
  * `stream` between stages; synchronises the stream and writes the device time of each stage in
  * milliseconds to stage_ms (host out, at least rom_num_stages() floats).  Stage i is named

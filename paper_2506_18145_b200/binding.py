@@ -27,7 +27,9 @@ EXPORTS = ("rom_workspace_size", "rom_route", "rom_scan", "rom_layer_forward", "
            "rom_num_stages", "rom_stage_name", "rom_route_noalloc", "rom_route_balance",
            "rom_ffn_moe_workspace_size", "rom_ffn_moe_forward", "rom_layer_step", "rom_layer_forward_host",
            "rom_scan_workspace_size", "rom_debug_check", "rom_scan_backward_workspace_size", "rom_scan_backward",
-           "rom_layer_backward_workspace_size", "rom_layer_backward", "rom_mamba2_workspace_size", "rom_mamba2_layer_forward")
+           "rom_layer_backward_workspace_size", "rom_layer_backward", "rom_mamba2_workspace_size", "rom_mamba2_layer_forward",
+           "rom_conv_ragged", "rom_scan_ragged_workspace_size", "rom_scan_ragged", "rom_conv_step", "rom_scan_step",
+           "rom_ffn_moe_step_workspace_size", "rom_ffn_moe_step")
 
 
 class RomConfig(ctypes.Structure):
@@ -49,6 +51,10 @@ class RomGrads(ctypes.Structure):
 class RomMamba2Weights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("W_r", "b_r", "W_in", "w_conv", "b_conv", "dt_bias", "A", "D", "w_norm", "W_out")]
+
+
+class RomRagged(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "rows", "n_slots")] + [(n, ctypes.c_void_p) for n in ("seq_start", "slot", "resume")]
 
 
 class RomError(RuntimeError):
@@ -95,6 +101,14 @@ def lib() -> ctypes.CDLL:
         L.rom_last_launch_count.argtypes = []
         L.rom_layer_forward_profile.argtypes = [cfgp, ctypes.POINTER(RomWeights), vp, vp, vp, ctypes.c_size_t, vp,
                                                 ctypes.POINTER(ctypes.c_float), ctypes.c_int]
+        i32, i64, ragp = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(RomRagged)
+        L.rom_conv_ragged.argtypes = [cfgp, ragp, vp, i64, vp, vp, vp, vp, vp, vp]
+        L.rom_scan_ragged_workspace_size.argtypes = [cfgp, i32, i32, szp]
+        L.rom_scan_ragged.argtypes = [cfgp, ragp, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.rom_conv_step.argtypes = [cfgp, vp, i64, vp, vp, vp, i32, vp, vp, vp, vp]
+        L.rom_scan_step.argtypes = [cfgp, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, i32, vp, vp, vp, vp]
+        L.rom_ffn_moe_step_workspace_size.argtypes = [cfgp, i32, szp]
+        L.rom_ffn_moe_step.argtypes = [cfgp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.rom_num_stages.argtypes = []
         L.rom_stage_name.argtypes = [ctypes.c_int]
         L.rom_stage_name.restype = ctypes.c_char_p
@@ -298,6 +312,104 @@ def rom_layer_step(cfg, weights: RomWeights, x, conv_state, ssm_state, out, topk
                               _ptr(topk_idx_out), _ptr(gates_out), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_layer_step")
+    return rc
+
+
+def _rows_ptr(t: Optional[torch.Tensor]):
+    """(address, elements between rows) of a [rows, width] tensor whose rows are contiguous; a column slice of wider rows is one."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if t.dim() != 2 or t.stride(1) != 1:
+        raise ValueError("expected a tensor [rows, width] with contiguous rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]      # (a single row has no pitch: torch may say anything)
+
+
+def _pool(*pools: Optional[torch.Tensor]) -> int:
+    """Slots of the state pools of a call."""
+    n = {p.shape[0] for p in pools if p is not None}
+    if len(n) > 1:
+        raise ValueError("the pools differ in their slots")
+    return n.pop() if n else 0
+
+
+def make_ragged(rows: int, n_slots: int, seq_start, slot=None, resume=None) -> RomRagged:
+    """Sequences packed in buffers of `rows` rows.  The tensors (int32, on the device) must outlive the calls that take the result."""
+    n_seq = seq_start.numel() - 1
+    for t, n in ((seq_start, n_seq + 1), (slot, n_seq), (resume, n_seq)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() != n):
+            raise ValueError("expected int32 tensors: n_seq + 1 offsets, n_seq slots, n_seq flags")
+    return RomRagged(n_seq, rows, n_slots, _ptr(seq_start), _ptr(slot), _ptr(resume))
+
+
+def rom_conv_ragged(cfg, seqs: RomRagged, x, w_conv, b_conv, win_in, win_out, y, stream=None, check=True) -> int:
+    """x: [rows, d_inner], rows may be a column slice of wider ones."""
+    px, ldx = _rows_ptr(x)
+    rc = lib().rom_conv_ragged(ctypes.byref(cfg), ctypes.byref(seqs), px, ldx, _ptr(w_conv), _ptr(b_conv), _ptr(win_in), _ptr(win_out),
+                               _ptr(y), _stream(stream))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_conv_ragged")
+    return rc
+
+
+def scan_ragged_workspace_size(cfg: RomConfig, n_seq: int, rows: int) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().rom_scan_ragged_workspace_size(ctypes.byref(cfg), int(n_seq), int(rows), ctypes.byref(n))
+    if rc != ROM_OK:
+        raise RomError(rc, "rom_scan_ragged_workspace_size")
+    return int(n.value)
+
+
+def _bc(Bm, Cm):
+    """Addresses of B and C and their common pitch."""
+    (pb, ldb), (pc, ldc) = _rows_ptr(Bm), _rows_ptr(Cm)
+    if ldb != ldc:
+        raise ValueError("Bm and Cm differ in their pitch")
+    return pb, pc, ldb
+
+
+def rom_scan_ragged(cfg, seqs: RomRagged, u, delta, A, Bm, Cm, D, z, h_in, h_out, y, ws, stream=None, check=True) -> int:
+    """Bm, Cm: [rows, d_state] of one pitch; z: [rows, d_inner]; both may be column slices of wider rows."""
+    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm), _rows_ptr(z)
+    rc = lib().rom_scan_ragged(ctypes.byref(cfg), ctypes.byref(seqs), _ptr(u), _ptr(delta), _ptr(A), pb, pc, ld, _ptr(D), pz, ldz, _ptr(h_in),
+                               _ptr(h_out), _ptr(y), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_scan_ragged")
+    return rc
+
+
+def rom_conv_step(cfg, x, w_conv, b_conv, slot, win_in, win_out, y, stream=None, check=True) -> int:
+    px, ldx = _rows_ptr(x)
+    rc = lib().rom_conv_step(ctypes.byref(cfg), px, ldx, _ptr(w_conv), _ptr(b_conv), _ptr(slot), _pool(win_in, win_out), _ptr(win_in),
+                             _ptr(win_out), _ptr(y), _stream(stream))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_conv_step")
+    return rc
+
+
+def rom_scan_step(cfg, u, delta, A, Bm, Cm, D, z, slot, h_in, h_out, y, stream=None, check=True) -> int:
+    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm), _rows_ptr(z)
+    rc = lib().rom_scan_step(ctypes.byref(cfg), _ptr(u), _ptr(delta), _ptr(A), pb, pc, ld, _ptr(D), pz, ldz, _ptr(slot), _pool(h_in, h_out),
+                             _ptr(h_in), _ptr(h_out), _ptr(y), _stream(stream))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_scan_step")
+    return rc
+
+
+def ffn_moe_step_workspace_size(cfg: RomConfig, d_ff: int) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().rom_ffn_moe_step_workspace_size(ctypes.byref(cfg), int(d_ff), ctypes.byref(n))
+    if rc != ROM_OK:
+        raise RomError(rc, "rom_ffn_moe_step_workspace_size")
+    return int(n.value)
+
+
+def rom_ffn_moe_step(cfg, d_ff, W_gu, W_down, x, topk_idx, gates, out, ws, stream=None, check=True) -> int:
+    rc = lib().rom_ffn_moe_step(ctypes.byref(cfg), int(d_ff), _ptr(W_gu), _ptr(W_down), _ptr(x), _ptr(topk_idx), _ptr(gates), _ptr(out),
+                                _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_ffn_moe_step")
     return rc
 
 
