@@ -1,64 +1,400 @@
 // Selective scan over packed sequences (rom_scan_ragged): h_t = exp(Delta A) h_{t-1} + B-bar u_t, y_t = (C_t h_t + D u_t) SiLU(z_t), each sequence
 // from its slot's state or from zeros.
 //
-// One warp per sequence and 8 channels, four lanes a channel with four states each, row by row.
+// The packed rows are cut into chunks of equal length whatever sequences they hold, so that the work is even for any lengths and the
+// host needs to know none of them.  A sequence that reaches over a chunk's end needs its state there: a first launch runs the last sequence of every
+// such chunk alone, states only (h_end from the sequence's own start, or from zeros and then with the sum of Delta); in the second, which
+// computes the outputs, a chunk that begins inside a sequence chains those: h <- exp(A sum Delta) h + h_end (exact: the recurrence is
+// linear in h).  A sequence inside one chunk is walked once.  The first launch also sets aside the initial state of a sequence that
+// reaches on, because the chunk with its end may write the slot (in place) before the chunk with its start has read it.
+//
+// A warp owns 32 channels of one chunk, a lane 4 states of 4 adjacent channels in packed pairs along the channels (the layout of
+// rom_scan_warp.cu, where the reasons stand): up to eight rows are staged in shared memory while the next are in registers.  A tile ends where a
+// sequence ends, so that states change hands between tiles only; the next sequence's initial state is copied to shared memory while the
+// present one runs.
+//
+// bf16: what bounds it is one exponential per state update on the special-function unit, then the fp32 pipe.  fp32: decay() keeps fp32
+// accuracy, about ten operations more an update.
 #include "rom_serve.cuh"
 
 namespace rom {
 namespace {
 
+constexpr int RR = 8;             // rows per tile
+constexpr int RWARPS = 4;         // warps per block
+
 struct RaggedScan {
   Ragged s;
   const void* u; const float* delta; const float* A; const float* Bm; const float* Cm; long long ldb; const float* D;
   const void* z; long long ldz; const float* h_in; float* h_out; void* y; int De;
+  int Lc, nch;                    // rows per chunk, chunks
+  int bc16;                       // rows of B and C on 16-byte boundaries
+  float* h_end;                   // [nch, De, 16]: state at the end of a chunk that a sequence reaches over
+  float* h_start;                 // [nch, De, 16]: initial state of the sequence that starts in the chunk and reaches on
+  float* sum_delta;               // [nch, De]
 };
 
-template <typename T, bool ZOH>
-__global__ void __launch_bounds__(128)
-scan_ragged_rows(const RaggedScan p) {
-  pdl_sync();
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int c = blockIdx.x * 32 + (threadIdx.x >> 5) * 8 + g, De = p.De;
-  const T* u = static_cast<const T*>(p.u);
-  const T* z = static_cast<const T*>(p.z);
-  const float4 a4 = __ldg(reinterpret_cast<const float4*>(p.A + (size_t)c * 16) + t);
-  const float av[4] = {a4.x, a4.y, a4.z, a4.w}, Dc = p.D ? __ldg(p.D + c) : 0.0f;
-  for (int i = blockIdx.y; i < p.s.n_seq; i += gridDim.y) {
-    const int first = p.s.start_of(i), end = p.s.end_of(i), slot = p.s.slot_of(i);
-    const size_t at = ((size_t)max(slot, 0) * De + c) * 16 + 4 * t;
-    float4 h4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (p.h_in && slot >= 0 && p.s.resumes(i)) h4 = *reinterpret_cast<const float4*>(p.h_in + at);
-    float h[4] = {h4.x, h4.y, h4.z, h4.w};
-    for (int r = first; r < end; ++r) {
-      const size_t o = (size_t)r * De + c;
-      const float dl = __ldg(p.delta + o), uu = to_f32(u[o]);
-      const float4 b4 = load4_any(p.Bm + (size_t)r * p.ldb + 4 * t), c4 = load4_any(p.Cm + (size_t)r * p.ldb + 4 * t);
-      const float bb[4] = {b4.x, b4.y, b4.z, b4.w}, cc[4] = {c4.x, c4.y, c4.z, c4.w};
-      float y = 0.0f;
+struct RaggedTile {
+  float4 dl[RR][8], u[RR][8];     // Delta, u (times Delta without zero-order hold) of 4 channels; group g of row r sits at g ^ r
+  float4 b[RR][4], c[RR][4];
+  float D[32];
+  float4 y[RR][32];               // partial sums of 4 channels over one lane's states
+  float4 h0[4][32];               // the next sequence's initial state: channel i of the lane
+};
+
+__device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
+// Slot of lane l's partial sums of row r: conflict-free for a quarter-warp of writers (eight lanes, one row) and of readers (lanes 8 g + const, two rows).
+__device__ __forceinline__ int y_slot(int l, int r) { return l ^ (2 * (l >> 3) + (r & 1)); }
+
+// Sequences base .. base+31 by lane: first row (the end of the last one behind it), slot to read (-1: zeros), slot to write (-1: none).
+struct SeqWindow {
+  int base, start, in, out;
+  __device__ __forceinline__ void load(const RaggedScan& p, int from) {
+    base = from;
+    const int i = from + (threadIdx.x & 31), n = p.s.n_seq;
+    start = i <= n ? p.s.start_of(i) : p.s.rows;
+    const int sl = i < n ? p.s.slot_of(i) : -1;
+    in = sl >= 0 && p.h_in && p.s.resumes(i) ? sl : -1;
+    out = p.h_out ? sl : -1;
+  }
+  // the window holds sequences i and i + 1 (all lanes call it alike)
+  __device__ __forceinline__ void reach(const RaggedScan& p, int i) { if (i - base >= 31) load(p, i); }
+  __device__ __forceinline__ int start_of(int i) const { return __shfl_sync(0xffffffffu, start, i - base); }
+  __device__ __forceinline__ int end_of(int i) const { return __shfl_sync(0xffffffffu, start, i + 1 - base); }
+  __device__ __forceinline__ int in_of(int i) const { return __shfl_sync(0xffffffffu, in, i - base); }
+  __device__ __forceinline__ int out_of(int i) const { return __shfl_sync(0xffffffffu, out, i - base); }
+};
+
+// STATE: the first launch.
+template <typename T, bool ZOH, bool STATE>
+__global__ void __launch_bounds__(RWARPS * 32, sizeof(T) == 2 ? 3 : 2)
+scan_ragged_chunks(const RaggedScan p) {
+  constexpr bool FINE = sizeof(T) == 4;
+  __shared__ __align__(16) RaggedTile tiles[RWARPS];
+  pdl_wait();
+  const int lane = threadIdx.x & 31, De = p.De, groups = De / 32;
+  const int item = blockIdx.x * RWARPS + (threadIdx.x >> 5), chunk = item / groups, c_warp = (item % groups) * 32;
+  if (chunk >= (STATE ? p.nch - 1 : p.nch)) return;
+  RaggedTile& s = tiles[threadIdx.x >> 5];
+  const int r0 = chunk * p.Lc, r1 = min(r0 + p.Lc, p.s.rows);
+  // ---- what this warp walks
+  int t, hi, cur_end, next = 0, cur_out = -1, cur_in = -1, first_chunk = chunk;
+  bool reach = false;
+  SeqWindow w;
+  if (STATE) {
+    const int q = p.s.first_from(r1) - 1;      // the last sequence that starts before the chunk's end
+    if (q < 0) return;
+    const int first = p.s.start_of(q);
+    if (p.s.end_of(q) <= r1) return;
+    t = max(first, r0); hi = r1; cur_end = r1;
+    if (first >= r0) cur_in = p.h_in && p.s.resumes(q) ? p.s.slot_of(q) : -1;
+  } else {
+    next = p.s.first_from(r0);
+    reach = chunk > 0 && next > 0 && p.s.end_of(next - 1) > r0;
+    hi = min(r1, p.s.start_of(p.s.n_seq));
+    w.load(p, max(next - 1, 0));
+    if (reach) {
+      w.reach(p, next - 1);
+      cur_end = w.end_of(next - 1); cur_out = w.out_of(next - 1);
+      first_chunk = min(w.start_of(next - 1) / p.Lc, chunk - 1);      // (offsets that descend stay in bounds)
+      t = r0;
+    } else {
+      w.reach(p, next);
+      t = next < p.s.n_seq ? w.start_of(next) : r1;
+      cur_end = t;
+    }
+  }
+
+  // ---- compute role: channels c0 .. c0+3 (pairs), states 4q .. 4q+3
+  const int q = lane & 3, cg = lane >> 2, c0 = c_warp + 4 * cg;
+  float2 a2[4][2], kin[4][2], h[4][2], sdel[2];
+  float av[4][4];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        float a, e;
-        decay(dl * av[n], a, e);
-        h[n] = fmaf(a, h[n], (ZOH ? __fdividef(e, av[n]) : dl) * (uu * bb[n]));
-        y = fmaf(cc[n], h[n], y);
+  for (int i = 0; i < 4; ++i) {
+    const float4 a4 = __ldg(reinterpret_cast<const float4*>(p.A + (size_t)(c0 + i) * 16) + q);
+    av[i][0] = a4.x; av[i][1] = a4.y; av[i][2] = a4.z; av[i][3] = a4.w;
+  }
+  auto set_state = [&](const float4 (&v)[4]) {
+    const float hv[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w}, {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) h[n][j] = make_float2(hv[2 * j][n], hv[2 * j + 1][n]);
+  };
+  auto state_at = [&](int i) { return (size_t)(c0 + i) * 16 + 4 * q; };      // within one sequence's or chunk's [De, 16]
+  auto put_state = [&](float* dst) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      *reinterpret_cast<float4*>(dst + state_at(2 * j)) = make_float4(h[0][j].x, h[1][j].x, h[2][j].x, h[3][j].x);
+      *reinterpret_cast<float4*>(dst + state_at(2 * j + 1)) = make_float4(h[0][j].y, h[1][j].y, h[2][j].y, h[3][j].y);
+    }
+  };
+  const float4 zero4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  {
+    float4 v[4] = {zero4, zero4, zero4, zero4};
+    if (STATE) {
+      if (cur_in >= 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = *reinterpret_cast<const float4*>(p.h_in + (size_t)cur_in * De * 16 + state_at(i));
+          *reinterpret_cast<float4*>(p.h_start + (size_t)chunk * De * 16 + state_at(i)) = v[i];
+        }
       }
-      y += __shfl_xor_sync(0xffffffffu, y, 1);
-      y += __shfl_xor_sync(0xffffffffu, y, 2);
-      if (t == 0) {
-        y = fmaf(Dc, uu, y);
-        if (z) y *= silu_f(to_f32(z[(size_t)r * p.ldz + c]));
-        static_cast<T*>(p.y)[o] = from_f32<T>(y);
+    } else if (reach) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(p.h_end + (size_t)first_chunk * De * 16 + state_at(i));
+      for (int k = first_chunk + 1; k < chunk; ++k) {
+        const float4 d4 = *reinterpret_cast<const float4*>(p.sum_delta + (size_t)k * De + c0);
+        const float dk[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 e = *reinterpret_cast<const float4*>(p.h_end + (size_t)k * De * 16 + state_at(i));
+          v[i].x = fmaf(expf(av[i][0] * dk[i]), v[i].x, e.x);
+          v[i].y = fmaf(expf(av[i][1] * dk[i]), v[i].y, e.y);
+          v[i].z = fmaf(expf(av[i][2] * dk[i]), v[i].z, e.z);
+          v[i].w = fmaf(expf(av[i][3] * dk[i]), v[i].w, e.w);
+        }
       }
     }
-    if (p.h_out && slot >= 0) *reinterpret_cast<float4*>(p.h_out + at) = make_float4(h[0], h[1], h[2], h[3]);
+    set_state(v);
   }
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float a = FINE ? 1.0f : kLog2eServe, k = FINE ? 1.0f : -1.0f;
+      a2[n][j] = make_float2(av[2 * j][n] * a, av[2 * j + 1][n] * a);
+      kin[n][j] = make_float2(k / av[2 * j][n], k / av[2 * j + 1][n]);
+    }
+  sdel[0] = make_float2(0.0f, 0.0f); sdel[1] = sdel[0];
+
+  if (!STATE) {
+    s.D[lane] = p.D ? __ldg(p.D + c_warp + lane) : 0.0f;
+    // sequences without a row that lie in this chunk (the last chunk: behind the last row too): their state is the initial one
+    for (int b = next; b < p.s.n_seq; b += 31) {
+      w.load(p, b);
+      const int after = __shfl_down_sync(0xffffffffu, w.start, 1);
+      const bool mine = lane < 31 && b + lane < p.s.n_seq && (w.start < r1 || chunk == p.nch - 1);
+      unsigned m = __ballot_sync(0xffffffffu, mine && after <= w.start && w.out >= 0);
+      while (m) {
+        const int i = b + __ffs(m) - 1, in = w.in_of(i), out = w.out_of(i);
+        m &= m - 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *reinterpret_cast<float4*>(p.h_out + (size_t)out * De * 16 + state_at(k)) =
+              in >= 0 ? *reinterpret_cast<const float4*>(p.h_in + (size_t)in * De * 16 + state_at(k)) : zero4;
+      }
+      if (!__all_sync(0xffffffffu, mine || lane == 31)) break;
+    }
+    w.load(p, next);
+  }
+  // the next sequence with rows; its initial state on the way to shared memory
+  int n_start = 0x7fffffff, n_end = 0, n_in = -1, n_out = -1;
+  auto look_ahead = [&]() {
+    while (next < p.s.n_seq) {
+      w.reach(p, next);
+      n_start = w.start_of(next); n_end = w.end_of(next);
+      if (n_end > n_start) break;
+      ++next;
+    }
+    if (next >= p.s.n_seq) { n_start = 0x7fffffff; n_end = 0x7fffffff; n_in = -1; n_out = -1; return; }
+    n_in = w.in_of(next); n_out = w.out_of(next);
+    ++next;
+    if (n_in >= 0 && n_start < r1) {
+      const float* src = n_end > r1 ? p.h_start + (size_t)chunk * De * 16 : p.h_in + (size_t)n_in * De * 16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&s.h0[i][lane])), "l"(src + state_at(i)) : "memory");
+    }
+  };
+  if (!STATE) look_ahead();
+
+  // ---- loader / output role: row lt of every tile, channels lc .. lc+7 (four lanes per row: a quarter-warp touches two rows of global memory)
+  const int lt = lane >> 2, l8 = lane & 3, lc = c_warp + 8 * l8;
+  const T* __restrict__ up = static_cast<const T*>(p.u) + lc;
+  const T* __restrict__ zp = STATE ? nullptr : static_cast<const T*>(p.z);
+  const float* __restrict__ dp = p.delta + lc;
+  Raw8<float> r_d;
+  Raw8<T> r_u, r_z, cur_u, cur_z;
+  float4 r_b, r_c;
+  auto bc_row = [&](const float* v, size_t row) {
+    const float* at = v + row * p.ldb + 4 * l8;
+    return p.bc16 ? __ldg(reinterpret_cast<const float4*>(at)) : make_float4(__ldg(at), __ldg(at + 1), __ldg(at + 2), __ldg(at + 3));
+  };
+  auto fetch = [&](int t0, int m) {
+    if (lt < m) {
+      const size_t row = t0 + lt;
+      r_d.load(dp + row * De);
+      r_u.load(up + row * De);
+      r_b = bc_row(p.Bm, row);
+      if (!STATE) {
+        r_c = bc_row(p.Cm, row);
+        if (zp) r_z.load(zp + row * p.ldz + lc);
+      }
+    } else {                      // rows past the tile's end change nothing
+      r_d.zero(); r_u.zero();
+      r_b = zero4; r_c = zero4;
+    }
+  };
+  // rows of the tile at t0, with the sequence that runs there ending at `end`
+  auto rows_of = [&](int t0, int end) { return max(min(RR, min(end, hi) - t0), 1); };
+
+  if (t < hi) fetch(t, rows_of(t, t < cur_end ? cur_end : n_end));
+  bool running = STATE || reach;
+  while (t < hi) {
+    if (!STATE && t >= cur_end) {
+      if (running && cur_out >= 0) put_state(p.h_out + (size_t)cur_out * De * 16);
+      float4 v[4] = {zero4, zero4, zero4, zero4};
+      if (n_in >= 0) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = s.h0[i][lane];
+      }
+      set_state(v);
+      running = true; cur_end = n_end; cur_out = n_out;
+      look_ahead();
+    }
+    const int m = rows_of(t, cur_end), t_next = t + m;
+    {
+      float d[8], uu[8];
+      r_d.get(d); r_u.get(uu);
+      if (!ZOH) {                 // B-bar = Delta B: the input enters as Delta u
+#pragma unroll
+        for (int i = 0; i < 8; ++i) uu[i] *= d[i];
+      }
+      s.dl[lt][(2 * l8) ^ lt] = make_float4(d[0], d[1], d[2], d[3]);
+      s.dl[lt][(2 * l8 + 1) ^ lt] = make_float4(d[4], d[5], d[6], d[7]);
+      s.u[lt][(2 * l8) ^ lt] = make_float4(uu[0], uu[1], uu[2], uu[3]);
+      s.u[lt][(2 * l8 + 1) ^ lt] = make_float4(uu[4], uu[5], uu[6], uu[7]);
+      s.b[lt][l8] = r_b;
+      if (!STATE) { s.c[lt][l8] = r_c; cur_u = r_u; cur_z = r_z; }
+    }
+    __syncwarp();
+    if (t_next < hi) fetch(t_next, rows_of(t_next, t_next < cur_end ? cur_end : n_end));
+    // the next row's operands are requested before this row's arithmetic: a load issued behind a row's exponentials waits for all of them
+    float4 nd = s.dl[0][cg], nu = s.u[0][cg], nb = s.b[0][q], nc = STATE ? zero4 : s.c[0][q];
+#pragma unroll
+    for (int r = 0; r < RR; ++r) {
+      if (r >= m) break;
+      const float4 d4 = nd, u4 = nu, b4 = nb, c4 = nc;
+      if (r + 1 < RR) {
+        nd = s.dl[r + 1][cg ^ (r + 1)]; nu = s.u[r + 1][cg ^ (r + 1)]; nb = s.b[r + 1][q];
+        if (!STATE) nc = s.c[r + 1][q];
+      }
+      const float2 dl[2] = {make_float2(d4.x, d4.y), make_float2(d4.z, d4.w)}, uu[2] = {make_float2(u4.x, u4.y), make_float2(u4.z, u4.w)};
+      const float bb[4] = {b4.x, b4.y, b4.z, b4.w}, cc[4] = {c4.x, c4.y, c4.z, c4.w};
+      float2 acc[2];
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 x = __fmul2_rn(dl[j], a2[n][j]);
+          const float2 uB = __fmul2_rn(uu[j], pair(bb[n]));
+          if (FINE) {
+            float2 a, e;
+            decay(x.x, a.x, e.x);
+            decay(x.y, a.y, e.y);
+            h[n][j] = __ffma2_rn(a, h[n][j], ZOH ? __fmul2_rn(e, __fmul2_rn(uB, kin[n][j])) : uB);
+          } else {
+            const float2 a = make_float2(ex2_ftz(x.x), ex2_ftz(x.y));
+            if (ZOH) {            // w = -B u / A, h <- a (h - w) + w
+              const float2 v = __fmul2_rn(uB, kin[n][j]);
+              h[n][j] = __ffma2_rn(a, __ffma2_rn(v, pair(-1.0f), h[n][j]), v);
+            } else {
+              h[n][j] = __ffma2_rn(a, h[n][j], uB);
+            }
+          }
+          if (!STATE) acc[j] = n == 0 ? __fmul2_rn(pair(cc[n]), h[n][j]) : __ffma2_rn(pair(cc[n]), h[n][j], acc[j]);
+        }
+      if (STATE) { sdel[0] = __fadd2_rn(sdel[0], dl[0]); sdel[1] = __fadd2_rn(sdel[1], dl[1]); }
+      else s.y[r][y_slot(lane, r)] = make_float4(acc[0].x, acc[0].y, acc[1].x, acc[1].y);
+    }
+    __syncwarp();
+    if (!STATE) {
+      if (lt < m) {               // y = (sum over the four lanes + D u) * gate, rounded
+        float o[8], uu[8], zz[8];
+        cur_u.get(uu);
+        if (zp) {
+          cur_z.get(zz);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) zz[i] = FINE ? silu_f(zz[i]) : silu_fast(zz[i]);
+        }
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const int g4 = 8 * l8 + 4 * hf;
+          const float4 x0 = s.y[lt][y_slot(g4, lt)], x1 = s.y[lt][y_slot(g4 + 1, lt)], x2 = s.y[lt][y_slot(g4 + 2, lt)], x3 = s.y[lt][y_slot(g4 + 3, lt)];
+          const float4 D4 = reinterpret_cast<const float4*>(s.D)[2 * l8 + hf];
+          const float sum[4] = {(x0.x + x1.x) + (x2.x + x3.x), (x0.y + x1.y) + (x2.y + x3.y), (x0.z + x1.z) + (x2.z + x3.z), (x0.w + x1.w) + (x2.w + x3.w)};
+          const float Dv[4] = {D4.x, D4.y, D4.z, D4.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = fmaf(Dv[i], uu[4 * hf + i], sum[i]);
+            o[4 * hf + i] = zp ? v * zz[4 * hf + i] : v;
+          }
+        }
+        Raw8<T>::store(static_cast<T*>(p.y) + (size_t)(t + lt) * De + lc, o);
+      }
+      __syncwarp();
+    }
+    t = t_next;
+  }
+  if (STATE) {
+    put_state(p.h_end + (size_t)chunk * De * 16);
+    if (q == 0) *reinterpret_cast<float4*>(p.sum_delta + (size_t)chunk * De + c0) = make_float4(sdel[0].x, sdel[0].y, sdel[1].x, sdel[1].y);
+  } else if (running && cur_end <= r1 && cur_out >= 0) {
+    put_state(p.h_out + (size_t)cur_out * De * 16);
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <typename T>
-cudaError_t launch_scan_ragged(const rom_config& c, const RaggedScan& p, cudaStream_t st) {
-  auto kern = c.disc_mode == 0 ? scan_ragged_rows<T, true> : scan_ragged_rows<T, false>;
+// Chunks of the packed rows: the count with the smallest time by the warp kernel's measured pace (scan_warp_time): a block of four warps takes
+// 139 / 192 / 272 ns a row with one / two / three of them on an SM, 115 / 161 / 230 ns states only, and the second launch costs about 7 us.
+// The first launch walks the rows of sequences that reach over a chunk's end: all of a chunk when sequences are longer than chunks, about
+// one mean sequence otherwise.  A function of the sizes alone, so that workspace sizing and the launch agree.
+int ragged_chunks(int De, int n_seq, int rows) {
+  auto pace = [](long long blocks, const double (&ns)[3]) {
+    const long long k = (blocks + 147) / 148;
+    return k <= 3 ? ns[k - 1] : ns[2] * (double)k / 3.0;
+  };
+  const double full[3] = {139.0, 192.0, 272.0}, state[3] = {115.0, 161.0, 230.0};
+  const double mean = (double)rows / (n_seq > 0 ? n_seq : 1);
+  int best = 1;
+  double best_t = 0.0;
+  for (int n = 1; n == 1 || (rows >= 16 * n && (long long)n * (De / 32) <= 148 * 12 * 4); ++n) {
+    const long long blocks = ((long long)n * (De / 32) + RWARPS - 1) / RWARPS;
+    const double Lc = (double)((rows + n - 1) / n);
+    const double t = Lc * pace(blocks, full) + (n == 1 ? 0.0 : (Lc < mean ? Lc : mean) * pace(blocks, state) + 7000.0);
+    if (n == 1 || t < best_t) { best = n; best_t = t; }
+  }
+  return best;
+}
+struct RaggedWs { int Lc, nch; size_t h_end, h_start, sum_delta, total; };
+RaggedWs ragged_ws(int De, int n_seq, int rows) {
+  RaggedWs l{};
+  const int n = ragged_chunks(De, n_seq, rows);
+  l.Lc = n == 1 ? (rows > 0 ? rows : 1) : (int)align_up((size_t)(rows + n - 1) / n, RR);
+  l.nch = rows > 0 ? (rows + l.Lc - 1) / l.Lc : 1;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
+  const size_t keep = l.nch > 1 ? l.nch : 0;
+  l.h_end = take(keep * De * 16 * sizeof(float));
+  l.h_start = take(keep * De * 16 * sizeof(float));
+  l.sum_delta = take(keep * De * sizeof(float));
+  l.total = o > 256 ? o : 256;
+  return l;
+}
+
+template <typename T, bool ZOH>
+cudaError_t launch_scan_ragged(const RaggedScan& p, cudaStream_t st) {
+  const long long groups = p.De / 32;
+  auto blocks = [&](long long chunks) { return dim3((unsigned)((chunks * groups + RWARPS - 1) / RWARPS)); };
+  if (p.nch > 1) {
+    const cudaError_t e = launch_k(scan_ragged_chunks<T, ZOH, true>, blocks(p.nch - 1), RWARPS * 32, 0, st, p);
+    if (e != cudaSuccess) return e;
+    count_launch();
+  }
   count_launch();
-  return launch_k(kern, dim3(c.d_inner / 32, p.s.n_seq < 4096 ? p.s.n_seq : 4096), 128, 0, st, p);
+  return launch_k(scan_ragged_chunks<T, ZOH, false>, blocks(p.nch), RWARPS * 32, 0, st, p);
 }
 
 }  // namespace
@@ -73,7 +409,7 @@ int rom_scan_ragged_workspace_size(const rom_config* cfg, int32_t n_seq, int32_t
   const int rc = check_config(cfg, 2);
   if (rc != ROM_OK) return rc;
   if (n_seq > kMaxRaggedSeqs || rows >= 1 << 30) return ROM_ERR_UNSUPPORTED;
-  *bytes = 256;
+  *bytes = ragged_ws(cfg->d_inner, n_seq, rows).total;
   return ROM_OK;
 }
 
@@ -93,14 +429,17 @@ int rom_scan_ragged(const rom_config* cfg, const rom_ragged* seqs, const void* u
     if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
   if (!aligned4(D) || !aligned4(Bm) || !aligned4(Cm)) return ROM_ERR_INVALID_ARG;
   if (!pools_ok(h_in, h_out, (size_t)seqs->n_slots * c.d_inner * c.d_state)) return ROM_ERR_INVALID_ARG;
-  size_t need = 0;
-  if ((rc = rom_scan_ragged_workspace_size(cfg, seqs->n_seq, seqs->rows, &need)) != ROM_OK) return rc;
-  if (ws_bytes < need) return ROM_ERR_WORKSPACE;
+  const RaggedWs lay = ragged_ws(c.d_inner, seqs->n_seq, seqs->rows);
+  if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
   if ((rc = check_device()) != ROM_OK) return rc;
   LaunchCounter::count = 0;
-  const RaggedScan p{device_view(*seqs), u, delta, A, Bm, Cm, ld_bc, D, z, ldz, h_in, h_out, y, c.d_inner};
-  auto launch = c.dtype == ROM_BF16 ? launch_scan_ragged<__nv_bfloat16> : launch_scan_ragged<float>;
-  return launch(c, p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
+  char* W = static_cast<char*>(ws);
+  const int bc16 = aligned16(Bm) && aligned16(Cm) && ld_bc % 4 == 0;
+  const RaggedScan p{device_view(*seqs), u, delta, A, Bm, Cm, ld_bc, D, z, ldz, h_in, h_out, y, c.d_inner, lay.Lc, lay.nch, bc16,
+                     reinterpret_cast<float*>(W + lay.h_end), reinterpret_cast<float*>(W + lay.h_start), reinterpret_cast<float*>(W + lay.sum_delta)};
+  auto launch = c.dtype == ROM_BF16 ? (c.disc_mode == 0 ? launch_scan_ragged<__nv_bfloat16, true> : launch_scan_ragged<__nv_bfloat16, false>)
+                                    : (c.disc_mode == 0 ? launch_scan_ragged<float, true> : launch_scan_ragged<float, false>);
+  return launch(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
 
 }  // extern "C"
