@@ -1,12 +1,19 @@
 // FFN-MoE of the few tokens of a generation step (rom_ffn_moe_step): out_t = sum_k g_tk W_down,e (SiLU(W_gate,e x_t) * (W_up,e x_t)), e = topk_idx[t, k].
 // Two launches: hidden rows g SiLU(gate) up of every assignment (token, slot), then the down projection with the sum over the slots.
 // The weights of the chosen experts, read once, are what counts: 6 d_model d_ff bytes an expert (bf16).
+#include <algorithm>
+#include <type_traits>
+
 #include "rom_serve.cuh"
+#include "rom_tc_ptx.cuh"
 
 namespace rom {
 namespace {
 
+typedef __nv_bfloat16 bf16;
 constexpr int kFfnStepTokens = 64, kFfnStepAssign = kFfnStepTokens * kMaxK;
+constexpr int kFfnMaxTiles = 1024;       // row tiles of the down projection
+constexpr int kFfnMaxSplits = 16;
 
 struct FfnStep {
   const void* x; const void* W_gu; const void* W_down; const int32_t* idx; const float* gates; void* out;
@@ -68,16 +75,16 @@ __device__ __forceinline__ float sum_to_lane(float (&v)[32]) {
   return v[0];
 }
 
+// ---------------------------------------------------------------------------------------------- fp32
 // Four weight rows times up to eight rows of activations, over the lanes of a warp; lane 8 r + j gets row r times activation j.
-template <typename T>
-__device__ __forceinline__ float rows_4x8(const T* const (&w)[4], const T* const (&x)[8], int n, int Kd) {
-  constexpr int V = V16<T>::N;
+__device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const float* const (&x)[8], int n, int Kd) {
+  constexpr int V = 4;
   const int lane = threadIdx.x & 31;
   float acc[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
   for (int k = lane * V; k < Kd; k += 32 * V) {
-    V16<T> wq[4];
+    V16<float> wq[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) wq[r].load(w[r] + k);
     float wv[4][V];
@@ -87,8 +94,8 @@ __device__ __forceinline__ float rows_4x8(const T* const (&w)[4], const T* const
     for (int j = 0; j < 8; ++j) {
       if (j >= n) break;
       float xv[V];
-      V16<T> xq;
-      xq.q = *reinterpret_cast<const decltype(xq.q)*>(x[j] + k);
+      V16<float> xq;
+      xq.q = *reinterpret_cast<const float4*>(x[j] + k);
       xq.get(xv);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -100,7 +107,6 @@ __device__ __forceinline__ float rows_4x8(const T* const (&w)[4], const T* const
 }
 
 constexpr int FR_WARPS = 4;
-template <typename T>
 __global__ void __launch_bounds__(FR_WARPS * 32)
 ffn_step_up(const FfnStep p) {
   __shared__ ByExpert by;
@@ -110,24 +116,23 @@ ffn_step_up(const FfnStep p) {
   const int lane = threadIdx.x & 31, j = lane & 7;
   const int f = (blockIdx.x * FR_WARPS + (threadIdx.x >> 5)) * 2;      // a warp has two hidden columns of every expert
   for (int e = 0; e < p.E; ++e) {
-    const T* g = static_cast<const T*>(p.W_gu) + ((size_t)e * 2 * p.F + f) * p.Dm;
-    const T* u = g + (size_t)p.F * p.Dm;
-    const T* const w[4] = {g, g + p.Dm, u, u + p.Dm};
+    const float* g = static_cast<const float*>(p.W_gu) + ((size_t)e * 2 * p.F + f) * p.Dm;
+    const float* u = g + (size_t)p.F * p.Dm;
+    const float* const w[4] = {g, g + p.Dm, u, u + p.Dm};
     for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
       const int n = min(8, by.off[e + 1] - a0);
-      const T* x[8];
+      const float* x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = static_cast<const T*>(p.x) + (size_t)(by.list[a0 + min(i, n - 1)] / p.K) * p.Dm;
-      const float v = rows_4x8<T>(w, x, n, p.Dm);
+      for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.x) + (size_t)(by.list[a0 + min(i, n - 1)] / p.K) * p.Dm;
+      const float v = rows_4x8(w, x, n, p.Dm);
       const float up = __shfl_down_sync(0xffffffffu, v, 16);
       if (lane < 16 && j < n) {
         const int a = by.list[a0 + j];
-        static_cast<T*>(p.hid)[(size_t)a * p.F + f + (lane >> 3)] = from_f32<T>(silu_f(v) * up * __ldg(p.gates + a));
+        static_cast<float*>(p.hid)[(size_t)a * p.F + f + (lane >> 3)] = (silu_f(v) * up * __ldg(p.gates + a));
       }
     }
   }
 }
-template <typename T>
 __global__ void __launch_bounds__(FR_WARPS * 32)
 ffn_step_down(const FfnStep p) {
   __shared__ ByExpert by;
@@ -140,31 +145,431 @@ ffn_step_down(const FfnStep p) {
   for (int t = lane; t < p.T * 4; t += 32) s[t >> 2][t & 3] = 0.0f;
   __syncwarp();
   for (int e = 0; e < p.E; ++e) {
-    const T* w0 = static_cast<const T*>(p.W_down) + ((size_t)e * p.Dm + d) * p.F;
-    const T* const w[4] = {w0, w0 + p.F, w0 + 2 * (size_t)p.F, w0 + 3 * (size_t)p.F};
+    const float* w0 = static_cast<const float*>(p.W_down) + ((size_t)e * p.Dm + d) * p.F;
+    const float* const w[4] = {w0, w0 + p.F, w0 + 2 * (size_t)p.F, w0 + 3 * (size_t)p.F};
     for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
       const int n = min(8, by.off[e + 1] - a0);
-      const T* x[8];
+      const float* x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = static_cast<const T*>(p.hid) + (size_t)by.list[a0 + min(i, n - 1)] * p.F;
-      const float v = rows_4x8<T>(w, x, n, p.F);
+      for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.hid) + (size_t)by.list[a0 + min(i, n - 1)] * p.F;
+      const float v = rows_4x8(w, x, n, p.F);
       for (int i = 0; i < n; ++i) {      // one at a time: two of them may be of one token
         if ((lane & 7) == i) s[by.list[a0 + i] / p.K][lane >> 3] += v;
         __syncwarp();
       }
     }
   }
-  for (int t = lane; t < p.T * 4; t += 32) static_cast<T*>(p.out)[(size_t)(t >> 2) * p.Dm + d + (t & 3)] = from_f32<T>(s[t >> 2][t & 3]);
+  for (int t = lane; t < p.T * 4; t += 32) static_cast<float*>(p.out)[(size_t)(t >> 2) * p.Dm + d + (t & 3)] = (s[t >> 2][t & 3]);
 }
 
-template <typename T>
 cudaError_t launch_ffn_rows(const FfnStep& p, cudaStream_t st) {
-  cudaError_t e = launch_k(ffn_step_up<T>, dim3(p.F / (2 * FR_WARPS)), FR_WARPS * 32, 0, st, p);
+  cudaError_t e = launch_k(ffn_step_up, dim3(p.F / (2 * FR_WARPS)), FR_WARPS * 32, 0, st, p);
   if (e != cudaSuccess) return e;
   count_launch();
-  e = launch_k(ffn_step_down<T>, dim3(p.Dm / (4 * FR_WARPS)), FR_WARPS * 32, 0, st, p);
+  e = launch_k(ffn_step_down, dim3(p.Dm / (4 * FR_WARPS)), FR_WARPS * 32, 0, st, p);
   count_launch();
   return e;
+}
+
+// ---------------------------------------------------------------------------------------------- bf16: streamed weights
+constexpr int FT_COLS = 64;                          // token columns per pass at most
+constexpr int FT_MAX_STAGES = 10;
+constexpr int FT_X_FLIGHT = 2;                       // stages of token rows in flight
+constexpr int FT_SMEM = 208 * 1024;                  // operand ring, with its alignment and what the MMA reads past a short tile
+constexpr int FT_THREADS = 320;
+constexpr int FT_K = 2 * BLOCK_K;                    // contracted elements per stage
+
+// Experts that T tokens with K choices each of E name, about.
+int chosen_experts(int T, int K, int E) {
+  double none = 1.0;
+  for (int t = 0; t < T; ++t) none *= 1.0 - (double)K / E;
+  const int n = (int)(E * (1.0 - none) + 0.5);
+  return n < 1 ? 1 : n;
+}
+constexpr int kSizingSms = 148;      // (workspace sizing and the launch agree)
+struct FfnCut { int h, splits; };
+// Rows per tile (and, of the down projection, parts of the contracted index) for which the rounds of tiles over the SMs bring the fewest bytes
+// through one of them: weights, token rows, and the parts written and added again.
+FfnCut cut_up(int T, int K, int E, int Dm, int F) {
+  const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Dm + FT_K - 1) / FT_K;
+  FfnCut best{64, 1};
+  long long least = -1;
+  for (int h = 64; h >= 8; h -= 8) {
+    const long long rounds = (n * ((F + h - 1) / h) + kSizingSms - 1) / kSizingSms, cost = rounds * kb * 2 * FT_K * (2 * h + m);
+    if (least < 0 || cost < least) { least = cost; best.h = h; }
+  }
+  return best;
+}
+FfnCut cut_down(int T, int K, int E, int Dm, int F) {
+  const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = F / FT_K;
+  FfnCut best{128, 1};
+  long long least = -1;
+  for (int s = 1; s <= kFfnMaxSplits && s <= kb; ++s)
+    for (int h = 128; h >= 32; h -= 8) {
+      const long long rounds = (n * s * ((Dm + h - 1) / h) + kSizingSms - 1) / kSizingSms;
+      const bool direct = K == 1 && s == 1;
+      const long long cost = rounds * ((kb + s - 1) / s * 2 * FT_K * (h + m) + (direct ? 0 : 4 * m * h)) + (direct ? 0 : 4ll * T * K * s * h);
+      if (least < 0 || cost < least) { least = cost; best.h = h; best.splits = s; }
+    }
+  return best;
+}
+
+struct FfnTc {
+  const bf16* x; int ldx;                            // rows of activations: up: x of the token; down: hid of the assignment
+  int Kd, w_rows, out_rows;                          // contracted length; weight rows per expert; rows of the product (up: pairs of them)
+  const int32_t* idx; const float* gates;
+  bf16* hid; float* part; bf16* out; int32_t* arrived; int32_t* status;
+  int T, K, E;
+  int h, tiles, splits, stages, cols_cap;            // rows per tile, tiles per expert, parts of the contracted index, ring, columns of a stage
+  int direct;                                        // down: one expert and one part a token: written at once
+};
+
+template <bool UP>
+__global__ void __launch_bounds__(FT_THREADS, 1)
+ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  __shared__ ByExpert by;
+  __shared__ int act[kMaxE], n_act_s, last_s;
+  __shared__ __align__(16) float exch[16][132];      // up: 16 columns of 128 accumulator rows
+  __shared__ __align__(8) unsigned long long bars[2 * FT_MAX_STAGES + 5];
+  __shared__ uint32_t tmem_s;
+  __shared__ int abort_s;
+  volatile int* abort_flag = &abort_s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, A = p.T * p.K;
+  auto full_bar = [&](int s) { return smem_u32(&bars[s]); };
+  auto empty_bar = [&](int s) { return smem_u32(&bars[FT_MAX_STAGES + s]); };
+  auto tfull_bar = [&](int a) { return smem_u32(&bars[2 * FT_MAX_STAGES + a]); };
+  auto tempty_bar = [&](int a) { return smem_u32(&bars[2 * FT_MAX_STAGES + 2 + a]); };
+  const uint32_t drain_bar = smem_u32(&bars[2 * FT_MAX_STAGES + 4]);
+
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) { mbar_init(full_bar(s), 1 + 4); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 4); }
+    mbar_init(drain_bar, 1);
+    abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * FT_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (UP) { pdl_wait(); pdl_trigger(); }             // (down: the choice of experts is older than the launch before)
+  by.build(p.idx, A, p.E);
+  if (tid == 0) {
+    int n = 0;
+    for (int e = 0; e < p.E; ++e)
+      if (by.off[e + 1] > by.off[e]) act[n++] = e;
+    n_act_s = n;
+  }
+  if (UP && blockIdx.x == 0) {
+    bool bad = false;
+    for (int a = tid; a < A; a += FT_THREADS) bad |= __ldg(p.idx + a) >= p.E;
+    bad = __syncthreads_or(bad);
+    if (tid < kStatusInts) p.status[tid] = tid == kStatCode && bad ? ROM_ERR_INVALID_ARG : 0;
+    for (int j = tid; j < kFfnMaxTiles; j += FT_THREADS) p.arrived[j] = 0;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_s;
+  const int n_act = n_act_s, per_expert = p.tiles * p.splits, total = n_act * per_expert;
+  const int num_kb = (p.Kd + FT_K - 1) / FT_K;
+  const uint32_t w_half = (UP ? 2 : 1) * p.h * 128, x_half = p.cols_cap * 128, x_at = 2 * w_half, stage_bytes = 2 * (w_half + x_half);
+  auto cols = [](int m) { return m > 32 ? 64 : m > 16 ? 32 : 16; };      // N of a pass over m tokens
+  // item w: expert, first row, stages [kb0, kb0 + n) of the contracted index, walked from a start of the tile's own: in step all CTAs
+  // would read the same columns of rows that are a power of two apart
+  struct Item { int e, tile, part, kb0, n, rot; };
+  auto item = [&](int w) {
+    Item it;
+    it.e = act[w / per_expert];
+    const int r = w % per_expert;
+    it.tile = r / p.splits; it.part = r % p.splits;
+    it.kb0 = num_kb * it.part / p.splits;
+    it.n = num_kb * (it.part + 1) / p.splits - it.kb0;
+    it.rot = it.tile * 5 % it.n;
+    return it;
+  };
+  auto k_of = [&](const Item& it, int q) { return (it.kb0 + (q + it.rot < it.n ? q + it.rot : q + it.rot - it.n)) * FT_K; };
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- TMA producer of the weights (nothing here depends on the launch before)
+    if (lane == 0) {
+      int stage = 0, issued = 0; uint32_t phase = 0;
+      bool ok = true;
+      for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
+        const Item it = item(w);
+        const int row = it.e * p.w_rows + it.tile * p.h, m = by.off[it.e + 1] - by.off[it.e];
+        for (int n0 = 0; n0 < m && ok; n0 += p.cols_cap)
+          for (int q = 0; q < it.n; ++q) {
+            if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
+            const int k0 = k_of(it, q);
+            const uint32_t dst = base + stage * stage_bytes;
+            mbar_expect_tx(full_bar(stage), 2 * w_half);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              tma_load_2d(dst + hf * w_half, &tmap_w, full_bar(stage), k0 + hf * BLOCK_K, row);
+              if (UP) tma_load_2d(dst + hf * w_half + p.h * 128, &tmap_w, full_bar(stage), k0 + hf * BLOCK_K, row + p.out_rows);
+            }
+            ++issued;
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          }
+      }
+      if (!ok) {
+        if (!*abort_flag) { atomicExch(p.status + kStatCode, ROM_ERR_DEVICE_TIMEOUT); atomicExch(p.status + kStatWhere, 4); }
+        *abort_flag = 1;
+      }
+      if (*abort_flag) {                             // give the copies still in flight a bounded time to land before the CTA exits
+        for (int i = 0; i < min(issued, p.stages); ++i) {
+          if (--stage < 0) { stage = p.stages - 1; phase ^= 1u; }
+          for (uint32_t k = 0; k < (wait_limit >> 2); ++k)
+            if (mbar_try_wait(full_bar(stage), phase)) break;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer: weights are the M operand, tokens the N columns
+    if (lane == 0) {
+      int stage = 0, acc = 0; uint32_t phase = 0, acc_phase = 0;
+      bool ok = true, issued_any = false;
+      for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
+        const Item it = item(w);
+        const int m = by.off[it.e + 1] - by.off[it.e];
+        for (int n0 = 0; n0 < m && ok; n0 += p.cols_cap) {
+          const int n16 = cols(min(m - n0, p.cols_cap));
+          const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n16 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+          if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
+          tc_fence_after();
+          for (int q = 0; q < it.n; ++q) {
+            if (!mbar_wait(full_bar(stage), phase, abort_flag, wait_limit)) { ok = false; break; }
+            tc_fence_after();
+            const int halves = k_of(it, q) + BLOCK_K < p.Kd ? 2 : 1;
+            for (int hf = 0; hf < halves; ++hf) {
+              const uint64_t adesc = make_smem_desc(base + stage * stage_bytes + hf * w_half);
+              const uint64_t bdesc = make_smem_desc(base + stage * stage_bytes + x_at + hf * x_half);
+#pragma unroll
+              for (int k = 0; k < BLOCK_K / UMMA_K; ++k)
+                umma_bf16(tmem_base + acc * FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc, (q | hf | k) != 0 ? 1u : 0u);
+            }
+            umma_commit(empty_bar(stage));
+            issued_any = true;
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          }
+          if (!ok) break;
+          umma_commit(tfull_bar(acc));
+          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+      }
+      if (!ok) {
+        if (!*abort_flag) { atomicExch(p.status + kStatCode, ROM_ERR_DEVICE_TIMEOUT); atomicExch(p.status + kStatWhere, 5); }
+        *abort_flag = 1;
+      }
+      if (*abort_flag && issued_any) {
+        umma_commit(drain_bar);
+        for (uint32_t k = 0; k < (wait_limit >> 2); ++k)
+          if (mbar_try_wait(drain_bar, 0)) break;
+      }
+    }
+  } else if (warp >= 6) {
+    // ---------------------------------------------------------------- token rows of every stage: 128 threads, 16-byte pieces into the swizzled layout
+    const int l = tid - 6 * 32, lrow = l >> 3, chunk = l & 7;
+    if (!UP) { pdl_wait(); pdl_trigger(); }
+    int stage = 0, pub = 0, pending = 0; uint32_t phase = 0;
+    bool ok = true;
+    auto publish = [&]() {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full_bar(pub));
+      if (++pub == p.stages) pub = 0;
+      --pending;
+    };
+    for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
+      const Item it = item(w);
+      const int m_all = by.off[it.e + 1] - by.off[it.e];
+      for (int n0 = 0; n0 < m_all && ok; n0 += p.cols_cap) {
+        const int m = min(m_all - n0, p.cols_cap);
+        const bf16* src[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {                // (columns past the last token hold whatever the stage held: nobody reads their sums)
+          const int a = by.list[by.off[it.e] + n0 + min(lrow + 16 * q, m - 1)];
+          src[q] = p.x + (size_t)(UP ? a / p.K : a) * p.ldx + chunk * 8;
+        }
+        for (int kb = 0; kb < it.n; ++kb) {
+          ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit));
+          if (!ok) break;
+          const uint32_t dst = base + stage * stage_bytes + x_at + lrow * 128 + ((chunk ^ (lrow & 7)) << 4);
+          const int k0 = k_of(it, kb);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (lrow + 16 * q < m) {
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + q * 16 * 128), "l"(src[q] + k0) : "memory");
+              if (k0 + BLOCK_K < p.Kd)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + x_half + q * 16 * 128), "l"(src[q] + k0 + BLOCK_K) : "memory");
+            }
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          // the stage of FT_X_FLIGHT copies ago has landed: publish it to the tensor cores
+          if (++pending > FT_X_FLIGHT) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(FT_X_FLIGHT) : "memory");
+            publish();
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    while (pending > 0) publish();
+    if (!ok && lane == 0) {
+      if (!*abort_flag) { atomicExch(p.status + kStatCode, ROM_ERR_DEVICE_TIMEOUT); atomicExch(p.status + kStatWhere, 7); }
+      *abort_flag = 1;
+    }
+  } else {
+    // ---------------------------------------------------------------- output: lane = weight row, column = token
+    const int quarter = warp & 3, r_acc = quarter * 32 + lane, ct = tid - 64;      // ct: thread of the 128 here
+    auto together = [&]() { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    if (!UP) {
+      pdl_wait();
+      for (int t = blockIdx.x; t < p.T; t += gridDim.x) {      // tokens without an expert
+        bool any = false;
+        for (int k = 0; k < p.K; ++k) { const int e = __ldg(p.idx + t * p.K + k); any |= e >= 0 && e < p.E; }
+        if (!any)
+          for (int d = 8 * ct; d < p.out_rows; d += 8 * 128) *reinterpret_cast<uint4*>(p.out + (size_t)t * p.out_rows + d) = make_uint4(0, 0, 0, 0);
+      }
+    }
+    int acc = 0; uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
+      const Item it = item(w);
+      const int row0 = it.tile * p.h, rows = min(p.h, p.out_rows - row0), m_all = by.off[it.e + 1] - by.off[it.e];
+      for (int n0 = 0; n0 < m_all && ok; n0 += p.cols_cap) {
+        const int m = min(m_all - n0, p.cols_cap);
+        const short* mine = by.list + by.off[it.e] + n0;
+        ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, wait_limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (UP) {                                    // (the four warps meet in the exchange below: they leave together)
+          int all;
+          asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.and.pred p, 2, 128, q;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(all) : "r"((int)ok) : "memory");
+          ok = all != 0;
+        }
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * FT_COLS;
+        for (int c0 = 0; c0 < m; c0 += 32) {
+          uint32_t r[32];
+          tmem_ld32_issue(taddr + c0, r);
+          tmem_ld_wait(r);
+          if (UP) {
+#pragma unroll
+            for (int jb = 0; jb < 32; jb += 16) {
+              const int nn = min(16, m - c0 - jb);
+              if (nn <= 0) break;
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < nn) exch[j][r_acc] = __uint_as_float(r[jb + j]);
+              together();
+              // gate rows are 0 .. h-1 of the accumulator, up rows h .. 2 h - 1: two hidden columns of one token a thread
+              const int half = p.h / 2;
+              for (int i = ct; i < nn * half; i += 128) {
+                const int j = i / half, rr = (i % half) * 2;
+                if (rr < rows) {
+                  const int a = mine[c0 + jb + j];
+                  const float2 g = *reinterpret_cast<const float2*>(&exch[j][rr]), u = *reinterpret_cast<const float2*>(&exch[j][p.h + rr]);
+                  const float gate = __ldg(p.gates + a);
+                  *reinterpret_cast<__nv_bfloat162*>(p.hid + (size_t)a * p.out_rows + row0 + rr) =
+                      __floats2bfloat162_rn(silu_fast(g.x) * u.x * gate, silu_fast(g.y) * u.y * gate);
+                }
+              }
+              together();
+            }
+          } else if (r_acc < rows) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              if (c0 + j >= m) break;
+              const int a = mine[c0 + j];
+              if (p.direct) p.out[(size_t)a * p.out_rows + row0 + r_acc] = __float2bfloat16_rn(__uint_as_float(r[j]));
+              else p.part[((size_t)it.part * A + a) * p.out_rows + row0 + r_acc] = __uint_as_float(r[j]);
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty_bar(acc));
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      }
+      if (!UP && !p.direct) {
+        // whoever brings the last part of these rows adds them all, in the order of slots and parts
+        __threadfence();
+        int all;
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.and.pred p, 2, 128, q;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(all) : "r"((int)ok) : "memory");
+        ok = all != 0;
+        if (!ok) break;
+        if (ct == 0) last_s = atomicAdd(p.arrived + it.tile, 1) == n_act * p.splits - 1;
+        together();
+        const bool last = last_s != 0;
+        if (last) {
+          __threadfence();
+          const int nv = rows / 4;
+          for (int i = ct; i < p.T * nv; i += 128) {
+            const int t = i / nv, d = row0 + (i % nv) * 4;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int k = 0; k < p.K; ++k) {
+              const int a = t * p.K + k, e = __ldg(p.idx + a);
+              if (e < 0 || e >= p.E) continue;
+              for (int q = 0; q < p.splits; ++q) {
+                const float4 f = __ldcg(reinterpret_cast<const float4*>(p.part + ((size_t)q * A + a) * p.out_rows + d));
+                v.x += f.x; v.y += f.y; v.z += f.z; v.w += f.w;
+              }
+            }
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+            *reinterpret_cast<uint2*>(p.out + (size_t)t * p.out_rows + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+          }
+        }
+        together();                                  // (last_s is read before it is written again)
+      }
+    }
+    if (!ok && lane == 0) {
+      if (!*abort_flag) { atomicExch(p.status + kStatCode, ROM_ERR_DEVICE_TIMEOUT); atomicExch(p.status + kStatWhere, 6); }
+      *abort_flag = 1;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * FT_COLS) : "memory");
+  }
+}
+
+cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaStream_t st) {
+  int sms = 0;
+  cudaError_t e = current_device_sm_count(&sms);
+  if (e != cudaSuccess) return e;
+  FfnTc p{};
+  p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
+  p.T = s.T; p.K = s.K; p.E = s.E;
+  // Token columns of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights
+  // again (from the L2 mostly), the others have deeper rings.
+  const int n_exp = chosen_experts(s.T, s.K, s.E), want = std::min(s.T, 2 * (s.T * s.K / n_exp) + 8);
+  p.cols_cap = want > 32 ? 64 : want > 16 ? 32 : 16;
+  auto launch = [&](auto up_tag, const void* W) {
+    constexpr bool up = decltype(up_tag)::value;
+    // (the MMA reads 128 rows from a tile's start: 16 KB past the ring's end at most)
+    const int stage = 2 * ((up ? 2 : 1) * p.h + p.cols_cap) * 128, room = FT_SMEM - 1024 - 16 * 1024;
+    p.stages = room / stage < FT_MAX_STAGES ? room / stage : FT_MAX_STAGES;
+    CUtensorMap tw;
+    if (!make_tmap(&tw, W, (uint64_t)s.E * p.w_rows, (uint64_t)p.Kd, (uint64_t)p.Kd, p.h)) return cudaErrorInvalidValue;
+    cudaError_t rc = cudaFuncSetAttribute(ffn_step_tc<up>, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
+    if (rc != cudaSuccess) return rc;
+    count_launch();
+    return launch_k(ffn_step_tc<up>, dim3(sms), FT_THREADS, FT_SMEM, st, tw, p, WAIT_LIMIT);
+  };
+  const FfnCut cu = cut_up(s.T, s.K, s.E, s.Dm, s.F), cd = cut_down(s.T, s.K, s.E, s.Dm, s.F);
+  p.x = static_cast<const bf16*>(s.x); p.ldx = s.Dm; p.Kd = s.Dm; p.w_rows = 2 * s.F; p.out_rows = s.F;
+  p.h = cu.h; p.tiles = (s.F + cu.h - 1) / cu.h; p.splits = 1;
+  if ((e = launch(std::true_type{}, s.W_gu)) != cudaSuccess) return e;
+  p.x = p.hid; p.ldx = s.F; p.Kd = s.F; p.w_rows = s.Dm; p.out_rows = s.Dm;
+  p.h = cd.h; p.tiles = (s.Dm + cd.h - 1) / cd.h; p.splits = cd.splits; p.direct = s.K == 1 && cd.splits == 1;
+  return launch(std::false_type{}, s.W_down);
 }
 
 int check_ffn_step(const rom_config* c, int d_ff) {
@@ -175,15 +580,21 @@ int check_ffn_step(const rom_config* c, int d_ff) {
   if (c->d_model < 64 || c->d_model % 64 != 0) return ROM_ERR_INVALID_ARG;
   if (d_ff < 128 || d_ff % 128 != 0) return d_ff < 1 ? ROM_ERR_INVALID_ARG : ROM_ERR_UNSUPPORTED;
   if ((int64_t)c->B * c->L > kFfnStepTokens) return ROM_ERR_UNSUPPORTED;
+  if (c->d_model > 32 * kFfnMaxTiles || (int64_t)c->E * 2 * d_ff >= (int64_t)1 << 31 || (int64_t)c->E * c->d_model >= (int64_t)1 << 31) return ROM_ERR_UNSUPPORTED;
   return ROM_OK;
 }
-struct FfnStepWs { size_t status, hid, total; };
+struct FfnStepWs { size_t status, arrived, hid, part, total; };
 FfnStepWs ffn_step_ws(const rom_config& c, int d_ff) {
   FfnStepWs l{};
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
   l.status = take(sizeof(int32_t) * kStatusInts);
-  l.hid = take((c.dtype == ROM_BF16 ? 2 : 4) * (size_t)c.B * c.L * c.K * d_ff);
+  const bool tc = c.dtype == ROM_BF16;
+  const size_t A = (size_t)c.B * c.L * c.K;
+  l.arrived = take(tc ? sizeof(int32_t) * kFfnMaxTiles : 0);
+  l.hid = take((tc ? 2 : 4) * A * d_ff);
+  const FfnCut cd = cut_down(c.B * c.L, c.K, c.E, c.d_model, d_ff);
+  l.part = take(tc && !(c.K == 1 && cd.splits == 1) ? sizeof(float) * cd.splits * A * c.d_model : 0);
   l.total = o;
   return l;
 }
@@ -220,7 +631,8 @@ int rom_ffn_moe_step(const rom_config* cfg, int32_t d_ff, const void* W_gu, cons
   char* W = static_cast<char*>(ws);
   const FfnStep p{x, W_gu, W_down, topk_idx, gates, out, W + lay.hid, reinterpret_cast<int32_t*>(W + lay.status), c.B * c.L, c.K, c.E, c.d_model, d_ff};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = c.dtype == ROM_BF16 ? launch_ffn_rows<__nv_bfloat16>(p, st) : launch_ffn_rows<float>(p, st);
+  const cudaError_t e = c.dtype == ROM_BF16 ? launch_ffn_tc(p, reinterpret_cast<float*>(W + lay.part), reinterpret_cast<int32_t*>(W + lay.arrived), st)
+                                            : launch_ffn_rows(p, st);
   return e == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
 
