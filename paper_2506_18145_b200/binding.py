@@ -146,7 +146,8 @@ def _ptr(t: Optional[torch.Tensor], cuda: bool = True) -> Optional[int]:
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
-    return (stream or torch.cuda.current_stream()).cuda_stream
+    # (the current stream's handle alone: 0.2 us, where the Stream object around it takes 3.3)
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def workspace_size(cfg: RomConfig) -> int:
@@ -321,17 +322,18 @@ def _rows_ptr(t: Optional[torch.Tensor]):
         return None, 0
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    if t.dim() != 2 or t.stride(1) != 1:
+    pitch = t.stride()
+    if len(pitch) != 2 or pitch[1] != 1:
         raise ValueError("expected a tensor [rows, width] with contiguous rows")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]      # (a single row has no pitch: torch may say anything)
+    rows, width = t.shape
+    return t.data_ptr(), pitch[0] if rows > 1 else width      # (a single row has no pitch: torch may say anything)
 
 
-def _pool(*pools: Optional[torch.Tensor]) -> int:
+def _pool(a: torch.Tensor, b: torch.Tensor) -> int:
     """Slots of the state pools of a call."""
-    n = {p.shape[0] for p in pools if p is not None}
-    if len(n) > 1:
+    if a.size(0) != b.size(0):
         raise ValueError("the pools differ in their slots")
-    return n.pop() if n else 0
+    return a.size(0)
 
 
 def make_ragged(rows: int, n_slots: int, seq_start, slot=None, resume=None) -> RomRagged:

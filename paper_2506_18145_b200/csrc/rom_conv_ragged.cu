@@ -1,7 +1,9 @@
 // Causal depthwise conv + SiLU over packed sequences (rom_conv_ragged): y_t = SiLU(b + sum_j w_j x_{t-(k-1)+j}), windows carried in slots.
 //
-// HBM bounds it: every row is read and written once, 4 bytes a channel (bf16).  A warp has 256 channels (16 or 32 bytes a lane) of a tile of
-// rows, which it walks with the window in registers, RB rows in flight; the rows before a tile are read again, from the L2 mostly.
+// HBM bounds it: every row is read and written once, 4 bytes a channel (bf16); the special-function unit is next (two operations a value).
+// A warp has 256 channels (16 or 32 bytes a lane) of a tile of rows, which it walks with the window in registers, RB rows computed while
+// the next RB are on their way; the rows before a tile are read again, from the L2 mostly.  The first rows are requested before the
+// search for the tile's sequences, which takes two dependent loads.
 //
 // A tile takes the sequences that start in it and what reaches into it from before.  The first k-1 rows of a sequence need its old window, so they all
 // belong to the tile in which it starts, even past the tile's end; the same thread then writes the new window.  Nobody else reads or
@@ -11,56 +13,71 @@
 namespace rom {
 namespace {
 
-constexpr int CR_WARPS = 4;
+constexpr int CR_WARPS = 4, CR_ROWS = 4;      // warps per block; rows in flight
+constexpr int kConvWarps = 148 * 16;
+
+// eight channels of a row as packed pairs
+__device__ __forceinline__ void unpack(const Raw8<__nv_bfloat16>& q, float2 (&v)[4]) {
+  const uint32_t w[4] = {q.q.x, q.q.y, q.q.z, q.q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void unpack(const Raw8<float>& q, float2 (&v)[4]) {
+  v[0] = make_float2(q.a.x, q.a.y); v[1] = make_float2(q.a.z, q.a.w); v[2] = make_float2(q.b.x, q.b.y); v[3] = make_float2(q.b.z, q.b.w);
+}
 
 template <typename T, int KC>
 struct ConvRows {
-  static constexpr int RB = sizeof(T) == 2 ? 8 : 4;      // rows in flight
   const T* x; long long ldx; T* y; int De, c;
-  float w[KC][8], bias[8], win[KC - 1][8];
+  float2 w[KC][4], bias[4], win[KC - 1][4];
 
-  __device__ __forceinline__ void shift(const float (&v)[8]) {
-#pragma unroll
-    for (int q = 0; q + 1 < KC - 1; ++q)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) win[q][i] = win[q + 1][i];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) win[KC - 2][i] = v[i];
-  }
-  __device__ __forceinline__ void load_row(int r, float (&v)[8]) const {
+  __device__ __forceinline__ Raw8<T> load(int r) const {
     Raw8<T> q;
     q.load(x + (size_t)r * ldx + c);
-    q.get(v);
+    return q;
   }
-  // rows [a, b), the window holding the k-1 rows before a
-  __device__ __forceinline__ void walk(int a, int b) {
-    for (int r0 = a; r0 < b; r0 += RB) {
-      Raw8<T> q[RB];
+  __device__ __forceinline__ void put(int r, const Raw8<T>& q) {
+    float2 v[4];
+    float o[8];
+    unpack(q, v);
 #pragma unroll
-      for (int k = 0; k < RB; ++k)
-        if (r0 + k < b) q[k].load(x + (size_t)(r0 + k) * ldx + c);
+    for (int i = 0; i < 4; ++i) {
+      float2 u = bias[i];
 #pragma unroll
-      for (int k = 0; k < RB; ++k)
-        if (r0 + k < b) {
-          float v[8], u[8];
-          q[k].get(v);
+      for (int j = 0; j < KC - 1; ++j) u = __ffma2_rn(w[j][i], win[j][i], u);
+      u = __ffma2_rn(w[KC - 1][i], v[i], u);
+      if (sizeof(T) == 2) {
+        const float2 t = __fmul2_rn(u, make_float2(-1.4426950408889634f, -1.4426950408889634f));
+        const float2 d = __fadd2_rn(make_float2(ex2_ftz(t.x), ex2_ftz(t.y)), make_float2(1.0f, 1.0f));
+        u = __fmul2_rn(u, make_float2(rcp_ftz(d.x), rcp_ftz(d.y)));
+      } else {
+        u = make_float2(silu_f(u.x), silu_f(u.y));
+      }
+      o[2 * i] = u.x; o[2 * i + 1] = u.y;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            u[i] = bias[i];
+      for (int j = 0; j + 1 < KC - 1; ++j) win[j][i] = win[j + 1][i];
+      win[KC - 2][i] = v[i];
+    }
+    Raw8<T>::store(y + (size_t)r * De + c, o);
+  }
+  // rows [a, b), the window holding the k-1 rows before a, the first CR_ROWS rows requested
+  __device__ __forceinline__ void walk(int a, int b, Raw8<T> (&q)[CR_ROWS]) {
+    for (int r0 = a; r0 < b; r0 += CR_ROWS) {
+      Raw8<T> cur[CR_ROWS];
 #pragma unroll
-            for (int j = 0; j < KC - 1; ++j) u[i] = fmaf(w[j][i], win[j][i], u[i]);
-            u[i] = fmaf(w[KC - 1][i], v[i], u[i]);
-            u[i] = sizeof(T) == 2 ? silu_fast(u[i]) : silu_f(u[i]);
-          }
-          Raw8<T>::store(y + (size_t)(r0 + k) * De + c, u);
-          shift(v);
-        }
+      for (int k = 0; k < CR_ROWS; ++k) cur[k] = q[k];
+      if (r0 + CR_ROWS < b)
+#pragma unroll
+        for (int k = 0; k < CR_ROWS; ++k) q[k] = load(min(r0 + CR_ROWS + k, b - 1));
+#pragma unroll
+      for (int k = 0; k < CR_ROWS; ++k)
+        if (r0 + k < b) put(r0 + k, cur[k]);
     }
   }
 };
 
 template <typename T, int KC>
-__global__ void __launch_bounds__(CR_WARPS * 32)
+__global__ void __launch_bounds__(CR_WARPS * 32, sizeof(T) == 2 ? 4 : 2)
 conv_ragged_kernel(const Ragged s, const T* __restrict__ x, long long ldx, const T* __restrict__ w, const float* __restrict__ bias,
                    const float* win_in, float* win_out, T* __restrict__ y, int De, int tile, int n_tiles) {
   pdl_sync();
@@ -71,64 +88,67 @@ conv_ragged_kernel(const Ragged s, const T* __restrict__ x, long long ldx, const
   const int c = ((int)(item % cb) * 32 + lane) * 8;
   const bool on = c < De;                                  // (a whole warp stays for the search)
   const int r0 = ti * tile, r1 = min(r0 + tile, s.rows);
+  ConvRows<T, KC> cr;
+  cr.x = x; cr.ldx = ldx; cr.y = y; cr.De = De; cr.c = on ? c : 0;
+  Raw8<T> q[CR_ROWS], halo[KC - 1], wq[KC];
+  if (s.rows > 0) {
+#pragma unroll
+    for (int k = 0; k < KC - 1; ++k) halo[k] = cr.load(max(r0 - (KC - 1) + k, 0));
+#pragma unroll
+    for (int k = 0; k < CR_ROWS; ++k) q[k] = cr.load(min(r0 + k, s.rows - 1));      // (a sequence may go on past r1)
+  }
+#pragma unroll
+  for (int j = 0; j < KC; ++j) wq[j].load(w + (size_t)j * De + cr.c);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) cr.bias[i] = bias ? make_float2(__ldg(bias + cr.c + 2 * i), __ldg(bias + cr.c + 2 * i + 1)) : make_float2(0.0f, 0.0f);
   const int s0 = s.first_from(r0);
   if (!on) return;
-  ConvRows<T, KC> cr;
-  cr.x = x; cr.ldx = ldx; cr.y = y; cr.De = De; cr.c = c;
-  {
-    Raw8<T> q[KC];
 #pragma unroll
-    for (int j = 0; j < KC; ++j) q[j].load(w + (size_t)j * De + c);
-#pragma unroll
-    for (int j = 0; j < KC; ++j) q[j].get(cr.w[j]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cr.bias[i] = bias ? __ldg(bias + c + i) : 0.0f;
-  }
-  if (s0 > 0) {                                            // what reaches into the tile: its rows from the k-1st on
-    const int first = s.start_of(s0 - 1), a = max(r0, first + KC - 1), b = min(r1, s.end_of(s0 - 1));
-    if (a < b) {
-#pragma unroll
-      for (int q = 0; q < KC - 1; ++q) cr.load_row(a - (KC - 1) + q, cr.win[q]);
-      cr.walk(a, b);
-    }
-  }
-  for (int i = s0; i < s.n_seq; ++i) {                     // what starts in it (the last tile: empty sequences behind the last row too)
+  for (int j = 0; j < KC; ++j) unpack(wq[j], cr.w[j]);
+  for (int i = max(s0 - 1, 0); i < s.n_seq; ++i) {
     const int first = s.start_of(i), end = s.end_of(i);
-    if (first >= r1 && !(r1 == s.rows && first == r1)) break;
-    const int slot = s.slot_of(i);
-    const size_t at = (size_t)max(slot, 0) * (KC - 1) * De + c;
-    const bool old = win_in && slot >= 0 && s.resumes(i);
-    float past[KC - 1][8];
+    int from, stop;
+    if (i < s0) {                                          // what reaches into the tile: its rows from the k-1st on
+      from = max(r0, first + KC - 1); stop = min(r1, end);
+      if (from >= stop) continue;
+      if (from > r0)
 #pragma unroll
-    for (int q = 0; q < KC - 1; ++q)
+        for (int k = 0; k < KC - 1; ++k) halo[k] = cr.load(from - (KC - 1) + k);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float4 v = old ? *reinterpret_cast<const float4*>(win_in + at + (size_t)q * De + 4 * h) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        past[q][4 * h] = v.x; past[q][4 * h + 1] = v.y; past[q][4 * h + 2] = v.z; past[q][4 * h + 3] = v.w;
-      }
-    if (win_out && slot >= 0) {                            // entry q: row end - (k-1) + q, or that far into the old window
+      for (int k = 0; k < KC - 1; ++k) unpack(halo[k], cr.win[k]);
+    } else {                                               // what starts in it (the last tile: empty sequences behind the last row too)
+      if (first >= r1 && !(r1 == s.rows && first == r1)) break;
+      from = first; stop = min(end, max(r1, first + KC - 1));
+      const int slot = s.slot_of(i);
+      const size_t at = (size_t)max(slot, 0) * (KC - 1) * De + c;
+      const bool old = win_in && slot >= 0 && s.resumes(i);
 #pragma unroll
-      for (int q = 0; q < KC - 1; ++q) {
-        float v[8];
-        const int r = end - (KC - 1) + q;
-        if (r >= first) cr.load_row(r, v);
-        else {
-#pragma unroll
-          for (int p = 0; p < KC - 1; ++p)
-            if (p == r - first + KC - 1)
-#pragma unroll
-              for (int k = 0; k < 8; ++k) v[k] = past[p][k];
+      for (int k = 0; k < KC - 1; ++k) {
+        Raw8<float> p;
+        p.zero();
+        if (old) {
+          p.a = *reinterpret_cast<const float4*>(win_in + at + (size_t)k * De);
+          p.b = *reinterpret_cast<const float4*>(win_in + at + (size_t)k * De + 4);
         }
-        float* o = win_out + at + (size_t)q * De;
-        *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        unpack(p, cr.win[k]);
       }
     }
+    if (from != r0 && from < stop)                         // (the rows at r0 are on their way)
 #pragma unroll
-    for (int q = 0; q < KC - 1; ++q)
+      for (int k = 0; k < CR_ROWS; ++k) q[k] = cr.load(min(from + k, stop - 1));
+    cr.walk(from, stop, q);
+    if (i < s0 || !win_out) continue;
+    const int slot = s.slot_of(i);
+    if (slot < 0) continue;
+    if (stop < end)                                        // it goes on past the tile, which has at least k-1 of its rows: its last ones
 #pragma unroll
-      for (int k = 0; k < 8; ++k) cr.win[q][k] = past[q][k];
-    cr.walk(first, min(end, max(r1, first + KC - 1)));
+      for (int k = 0; k < KC - 1; ++k) unpack(cr.load(end - (KC - 1) + k), cr.win[k]);
+#pragma unroll
+    for (int k = 0; k < KC - 1; ++k) {
+      float* o = win_out + ((size_t)slot * (KC - 1) + k) * De + c;
+      *reinterpret_cast<float4*>(o) = make_float4(cr.win[k][0].x, cr.win[k][0].y, cr.win[k][1].x, cr.win[k][1].y);
+      *reinterpret_cast<float4*>(o + 4) = make_float4(cr.win[k][2].x, cr.win[k][2].y, cr.win[k][3].x, cr.win[k][3].y);
+    }
   }
 }
 
@@ -136,8 +156,10 @@ template <typename T>
 cudaError_t launch_conv_ragged(const rom_config& c, const Ragged& s, const void* x, int64_t ldx, const void* w, const float* bias, const float* win_in,
                                float* win_out, void* y, cudaStream_t st) {
   auto kern = c.d_conv == 2 ? conv_ragged_kernel<T, 2> : c.d_conv == 3 ? conv_ragged_kernel<T, 3> : conv_ragged_kernel<T, 4>;
-  const int tile = 16;
   const long long cb = (c.d_inner / 8 + 31) / 32;
+  // Rows per tile: 16, fewer while that leaves the GPU short of warps: the sequences that start in a tile are walked one after the other.
+  const long long fit = (cb * s.rows + kConvWarps - 1) / kConvWarps;
+  const int tile = fit < 1 ? 1 : fit > 16 ? 16 : (int)fit;
   const int n_tiles = s.rows > 0 ? (s.rows + tile - 1) / tile : 1;
   const long long blocks = (cb * n_tiles + CR_WARPS - 1) / CR_WARPS;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
