@@ -1,7 +1,7 @@
 // Causal depthwise conv + SiLU over packed sequences (rom_conv_ragged): y_t = SiLU(b + sum_j w_j x_{t-(k-1)+j}), windows carried in slots.
 //
 // HBM bounds it: every row is read and written once, 4 bytes a channel (bf16); the special-function unit is next (two operations a value).
-// A warp has 256 channels (16 or 32 bytes a lane) of a tile of rows, which it walks with the window in registers, RB rows computed while
+// A warp has 256 (bf16) or 128 channels, 16 bytes a lane, of a tile of rows, which it walks with the window in registers, RB rows computed while
 // the next RB are on their way; the rows before a tile are read again, from the L2 mostly.  The first rows are requested before the
 // search for the tile's sequences, which takes two dependent loads.
 //
@@ -16,32 +16,32 @@ namespace {
 constexpr int CR_WARPS = 4, CR_ROWS = 4;      // warps per block; rows in flight
 constexpr int kConvWarps = 148 * 16;
 
-// eight channels of a row as packed pairs
-__device__ __forceinline__ void unpack(const Raw8<__nv_bfloat16>& q, float2 (&v)[4]) {
-  const uint32_t w[4] = {q.q.x, q.q.y, q.q.z, q.q.w};
+// 16 bytes of a row as packed pairs
+template <typename T>
+__device__ __forceinline__ void unpack(const V16<T>& q, float2 (&v)[V16<T>::N / 2]) {
+  float f[V16<T>::N];
+  q.get(f);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-}
-__device__ __forceinline__ void unpack(const Raw8<float>& q, float2 (&v)[4]) {
-  v[0] = make_float2(q.a.x, q.a.y); v[1] = make_float2(q.a.z, q.a.w); v[2] = make_float2(q.b.x, q.b.y); v[3] = make_float2(q.b.z, q.b.w);
+  for (int i = 0; i < V16<T>::N / 2; ++i) v[i] = make_float2(f[2 * i], f[2 * i + 1]);
 }
 
 template <typename T, int KC>
 struct ConvRows {
+  static constexpr int P = V16<T>::N / 2;      // pairs a lane
   const T* x; long long ldx; T* y; int De, c;
-  float2 w[KC][4], bias[4], win[KC - 1][4];
+  float2 w[KC][P], bias[P], win[KC - 1][P];
 
-  __device__ __forceinline__ Raw8<T> load(int r) const {
-    Raw8<T> q;
+  __device__ __forceinline__ V16<T> load(int r) const {
+    V16<T> q;
     q.load(x + (size_t)r * ldx + c);
     return q;
   }
-  __device__ __forceinline__ void put(int r, const Raw8<T>& q) {
-    float2 v[4];
-    float o[8];
+  __device__ __forceinline__ void put(int r, const V16<T>& q) {
+    float2 v[P];
+    float o[2 * P];
     unpack(q, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < P; ++i) {
       float2 u = bias[i];
 #pragma unroll
       for (int j = 0; j < KC - 1; ++j) u = __ffma2_rn(w[j][i], win[j][i], u);
@@ -58,12 +58,12 @@ struct ConvRows {
       for (int j = 0; j + 1 < KC - 1; ++j) win[j][i] = win[j + 1][i];
       win[KC - 2][i] = v[i];
     }
-    Raw8<T>::store(y + (size_t)r * De + c, o);
+    V16<T>::store(y + (size_t)r * De + c, o);
   }
   // rows [a, b), the window holding the k-1 rows before a, the first CR_ROWS rows requested
-  __device__ __forceinline__ void walk(int a, int b, Raw8<T> (&q)[CR_ROWS]) {
+  __device__ __forceinline__ void walk(int a, int b, V16<T> (&q)[CR_ROWS]) {
     for (int r0 = a; r0 < b; r0 += CR_ROWS) {
-      Raw8<T> cur[CR_ROWS];
+      V16<T> cur[CR_ROWS];
 #pragma unroll
       for (int k = 0; k < CR_ROWS; ++k) cur[k] = q[k];
       if (r0 + CR_ROWS < b)
@@ -77,20 +77,21 @@ struct ConvRows {
 };
 
 template <typename T, int KC>
-__global__ void __launch_bounds__(CR_WARPS * 32, sizeof(T) == 2 ? 4 : 2)
+__global__ void __launch_bounds__(CR_WARPS * 32, 4)
 conv_ragged_kernel(const Ragged s, const T* __restrict__ x, long long ldx, const T* __restrict__ w, const float* __restrict__ bias,
                    const float* win_in, float* win_out, T* __restrict__ y, int De, int tile, int n_tiles) {
   pdl_sync();
   const int lane = threadIdx.x & 31;
   const long long item = (long long)blockIdx.x * CR_WARPS + (threadIdx.x >> 5);
-  const int cb = (De / 8 + 31) / 32, ti = (int)(item / cb);
+  constexpr int P = V16<T>::N / 2;
+  const int cb = (De + 64 * P - 1) / (64 * P), ti = (int)(item / cb);
   if (ti >= n_tiles) return;
-  const int c = ((int)(item % cb) * 32 + lane) * 8;
+  const int c = ((int)(item % cb) * 32 + lane) * 2 * P;
   const bool on = c < De;                                  // (a whole warp stays for the search)
   const int r0 = ti * tile, r1 = min(r0 + tile, s.rows);
   ConvRows<T, KC> cr;
   cr.x = x; cr.ldx = ldx; cr.y = y; cr.De = De; cr.c = on ? c : 0;
-  Raw8<T> q[CR_ROWS], halo[KC - 1], wq[KC];
+  V16<T> q[CR_ROWS], halo[KC - 1], wq[KC];
   if (s.rows > 0) {
 #pragma unroll
     for (int k = 0; k < KC - 1; ++k) halo[k] = cr.load(max(r0 - (KC - 1) + k, 0));
@@ -100,7 +101,7 @@ conv_ragged_kernel(const Ragged s, const T* __restrict__ x, long long ldx, const
 #pragma unroll
   for (int j = 0; j < KC; ++j) wq[j].load(w + (size_t)j * De + cr.c);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) cr.bias[i] = bias ? make_float2(__ldg(bias + cr.c + 2 * i), __ldg(bias + cr.c + 2 * i + 1)) : make_float2(0.0f, 0.0f);
+  for (int i = 0; i < P; ++i) cr.bias[i] = bias ? make_float2(__ldg(bias + cr.c + 2 * i), __ldg(bias + cr.c + 2 * i + 1)) : make_float2(0.0f, 0.0f);
   const int s0 = s.first_from(r0);
   if (!on) return;
 #pragma unroll
@@ -123,15 +124,12 @@ conv_ragged_kernel(const Ragged s, const T* __restrict__ x, long long ldx, const
       const size_t at = (size_t)max(slot, 0) * (KC - 1) * De + c;
       const bool old = win_in && slot >= 0 && s.resumes(i);
 #pragma unroll
-      for (int k = 0; k < KC - 1; ++k) {
-        Raw8<float> p;
-        p.zero();
-        if (old) {
-          p.a = *reinterpret_cast<const float4*>(win_in + at + (size_t)k * De);
-          p.b = *reinterpret_cast<const float4*>(win_in + at + (size_t)k * De + 4);
+      for (int k = 0; k < KC - 1; ++k)
+#pragma unroll
+        for (int n = 0; n < P / 2; ++n) {
+          const float4 p = old ? *reinterpret_cast<const float4*>(win_in + at + (size_t)k * De + 4 * n) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          cr.win[k][2 * n] = make_float2(p.x, p.y); cr.win[k][2 * n + 1] = make_float2(p.z, p.w);
         }
-        unpack(p, cr.win[k]);
-      }
     }
     if (from != r0 && from < stop)                         // (the rows at r0 are on their way)
 #pragma unroll
@@ -146,8 +144,9 @@ conv_ragged_kernel(const Ragged s, const T* __restrict__ x, long long ldx, const
 #pragma unroll
     for (int k = 0; k < KC - 1; ++k) {
       float* o = win_out + ((size_t)slot * (KC - 1) + k) * De + c;
-      *reinterpret_cast<float4*>(o) = make_float4(cr.win[k][0].x, cr.win[k][0].y, cr.win[k][1].x, cr.win[k][1].y);
-      *reinterpret_cast<float4*>(o + 4) = make_float4(cr.win[k][2].x, cr.win[k][2].y, cr.win[k][3].x, cr.win[k][3].y);
+#pragma unroll
+      for (int i = 0; i < P / 2; ++i)
+        *reinterpret_cast<float4*>(o + 4 * i) = make_float4(cr.win[k][2 * i].x, cr.win[k][2 * i].y, cr.win[k][2 * i + 1].x, cr.win[k][2 * i + 1].y);
     }
   }
 }
@@ -156,10 +155,10 @@ template <typename T>
 cudaError_t launch_conv_ragged(const rom_config& c, const Ragged& s, const void* x, int64_t ldx, const void* w, const float* bias, const float* win_in,
                                float* win_out, void* y, cudaStream_t st) {
   auto kern = c.d_conv == 2 ? conv_ragged_kernel<T, 2> : c.d_conv == 3 ? conv_ragged_kernel<T, 3> : conv_ragged_kernel<T, 4>;
-  const long long cb = (c.d_inner / 8 + 31) / 32;
-  // Rows per tile: 16, fewer while that leaves the GPU short of warps: the sequences that start in a tile are walked one after the other.
+  const long long cb = (c.d_inner + 32 * V16<T>::N - 1) / (32 * V16<T>::N);
+  // Rows per tile: 32 (16384 x 4096: 8 rows 64.2 us, 16 56.2, 32 53.8, 56 53.1, 111 52.6), fewer while that leaves the GPU short of warps: the sequences that start in a tile are walked one after the other.
   const long long fit = (cb * s.rows + kConvWarps - 1) / kConvWarps;
-  const int tile = fit < 1 ? 1 : fit > 16 ? 16 : (int)fit;
+  const int tile = fit < 1 ? 1 : fit > 32 ? 32 : (int)fit;
   const int n_tiles = s.rows > 0 ? (s.rows + tile - 1) / tile : 1;
   const long long blocks = (cb * n_tiles + CR_WARPS - 1) / CR_WARPS;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
