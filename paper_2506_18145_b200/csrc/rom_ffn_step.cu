@@ -26,30 +26,51 @@ struct FfnStep {
 struct ByExpert {
   int off[kMaxE + 1];
   short list[kFfnStepAssign];
+  signed char of[kFfnStepAssign];      // expert of an assignment, -1: none
   // all threads of the block; ends with a barrier
   __device__ __forceinline__ void build(const int32_t* idx, int A, int E) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    for (int a = threadIdx.x; a < A; a += blockDim.x) {
+      const int e = __ldg(idx + a);
+      of[a] = e >= 0 && e < E ? (signed char)e : (signed char)-1;
+    }
+    __syncthreads();
     for (int e = warp; e < E; e += warps) {
       int n = 0;
-      for (int a0 = 0; a0 < A; a0 += 32) n += __popc(__ballot_sync(0xffffffffu, a0 + lane < A && __ldg(idx + a0 + lane) == e));
+      for (int a0 = 0; a0 < A; a0 += 32) n += __popc(__ballot_sync(0xffffffffu, a0 + lane < A && of[a0 + lane] == e));
       if (lane == 0) off[e + 1] = n;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      off[0] = 0;
-      for (int e = 0; e < E; ++e) off[e + 1] += off[e];
+    if (warp == 0) {                   // sums before every expert: two experts a lane
+      const int c0 = 2 * lane < E ? off[2 * lane + 1] : 0, c1 = 2 * lane + 1 < E ? off[2 * lane + 2] : 0;
+      int sum = c0 + c1;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += v;
+      }
+      __syncwarp();
+      if (lane == 0) off[0] = 0;
+      if (2 * lane < E) off[2 * lane + 1] = sum - c1;
+      if (2 * lane + 1 < E) off[2 * lane + 2] = sum;
     }
     __syncthreads();
     for (int e = warp; e < E; e += warps) {
       int n = off[e];
       if (n == off[e + 1]) continue;
       for (int a0 = 0; a0 < A; a0 += 32) {
-        const unsigned m = __ballot_sync(0xffffffffu, a0 + lane < A && __ldg(idx + a0 + lane) == e);
+        const unsigned m = __ballot_sync(0xffffffffu, a0 + lane < A && of[a0 + lane] == e);
         if ((m >> lane) & 1u) list[n + __popc(m & ((1u << lane) - 1u))] = (short)(a0 + lane);
         n += __popc(m);
       }
     }
     __syncthreads();
+  }
+  // the i-th expert that somebody chose, -1: there are fewer
+  __device__ __forceinline__ int chosen(int i, int E) const {
+    for (int e = 0; e < E; ++e)
+      if (off[e + 1] > off[e] && i-- == 0) return e;
+    return -1;
   }
 };
 // The status word of the call: cleared, or an expert index beyond the last one.
@@ -76,14 +97,14 @@ __device__ __forceinline__ float sum_to_lane(float (&v)[32]) {
 }
 
 // ---------------------------------------------------------------------------------------------- fp32
-// Four weight rows times up to eight rows of activations, over the lanes of a warp; lane 8 r + j gets row r times activation j.
-__device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const float* const (&x)[8], int n, int Kd) {
+// Four weight rows times up to eight rows of activations, elements [k0, k1), over the lanes of a warp; lane 8 r + j gets row r times activation j.
+__device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const float* const (&x)[8], int n, int k0, int k1) {
   constexpr int V = 4;
   const int lane = threadIdx.x & 31;
   float acc[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
-  for (int k = lane * V; k < Kd; k += 32 * V) {
+  for (int k = k0 + lane * V; k < k1; k += 32 * V) {
     V16<float> wq[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) wq[r].load(w[r] + k);
@@ -106,45 +127,47 @@ __device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const floa
   return sum_to_lane(acc);
 }
 
-constexpr int FR_WARPS = 4;
-__global__ void __launch_bounds__(FR_WARPS * 32)
+// A warp has two hidden columns of one expert.
+constexpr int FR_UP_WARPS = 4;
+__global__ void __launch_bounds__(FR_UP_WARPS * 32)
 ffn_step_up(const FfnStep p) {
   __shared__ ByExpert by;
   pdl_sync();
-  if (blockIdx.x == 0) ffn_status(p);
+  if (blockIdx.x == 0 && blockIdx.y == 0) ffn_status(p);
   by.build(p.idx, p.T * p.K, p.E);
   const int lane = threadIdx.x & 31, j = lane & 7;
-  const int f = (blockIdx.x * FR_WARPS + (threadIdx.x >> 5)) * 2;      // a warp has two hidden columns of every expert
-  for (int e = 0; e < p.E; ++e) {
-    const float* g = static_cast<const float*>(p.W_gu) + ((size_t)e * 2 * p.F + f) * p.Dm;
-    const float* u = g + (size_t)p.F * p.Dm;
-    const float* const w[4] = {g, g + p.Dm, u, u + p.Dm};
-    for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
-      const int n = min(8, by.off[e + 1] - a0);
-      const float* x[8];
+  const int f = (blockIdx.x * FR_UP_WARPS + (threadIdx.x >> 5)) * 2, e = by.chosen(blockIdx.y, p.E);
+  if (e < 0) return;
+  const float* g = static_cast<const float*>(p.W_gu) + ((size_t)e * 2 * p.F + f) * p.Dm;
+  const float* u = g + (size_t)p.F * p.Dm;
+  const float* const w[4] = {g, g + p.Dm, u, u + p.Dm};
+  for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
+    const int n = min(8, by.off[e + 1] - a0);
+    const float* x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.x) + (size_t)(by.list[a0 + min(i, n - 1)] / p.K) * p.Dm;
-      const float v = rows_4x8(w, x, n, p.Dm);
-      const float up = __shfl_down_sync(0xffffffffu, v, 16);
-      if (lane < 16 && j < n) {
-        const int a = by.list[a0 + j];
-        static_cast<float*>(p.hid)[(size_t)a * p.F + f + (lane >> 3)] = (silu_f(v) * up * __ldg(p.gates + a));
-      }
+    for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.x) + (size_t)(by.list[a0 + min(i, n - 1)] / p.K) * p.Dm;
+    const float v = rows_4x8(w, x, n, 0, p.Dm);
+    const float up = __shfl_down_sync(0xffffffffu, v, 16);
+    if (lane < 16 && j < n) {
+      const int a = by.list[a0 + j];
+      static_cast<float*>(p.hid)[(size_t)a * p.F + f + (lane >> 3)] = silu_f(v) * up * __ldg(p.gates + a);
     }
   }
 }
-__global__ void __launch_bounds__(FR_WARPS * 32)
+// A block has four rows of the output; its warps share the contracted index of every expert and add their sums at the end, in order.
+constexpr int FR_DOWN_WARPS = 8;
+__global__ void __launch_bounds__(FR_DOWN_WARPS * 32)
 ffn_step_down(const FfnStep p) {
   __shared__ ByExpert by;
-  __shared__ float sum[FR_WARPS][kFfnStepTokens][4];
+  __shared__ float sum[FR_DOWN_WARPS][kFfnStepTokens][4];
   by.build(p.idx, p.T * p.K, p.E);
   pdl_sync();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int d = (blockIdx.x * FR_WARPS + warp) * 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 4;
+  const int part = (p.F / 128 + FR_DOWN_WARPS - 1) / FR_DOWN_WARPS * 128, k0 = min(warp * part, p.F), k1 = min(k0 + part, p.F);
   float (*s)[4] = sum[warp];
   for (int t = lane; t < p.T * 4; t += 32) s[t >> 2][t & 3] = 0.0f;
   __syncwarp();
-  for (int e = 0; e < p.E; ++e) {
+  for (int e = 0; e < p.E && k0 < k1; ++e) {
     const float* w0 = static_cast<const float*>(p.W_down) + ((size_t)e * p.Dm + d) * p.F;
     const float* const w[4] = {w0, w0 + p.F, w0 + 2 * (size_t)p.F, w0 + 3 * (size_t)p.F};
     for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
@@ -152,32 +175,38 @@ ffn_step_down(const FfnStep p) {
       const float* x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.hid) + (size_t)by.list[a0 + min(i, n - 1)] * p.F;
-      const float v = rows_4x8(w, x, n, p.F);
+      const float v = rows_4x8(w, x, n, k0, k1);
       for (int i = 0; i < n; ++i) {      // one at a time: two of them may be of one token
         if ((lane & 7) == i) s[by.list[a0 + i] / p.K][lane >> 3] += v;
         __syncwarp();
       }
     }
   }
-  for (int t = lane; t < p.T * 4; t += 32) static_cast<float*>(p.out)[(size_t)(t >> 2) * p.Dm + d + (t & 3)] = (s[t >> 2][t & 3]);
+  __syncthreads();
+  for (int t = threadIdx.x; t < p.T * 4; t += FR_DOWN_WARPS * 32) {
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < FR_DOWN_WARPS; ++w) v += sum[w][t >> 2][t & 3];
+    static_cast<float*>(p.out)[(size_t)(t >> 2) * p.Dm + d + (t & 3)] = v;
+  }
 }
 
 cudaError_t launch_ffn_rows(const FfnStep& p, cudaStream_t st) {
-  cudaError_t e = launch_k(ffn_step_up, dim3(p.F / (2 * FR_WARPS)), FR_WARPS * 32, 0, st, p);
+  const int A = p.T * p.K;
+  cudaError_t e = launch_k(ffn_step_up, dim3(p.F / (2 * FR_UP_WARPS), A < p.E ? A : p.E), FR_UP_WARPS * 32, 0, st, p);
   if (e != cudaSuccess) return e;
   count_launch();
-  e = launch_k(ffn_step_down, dim3(p.Dm / (4 * FR_WARPS)), FR_WARPS * 32, 0, st, p);
+  e = launch_k(ffn_step_down, dim3(p.Dm / 4), FR_DOWN_WARPS * 32, 0, st, p);
   count_launch();
   return e;
 }
 
 // ---------------------------------------------------------------------------------------------- bf16: streamed weights
 constexpr int FT_COLS = 64;                          // token columns per pass at most
-constexpr int FT_MAX_STAGES = 10;
-constexpr int FT_X_FLIGHT = 2;                       // stages of token rows in flight
-constexpr int FT_SMEM = 208 * 1024;                  // operand ring, with its alignment and what the MMA reads past a short tile
+constexpr int FT_MAX_STAGES = 12;
+constexpr int FT_SMEM = 208 * 1024, FT_SMEM_PAIR = 104 * 1024;      // operand ring, alone on an SM or beside the other launch's
 constexpr int FT_THREADS = 320;
-constexpr int FT_K = 2 * BLOCK_K;                    // contracted elements per stage
+constexpr int FT_K = BLOCK_K;                        // contracted elements per stage: one swizzled row
 
 // Experts that T tokens with K choices each of E name, about.
 int chosen_experts(int T, int K, int E) {
@@ -224,8 +253,9 @@ struct FfnTc {
   int direct;                                        // down: one expert and one part a token: written at once
 };
 
-template <bool UP>
-__global__ void __launch_bounds__(FT_THREADS, 1)
+// FLIGHT: stages of token rows in flight, fewer than there are stages.
+template <bool UP, int FLIGHT>
+__global__ void __launch_bounds__(FT_THREADS, 2)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -257,11 +287,12 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   }
   if (UP) { pdl_wait(); pdl_trigger(); }             // (down: the choice of experts is older than the launch before)
   by.build(p.idx, A, p.E);
-  if (tid == 0) {
-    int n = 0;
-    for (int e = 0; e < p.E; ++e)
-      if (by.off[e + 1] > by.off[e]) act[n++] = e;
-    n_act_s = n;
+  if (warp == 0) {                                   // the experts that somebody chose
+    const bool lo = lane < p.E && by.off[lane + 1] > by.off[lane], hi = 32 + lane < p.E && by.off[33 + lane] > by.off[32 + lane];
+    const unsigned ml = __ballot_sync(0xffffffffu, lo), mh = __ballot_sync(0xffffffffu, hi), below = (1u << lane) - 1u;
+    if (lo) act[__popc(ml & below)] = lane;
+    if (hi) act[__popc(ml) + __popc(mh & below)] = 32 + lane;
+    if (lane == 0) n_act_s = __popc(ml) + __popc(mh);
   }
   if (UP && blockIdx.x == 0) {
     bool bad = false;
@@ -276,7 +307,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   const uint32_t tmem_base = tmem_s;
   const int n_act = n_act_s, per_expert = p.tiles * p.splits, total = n_act * per_expert;
   const int num_kb = (p.Kd + FT_K - 1) / FT_K;
-  const uint32_t w_half = (UP ? 2 : 1) * p.h * 128, x_half = p.cols_cap * 128, x_at = 2 * w_half, stage_bytes = 2 * (w_half + x_half);
+  const uint32_t w_bytes = (UP ? 2 : 1) * p.h * 128, stage_bytes = w_bytes + p.cols_cap * 128;
   auto cols = [](int m) { return m > 32 ? 64 : m > 16 ? 32 : 16; };      // N of a pass over m tokens
   // item w: expert, first row, stages [kb0, kb0 + n) of the contracted index, walked from a start of the tile's own: in step all CTAs
   // would read the same columns of rows that are a power of two apart
@@ -306,12 +337,9 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
             if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
             const int k0 = k_of(it, q);
             const uint32_t dst = base + stage * stage_bytes;
-            mbar_expect_tx(full_bar(stage), 2 * w_half);
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              tma_load_2d(dst + hf * w_half, &tmap_w, full_bar(stage), k0 + hf * BLOCK_K, row);
-              if (UP) tma_load_2d(dst + hf * w_half + p.h * 128, &tmap_w, full_bar(stage), k0 + hf * BLOCK_K, row + p.out_rows);
-            }
+            mbar_expect_tx(full_bar(stage), w_bytes);
+            tma_load_2d(dst, &tmap_w, full_bar(stage), k0, row);
+            if (UP) tma_load_2d(dst + p.h * 128, &tmap_w, full_bar(stage), k0, row + p.out_rows);
             ++issued;
             if (++stage == p.stages) { stage = 0; phase ^= 1u; }
           }
@@ -344,14 +372,10 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
           for (int q = 0; q < it.n; ++q) {
             if (!mbar_wait(full_bar(stage), phase, abort_flag, wait_limit)) { ok = false; break; }
             tc_fence_after();
-            const int halves = k_of(it, q) + BLOCK_K < p.Kd ? 2 : 1;
-            for (int hf = 0; hf < halves; ++hf) {
-              const uint64_t adesc = make_smem_desc(base + stage * stage_bytes + hf * w_half);
-              const uint64_t bdesc = make_smem_desc(base + stage * stage_bytes + x_at + hf * x_half);
+            const uint64_t adesc = make_smem_desc(base + stage * stage_bytes), bdesc = make_smem_desc(base + stage * stage_bytes + w_bytes);
 #pragma unroll
-              for (int k = 0; k < BLOCK_K / UMMA_K; ++k)
-                umma_bf16(tmem_base + acc * FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc, (q | hf | k) != 0 ? 1u : 0u);
-            }
+            for (int k = 0; k < FT_K / UMMA_K; ++k)
+              umma_bf16(tmem_base + acc * FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc, (q | k) != 0 ? 1u : 0u);
             umma_commit(empty_bar(stage));
             issued_any = true;
             if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -398,20 +422,16 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
         for (int kb = 0; kb < it.n; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit));
           if (!ok) break;
-          const uint32_t dst = base + stage * stage_bytes + x_at + lrow * 128 + ((chunk ^ (lrow & 7)) << 4);
+          const uint32_t dst = base + stage * stage_bytes + w_bytes + lrow * 128 + ((chunk ^ (lrow & 7)) << 4);
           const int k0 = k_of(it, kb);
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (lrow + 16 * q < m) {
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + q * 16 * 128), "l"(src[q] + k0) : "memory");
-              if (k0 + BLOCK_K < p.Kd)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + x_half + q * 16 * 128), "l"(src[q] + k0 + BLOCK_K) : "memory");
-            }
+            if (lrow + 16 * q < m) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + q * 16 * 128), "l"(src[q] + k0) : "memory");
           asm volatile("cp.async.commit_group;" ::: "memory");
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-          // the stage of FT_X_FLIGHT copies ago has landed: publish it to the tensor cores
-          if (++pending > FT_X_FLIGHT) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(FT_X_FLIGHT) : "memory");
+          // the stage of FLIGHT copies ago has landed: publish it to the tensor cores
+          if (++pending > FLIGHT) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(FLIGHT) : "memory");
             publish();
           }
         }
@@ -431,7 +451,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       pdl_wait();
       for (int t = blockIdx.x; t < p.T; t += gridDim.x) {      // tokens without an expert
         bool any = false;
-        for (int k = 0; k < p.K; ++k) { const int e = __ldg(p.idx + t * p.K + k); any |= e >= 0 && e < p.E; }
+        for (int k = 0; k < p.K; ++k) any |= by.of[t * p.K + k] >= 0;
         if (!any)
           for (int d = 8 * ct; d < p.out_rows; d += 8 * 128) *reinterpret_cast<uint4*>(p.out + (size_t)t * p.out_rows + d) = make_uint4(0, 0, 0, 0);
       }
@@ -513,8 +533,8 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
             const int t = i / nv, d = row0 + (i % nv) * 4;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             for (int k = 0; k < p.K; ++k) {
-              const int a = t * p.K + k, e = __ldg(p.idx + a);
-              if (e < 0 || e >= p.E) continue;
+              const int a = t * p.K + k;
+              if (by.of[a] < 0) continue;
               for (int q = 0; q < p.splits; ++q) {
                 const float4 f = __ldcg(reinterpret_cast<const float4*>(p.part + ((size_t)q * A + a) * p.out_rows + d));
                 v.x += f.x; v.y += f.y; v.z += f.z; v.w += f.w;
@@ -551,17 +571,19 @@ cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaS
   // again (from the L2 mostly), the others have deeper rings.
   const int n_exp = chosen_experts(s.T, s.K, s.E), want = std::min(s.T, 2 * (s.T * s.K / n_exp) + 8);
   p.cols_cap = want > 32 ? 64 : want > 16 ? 32 : 16;
+  const int smem = FT_SMEM_PAIR;
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
-    // (the MMA reads 128 rows from a tile's start: 16 KB past the ring's end at most)
-    const int stage = 2 * ((up ? 2 : 1) * p.h + p.cols_cap) * 128, room = FT_SMEM - 1024 - 16 * 1024;
-    p.stages = room / stage < FT_MAX_STAGES ? room / stage : FT_MAX_STAGES;
+    // (the MMA reads 128 rows from a tile's start, past the ring's end where a tile has fewer)
+    const int rows = (up ? 2 : 1) * p.h, stage = (rows + p.cols_cap) * 128, room = smem - 1024 - std::max(128 - rows - p.cols_cap, 0) * 128;
+    p.stages = std::min(room / stage, FT_MAX_STAGES);
     CUtensorMap tw;
     if (!make_tmap(&tw, W, (uint64_t)s.E * p.w_rows, (uint64_t)p.Kd, (uint64_t)p.Kd, p.h)) return cudaErrorInvalidValue;
-    cudaError_t rc = cudaFuncSetAttribute(ffn_step_tc<up>, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
+    auto kern = p.stages > 5 ? ffn_step_tc<up, 4> : ffn_step_tc<up, 2>;
+    cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
     if (rc != cudaSuccess) return rc;
     count_launch();
-    return launch_k(ffn_step_tc<up>, dim3(sms), FT_THREADS, FT_SMEM, st, tw, p, WAIT_LIMIT);
+    return launch_k(kern, dim3(sms), FT_THREADS, smem, st, tw, p, WAIT_LIMIT);
   };
   const FfnCut cu = cut_up(s.T, s.K, s.E, s.Dm, s.F), cd = cut_down(s.T, s.K, s.E, s.Dm, s.F);
   p.x = static_cast<const bf16*>(s.x); p.ldx = s.Dm; p.Kd = s.Dm; p.w_rows = 2 * s.F; p.out_rows = s.F;
