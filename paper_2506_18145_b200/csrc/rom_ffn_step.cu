@@ -202,12 +202,6 @@ cudaError_t launch_ffn_rows(const FfnStep& p, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------------------- bf16: streamed weights
-constexpr int FT_COLS = 64;                          // token columns per pass at most
-constexpr int FT_MAX_STAGES = 12;
-constexpr int FT_SMEM = 208 * 1024, FT_SMEM_PAIR = 104 * 1024;      // operand ring, alone on an SM or beside the other launch's
-constexpr int FT_THREADS = 320;
-constexpr int FT_K = BLOCK_K;                        // contracted elements per stage: one swizzled row
-
 // Experts that T tokens with K choices each of E name, about.
 int chosen_experts(int T, int K, int E) {
   double none = 1.0;
@@ -216,28 +210,34 @@ int chosen_experts(int T, int K, int E) {
   return n < 1 ? 1 : n;
 }
 constexpr int kSizingSms = 148;      // (workspace sizing and the launch agree)
-struct FfnCut { int h, splits; };
-// Rows per tile (and, of the down projection, parts of the contracted index) for which the rounds of tiles over the SMs bring the fewest bytes
-// through one of them: weights, token rows, and the parts written and added again.
-FfnCut cut_up(int T, int K, int E, int Dm, int F) {
-  const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Dm + FT_K - 1) / FT_K;
-  FfnCut best{64, 1};
-  long long least = -1;
-  for (int h = 64; h >= 8; h -= 8) {
-    const long long rounds = (n * ((F + h - 1) / h) + kSizingSms - 1) / kSizingSms, cost = rounds * kb * 2 * FT_K * (2 * h + m);
-    if (least < 0 || cost < least) { least = cost; best.h = h; }
-  }
-  return best;
+constexpr int FT_COLS = 64;                          // token columns per pass at most
+constexpr int FT_MIN_STAGES = 4, FT_MAX_STAGES = 12; // (each of the four warps that bring token rows has a stage of its own at least)
+constexpr int FT_KB = 2, FT_K = FT_KB * BLOCK_K;     // contracted elements per stage: two swizzled rows
+constexpr int FT_SMEM = 208 * 1024;                  // operand ring
+constexpr int FT_ROOM = FT_SMEM - 1024 - 128 * 128;  // (alignment; the MMA reads 128 rows from a tile's start, up to 16 KB past the ring's end)
+constexpr int FT_THREADS = 320;
+constexpr int ffn_stages(int rows, int cols) { return std::min(FT_ROOM / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES); }
+// Token columns of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights again (from the
+// L2 mostly), the others have deeper rings.
+int ffn_columns(int T, int K, int E) {
+  const int want = std::min(T, 2 * (T * K / chosen_experts(T, K, E)) + 8);
+  return want > 32 ? 64 : want > 16 ? 32 : 16;
 }
-FfnCut cut_down(int T, int K, int E, int Dm, int F) {
-  const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = F / FT_K;
-  FfnCut best{128, 1};
+// How the weights are cut into tiles: rows per tile and, of the down projection, parts of the contracted index.  The cheapest by the time that the
+// fullest SM takes, in ns: rounds of tiles times stages of at least 150 ns (what the issuer takes for eight MMAs) or their bytes at 44 a ns (an
+// SM's share of HBM), 1000 for a tile's end; parts of a sum that are written and read again at 100 a ns.
+struct FfnCut { int h, splits; };
+FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
+  const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Kd + FT_K - 1) / FT_K, per = up ? 2 : 1;
+  const int cols = ffn_columns(T, K, E);
+  FfnCut best{8, 1};
   long long least = -1;
-  for (int s = 1; s <= kFfnMaxSplits && s <= kb; ++s)
-    for (int h = 128; h >= 32; h -= 8) {
-      const long long rounds = (n * s * ((Dm + h - 1) / h) + kSizingSms - 1) / kSizingSms;
-      const bool direct = K == 1 && s == 1;
-      const long long cost = rounds * ((kb + s - 1) / s * 2 * FT_K * (h + m) + (direct ? 0 : 4 * m * h)) + (direct ? 0 : 4ll * T * K * s * h);
+  for (int s = 1; s <= (up ? 1 : kFfnMaxSplits) && s <= kb; ++s)
+    for (int h = up ? 64 : 128; h >= (up ? 8 : 32); h -= 8) {
+      if (ffn_stages((int)per * h, cols) < FT_MIN_STAGES) continue;
+      const long long rounds = (n * s * ((rows_out + h - 1) / h) + kSizingSms - 1) / kSizingSms;
+      const long long stage = std::max(150ll, 2 * FT_K * (per * h + m) / 44), parts = up || (K == 1 && s == 1) ? 0 : (4 * m * h * rounds + 4ll * T * K * s * h) / 100;
+      const long long cost = rounds * ((kb + s - 1) / s * stage + 1000) + parts;
       if (least < 0 || cost < least) { least = cost; best.h = h; best.splits = s; }
     }
   return best;
@@ -253,9 +253,32 @@ struct FfnTc {
   int direct;                                        // down: one expert and one part a token: written at once
 };
 
-// FLIGHT: stages of token rows in flight, fewer than there are stages.
+// Whether a phase is over; does not wait.  A wait takes 200 to 250 cycles even then, as long as three MMAs: the producer and the issuer look at
+// their next stage while they work on the present one.
+__device__ __forceinline__ bool mbar_ready(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+// A warp's wait, polled by one lane: 32 lanes' polls of one barrier are served one after the other, and eight warps that polled so kept the
+// producer's and the issuer's own barrier operations waiting (0.26 us a stage).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, abort_flag, limit);
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+// FLIGHT: stages of token rows that each of the four warps has in flight besides the one it asks for: 4 (FLIGHT + 1) + 1 stages at least.
 template <bool UP, int FLIGHT>
-__global__ void __launch_bounds__(FT_THREADS, 2)
+__global__ void __launch_bounds__(FT_THREADS, 1)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -266,7 +289,10 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, A = p.T * p.K;
+  // (the warp's number from a shuffle and elect.sync tell the compiler that the roles' branches are uniform: with `lane == 0` the producer's and
+  // the issuer's loops took 500 and 640 cycles a stage, whatever its size)
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), A = p.T * p.K;
+  const bool leader = elect_one();
   auto full_bar = [&](int s) { return smem_u32(&bars[s]); };
   auto empty_bar = [&](int s) { return smem_u32(&bars[FT_MAX_STAGES + s]); };
   auto tfull_bar = [&](int a) { return smem_u32(&bars[2 * FT_MAX_STAGES + a]); };
@@ -274,7 +300,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   const uint32_t drain_bar = smem_u32(&bars[2 * FT_MAX_STAGES + 4]);
 
   if (tid == 0) {
-    for (int s = 0; s < p.stages; ++s) { mbar_init(full_bar(s), 1 + 4); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < p.stages; ++s) { mbar_init(full_bar(s), 1 + 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 4); }
     mbar_init(drain_bar, 1);
     abort_s = 0;
@@ -307,7 +333,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   const uint32_t tmem_base = tmem_s;
   const int n_act = n_act_s, per_expert = p.tiles * p.splits, total = n_act * per_expert;
   const int num_kb = (p.Kd + FT_K - 1) / FT_K;
-  const uint32_t w_bytes = (UP ? 2 : 1) * p.h * 128, stage_bytes = w_bytes + p.cols_cap * 128;
+  const uint32_t w_bytes = (UP ? 2 : 1) * p.h * 128, x_bytes = p.cols_cap * 128, stage_bytes = FT_KB * (w_bytes + x_bytes);
   auto cols = [](int m) { return m > 32 ? 64 : m > 16 ? 32 : 16; };      // N of a pass over m tokens
   // item w: expert, first row, stages [kb0, kb0 + n) of the contracted index, walked from a start of the tile's own: in step all CTAs
   // would read the same columns of rows that are a power of two apart
@@ -326,22 +352,27 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
 
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA producer of the weights (nothing here depends on the launch before)
-    if (lane == 0) {
+    if (leader) {
       int stage = 0, issued = 0; uint32_t phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;                 // ready: the next stage was free when it was looked at
       for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
         const Item it = item(w);
         const int row = it.e * p.w_rows + it.tile * p.h, m = by.off[it.e + 1] - by.off[it.e];
         for (int n0 = 0; n0 < m && ok; n0 += p.cols_cap)
           for (int q = 0; q < it.n; ++q) {
-            if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
-            const int k0 = k_of(it, q);
+            if (!ready && !mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
+            const int k0 = k_of(it, q), next = stage + 1 == p.stages ? 0 : stage + 1;
             const uint32_t dst = base + stage * stage_bytes;
-            mbar_expect_tx(full_bar(stage), w_bytes);
-            tma_load_2d(dst, &tmap_w, full_bar(stage), k0, row);
-            if (UP) tma_load_2d(dst + p.h * 128, &tmap_w, full_bar(stage), k0, row + p.out_rows);
+            ready = mbar_ready(empty_bar(next), (next ? phase : phase ^ 1u) ^ 1u);
+            mbar_expect_tx(full_bar(stage), FT_KB * w_bytes);
+#pragma unroll
+            for (int b = 0; b < FT_KB; ++b) {
+              tma_load_2d(dst + b * w_bytes, &tmap_w, full_bar(stage), k0 + b * BLOCK_K, row);
+              if (UP) tma_load_2d(dst + b * w_bytes + p.h * 128, &tmap_w, full_bar(stage), k0 + b * BLOCK_K, row + p.out_rows);
+            }
             ++issued;
-            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            stage = next;
+            if (!next) phase ^= 1u;
           }
       }
       if (!ok) {
@@ -358,9 +389,9 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer: weights are the M operand, tokens the N columns
-    if (lane == 0) {
+    if (leader) {
       int stage = 0, acc = 0; uint32_t phase = 0, acc_phase = 0;
-      bool ok = true, issued_any = false;
+      bool ok = true, issued_any = false, ready = false;
       for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
         const Item it = item(w);
         const int m = by.off[it.e + 1] - by.off[it.e];
@@ -370,15 +401,23 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
           if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
           tc_fence_after();
           for (int q = 0; q < it.n; ++q) {
-            if (!mbar_wait(full_bar(stage), phase, abort_flag, wait_limit)) { ok = false; break; }
+            if (!ready && !mbar_wait(full_bar(stage), phase, abort_flag, wait_limit)) { ok = false; break; }
             tc_fence_after();
-            const uint64_t adesc = make_smem_desc(base + stage * stage_bytes), bdesc = make_smem_desc(base + stage * stage_bytes + w_bytes);
+            const int next = stage + 1 == p.stages ? 0 : stage + 1;
+            ready = mbar_ready(full_bar(next), next ? phase : phase ^ 1u);
+            const int blocks = min(FT_KB, (p.Kd - k_of(it, q)) / BLOCK_K);
+            for (int b = 0; b < blocks; ++b) {
+              const uint64_t adesc = make_smem_desc(base + stage * stage_bytes + b * w_bytes), bdesc = make_smem_desc(base + stage * stage_bytes + FT_KB * w_bytes + b * x_bytes);
 #pragma unroll
-            for (int k = 0; k < FT_K / UMMA_K; ++k)
-              umma_bf16(tmem_base + acc * FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc, (q | k) != 0 ? 1u : 0u);
+              for (int k = 0; k < BLOCK_K / UMMA_K; ++k)
+                // few columns: into 64 / n16 accumulators in turns, so that an MMA does not wait for the one before
+                umma_bf16(tmem_base + acc * FT_COLS + k * n16 % FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc,
+                          (q | b) != 0 || k * n16 >= FT_COLS ? 1u : 0u);
+            }
             umma_commit(empty_bar(stage));
             issued_any = true;
-            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            stage = next;
+            if (!next) phase ^= 1u;
           }
           if (!ok) break;
           umma_commit(tfull_bar(acc));
@@ -396,16 +435,17 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       }
     }
   } else if (warp >= 6) {
-    // ---------------------------------------------------------------- token rows of every stage: 128 threads, 16-byte pieces into the swizzled layout
-    const int l = tid - 6 * 32, lrow = l >> 3, chunk = l & 7;
+    // ---------------------------------------------------------------- token rows, 16-byte pieces into the swizzled layout: a stage is one warp's,
+    // the four warps take them in turns (one after the other by all of them, 0.37 us a stage bounded the kernel: a load's latency over those in flight)
+    const int xw = warp - 6, lrow = lane >> 3, chunk = lane & 7;
     if (!UP) { pdl_wait(); pdl_trigger(); }
-    int stage = 0, pub = 0, pending = 0; uint32_t phase = 0;
+    int count = 0, stage = 0, pub = xw, pending = 0; uint32_t phase = 0;      // count: stages so far
     bool ok = true;
     auto publish = [&]() {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(full_bar(pub));
-      if (++pub == p.stages) pub = 0;
+      if ((pub += 4) >= p.stages) pub -= p.stages;
       --pending;
     };
     for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
@@ -413,27 +453,26 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       const int m_all = by.off[it.e + 1] - by.off[it.e];
       for (int n0 = 0; n0 < m_all && ok; n0 += p.cols_cap) {
         const int m = min(m_all - n0, p.cols_cap);
-        const bf16* src[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {                // (columns past the last token hold whatever the stage held: nobody reads their sums)
-          const int a = by.list[by.off[it.e] + n0 + min(lrow + 16 * q, m - 1)];
-          src[q] = p.x + (size_t)(UP ? a / p.K : a) * p.ldx + chunk * 8;
-        }
+        const short* mine = by.list + by.off[it.e] + n0;
         for (int kb = 0; kb < it.n; ++kb) {
-          ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit));
-          if (!ok) break;
-          const uint32_t dst = base + stage * stage_bytes + w_bytes + lrow * 128 + ((chunk ^ (lrow & 7)) << 4);
-          const int k0 = k_of(it, kb);
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (lrow + 16 * q < m) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + q * 16 * 128), "l"(src[q] + k0) : "memory");
-          asm volatile("cp.async.commit_group;" ::: "memory");
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-          // the stage of FLIGHT copies ago has landed: publish it to the tensor cores
-          if (++pending > FLIGHT) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(FLIGHT) : "memory");
-            publish();
+          if ((count++ & 3) == xw) {
+            ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit);
+            if (!ok) break;
+            const uint32_t dst = base + stage * stage_bytes + FT_KB * w_bytes;
+            const int k0 = k_of(it, kb), blocks = min(FT_KB, (p.Kd - k0) / BLOCK_K);
+            for (int r = lrow; r < m; r += 4) {      // (columns past the last token hold whatever the stage held: nobody reads their sums)
+              const int a = mine[r];
+              const bf16* src = p.x + (size_t)(UP ? a / p.K : a) * p.ldx + k0 + chunk * 8;
+              for (int b = 0; b < blocks; ++b)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + b * x_bytes + r * 128 + ((chunk ^ (r & 7)) << 4)), "l"(src + b * BLOCK_K) : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++pending > FLIGHT) {                // this warp's stage of FLIGHT copies ago has landed: publish it to the tensor cores
+              asm volatile("cp.async.wait_group %0;" ::"n"(FLIGHT) : "memory");
+              publish();
+            }
           }
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
     }
@@ -462,10 +501,9 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       const Item it = item(w);
       const int row0 = it.tile * p.h, rows = min(p.h, p.out_rows - row0), m_all = by.off[it.e + 1] - by.off[it.e];
       for (int n0 = 0; n0 < m_all && ok; n0 += p.cols_cap) {
-        const int m = min(m_all - n0, p.cols_cap);
+        const int m = min(m_all - n0, p.cols_cap), n16 = cols(m);
         const short* mine = by.list + by.off[it.e] + n0;
-        ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, wait_limit);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = warp_wait(tfull_bar(acc), acc_phase, abort_flag, wait_limit);
         if (UP) {                                    // (the four warps meet in the exchange below: they leave together)
           int all;
           asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.and.pred p, 2, 128, q;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(all) : "r"((int)ok) : "memory");
@@ -478,6 +516,16 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
           uint32_t r[32];
           tmem_ld32_issue(taddr + c0, r);
           tmem_ld_wait(r);
+          if (n16 < FT_COLS) {                       // the sums of the turns
+            uint32_t r2[32];
+            tmem_ld32_issue(taddr + 32, r2);
+            tmem_ld_wait(r2);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r2[j]));
+            if (n16 == 16)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r[16 + j]));
+          }
           if (UP) {
 #pragma unroll
             for (int jb = 0; jb < 32; jb += 16) {
@@ -567,25 +615,20 @@ cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaS
   FfnTc p{};
   p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
   p.T = s.T; p.K = s.K; p.E = s.E;
-  // Token columns of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights
-  // again (from the L2 mostly), the others have deeper rings.
-  const int n_exp = chosen_experts(s.T, s.K, s.E), want = std::min(s.T, 2 * (s.T * s.K / n_exp) + 8);
-  p.cols_cap = want > 32 ? 64 : want > 16 ? 32 : 16;
-  const int smem = FT_SMEM_PAIR;
+  p.cols_cap = ffn_columns(s.T, s.K, s.E);
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
-    // (the MMA reads 128 rows from a tile's start, past the ring's end where a tile has fewer)
-    const int rows = (up ? 2 : 1) * p.h, stage = (rows + p.cols_cap) * 128, room = smem - 1024 - std::max(128 - rows - p.cols_cap, 0) * 128;
-    p.stages = std::min(room / stage, FT_MAX_STAGES);
+    p.stages = ffn_stages((up ? 2 : 1) * p.h, p.cols_cap);
+    if (p.stages < FT_MIN_STAGES) return cudaErrorInvalidValue;      // (cut_tiles takes no such tile)
     CUtensorMap tw;
     if (!make_tmap(&tw, W, (uint64_t)s.E * p.w_rows, (uint64_t)p.Kd, (uint64_t)p.Kd, p.h)) return cudaErrorInvalidValue;
-    auto kern = p.stages > 5 ? ffn_step_tc<up, 4> : ffn_step_tc<up, 2>;
+    auto kern = p.stages >= 9 ? ffn_step_tc<up, 1> : ffn_step_tc<up, 0>;
     cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
     if (rc != cudaSuccess) return rc;
     count_launch();
-    return launch_k(kern, dim3(sms), FT_THREADS, smem, st, tw, p, WAIT_LIMIT);
+    return launch_k(kern, dim3(sms), FT_THREADS, FT_SMEM, st, tw, p, WAIT_LIMIT);
   };
-  const FfnCut cu = cut_up(s.T, s.K, s.E, s.Dm, s.F), cd = cut_down(s.T, s.K, s.E, s.Dm, s.F);
+  const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true), cd = cut_tiles(s.T, s.K, s.E, s.Dm, s.F, false);
   p.x = static_cast<const bf16*>(s.x); p.ldx = s.Dm; p.Kd = s.Dm; p.w_rows = 2 * s.F; p.out_rows = s.F;
   p.h = cu.h; p.tiles = (s.F + cu.h - 1) / cu.h; p.splits = 1;
   if ((e = launch(std::true_type{}, s.W_gu)) != cudaSuccess) return e;
@@ -615,7 +658,7 @@ FfnStepWs ffn_step_ws(const rom_config& c, int d_ff) {
   const size_t A = (size_t)c.B * c.L * c.K;
   l.arrived = take(tc ? sizeof(int32_t) * kFfnMaxTiles : 0);
   l.hid = take((tc ? 2 : 4) * A * d_ff);
-  const FfnCut cd = cut_down(c.B * c.L, c.K, c.E, c.d_model, d_ff);
+  const FfnCut cd = cut_tiles(c.B * c.L, c.K, c.E, c.d_model, d_ff, false);
   l.part = take(tc && !(c.K == 1 && cd.splits == 1) ? sizeof(float) * cd.splits * A * c.d_model : 0);
   l.total = o;
   return l;
