@@ -35,29 +35,11 @@ struct ByExpert {
       of[a] = e >= 0 && e < E ? (signed char)e : (signed char)-1;
     }
     __syncthreads();
-    for (int e = warp; e < E; e += warps) {
-      int n = 0;
-      for (int a0 = 0; a0 < A; a0 += 32) n += __popc(__ballot_sync(0xffffffffu, a0 + lane < A && of[a0 + lane] == e));
-      if (lane == 0) off[e + 1] = n;
-    }
-    __syncthreads();
-    if (warp == 0) {                   // sums before every expert: two experts a lane
-      const int c0 = 2 * lane < E ? off[2 * lane + 1] : 0, c1 = 2 * lane + 1 < E ? off[2 * lane + 2] : 0;
-      int sum = c0 + c1;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, sum, d);
-        if (lane >= d) sum += v;
-      }
-      __syncwarp();
-      if (lane == 0) off[0] = 0;
-      if (2 * lane < E) off[2 * lane + 1] = sum - c1;
-      if (2 * lane + 1 < E) off[2 * lane + 2] = sum;
-    }
-    __syncthreads();
-    for (int e = warp; e < E; e += warps) {
-      int n = off[e];
-      if (n == off[e + 1]) continue;
+    for (int e = warp; e <= E; e += warps) {
+      int n = 0;                       // assignments of the experts before e
+      for (int a0 = 0; a0 < A; a0 += 32) n += __popc(__ballot_sync(0xffffffffu, a0 + lane < A && of[a0 + lane] >= 0 && of[a0 + lane] < e));
+      if (lane == 0) off[e] = n;
+      if (e == E) break;
       for (int a0 = 0; a0 < A; a0 += 32) {
         const unsigned m = __ballot_sync(0xffffffffu, a0 + lane < A && of[a0 + lane] == e);
         if ((m >> lane) & 1u) list[n + __popc(m & ((1u << lane) - 1u))] = (short)(a0 + lane);
@@ -213,10 +195,16 @@ constexpr int kSizingSms = 148;      // (workspace sizing and the launch agree)
 constexpr int FT_COLS = 64;                          // token columns per pass at most
 constexpr int FT_MIN_STAGES = 4, FT_MAX_STAGES = 12; // (each of the four warps that bring token rows has a stage of its own at least)
 constexpr int FT_KB = 2, FT_K = FT_KB * BLOCK_K;     // contracted elements per stage: two swizzled rows
-constexpr int FT_SMEM = 208 * 1024;                  // operand ring
-constexpr int FT_ROOM = FT_SMEM - 1024 - 128 * 128;  // (alignment; the MMA reads 128 rows from a tile's start, up to 16 KB past the ring's end)
+constexpr int FT_SMEM = 208 * 1024;                  // operand ring of a CTA alone on its SM
+constexpr int FT_SMEM_PAIR = 212 * 1024;             // rings of both launches together where they share the SMs
 constexpr int FT_THREADS = 320;
-constexpr int ffn_stages(int rows, int cols) { return std::min(FT_ROOM / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES); }
+// Bytes of a ring: its alignment, its stages, and what the MMA reads past the last one (always 128 rows from a tile's start).
+constexpr int ffn_ring(int rows, int cols, int stages) {
+  return 1024 + stages * FT_KB * (rows + cols) * 128 + std::max(128 * 128 - (rows + FT_KB * cols) * 128, 0);
+}
+constexpr int ffn_stages(int rows, int cols, int room = FT_SMEM) {
+  return std::min((room - ffn_ring(rows, cols, 0)) / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES);
+}
 // Token columns of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights again (from the
 // L2 mostly), the others have deeper rings.
 int ffn_columns(int T, int K, int E) {
@@ -224,8 +212,7 @@ int ffn_columns(int T, int K, int E) {
   return want > 32 ? 64 : want > 16 ? 32 : 16;
 }
 // How the weights are cut into tiles: rows per tile and, of the down projection, parts of the contracted index.  The cheapest by the time that the
-// fullest SM takes, in ns: rounds of tiles times stages of at least 150 ns (what the issuer takes for eight MMAs) or their bytes at 44 a ns (an
-// SM's share of HBM), 1000 for a tile's end; parts of a sum that are written and read again at 100 a ns.
+// fullest SM takes, in ns: rounds of tiles times stages of 60 ns and their bytes at 44 a ns (an SM's share of HBM), 1000 for a tile's end; parts of a sum that are written (100 bytes a ns) and read again (20).
 struct FfnCut { int h, splits; };
 FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
   const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Kd + FT_K - 1) / FT_K, per = up ? 2 : 1;
@@ -236,7 +223,7 @@ FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
     for (int h = up ? 64 : 128; h >= (up ? 8 : 32); h -= 8) {
       if (ffn_stages((int)per * h, cols) < FT_MIN_STAGES) continue;
       const long long rounds = (n * s * ((rows_out + h - 1) / h) + kSizingSms - 1) / kSizingSms;
-      const long long stage = std::max(150ll, 2 * FT_K * (per * h + m) / 44), parts = up || (K == 1 && s == 1) ? 0 : (4 * m * h * rounds + 4ll * T * K * s * h) / 100;
+      const long long stage = 60 + 2 * FT_K * (per * h + m) / 44, parts = up || (K == 1 && s == 1) ? 0 : 4 * m * h * rounds / 100 + 4ll * T * K * s * h / 20;
       const long long cost = rounds * ((kb + s - 1) / s * stage + 1000) + parts;
       if (least < 0 || cost < least) { least = cost; best.h = h; best.splits = s; }
     }
@@ -278,7 +265,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 }
 // FLIGHT: stages of token rows that each of the four warps has in flight besides the one it asks for: 4 (FLIGHT + 1) + 1 stages at least.
 template <bool UP, int FLIGHT>
-__global__ void __launch_bounds__(FT_THREADS, 1)
+__global__ void __launch_bounds__(FT_THREADS, 2)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -307,6 +294,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  if (tid == 32 * 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * FT_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -340,11 +328,15 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   struct Item { int e, tile, part, kb0, n, rot; };
   auto item = [&](int w) {
     Item it;
-    it.e = act[w / per_expert];
-    const int r = w % per_expert;
-    it.tile = r / p.splits; it.part = r % p.splits;
-    it.kb0 = num_kb * it.part / p.splits;
-    it.n = num_kb * (it.part + 1) / p.splits - it.kb0;
+    const int i = w / per_expert, r = w - i * per_expert;
+    it.e = act[i];
+    if (UP) {
+      it.tile = r; it.part = 0; it.kb0 = 0; it.n = num_kb;
+    } else {
+      it.tile = r / p.splits; it.part = r - it.tile * p.splits;
+      it.kb0 = num_kb * it.part / p.splits;
+      it.n = num_kb * (it.part + 1) / p.splits - it.kb0;
+    }
     it.rot = it.tile * 5 % it.n;
     return it;
   };
@@ -577,20 +569,43 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
         if (last) {
           __threadfence();
           const int nv = rows / 4;
-          for (int i = ct; i < p.T * nv; i += 128) {
-            const int t = i / nv, d = row0 + (i % nv) * 4;
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int k = 0; k < p.K; ++k) {
-              const int a = t * p.K + k;
-              if (by.of[a] < 0) continue;
-              for (int q = 0; q < p.splits; ++q) {
-                const float4 f = __ldcg(reinterpret_cast<const float4*>(p.part + ((size_t)q * A + a) * p.out_rows + d));
-                v.x += f.x; v.y += f.y; v.z += f.z; v.w += f.w;
-              }
+          const int outs = p.T * nv;
+          auto add = [&](auto u_tag) {               // U outputs of a thread in flight
+          constexpr int U = decltype(u_tag)::value;
+          for (int i0 = 0; i0 < outs; i0 += 128 * U) {
+            float4 v[U];
+            int at[U], a0[U];                        // column and first assignment of an output
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const int i = min(i0 + 128 * u + ct, outs - 1), t = i / nv;
+              at[u] = row0 + (i - t * nv) * 4;
+              a0[u] = t * p.K;
+              v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
-            *reinterpret_cast<uint2*>(p.out + (size_t)t * p.out_rows + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            for (int k = 0; k < p.K; ++k)
+              for (int q = 0; q < p.splits; ++q) {
+                float4 f[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                  if (i0 + 128 * u >= outs) break;   // (the same for all threads)
+                  f[u] = by.of[a0[u] + k] >= 0 ? __ldcg(reinterpret_cast<const float4*>(p.part + ((size_t)q * A + a0[u] + k) * p.out_rows + at[u])) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                  if (i0 + 128 * u >= outs) break;
+                  v[u].x += f[u].x; v[u].y += f[u].y; v[u].z += f[u].z; v[u].w += f[u].w;
+                }
+              }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if (i0 + 128 * u + ct >= outs) break;
+              const __nv_bfloat162 lo = __floats2bfloat162_rn(v[u].x, v[u].y), hi = __floats2bfloat162_rn(v[u].z, v[u].w);
+              *reinterpret_cast<uint2*>(p.out + (size_t)(a0[u] / p.K) * p.out_rows + at[u]) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            }
           }
+          };
+          if (outs <= 256) add(std::integral_constant<int, 1>{});      // (a token or a few: 1 us less than with the longer code)
+          else add(std::integral_constant<int, 4>{});
         }
         together();                                  // (last_s is read before it is written again)
       }
@@ -616,19 +631,24 @@ cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaS
   p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
   p.T = s.T; p.K = s.K; p.E = s.E;
   p.cols_cap = ffn_columns(s.T, s.K, s.E);
+  const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true), cd = cut_tiles(s.T, s.K, s.E, s.Dm, s.F, false);
+  // Where rings of the fewest stages let both launches share the SMs, the second one is resident, has its lists and its first weights when
+  // the first ends.
+  const bool paired = ffn_ring(2 * cu.h, p.cols_cap, FT_MIN_STAGES) + ffn_ring(cd.h, p.cols_cap, FT_MIN_STAGES) <= FT_SMEM_PAIR;
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
-    p.stages = ffn_stages((up ? 2 : 1) * p.h, p.cols_cap);
+    const int rows = (up ? 2 : 1) * p.h;
+    p.stages = paired ? FT_MIN_STAGES : ffn_stages(rows, p.cols_cap);
     if (p.stages < FT_MIN_STAGES) return cudaErrorInvalidValue;      // (cut_tiles takes no such tile)
     CUtensorMap tw;
     if (!make_tmap(&tw, W, (uint64_t)s.E * p.w_rows, (uint64_t)p.Kd, (uint64_t)p.Kd, p.h)) return cudaErrorInvalidValue;
     auto kern = p.stages >= 9 ? ffn_step_tc<up, 1> : ffn_step_tc<up, 0>;
     cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
+    if (rc == cudaSuccess) rc = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (rc != cudaSuccess) return rc;
     count_launch();
-    return launch_k(kern, dim3(sms), FT_THREADS, FT_SMEM, st, tw, p, WAIT_LIMIT);
+    return launch_k(kern, dim3(sms), FT_THREADS, ffn_ring(rows, p.cols_cap, p.stages), st, tw, p, WAIT_LIMIT);
   };
-  const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true), cd = cut_tiles(s.T, s.K, s.E, s.Dm, s.F, false);
   p.x = static_cast<const bf16*>(s.x); p.ldx = s.Dm; p.Kd = s.Dm; p.w_rows = 2 * s.F; p.out_rows = s.F;
   p.h = cu.h; p.tiles = (s.F + cu.h - 1) / cu.h; p.splits = 1;
   if ((e = launch(std::true_type{}, s.W_gu)) != cudaSuccess) return e;
