@@ -271,16 +271,13 @@ scan_ragged_chunks(const RaggedScan p) {
     }
     __syncwarp();
     if (t_next < hi) fetch(t_next, rows_of(t_next, t_next < cur_end ? cur_end : n_end));
-    // the next row's operands are requested before this row's arithmetic: a load issued behind a row's exponentials waits for all of them
+    // one row; its operands have been requested, those of row `ahead` are before this row's arithmetic: a load issued behind a row's exponentials
+    // waits for all of them
     float4 nd = s.dl[0][cg], nu = s.u[0][cg], nb = s.b[0][q], nc = STATE ? zero4 : s.c[0][q];
-#pragma unroll
-    for (int r = 0; r < RR; ++r) {
-      if (r >= m) break;
+    auto row = [&](int r, int ahead) {
       const float4 d4 = nd, u4 = nu, b4 = nb, c4 = nc;
-      if (r + 1 < RR) {
-        nd = s.dl[r + 1][cg ^ (r + 1)]; nu = s.u[r + 1][cg ^ (r + 1)]; nb = s.b[r + 1][q];
-        if (!STATE) nc = s.c[r + 1][q];
-      }
+      nd = s.dl[ahead][cg ^ ahead]; nu = s.u[ahead][cg ^ ahead]; nb = s.b[ahead][q];
+      if (!STATE) nc = s.c[ahead][q];
       const float2 dl[2] = {make_float2(d4.x, d4.y), make_float2(d4.z, d4.w)}, uu[2] = {make_float2(u4.x, u4.y), make_float2(u4.z, u4.w)};
       const float bb[4] = {b4.x, b4.y, b4.z, b4.w}, cc[4] = {c4.x, c4.y, c4.z, c4.w};
       float2 acc[2];
@@ -308,6 +305,14 @@ scan_ragged_chunks(const RaggedScan p) {
         }
       if (STATE) { sdel[0] = __fadd2_rn(sdel[0], dl[0]); sdel[1] = __fadd2_rn(sdel[1], dl[1]); }
       else s.y[r][y_slot(lane, r)] = make_float4(acc[0].x, acc[0].y, acc[1].x, acc[1].y);
+    };
+    constexpr int UF = FINE ? 2 : STATE ? 4 : RR;
+    if (m == RR) {
+#pragma unroll UF
+      for (int r = 0; r < RR; ++r) row(r, min(r + 1, RR - 1));
+    } else {
+#pragma unroll 1
+      for (int r = 0; r < m; ++r) row(r, min(r + 1, RR - 1));
     }
     __syncwarp();
     if (!STATE) {
@@ -324,13 +329,15 @@ scan_ragged_chunks(const RaggedScan p) {
           const int g4 = 8 * l8 + 4 * hf;
           const float4 x0 = s.y[lt][y_slot(g4, lt)], x1 = s.y[lt][y_slot(g4 + 1, lt)], x2 = s.y[lt][y_slot(g4 + 2, lt)], x3 = s.y[lt][y_slot(g4 + 3, lt)];
           const float4 D4 = reinterpret_cast<const float4*>(s.D)[2 * l8 + hf];
-          const float sum[4] = {(x0.x + x1.x) + (x2.x + x3.x), (x0.y + x1.y) + (x2.y + x3.y), (x0.z + x1.z) + (x2.z + x3.z), (x0.w + x1.w) + (x2.w + x3.w)};
-          const float Dv[4] = {D4.x, D4.y, D4.z, D4.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float v = fmaf(Dv[i], uu[4 * hf + i], sum[i]);
-            o[4 * hf + i] = zp ? v * zz[4 * hf + i] : v;
+          float2 v0 = __fadd2_rn(__fadd2_rn(make_float2(x0.x, x0.y), make_float2(x1.x, x1.y)), __fadd2_rn(make_float2(x2.x, x2.y), make_float2(x3.x, x3.y)));
+          float2 v1 = __fadd2_rn(__fadd2_rn(make_float2(x0.z, x0.w), make_float2(x1.z, x1.w)), __fadd2_rn(make_float2(x2.z, x2.w), make_float2(x3.z, x3.w)));
+          v0 = __ffma2_rn(make_float2(D4.x, D4.y), make_float2(uu[4 * hf], uu[4 * hf + 1]), v0);
+          v1 = __ffma2_rn(make_float2(D4.z, D4.w), make_float2(uu[4 * hf + 2], uu[4 * hf + 3]), v1);
+          if (zp) {
+            v0 = __fmul2_rn(v0, make_float2(zz[4 * hf], zz[4 * hf + 1]));
+            v1 = __fmul2_rn(v1, make_float2(zz[4 * hf + 2], zz[4 * hf + 3]));
           }
+          o[4 * hf] = v0.x; o[4 * hf + 1] = v0.y; o[4 * hf + 2] = v1.x; o[4 * hf + 3] = v1.y;
         }
         Raw8<T>::store(static_cast<T*>(p.y) + (size_t)(t + lt) * De + lc, o);
       }
