@@ -15,6 +15,8 @@
 //
 // bf16: what bounds it is one exponential per state update on the special-function unit, then the fp32 pipe.  fp32: decay() keeps fp32
 // accuracy, about ten operations more an update.
+#include <cmath>
+
 #include "rom_serve.cuh"
 
 namespace rom {
@@ -143,16 +145,26 @@ scan_ragged_chunks(const RaggedScan p) {
     } else if (reach) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(p.h_end + (size_t)first_chunk * De * 16 + state_at(i));
-      for (int k = first_chunk + 1; k < chunk; ++k) {
-        const float4 d4 = *reinterpret_cast<const float4*>(p.sum_delta + (size_t)k * De + c0);
-        const float dk[4] = {d4.x, d4.y, d4.z, d4.w};
+      for (int k0 = first_chunk + 1; k0 < chunk; k0 += 4) {      // four chunks' loads in flight; past the last one: the identity
+        float4 d4[4], e4[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 e = *reinterpret_cast<const float4*>(p.h_end + (size_t)k * De * 16 + state_at(i));
-          v[i].x = fmaf(expf(av[i][0] * dk[i]), v[i].x, e.x);
-          v[i].y = fmaf(expf(av[i][1] * dk[i]), v[i].y, e.y);
-          v[i].z = fmaf(expf(av[i][2] * dk[i]), v[i].z, e.z);
-          v[i].w = fmaf(expf(av[i][3] * dk[i]), v[i].w, e.w);
+        for (int k = 0; k < 4; ++k) {
+          const bool in = k0 + k < chunk;
+          d4[k] = in ? *reinterpret_cast<const float4*>(p.sum_delta + (size_t)(k0 + k) * De + c0) : zero4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e4[k][i] = in ? *reinterpret_cast<const float4*>(p.h_end + (size_t)(k0 + k) * De * 16 + state_at(i)) : zero4;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float dk[4] = {d4[k].x, d4[k].y, d4[k].z, d4[k].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float al[4] = {av[i][0] * kLog2eServe, av[i][1] * kLog2eServe, av[i][2] * kLog2eServe, av[i][3] * kLog2eServe};
+            v[i].x = fmaf(ex2_ftz(al[0] * dk[i]), v[i].x, e4[k][i].x);
+            v[i].y = fmaf(ex2_ftz(al[1] * dk[i]), v[i].y, e4[k][i].y);
+            v[i].z = fmaf(ex2_ftz(al[2] * dk[i]), v[i].z, e4[k][i].z);
+            v[i].w = fmaf(ex2_ftz(al[3] * dk[i]), v[i].w, e4[k][i].w);
+          }
         }
       }
     }
@@ -354,31 +366,37 @@ scan_ragged_chunks(const RaggedScan p) {
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Chunks of the packed rows: the count with the smallest time by the warp kernel's measured pace (scan_warp_time): a block of four warps takes
-// 139 / 192 / 272 ns a row with one / two / three of them on an SM, 115 / 161 / 230 ns states only, and the second launch costs about 7 us.
-// The first launch walks the rows of sequences that reach over a chunk's end: all of a chunk when sequences are longer than chunks, about
-// one mean sequence otherwise.  A function of the sizes alone, so that workspace sizing and the launch agree.
-int ragged_chunks(int De, int n_seq, int rows) {
-  auto pace = [](long long blocks, const double (&ns)[3]) {
-    const long long k = (blocks + 147) / 148;
-    return k <= 3 ? ns[k - 1] : ns[2] * (double)k / 3.0;
+// Chunks of the packed rows: the count with the smallest time by what the kernels were measured to take.  A block of four warps takes
+// 155 / 235 / 330 ns a row with one / two / three of them on an SM, 128 / 188 / 255 ns states only; rounds of three overlap to 268 and 200.  fp32:
+// two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains, 1.2 us from one sequence to
+// the next.  The first launch walks the rows of sequences that reach over a chunk's end, of one of length `mean` about
+// mean (1 - exp(-Lc / mean)).  A function of the sizes alone, so that workspace sizing and the launch agree.
+int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
+  const double full[4] = {155.0, 235.0, 330.0, 268.0}, state[4] = {128.0, 188.0, 255.0, 200.0};
+  const double mean = rows > 0 && n_seq > 0 ? (double)rows / n_seq : 1.0;
+  const int most = fp32 ? 2 : 3;
+  // blocks that each take fixed + rows_each * pace ns
+  auto time = [&](double blocks, const double (&pace)[4], double rows_each, double fixed) {
+    const int k = (int)((blocks + 147.0) / 148.0);
+    const double slow = fp32 ? 2.0 : 1.0;
+    if (k <= most) return fixed + rows_each * pace[k - 1] * slow;
+    return (blocks / (148.0 * most) + 0.3) * (fixed + rows_each * pace[fp32 ? 1 : 3] * slow);
   };
-  const double full[3] = {139.0, 192.0, 272.0}, state[3] = {115.0, 161.0, 230.0};
-  const double mean = (double)rows / (n_seq > 0 ? n_seq : 1);
   int best = 1;
   double best_t = 0.0;
-  for (int n = 1; n == 1 || (rows >= 16 * n && (long long)n * (De / 32) <= 148 * 12 * 4); ++n) {
-    const long long blocks = ((long long)n * (De / 32) + RWARPS - 1) / RWARPS;
-    const double Lc = (double)((rows + n - 1) / n);
-    const double t = Lc * pace(blocks, full) + (n == 1 ? 0.0 : (Lc < mean ? Lc : mean) * pace(blocks, state) + 7000.0);
+  for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); ++n) {
+    const double blocks = ((double)n * (De / 32) + RWARPS - 1) / RWARPS, Lc = (double)rows / n, chained = mean < Lc ? 0.0 : mean / Lc < n ? mean / Lc : n;
+    double t = time(blocks, full, Lc, 3000.0 + 100.0 * chained + 1200.0 * Lc / mean);
+    if (n > 1) t += time(blocks, state, mean * (1.0 - exp(-Lc / mean)), 2000.0) + 3000.0;
     if (n == 1 || t < best_t) { best = n; best_t = t; }
   }
   return best;
 }
 struct RaggedWs { int Lc, nch; size_t h_end, h_start, sum_delta, total; };
-RaggedWs ragged_ws(int De, int n_seq, int rows) {
+RaggedWs ragged_ws(const rom_config& c, int n_seq, int rows) {
+  const int De = c.d_inner;
   RaggedWs l{};
-  const int n = ragged_chunks(De, n_seq, rows);
+  const int n = ragged_chunks(De, n_seq, rows, c.dtype == ROM_F32);
   l.Lc = n == 1 ? (rows > 0 ? rows : 1) : (int)align_up((size_t)(rows + n - 1) / n, RR);
   l.nch = rows > 0 ? (rows + l.Lc - 1) / l.Lc : 1;
   size_t o = 0;
@@ -416,7 +434,7 @@ int rom_scan_ragged_workspace_size(const rom_config* cfg, int32_t n_seq, int32_t
   const int rc = check_config(cfg, 2);
   if (rc != ROM_OK) return rc;
   if (n_seq > kMaxRaggedSeqs || rows >= 1 << 30) return ROM_ERR_UNSUPPORTED;
-  *bytes = ragged_ws(cfg->d_inner, n_seq, rows).total;
+  *bytes = ragged_ws(*cfg, n_seq, rows).total;
   return ROM_OK;
 }
 
@@ -436,7 +454,7 @@ int rom_scan_ragged(const rom_config* cfg, const rom_ragged* seqs, const void* u
     if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
   if (!aligned4(D) || !aligned4(Bm) || !aligned4(Cm)) return ROM_ERR_INVALID_ARG;
   if (!pools_ok(h_in, h_out, (size_t)seqs->n_slots * c.d_inner * c.d_state)) return ROM_ERR_INVALID_ARG;
-  const RaggedWs lay = ragged_ws(c.d_inner, seqs->n_seq, seqs->rows);
+  const RaggedWs lay = ragged_ws(c, seqs->n_seq, seqs->rows);
   if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
   if ((rc = check_device()) != ROM_OK) return rc;
   LaunchCounter::count = 0;
