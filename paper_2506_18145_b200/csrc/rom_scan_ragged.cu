@@ -9,9 +9,8 @@
 // reaches on, because the chunk with its end may write the slot (in place) before the chunk with its start has read it.
 //
 // A warp owns 32 channels of one chunk, a lane 4 states of 4 adjacent channels in packed pairs along the channels (the layout of
-// rom_scan_warp.cu, where the reasons stand): up to eight rows are staged in shared memory while the next are in registers.  A tile ends where a
-// sequence ends, so that states change hands between tiles only; the next sequence's initial state is copied to shared memory while the
-// present one runs.
+// rom_scan_warp.cu, where the reasons stand): eight rows are staged in shared memory, whatever sequences they belong to, while the next eight
+// are in registers, and the initial states of the next four sequences are on their way to shared memory.
 //
 // bf16: what bounds it is one exponential per state update on the special-function unit, then the fp32 pipe.  fp32: decay() keeps fp32
 // accuracy, about ten operations more an update.
@@ -24,6 +23,7 @@ namespace {
 
 constexpr int RR = 8;             // rows per tile
 constexpr int RWARPS = 4;         // warps per block
+constexpr int NEXT = 4;           // sequences whose initial states are on their way
 
 struct RaggedScan {
   Ragged s;
@@ -41,7 +41,8 @@ struct RaggedTile {
   float4 b[RR][4], c[RR][4];
   float D[32];
   float4 y[RR][32];               // partial sums of 4 channels over one lane's states
-  float4 h0[4][32];               // the next sequence's initial state: channel i of the lane
+  float4 h0[NEXT][4][32];         // initial states of the sequences to come: channel i of the lane
+  int4 next[NEXT];                // those sequences: first row, row behind the last, slot to read, slot to write (-1: none)
 };
 
 __device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
@@ -72,12 +73,12 @@ template <typename T, bool ZOH, bool STATE>
 __global__ void __launch_bounds__(RWARPS * 32, sizeof(T) == 2 ? 3 : 2)
 scan_ragged_chunks(const RaggedScan p) {
   constexpr bool FINE = sizeof(T) == 4;
-  __shared__ __align__(16) RaggedTile tiles[RWARPS];
+  extern __shared__ __align__(16) unsigned char smem_raw[];
   pdl_wait();
   const int lane = threadIdx.x & 31, De = p.De, groups = De / 32;
   const int item = blockIdx.x * RWARPS + (threadIdx.x >> 5), chunk = item / groups, c_warp = (item % groups) * 32;
   if (chunk >= (STATE ? p.nch - 1 : p.nch)) return;
-  RaggedTile& s = tiles[threadIdx.x >> 5];
+  RaggedTile& s = reinterpret_cast<RaggedTile*>(smem_raw)[threadIdx.x >> 5];
   const int r0 = chunk * p.Lc, r1 = min(r0 + p.Lc, p.s.rows);
   // ---- what this warp walks
   int t, hi, cur_end, next = 0, cur_out = -1, cur_in = -1, first_chunk = chunk;
@@ -200,26 +201,34 @@ scan_ragged_chunks(const RaggedScan p) {
     }
     w.load(p, next);
   }
-  // the next sequence with rows; its initial state on the way to shared memory
-  int n_start = 0x7fffffff, n_end = 0, n_in = -1, n_out = -1;
-  auto look_ahead = [&]() {
+  // the next sequence with rows into place `at` of the ring, its initial state on the way to shared memory
+  auto look_ahead = [&](int at) {
+    int4 e = make_int4(0x7fffffff, 0x7fffffff, -1, -1);
     while (next < p.s.n_seq) {
       w.reach(p, next);
-      n_start = w.start_of(next); n_end = w.end_of(next);
-      if (n_end > n_start) break;
+      const int first = w.start_of(next), end = w.end_of(next);
+      if (end > first) {
+        e = make_int4(first, end, w.in_of(next), w.out_of(next));
+        ++next;
+        break;
+      }
       ++next;
     }
-    if (next >= p.s.n_seq) { n_start = 0x7fffffff; n_end = 0x7fffffff; n_in = -1; n_out = -1; return; }
-    n_in = w.in_of(next); n_out = w.out_of(next);
-    ++next;
-    if (n_in >= 0 && n_start < r1) {
-      const float* src = n_end > r1 ? p.h_start + (size_t)chunk * De * 16 : p.h_in + (size_t)n_in * De * 16;
+    if (e.z >= 0 && e.x < r1) {
+      const float* src = e.y > r1 ? p.h_start + (size_t)chunk * De * 16 : p.h_in + (size_t)e.z * De * 16;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&s.h0[i][lane])), "l"(src + state_at(i)) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&s.h0[at][i][lane])), "l"(src + state_at(i)) : "memory");
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (lane == 0) s.next[at] = e;
   };
-  if (!STATE) look_ahead();
+  int head = 0;
+  if (!STATE) {
+#pragma unroll 1
+    for (int i = 0; i < NEXT; ++i) look_ahead(i);
+    __syncwarp();
+  }
 
   // ---- loader / output role: row lt of every tile, channels lc .. lc+7 (four lanes per row: a quarter-warp touches two rows of global memory)
   const int lt = lane >> 2, l8 = lane & 3, lc = c_warp + 8 * l8;
@@ -248,25 +257,26 @@ scan_ragged_chunks(const RaggedScan p) {
       r_b = zero4; r_c = zero4;
     }
   };
-  // rows of the tile at t0, with the sequence that runs there ending at `end`
-  auto rows_of = [&](int t0, int end) { return max(min(RR, min(end, hi) - t0), 1); };
-
-  if (t < hi) fetch(t, rows_of(t, t < cur_end ? cur_end : n_end));
   bool running = STATE || reach;
-  while (t < hi) {
-    if (!STATE && t >= cur_end) {
-      if (running && cur_out >= 0) put_state(p.h_out + (size_t)cur_out * De * 16);
-      float4 v[4] = {zero4, zero4, zero4, zero4};
-      if (n_in >= 0) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
+  // the sequence that starts at the present row takes over
+  auto enter = [&]() {
+    if (running && cur_out >= 0) put_state(p.h_out + (size_t)cur_out * De * 16);
+    const int4 e = s.next[head];
+    asm volatile("cp.async.wait_group %0;" ::"n"(NEXT - 1) : "memory");
+    float4 v[4] = {zero4, zero4, zero4, zero4};
+    if (e.z >= 0)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = s.h0[i][lane];
-      }
-      set_state(v);
-      running = true; cur_end = n_end; cur_out = n_out;
-      look_ahead();
-    }
-    const int m = rows_of(t, cur_end), t_next = t + m;
+      for (int i = 0; i < 4; ++i) v[i] = s.h0[head][i][lane];
+    set_state(v);
+    running = true; cur_end = e.y; cur_out = e.w;
+    __syncwarp();
+    look_ahead(head);
+    __syncwarp();
+    if (++head == NEXT) head = 0;
+  };
+  if (t < hi) fetch(t, min(RR, hi - t));
+  while (t < hi) {
+    const int m = min(RR, hi - t), t_next = t + m;
     {
       float d[8], uu[8];
       r_d.get(d); r_u.get(uu);
@@ -282,7 +292,8 @@ scan_ragged_chunks(const RaggedScan p) {
       if (!STATE) { s.c[lt][l8] = r_c; cur_u = r_u; cur_z = r_z; }
     }
     __syncwarp();
-    if (t_next < hi) fetch(t_next, rows_of(t_next, t_next < cur_end ? cur_end : n_end));
+    if (t_next < hi) fetch(t_next, min(RR, hi - t_next));
+    if (!STATE && t >= cur_end) enter();
     // one row; its operands have been requested, those of row `ahead` are before this row's arithmetic: a load issued behind a row's exponentials
     // waits for all of them
     float4 nd = s.dl[0][cg], nu = s.u[0][cg], nb = s.b[0][q], nc = STATE ? zero4 : s.c[0][q];
@@ -319,12 +330,15 @@ scan_ragged_chunks(const RaggedScan p) {
       else s.y[r][y_slot(lane, r)] = make_float4(acc[0].x, acc[0].y, acc[1].x, acc[1].y);
     };
     constexpr int UF = FINE ? 2 : STATE ? 4 : RR;
-    if (m == RR) {
+    if (m == RR && (STATE || cur_end >= t_next)) {
 #pragma unroll UF
       for (int r = 0; r < RR; ++r) row(r, min(r + 1, RR - 1));
-    } else {
+    } else {                      // the chunk's last rows, or sequences that end here
 #pragma unroll 1
-      for (int r = 0; r < m; ++r) row(r, min(r + 1, RR - 1));
+      for (int r = 0; r < m; ++r) {
+        if (!STATE && t + r >= cur_end) enter();
+        row(r, min(r + 1, RR - 1));
+      }
     }
     __syncwarp();
     if (!STATE) {
@@ -368,7 +382,7 @@ scan_ragged_chunks(const RaggedScan p) {
 
 // Chunks of the packed rows: the count with the smallest time by what the kernels were measured to take.  A block of four warps takes
 // 155 / 235 / 330 ns a row with one / two / three of them on an SM, 128 / 188 / 255 ns states only; rounds of three overlap to 268 and 200.  fp32:
-// two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains, 1.2 us from one sequence to
+// two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains, 0.4 us from one sequence to
 // the next.  The first launch walks the rows of sequences that reach over a chunk's end, of one of length `mean` about
 // mean (1 - exp(-Lc / mean)).  A function of the sizes alone, so that workspace sizing and the launch agree.
 int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
@@ -386,7 +400,7 @@ int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
   double best_t = 0.0;
   for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); ++n) {
     const double blocks = ((double)n * (De / 32) + RWARPS - 1) / RWARPS, Lc = (double)rows / n, chained = mean < Lc ? 0.0 : mean / Lc < n ? mean / Lc : n;
-    double t = time(blocks, full, Lc, 3000.0 + 100.0 * chained + 1200.0 * Lc / mean);
+    double t = time(blocks, full, Lc, 3000.0 + 100.0 * chained + 400.0 * Lc / mean);
     if (n > 1) t += time(blocks, state, mean * (1.0 - exp(-Lc / mean)), 2000.0) + 3000.0;
     if (n == 1 || t < best_t) { best = n; best_t = t; }
   }
@@ -411,15 +425,18 @@ RaggedWs ragged_ws(const rom_config& c, int n_seq, int rows) {
 
 template <typename T, bool ZOH>
 cudaError_t launch_scan_ragged(const RaggedScan& p, cudaStream_t st) {
+  constexpr int smem = RWARPS * (int)sizeof(RaggedTile);
+  cudaError_t e = cudaFuncSetAttribute(scan_ragged_chunks<T, ZOH, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(scan_ragged_chunks<T, ZOH, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
   const long long groups = p.De / 32;
   auto blocks = [&](long long chunks) { return dim3((unsigned)((chunks * groups + RWARPS - 1) / RWARPS)); };
   if (p.nch > 1) {
-    const cudaError_t e = launch_k(scan_ragged_chunks<T, ZOH, true>, blocks(p.nch - 1), RWARPS * 32, 0, st, p);
-    if (e != cudaSuccess) return e;
+    if ((e = launch_k(scan_ragged_chunks<T, ZOH, true>, blocks(p.nch - 1), RWARPS * 32, smem, st, p)) != cudaSuccess) return e;
     count_launch();
   }
   count_launch();
-  return launch_k(scan_ragged_chunks<T, ZOH, false>, blocks(p.nch), RWARPS * 32, 0, st, p);
+  return launch_k(scan_ragged_chunks<T, ZOH, false>, blocks(p.nch), RWARPS * 32, smem, st, p);
 }
 
 }  // namespace
