@@ -63,62 +63,81 @@ cudaError_t launch_conv_slot_step(const rom_config& c, const void* x, int64_t ld
 // A warp has 32 channels of one token: four float4 of state a lane (states 4 t .. of channels 8 i + g, i < 4, lane = 4 g + t), so that states move
 // as whole 512-byte rows.  u, Delta, z and y go by the lane's own channel 8 t + g: whole 64- or 128-byte rows too; the quad's lanes hand
 // their u and Delta round and meet for the sums over states so that each ends with its own channel's.
-// The eight warps of a block share their channels, that is A.
-constexpr int SS_WARPS = 8;
-template <typename T, bool ZOH>
+// The two warps of a block share their channels, that is A; beyond some thousand blocks a warp has TOK tokens, whose states are requested
+// together.
+constexpr int SS_WARPS = 2, kSlotBlocks = 148 * 32;
+template <typename T, bool ZOH, int TOK>
 __global__ void __launch_bounds__(SS_WARPS * 32)
 scan_slot_step(const T* __restrict__ u, const float* __restrict__ delta, const float* __restrict__ A, const float* __restrict__ Bm,
                const float* __restrict__ Cm, long long ldb, const float* __restrict__ D, const T* __restrict__ z, long long ldz,
                const int32_t* __restrict__ slot, int n_slots, const float* h_in, float* h_out, T* __restrict__ y, int De, int B) {
   pdl_sync();
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int b = blockIdx.y * SS_WARPS + (threadIdx.x >> 5), c0 = blockIdx.x * 32, mine = c0 + 8 * t + g;
-  if (b >= B) return;
-  const int sl = slot ? __ldg(slot + b) : b;
-  const size_t at = (size_t)b * De + mine;
-  const float uu = to_f32(u[at]), dl = __ldg(delta + at), zz = z ? to_f32(z[(size_t)b * ldz + mine]) : 0.0f, Dc = D ? __ldg(D + mine) : 0.0f;
-  const float4 b4 = load4_any(Bm + (size_t)b * ldb + 4 * t), c4 = load4_any(Cm + (size_t)b * ldb + 4 * t);
-  float4 a4[4], h4[4];
+  const int b0 = blockIdx.y * SS_WARPS * TOK + (threadIdx.x >> 5), c0 = blockIdx.x * 32, mine = c0 + 8 * t + g;
+  int sl[TOK];
+#pragma unroll
+  for (int k = 0; k < TOK; ++k) {
+    const int b = b0 + k * SS_WARPS;
+    sl[k] = b >= B ? -1 : slot ? __ldg(slot + b) : b;
+    if (sl[k] >= n_slots) sl[k] = -1;
+  }
+  float4 a4[4], h4[TOK][4], b4[TOK], c4[TOK];
+  float uu[TOK], dl[TOK], zz[TOK];
 #pragma unroll
   for (int i = 0; i < 4; ++i) a4[i] = __ldg(reinterpret_cast<const float4*>(A + (size_t)(c0 + 8 * i + g) * 16) + t);
-  if (sl < 0 || sl >= n_slots) return;
-  const size_t hp = ((size_t)sl * De + c0 + g) * 16 + 4 * t;
+  const float Dc = D ? __ldg(D + mine) : 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h4[i] = *reinterpret_cast<const float4*>(h_in + hp + (size_t)i * 128);
-  const float bb[4] = {b4.x, b4.y, b4.z, b4.w}, cc[4] = {c4.x, c4.y, c4.z, c4.w};
-  float part[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float ui = __shfl_sync(0xffffffffu, uu, (lane & 28) + i), di = __shfl_sync(0xffffffffu, dl, (lane & 28) + i);
-    const float av[4] = {a4[i].x, a4[i].y, a4[i].z, a4[i].w};
-    float hv[4] = {h4[i].x, h4[i].y, h4[i].z, h4[i].w}, p = 0.0f;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      float a, e;
-      decay(di * av[n], a, e);
-      hv[n] = fmaf(a, hv[n], (ZOH ? __fdividef(e, av[n]) : di) * (ui * bb[n]));
-      p = fmaf(cc[n], hv[n], p);
-    }
-    *reinterpret_cast<float4*>(h_out + hp + (size_t)i * 128) = make_float4(hv[0], hv[1], hv[2], hv[3]);
-    part[i] = p;
+  for (int k = 0; k < TOK; ++k) {
+    const size_t b = min(b0 + k * SS_WARPS, B - 1), at = b * De + mine;
+    uu[k] = to_f32(u[at]); dl[k] = __ldg(delta + at); zz[k] = z ? to_f32(z[b * ldz + mine]) : 0.0f;
+    b4[k] = load4_any(Bm + b * ldb + 4 * t); c4[k] = load4_any(Cm + b * ldb + 4 * t);
   }
-  // sums over the quad: lane t keeps channel group t
-  const bool hi = t & 2, odd = t & 1;
-  const float s0 = (hi ? part[2] : part[0]) + __shfl_xor_sync(0xffffffffu, hi ? part[0] : part[2], 2);
-  const float s1 = (hi ? part[3] : part[1]) + __shfl_xor_sync(0xffffffffu, hi ? part[1] : part[3], 2);
-  float o = (odd ? s1 : s0) + __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, 1);
-  o = fmaf(Dc, uu, o);
-  if (z) o *= sizeof(T) == 2 ? silu_fast(zz) : silu_f(zz);
-  y[at] = from_f32<T>(o);
+#pragma unroll
+  for (int k = 0; k < TOK; ++k)
+    if (sl[k] >= 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h4[k][i] = *reinterpret_cast<const float4*>(h_in + ((size_t)sl[k] * De + c0 + 8 * i + g) * 16 + 4 * t);
+#pragma unroll
+  for (int k = 0; k < TOK; ++k) {
+    if (sl[k] < 0) continue;
+    const float bb[4] = {b4[k].x, b4[k].y, b4[k].z, b4[k].w}, cc[4] = {c4[k].x, c4[k].y, c4[k].z, c4[k].w};
+    float part[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float ui = __shfl_sync(0xffffffffu, uu[k], (lane & 28) + i), di = __shfl_sync(0xffffffffu, dl[k], (lane & 28) + i);
+      const float av[4] = {a4[i].x, a4[i].y, a4[i].z, a4[i].w};
+      float hv[4] = {h4[k][i].x, h4[k][i].y, h4[k][i].z, h4[k][i].w}, p = 0.0f;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        float a, e;
+        decay(di * av[n], a, e);
+        hv[n] = fmaf(a, hv[n], (ZOH ? __fdividef(e, av[n]) : di) * (ui * bb[n]));
+        p = fmaf(cc[n], hv[n], p);
+      }
+      __stcs(reinterpret_cast<float4*>(h_out + ((size_t)sl[k] * De + c0 + 8 * i + g) * 16 + 4 * t), make_float4(hv[0], hv[1], hv[2], hv[3]));
+      part[i] = p;
+    }
+    // sums over the quad: lane t keeps channel group t
+    const bool hi = t & 2, odd = t & 1;
+    const float s0 = (hi ? part[2] : part[0]) + __shfl_xor_sync(0xffffffffu, hi ? part[0] : part[2], 2);
+    const float s1 = (hi ? part[3] : part[1]) + __shfl_xor_sync(0xffffffffu, hi ? part[1] : part[3], 2);
+    float o = (odd ? s1 : s0) + __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, 1);
+    o = fmaf(Dc, uu[k], o);
+    if (z) o *= sizeof(T) == 2 ? silu_fast(zz[k]) : silu_f(zz[k]);
+    y[(size_t)(b0 + k * SS_WARPS) * De + mine] = from_f32<T>(o);
+  }
 }
 
 template <typename T>
 cudaError_t launch_scan_slot_step(const rom_config& c, const void* u, const float* delta, const float* A, const float* Bm, const float* Cm, int64_t ldb,
                                   const float* D, const void* z, int64_t ldz, const int32_t* slot, int n_slots, const float* h_in, float* h_out, void* y,
                                   cudaStream_t st) {
-  auto kern = c.disc_mode == 0 ? scan_slot_step<T, true> : scan_slot_step<T, false>;
+  const bool many = (long long)(c.d_inner / 32) * ((c.B + SS_WARPS - 1) / SS_WARPS) >= kSlotBlocks;
+  auto kern = many ? (c.disc_mode == 0 ? scan_slot_step<T, true, 2> : scan_slot_step<T, false, 2>)
+                   : (c.disc_mode == 0 ? scan_slot_step<T, true, 1> : scan_slot_step<T, false, 1>);
+  const int per = SS_WARPS * (many ? 2 : 1);
   count_launch();
-  return launch_k(kern, dim3(c.d_inner / 32, (c.B + SS_WARPS - 1) / SS_WARPS), SS_WARPS * 32, 0, st, (const T*)u, delta, A, Bm, Cm, (long long)ldb, D,
+  return launch_k(kern, dim3(c.d_inner / 32, (c.B + per - 1) / per), SS_WARPS * 32, 0, st, (const T*)u, delta, A, Bm, Cm, (long long)ldb, D,
                   (const T*)z, (long long)ldz, slot, n_slots, h_in, h_out, (T*)y, c.d_inner, c.B);
 }
 
