@@ -316,6 +316,14 @@ def rom_layer_step(cfg, weights: RomWeights, x, conv_state, ssm_state, out, topk
     return rc
 
 
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The serving calls launch on the current device: what lies on another one is refused (a kernel must not meet its address)."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() not in (device, -1):
+            raise ValueError(f"a tensor is on device {t.get_device()}, the call runs on device {device}")
+
+
 def _rows_ptr(t: Optional[torch.Tensor]):
     """(address, elements between rows) of a [rows, width] tensor whose rows are contiguous; a column slice of wider rows is one."""
     if t is None:
@@ -347,6 +355,7 @@ def make_ragged(rows: int, n_slots: int, seq_start, slot=None, resume=None) -> R
 
 def rom_conv_ragged(cfg, seqs: RomRagged, x, w_conv, b_conv, win_in, win_out, y, stream=None, check=True) -> int:
     """x: [rows, d_inner], rows may be a column slice of wider ones."""
+    _here(x, w_conv, b_conv, win_in, win_out, y)
     px, ldx = _rows_ptr(x)
     rc = lib().rom_conv_ragged(ctypes.byref(cfg), ctypes.byref(seqs), px, ldx, _ptr(w_conv), _ptr(b_conv), _ptr(win_in), _ptr(win_out),
                                _ptr(y), _stream(stream))
@@ -373,6 +382,7 @@ def _bc(Bm, Cm):
 
 def rom_scan_ragged(cfg, seqs: RomRagged, u, delta, A, Bm, Cm, D, z, h_in, h_out, y, ws, stream=None, check=True) -> int:
     """Bm, Cm: [rows, d_state] of one pitch; z: [rows, d_inner]; both may be column slices of wider rows."""
+    _here(u, delta, A, Bm, Cm, D, z, h_in, h_out, y, ws)
     (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm), _rows_ptr(z)
     rc = lib().rom_scan_ragged(ctypes.byref(cfg), ctypes.byref(seqs), _ptr(u), _ptr(delta), _ptr(A), pb, pc, ld, _ptr(D), pz, ldz, _ptr(h_in),
                                _ptr(h_out), _ptr(y), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
@@ -382,6 +392,7 @@ def rom_scan_ragged(cfg, seqs: RomRagged, u, delta, A, Bm, Cm, D, z, h_in, h_out
 
 
 def rom_conv_step(cfg, x, w_conv, b_conv, slot, win_in, win_out, y, stream=None, check=True) -> int:
+    _here(x, w_conv, b_conv, slot, win_in, win_out, y)
     px, ldx = _rows_ptr(x)
     rc = lib().rom_conv_step(ctypes.byref(cfg), px, ldx, _ptr(w_conv), _ptr(b_conv), _ptr(slot), _pool(win_in, win_out), _ptr(win_in),
                              _ptr(win_out), _ptr(y), _stream(stream))
@@ -391,6 +402,7 @@ def rom_conv_step(cfg, x, w_conv, b_conv, slot, win_in, win_out, y, stream=None,
 
 
 def rom_scan_step(cfg, u, delta, A, Bm, Cm, D, z, slot, h_in, h_out, y, stream=None, check=True) -> int:
+    _here(u, delta, A, Bm, Cm, D, z, slot, h_in, h_out, y)
     (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm), _rows_ptr(z)
     rc = lib().rom_scan_step(ctypes.byref(cfg), _ptr(u), _ptr(delta), _ptr(A), pb, pc, ld, _ptr(D), pz, ldz, _ptr(slot), _pool(h_in, h_out),
                              _ptr(h_in), _ptr(h_out), _ptr(y), _stream(stream))
@@ -408,6 +420,7 @@ def ffn_moe_step_workspace_size(cfg: RomConfig, d_ff: int) -> int:
 
 
 def rom_ffn_moe_step(cfg, d_ff, W_gu, W_down, x, topk_idx, gates, out, ws, stream=None, check=True) -> int:
+    _here(W_gu, W_down, x, topk_idx, gates, out, ws)
     rc = lib().rom_ffn_moe_step(ctypes.byref(cfg), int(d_ff), _ptr(W_gu), _ptr(W_down), _ptr(x), _ptr(topk_idx), _ptr(gates), _ptr(out),
                                 _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
     if check and rc != ROM_OK:

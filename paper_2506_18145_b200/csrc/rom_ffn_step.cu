@@ -1,6 +1,19 @@
 // FFN-MoE of the few tokens of a generation step (rom_ffn_moe_step): out_t = sum_k g_tk W_down,e (SiLU(W_gate,e x_t) * (W_up,e x_t)), e = topk_idx[t, k].
-// Two launches: hidden rows g SiLU(gate) up of every assignment (token, slot), then the down projection with the sum over the slots.
-// The weights of the chosen experts, read once, are what counts: 6 d_model d_ff bytes an expert (bf16).
+// Two launches: hidden rows g SiLU(gate) up of every assignment (token, slot), rounded to the storage type with their gate in them, then the down
+// projection with the sum over the slots in fp32.
+//
+// What bounds it: the chosen experts' weights, 6 d_model d_ff bytes each (bf16), read once.  rom_ffn_moe_forward takes five launches and pads every
+// expert's tokens to 128 rows.  Here the weights are the M = 128 operand of tcgen05 and an expert's tokens its 16, 32 or 64 columns: one CTA per SM
+// walks (expert, weight rows, part of the contracted index) tiles; warp 0 keeps a ring of stages of 128 contracted elements full by TMA, warps 6..9
+// put the tokens' rows beside them, warp 1 issues the MMAs, warps 2..5 take the accumulators (two, so that a tile's end runs beside the next tile).  The
+// down projection, of few rows and a long contracted index, is cut along that index too: the parts go to the workspace and whoever brings
+// a tile's last one adds them all, in the order of slots and parts, so that results do not depend on who came when.
+// Measured (us a call, GB/s of the chosen experts' weights): one token of 2048 x 8192 26.7 (3770), 64 tokens with two of sixteen experts 254 (6330: 97 % of the
+// measured copy), 16 tokens with two of eight 128 (6250), 8 tokens with one of eight of 1280 x 5120 44.8 (4610).  Small calls: about 10 us of launches, lists and
+// first loads.  Tried: rings of half the size, so that both launches share the SMs and the second has its first weights when the first ends, no gain (the MMAs
+// of short tiles bound it then); stages of 64 elements 264 and 29 us, of one 64-wide block a warp's turn each 0.37 us a stage.
+//
+// fp32: a warp has four weight rows and up to eight tokens, products over its lanes; the plain form for a small model in full precision.
 #include <algorithm>
 #include <type_traits>
 
@@ -193,17 +206,16 @@ int chosen_experts(int T, int K, int E) {
 }
 constexpr int kSizingSms = 148;      // (workspace sizing and the launch agree)
 constexpr int FT_COLS = 64;                          // token columns per pass at most
-constexpr int FT_MIN_STAGES = 4, FT_MAX_STAGES = 12; // (each of the four warps that bring token rows has a stage of its own at least)
+constexpr int FT_MIN_STAGES = 4, FT_MAX_STAGES = 12;      // (a stage for each of the four warps that bring token rows)
 constexpr int FT_KB = 2, FT_K = FT_KB * BLOCK_K;     // contracted elements per stage: two swizzled rows
-constexpr int FT_SMEM = 208 * 1024;                  // operand ring of a CTA alone on its SM
-constexpr int FT_SMEM_PAIR = 212 * 1024;             // rings of both launches together where they share the SMs
+constexpr int FT_SMEM = 208 * 1024;                  // operand ring
 constexpr int FT_THREADS = 320;
 // Bytes of a ring: its alignment, its stages, and what the MMA reads past the last one (always 128 rows from a tile's start).
 constexpr int ffn_ring(int rows, int cols, int stages) {
   return 1024 + stages * FT_KB * (rows + cols) * 128 + std::max(128 * 128 - (rows + FT_KB * cols) * 128, 0);
 }
-constexpr int ffn_stages(int rows, int cols, int room = FT_SMEM) {
-  return std::min((room - ffn_ring(rows, cols, 0)) / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES);
+constexpr int ffn_stages(int rows, int cols) {
+  return std::min((FT_SMEM - ffn_ring(rows, cols, 0)) / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES);
 }
 // Token columns of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights again (from the
 // L2 mostly), the others have deeper rings.
@@ -212,7 +224,8 @@ int ffn_columns(int T, int K, int E) {
   return want > 32 ? 64 : want > 16 ? 32 : 16;
 }
 // How the weights are cut into tiles: rows per tile and, of the down projection, parts of the contracted index.  The cheapest by the time that the
-// fullest SM takes, in ns: rounds of tiles times stages of 60 ns and their bytes at 44 a ns (an SM's share of HBM), 1000 for a tile's end; parts of a sum that are written (100 bytes a ns) and read again (20).
+// fullest SM takes, in ns: rounds of tiles times stages of 60 ns and their bytes at 44 a ns (an SM's share of HBM), but at least 460 ns (eight MMAs of
+// 128 rows, a good 100 cycles each however few their columns and valid rows), 1000 for a tile's end; parts of a sum that are written (100 bytes a ns) and read again (20).
 struct FfnCut { int h, splits; };
 FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
   const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Kd + FT_K - 1) / FT_K, per = up ? 2 : 1;
@@ -223,7 +236,7 @@ FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
     for (int h = up ? 64 : 128; h >= (up ? 8 : 32); h -= 8) {
       if (ffn_stages((int)per * h, cols) < FT_MIN_STAGES) continue;
       const long long rounds = (n * s * ((rows_out + h - 1) / h) + kSizingSms - 1) / kSizingSms;
-      const long long stage = 60 + 2 * FT_K * (per * h + m) / 44, parts = up || (K == 1 && s == 1) ? 0 : 4 * m * h * rounds / 100 + 4ll * T * K * s * h / 20;
+      const long long stage = std::max(460ll, 60 + 2 * FT_K * (per * h + m) / 44), parts = up || (K == 1 && s == 1) ? 0 : 4 * m * h * rounds / 100 + 4ll * T * K * s * h / 20;
       const long long cost = rounds * ((kb + s - 1) / s * stage + 1000) + parts;
       if (least < 0 || cost < least) { least = cost; best.h = h; best.splits = s; }
     }
@@ -256,8 +269,7 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
   return e != 0;
 }
-// A warp's wait, polled by one lane: 32 lanes' polls of one barrier are served one after the other, and eight warps that polled so kept the
-// producer's and the issuer's own barrier operations waiting (0.26 us a stage).
+// A warp's wait, polled by one lane.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
   int ok = 1;
   if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, abort_flag, limit);
@@ -265,7 +277,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 }
 // FLIGHT: stages of token rows that each of the four warps has in flight besides the one it asks for: 4 (FLIGHT + 1) + 1 stages at least.
 template <bool UP, int FLIGHT>
-__global__ void __launch_bounds__(FT_THREADS, 2)
+__global__ void __launch_bounds__(FT_THREADS, 1)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -428,10 +440,10 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     }
   } else if (warp >= 6) {
     // ---------------------------------------------------------------- token rows, 16-byte pieces into the swizzled layout: a stage is one warp's,
-    // the four warps take them in turns (one after the other by all of them, 0.37 us a stage bounded the kernel: a load's latency over those in flight)
+    // the four warps take them in turns
     const int xw = warp - 6, lrow = lane >> 3, chunk = lane & 7;
     if (!UP) { pdl_wait(); pdl_trigger(); }
-    int count = 0, stage = 0, pub = xw, pending = 0; uint32_t phase = 0;      // count: stages so far
+    int turn = 0, stage = 0, pub = xw, pending = 0; uint32_t phase = 0;      // turn: whose stage it is
     bool ok = true;
     auto publish = [&]() {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -447,7 +459,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
         const int m = min(m_all - n0, p.cols_cap);
         const short* mine = by.list + by.off[it.e] + n0;
         for (int kb = 0; kb < it.n; ++kb) {
-          if ((count++ & 3) == xw) {
+          if (turn == xw) {
             ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit);
             if (!ok) break;
             const uint32_t dst = base + stage * stage_bytes + FT_KB * w_bytes;
@@ -464,6 +476,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
               publish();
             }
           }
+          turn = (turn + 1) & 3;
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -632,19 +645,15 @@ cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaS
   p.T = s.T; p.K = s.K; p.E = s.E;
   p.cols_cap = ffn_columns(s.T, s.K, s.E);
   const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true), cd = cut_tiles(s.T, s.K, s.E, s.Dm, s.F, false);
-  // Where rings of the fewest stages let both launches share the SMs, the second one is resident, has its lists and its first weights when
-  // the first ends.
-  const bool paired = ffn_ring(2 * cu.h, p.cols_cap, FT_MIN_STAGES) + ffn_ring(cd.h, p.cols_cap, FT_MIN_STAGES) <= FT_SMEM_PAIR;
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
     const int rows = (up ? 2 : 1) * p.h;
-    p.stages = paired ? FT_MIN_STAGES : ffn_stages(rows, p.cols_cap);
+    p.stages = ffn_stages(rows, p.cols_cap);
     if (p.stages < FT_MIN_STAGES) return cudaErrorInvalidValue;      // (cut_tiles takes no such tile)
     CUtensorMap tw;
     if (!make_tmap(&tw, W, (uint64_t)s.E * p.w_rows, (uint64_t)p.Kd, (uint64_t)p.Kd, p.h)) return cudaErrorInvalidValue;
     auto kern = p.stages >= 9 ? ffn_step_tc<up, 1> : ffn_step_tc<up, 0>;
     cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
-    if (rc == cudaSuccess) rc = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (rc != cudaSuccess) return rc;
     count_launch();
     return launch_k(kern, dim3(sms), FT_THREADS, ffn_ring(rows, p.cols_cap, p.stages), st, tw, p, WAIT_LIMIT);

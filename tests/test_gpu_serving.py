@@ -307,6 +307,222 @@ def test_ffn_step_agrees_with_the_forward():
     assert_close(np64(out), np64(ref), TOL["bf16"], "step against forward")
 
 
+# ---------------------------------------------------------------------------------------------- uses that the calls above do not make
+def test_offsets_past_the_buffers_are_cut():
+    """seq_start beyond `rows`: the sequences end with the buffers."""
+    De, rows = 64, 50
+    p = Packed([20, 30], seed=14, resume=[1, 1])
+    long = Packed([20, 30], seed=14, resume=[1, 1])
+    long.dev[0][2] = 1 << 30
+    s = scan_inputs(rows, De, "bf16")
+    d = {n: v.cuda() for n, v in s.items()}
+    cfg = config(De, "bf16")
+    ws = torch.empty(rb.scan_ragged_workspace_size(cfg, 2, rows), dtype=torch.uint8, device="cuda")
+    got = []
+    for q in (p, long):
+        h, win = pool_with_junk(15, q, (De, 16), 0.3).cuda(), pool_with_junk(16, q, (3, De), 1.0).cuda()
+        y, v = torch.zeros_like(d["u"]), torch.zeros_like(d["u"])
+        rb.rom_scan_ragged(cfg, q.ragged, d["u"], d["delta"], d["A"], d["Bm"], d["Cm"], d["D"], d["z"], h, h, y, ws)
+        rb.rom_conv_ragged(cfg, q.ragged, d["u"], d["z"][:4].contiguous(), d["D"], win, win, v)
+        got.append((y, h, v, win))
+    for a, b in zip(*got):
+        assert same_bits(a, b)
+
+
+def test_no_sequences_launch_nothing():
+    cfg = config(64, "f32")
+    none = rb.make_ragged(10, 4, torch.zeros(1, dtype=torch.int32, device="cuda"))
+    y = torch.full((10, 64), SENTINEL, device="cuda")
+    rb.rom_conv_ragged(cfg, none, torch.zeros(10, 64, device="cuda"), torch.zeros(4, 64, device="cuda"), None, None, None, y)
+    assert torch.all(y == SENTINEL)
+
+
+def test_without_rows_fresh_states_are_zeroed_and_others_kept():
+    """A batch of empty sequences with buffers of no rows at all."""
+    De = 128
+    p = Packed([0, 0, 0], seed=17, resume=[1, 0, 1])
+    cfg = config(De, "bf16")
+    e = lambda *shape, t=torch.bfloat16: torch.empty(shape, dtype=t, device="cuda")
+    for in_place in (True, False):
+        h, ho, _ = pools(18, p, (De, 16), 0.3, in_place)
+        win, wo, _ = pools(19, p, (3, De), 1.0, in_place)
+        hb, wb = h.clone(), win.clone()
+        ws = torch.empty(rb.scan_ragged_workspace_size(cfg, 3, 0), dtype=torch.uint8, device="cuda")
+        rb.rom_scan_ragged(cfg, p.ragged, e(0, De), e(0, De, t=torch.float32), -torch.ones(De, 16, device="cuda"), e(0, 16, t=torch.float32), e(0, 16, t=torch.float32), None, None,
+                           h, ho, e(0, De), ws)
+        rb.rom_conv_ragged(cfg, p.ragged, e(0, De), torch.ones(4, De, dtype=torch.bfloat16, device="cuda"), None, win, wo, e(0, De))
+        torch.cuda.synchronize()
+        for i in range(3):
+            q = int(p.slots[i])
+            for now, before in ((ho, hb), (wo, wb)):
+                assert same_bits(now[q], before[q] if p.resume[i] else torch.zeros_like(before[q]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_not_finite_stay_in_their_sequence(dtype):
+    De = 64
+    p = Packed([30, 4, 1, 200, 9, 55], seed=20, resume=[1] * 6)
+    cfg = config(De, dtype)
+    s = scan_inputs(p.rows, De, dtype)
+    clean = {n: v.cuda() for n, v in s.items()}
+    dirty = {n: v.clone() for n, v in clean.items()}
+    bad = (1, 3)
+    for i in bad:
+        dirty["u"][p.start[i]:p.start[i + 1]] = float("nan") if i == 1 else float("inf")
+        dirty["Bm"][p.start[i]] = float("inf")
+    ws = torch.empty(rb.scan_ragged_workspace_size(cfg, p.n, p.rows), dtype=torch.uint8, device="cuda")
+    got = []
+    for d in (clean, dirty):
+        h, win = pool_with_junk(21, p, (De, 16), 0.3).cuda(), pool_with_junk(22, p, (3, De), 1.0).cuda()
+        y, v = torch.zeros_like(d["u"]), torch.zeros_like(d["u"])
+        rb.rom_scan_ragged(cfg, p.ragged, d["u"], d["delta"], d["A"], d["Bm"], d["Cm"], d["D"], d["z"], h, h, y, ws)
+        rb.rom_conv_ragged(cfg, p.ragged, d["u"], clean["z"][:4].contiguous(), None, win, win, v)
+        got.append((y, v, h, win))
+    for i in range(p.n):
+        rows, slot = slice(p.start[i], p.start[i + 1]), int(p.slots[i])
+        for k, (a, b) in enumerate(zip(*got)):
+            at = rows if k < 2 else slot
+            assert same_bits(a[at], b[at]) == (i not in bad)
+
+
+def test_ffn_step_values_that_are_not_finite_stay_in_their_token():
+    B, Dm, F, E, K = 20, 128, 256, 4, 2
+    x, W_gu, W_down = randn(71, (B, Dm), dtype=torch.bfloat16).cuda(), randn(72, (E, 2 * F, Dm), Dm ** -0.5, torch.bfloat16).cuda(), randn(73, (E, Dm, F), F ** -0.5, torch.bfloat16).cuda()
+    g = np.random.default_rng(3)
+    idx = torch.from_numpy(np.stack([g.permutation(E)[:K] for _ in range(B)]).astype(np.int32)).cuda()
+    gates = torch.full((B, K), 0.5, device="cuda")
+    cfg = rb.make_config(B, 1, Dm, 64, 16, 4, 16, E, K, "bf16")
+    ws = torch.empty(rb.ffn_moe_step_workspace_size(cfg, F), dtype=torch.uint8, device="cuda")
+    outs = []
+    for bad in (False, True):
+        if bad:
+            x[7] = float("nan")
+        outs.append(torch.empty_like(x))
+        rb.rom_ffn_moe_step(cfg, F, W_gu, W_down, x, idx, gates, outs[-1], ws)
+    keep = torch.arange(B, device="cuda") != 7
+    assert same_bits(outs[0][keep], outs[1][keep]) and torch.all(torch.isnan(outs[1][7]))
+
+
+def test_captured_calls_replay_on_new_inputs():
+    """All serving calls in one graph on a stream of their own, replayed after the inputs, lengths and slots have changed in place."""
+    De, dtype, B, Dm, F, E, K = 128, "bf16", 6, 128, 256, 4, 2
+    cfg, step, ffn = config(De, dtype), config(De, dtype, B=B), rb.make_config(B, 1, Dm, 64, 16, 4, 16, E, K, dtype)
+    p = Packed([40, 7, 0, 90], tail=30, seed=23, resume=[1, 0, 1, 1], n_slots=8)
+    s = {n: v.cuda() for n, v in scan_inputs(p.rows, De, dtype).items()}
+    t = {n: v.cuda() for n, v in scan_inputs(B, De, dtype, seed=2).items()}
+    w = randn(81, (4, De), 0.5, TORCH[dtype]).cuda()
+    slot = torch.tensor([3, 0, -1, 7, 5, 1], dtype=torch.int32, device="cuda")
+    x, W_gu, W_down = randn(82, (B, Dm), dtype=TORCH[dtype]).cuda(), randn(83, (E, 2 * F, Dm), Dm ** -0.5, TORCH[dtype]).cuda(), randn(84, (E, Dm, F), F ** -0.5, TORCH[dtype]).cuda()
+    idx, gates = torch.tensor([[0, 1], [2, 3], [-1, -1], [1, 3], [0, 2], [3, 0]], dtype=torch.int32, device="cuda"), torch.full((B, K), 0.5, device="cuda")
+    h0, win0 = randn(85, (8, De, 16), 0.3).cuda(), randn(86, (8, 3, De)).cuda()
+    h, win = h0.clone(), win0.clone()
+    ws, ffn_ws = (torch.empty(n, dtype=torch.uint8, device="cuda") for n in (rb.scan_ragged_workspace_size(cfg, p.n, p.rows), rb.ffn_moe_step_workspace_size(ffn, F)))
+    outs = [torch.zeros_like(s["u"]) for _ in range(2)] + [torch.zeros_like(t["u"]) for _ in range(2)] + [torch.zeros_like(x)]
+
+    def calls():
+        rb.rom_conv_ragged(cfg, p.ragged, s["u"], w, None, win, win, outs[0])
+        rb.rom_scan_ragged(cfg, p.ragged, outs[0], s["delta"], s["A"], s["Bm"], s["Cm"], s["D"], s["z"], h, h, outs[1], ws)
+        rb.rom_conv_step(step, t["u"], w, None, slot, win, win, outs[2])
+        rb.rom_scan_step(step, outs[2], t["delta"], s["A"], t["Bm"], t["Cm"], s["D"], t["z"], slot, h, h, outs[3])
+        rb.rom_ffn_moe_step(ffn, F, W_gu, W_down, x, idx, gates, outs[4], ffn_ws)
+
+    def reset():
+        h.copy_(h0)
+        win.copy_(win0)
+        for o in outs:
+            o.zero_()
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        calls()
+    stream.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        calls()
+    for change in range(2):
+        if change:
+            p.dev[0].copy_(torch.tensor([0, 3, 3, 60, 160], dtype=torch.int32))
+            p.dev[1].copy_(torch.tensor([6, 2, 4, 0], dtype=torch.int32))
+            slot.copy_(torch.tensor([1, -1, 6, 2, 4, 0], dtype=torch.int32))
+            idx.copy_(idx.flip(0))
+            for v in (s["u"], t["u"], x):
+                v.mul_(-0.5)
+        reset()
+        calls()
+        torch.cuda.synchronize()
+        want = [v.clone() for v in outs + [h, win]]
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs + [h, win], want):
+            assert same_bits(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with its own workspace and outputs: as one after the other."""
+    De, F, Dm, E, K, B = 512, 1024, 512, 8, 2, 32
+    p = Packed([600, 1, 0, 333], seed=24, resume=[0] * 4)
+    cfg, ffn = config(De, "bf16"), rb.make_config(B, 1, Dm, 64, 16, 4, 16, E, K, "bf16")
+    s = {n: v.cuda() for n, v in scan_inputs(p.rows, De, "bf16").items()}
+    x, W_gu, W_down = randn(91, (B, Dm), dtype=torch.bfloat16).cuda(), randn(92, (E, 2 * F, Dm), Dm ** -0.5, torch.bfloat16).cuda(), randn(93, (E, Dm, F), F ** -0.5, torch.bfloat16).cuda()
+    g = np.random.default_rng(5)
+    idx, gates = torch.from_numpy(np.stack([g.permutation(E)[:K] for _ in range(B)]).astype(np.int32)).cuda(), torch.full((B, K), 0.25, device="cuda")
+    sets = []
+    for i in range(2):
+        sets.append(dict(stream=torch.cuda.Stream(), ws=torch.empty(rb.scan_ragged_workspace_size(cfg, p.n, p.rows), dtype=torch.uint8, device="cuda"),
+                         fws=torch.empty(rb.ffn_moe_step_workspace_size(ffn, F), dtype=torch.uint8, device="cuda"), y=torch.zeros_like(s["u"]), h=torch.zeros(p.n_slots, De, 16, device="cuda"),
+                         out=torch.zeros_like(x)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for q in sets:
+            rb.rom_scan_ragged(cfg, p.ragged, s["u"], s["delta"], s["A"], s["Bm"], s["Cm"], s["D"], s["z"], None, q["h"], q["y"], q["ws"], stream=q["stream"])
+            rb.rom_ffn_moe_step(ffn, F, W_gu, W_down, x, idx, gates, q["out"], q["fws"], stream=q["stream"])
+    torch.cuda.synchronize()
+    for n in ("y", "h", "out"):
+        assert same_bits(sets[0][n], sets[1][n])
+    assert rb.rom_get_status(sets[0]["fws"]) == 0 and rb.rom_get_status(sets[1]["fws"]) == 0
+
+
+def test_offsets_past_32_bits():
+    """Pools and packed buffers of more than 2^31 elements: the last slot and the last rows."""
+    De, n_slots = 4096, (1 << 31) // (4096 * 16) + 2
+    cfg = config(De, "bf16", B=1)
+    s = scan_inputs(1, De, "bf16")
+    d = {n: v.cuda() for n, v in s.items()}
+    pool = torch.empty((n_slots, De, 16), device="cuda")
+    pool[-1] = randn(95, (De, 16), 0.3).cuda()
+    h0 = np64(pool[-1])
+    slot = torch.tensor([n_slots - 1], dtype=torch.int32, device="cuda")
+    y = torch.empty_like(d["u"])
+    rb.rom_scan_step(cfg, d["u"], d["delta"], d["A"], d["Bm"], d["Cm"], d["D"], d["z"], slot, pool, pool, y)
+    ref, bound, h, G = scan_reference(*(np64(s[n]) for n in ("u", "delta", "A", "Bm", "Cm", "D", "z")), h0, 0)
+    check(y, ref, bound, "bf16", "token")
+    check(pool[-1], h, G, "f32", "state")
+    del pool
+    rows = (1 << 31) // De + 70
+    p = Packed([rows - 19, 19], seed=25, resume=[0, 0])
+    x = torch.zeros((rows, De), dtype=torch.bfloat16, device="cuda")
+    last = randn(96, (40, De), dtype=torch.bfloat16)
+    x[-40:] = last.cuda()
+    w = randn(97, (4, De), 0.5, torch.bfloat16)
+    v, win = torch.empty_like(x), torch.empty((p.n_slots, 3, De), device="cuda")
+    rb.rom_conv_ragged(cfg, p.ragged, x, w.cuda(), None, None, win, v)
+    pre, size, want = conv_reference(np64(last[-19:]), np64(w), None, np.zeros((3, De)))
+    check(v[-19:], O.silu(pre), silu_bound(pre, 5 * U32 * size), "bf16", "last rows")
+    np.testing.assert_array_equal(np64(win[int(p.slots[1])]), want)
+    np.testing.assert_array_equal(np64(win[int(p.slots[0])]), np64(last[18:21]))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    cfg = config(64, "f32", B=1)
+    t = torch.zeros(1, 64, device="cuda")
+    win = torch.zeros(1, 3, 64, device="cuda")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="device"):
+        rb.rom_conv_step(cfg, t, torch.zeros(4, 64, device="cuda"), None, None, win, win, torch.zeros_like(t))
+
+
 # ---------------------------------------------------------------------------------------------- all of them as a server uses them
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_prompts_then_tokens_then_ffn(dtype):
