@@ -145,9 +145,9 @@ def _ptr(t: Optional[torch.Tensor], cuda: bool = True) -> Optional[int]:
     return t.data_ptr()
 
 
-def _stream(stream: Optional[torch.cuda.Stream]) -> int:
+def _stream(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> int:
     # (the current stream's handle alone: 0.2 us, where the Stream object around it takes 3.3)
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
 
 
 def workspace_size(cfg: RomConfig) -> int:
@@ -316,20 +316,23 @@ def rom_layer_step(cfg, weights: RomWeights, x, conv_state, ssm_state, out, topk
     return rc
 
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """The serving calls launch on the current device: what lies on another one is refused (a kernel must not meet its address)."""
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() not in (device, -1):
-            raise ValueError(f"a tensor is on device {t.get_device()}, the call runs on device {device}")
+def _at(t: Optional[torch.Tensor], device: int) -> Optional[int]:
+    """Address of a contiguous tensor of a serving call.  These launch on the current device: what lies on another one (or on the host) is refused."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"a tensor is on device {t.device}, the call runs on cuda:{device}")
+    if not t.is_contiguous():
+        raise ValueError("expected a contiguous tensor")
+    return t.data_ptr()
 
 
-def _rows_ptr(t: Optional[torch.Tensor]):
+def _rows_at(t: Optional[torch.Tensor], device: int):
     """(address, elements between rows) of a [rows, width] tensor whose rows are contiguous; a column slice of wider rows is one."""
     if t is None:
         return None, 0
-    if not t.is_cuda:
-        raise ValueError("expected a CUDA tensor")
+    if t.get_device() != device:
+        raise ValueError(f"a tensor is on device {t.device}, the call runs on cuda:{device}")
     pitch = t.stride()
     if len(pitch) != 2 or pitch[1] != 1:
         raise ValueError("expected a tensor [rows, width] with contiguous rows")
@@ -337,28 +340,39 @@ def _rows_ptr(t: Optional[torch.Tensor]):
     return t.data_ptr(), pitch[0] if rows > 1 else width      # (a single row has no pitch: torch may say anything)
 
 
-def _pool(a: torch.Tensor, b: torch.Tensor) -> int:
+def _slots(a: torch.Tensor, b: torch.Tensor) -> int:
     """Slots of the state pools of a call."""
-    if a.size(0) != b.size(0):
+    n = a.size(0)
+    if b is not a and b.size(0) != n:
         raise ValueError("the pools differ in their slots")
-    return a.size(0)
+    return n
+
+
+def _bc(Bm, Cm, device: int):
+    """Addresses of B and C and their common pitch."""
+    (pb, ldb), (pc, ldc) = _rows_at(Bm, device), _rows_at(Cm, device)
+    if ldb != ldc:
+        raise ValueError("Bm and Cm differ in their pitch")
+    return pb, pc, ldb
 
 
 def make_ragged(rows: int, n_slots: int, seq_start, slot=None, resume=None) -> RomRagged:
-    """Sequences packed in buffers of `rows` rows.  The tensors (int32, on the device) must outlive the calls that take the result."""
+    """Sequences packed in buffers of `rows` rows.  The tensors (int32, on the device) may change in place between calls."""
     n_seq = seq_start.numel() - 1
     for t, n in ((seq_start, n_seq + 1), (slot, n_seq), (resume, n_seq)):
         if t is not None and (t.dtype != torch.int32 or t.numel() != n):
             raise ValueError("expected int32 tensors: n_seq + 1 offsets, n_seq slots, n_seq flags")
-    return RomRagged(n_seq, rows, n_slots, _ptr(seq_start), _ptr(slot), _ptr(resume))
+    r = RomRagged(n_seq, rows, n_slots, _ptr(seq_start), _ptr(slot), _ptr(resume))
+    r.tensors = (seq_start, slot, resume)      # (they live as long as the addresses do)
+    return r
 
 
 def rom_conv_ragged(cfg, seqs: RomRagged, x, w_conv, b_conv, win_in, win_out, y, stream=None, check=True) -> int:
     """x: [rows, d_inner], rows may be a column slice of wider ones."""
-    _here(x, w_conv, b_conv, win_in, win_out, y)
-    px, ldx = _rows_ptr(x)
-    rc = lib().rom_conv_ragged(ctypes.byref(cfg), ctypes.byref(seqs), px, ldx, _ptr(w_conv), _ptr(b_conv), _ptr(win_in), _ptr(win_out),
-                               _ptr(y), _stream(stream))
+    d = torch.cuda.current_device()
+    px, ldx = _rows_at(x, d)
+    rc = lib().rom_conv_ragged(ctypes.byref(cfg), ctypes.byref(seqs), px, ldx, _at(w_conv, d), _at(b_conv, d), _at(win_in, d), _at(win_out, d),
+                               _at(y, d), _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_conv_ragged")
     return rc
@@ -372,40 +386,32 @@ def scan_ragged_workspace_size(cfg: RomConfig, n_seq: int, rows: int) -> int:
     return int(n.value)
 
 
-def _bc(Bm, Cm):
-    """Addresses of B and C and their common pitch."""
-    (pb, ldb), (pc, ldc) = _rows_ptr(Bm), _rows_ptr(Cm)
-    if ldb != ldc:
-        raise ValueError("Bm and Cm differ in their pitch")
-    return pb, pc, ldb
-
-
 def rom_scan_ragged(cfg, seqs: RomRagged, u, delta, A, Bm, Cm, D, z, h_in, h_out, y, ws, stream=None, check=True) -> int:
     """Bm, Cm: [rows, d_state] of one pitch; z: [rows, d_inner]; both may be column slices of wider rows."""
-    _here(u, delta, A, Bm, Cm, D, z, h_in, h_out, y, ws)
-    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm), _rows_ptr(z)
-    rc = lib().rom_scan_ragged(ctypes.byref(cfg), ctypes.byref(seqs), _ptr(u), _ptr(delta), _ptr(A), pb, pc, ld, _ptr(D), pz, ldz, _ptr(h_in),
-                               _ptr(h_out), _ptr(y), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+    d = torch.cuda.current_device()
+    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm, d), _rows_at(z, d)
+    rc = lib().rom_scan_ragged(ctypes.byref(cfg), ctypes.byref(seqs), _at(u, d), _at(delta, d), _at(A, d), pb, pc, ld, _at(D, d), pz, ldz, _at(h_in, d),
+                               _at(h_out, d), _at(y, d), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_scan_ragged")
     return rc
 
 
 def rom_conv_step(cfg, x, w_conv, b_conv, slot, win_in, win_out, y, stream=None, check=True) -> int:
-    _here(x, w_conv, b_conv, slot, win_in, win_out, y)
-    px, ldx = _rows_ptr(x)
-    rc = lib().rom_conv_step(ctypes.byref(cfg), px, ldx, _ptr(w_conv), _ptr(b_conv), _ptr(slot), _pool(win_in, win_out), _ptr(win_in),
-                             _ptr(win_out), _ptr(y), _stream(stream))
+    d = torch.cuda.current_device()
+    px, ldx = _rows_at(x, d)
+    rc = lib().rom_conv_step(ctypes.byref(cfg), px, ldx, _at(w_conv, d), _at(b_conv, d), _at(slot, d), _slots(win_in, win_out), _at(win_in, d),
+                             _at(win_out, d), _at(y, d), _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_conv_step")
     return rc
 
 
 def rom_scan_step(cfg, u, delta, A, Bm, Cm, D, z, slot, h_in, h_out, y, stream=None, check=True) -> int:
-    _here(u, delta, A, Bm, Cm, D, z, slot, h_in, h_out, y)
-    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm), _rows_ptr(z)
-    rc = lib().rom_scan_step(ctypes.byref(cfg), _ptr(u), _ptr(delta), _ptr(A), pb, pc, ld, _ptr(D), pz, ldz, _ptr(slot), _pool(h_in, h_out),
-                             _ptr(h_in), _ptr(h_out), _ptr(y), _stream(stream))
+    d = torch.cuda.current_device()
+    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm, d), _rows_at(z, d)
+    rc = lib().rom_scan_step(ctypes.byref(cfg), _at(u, d), _at(delta, d), _at(A, d), pb, pc, ld, _at(D, d), pz, ldz, _at(slot, d), _slots(h_in, h_out),
+                             _at(h_in, d), _at(h_out, d), _at(y, d), _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_scan_step")
     return rc
@@ -420,9 +426,9 @@ def ffn_moe_step_workspace_size(cfg: RomConfig, d_ff: int) -> int:
 
 
 def rom_ffn_moe_step(cfg, d_ff, W_gu, W_down, x, topk_idx, gates, out, ws, stream=None, check=True) -> int:
-    _here(W_gu, W_down, x, topk_idx, gates, out, ws)
-    rc = lib().rom_ffn_moe_step(ctypes.byref(cfg), int(d_ff), _ptr(W_gu), _ptr(W_down), _ptr(x), _ptr(topk_idx), _ptr(gates), _ptr(out),
-                                _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+    d = torch.cuda.current_device()
+    rc = lib().rom_ffn_moe_step(ctypes.byref(cfg), int(d_ff), _at(W_gu, d), _at(W_down, d), _at(x, d), _at(topk_idx, d), _at(gates, d), _at(out, d),
+                                _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_ffn_moe_step")
     return rc

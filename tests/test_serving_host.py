@@ -144,12 +144,19 @@ def test_workspaces(L):
 
 def test_binding_refuses_what_it_cannot_describe():
     rows = torch.zeros(4, 64)
-    with pytest.raises(ValueError):
-        rb._rows_ptr(rows)                                                    # not on a GPU
+    with pytest.raises(ValueError, match="device"):
+        rb._rows_at(rows, 0)                                                  # not on a GPU
+    with pytest.raises(ValueError, match="device"):
+        rb._at(rows, 0)
+    with pytest.raises(ValueError, match="contiguous"):
+        rb._at(rows.t(), -1)
+    with pytest.raises(ValueError, match="contiguous"):
+        rb._rows_at(rows.t(), -1)
+    assert rb._rows_at(torch.zeros(4, 96)[:, 32:], -1)[1] == 96 and rb._rows_at(torch.zeros(1, 96)[:, 32:], -1)[1] == 64
     i32 = torch.zeros(4, dtype=torch.int32)
     with pytest.raises(ValueError):
         rb.make_ragged(10, 4, i32.long())
     with pytest.raises(ValueError):
         rb.make_ragged(10, 4, i32, slot=i32)                                  # three sequences, four slots
     with pytest.raises(ValueError):
-        rb._pool(torch.zeros(3, 2), torch.zeros(4, 2))
+        rb._slots(torch.zeros(3, 2), torch.zeros(4, 2))
