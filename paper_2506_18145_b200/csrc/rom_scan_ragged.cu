@@ -31,6 +31,7 @@ struct RaggedScan {
   const void* z; long long ldz; const float* h_in; float* h_out; void* y; int De;
   int Lc, nch;                    // rows per chunk, chunks
   int bc16;                       // rows of B and C on 16-byte boundaries
+  int early;                      // both launches' blocks fit the GPU together: the second is let in at once
   float* h_end;                   // [nch, De, 16]: state at the end of a chunk that a sequence reaches over
   float* h_start;                 // [nch, De, 16]: initial state of the sequence that starts in the chunk and reaches on
   float* sum_delta;               // [nch, De]
@@ -74,7 +75,10 @@ __global__ void __launch_bounds__(RWARPS * 32, sizeof(T) == 2 ? 3 : 2)
 scan_ragged_chunks(const RaggedScan p) {
   constexpr bool FINE = sizeof(T) == 4;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  pdl_wait();
+  // (behind the first launch the second reads what that one writes from the chained states on only)
+  const bool second = !STATE && p.nch > 1;
+  if (!second) pdl_wait();
+  if (STATE && p.early) pdl_trigger();
   const int lane = threadIdx.x & 31, De = p.De, groups = De / 32;
   const int item = blockIdx.x * RWARPS + (threadIdx.x >> 5), chunk = item / groups, c_warp = (item % groups) * 32;
   if (chunk >= (STATE ? p.nch - 1 : p.nch)) return;
@@ -133,6 +137,15 @@ scan_ragged_chunks(const RaggedScan p) {
     }
   };
   const float4 zero4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float a = FINE ? 1.0f : kLog2eServe, k = FINE ? 1.0f : -1.0f;
+      a2[n][j] = make_float2(av[2 * j][n] * a, av[2 * j + 1][n] * a);
+      kin[n][j] = make_float2(k / av[2 * j][n], k / av[2 * j + 1][n]);
+    }
+  if (second) pdl_wait();
   {
     float4 v[4] = {zero4, zero4, zero4, zero4};
     if (STATE) {
@@ -171,14 +184,6 @@ scan_ragged_chunks(const RaggedScan p) {
     }
     set_state(v);
   }
-#pragma unroll
-  for (int n = 0; n < 4; ++n)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float a = FINE ? 1.0f : kLog2eServe, k = FINE ? 1.0f : -1.0f;
-      a2[n][j] = make_float2(av[2 * j][n] * a, av[2 * j + 1][n] * a);
-      kin[n][j] = make_float2(k / av[2 * j][n], k / av[2 * j + 1][n]);
-    }
   sdel[0] = make_float2(0.0f, 0.0f); sdel[1] = sdel[0];
 
   if (!STATE) {
@@ -406,13 +411,14 @@ int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
   }
   return best;
 }
-struct RaggedWs { int Lc, nch; size_t h_end, h_start, sum_delta, total; };
+struct RaggedWs { int Lc, nch, early; size_t h_end, h_start, sum_delta, total; };
 RaggedWs ragged_ws(const rom_config& c, int n_seq, int rows) {
   const int De = c.d_inner;
   RaggedWs l{};
   const int n = ragged_chunks(De, n_seq, rows, c.dtype == ROM_F32);
   l.Lc = n == 1 ? (rows > 0 ? rows : 1) : (int)align_up((size_t)(rows + n - 1) / n, RR);
   l.nch = rows > 0 ? (rows + l.Lc - 1) / l.Lc : 1;
+  l.early = 2ll * l.nch * (De / 32) <= 148ll * RWARPS * (c.dtype == ROM_F32 ? 2 : 3);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
   const size_t keep = l.nch > 1 ? l.nch : 0;
@@ -477,7 +483,7 @@ int rom_scan_ragged(const rom_config* cfg, const rom_ragged* seqs, const void* u
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
   const int bc16 = aligned16(Bm) && aligned16(Cm) && ld_bc % 4 == 0;
-  const RaggedScan p{device_view(*seqs), u, delta, A, Bm, Cm, ld_bc, D, z, ldz, h_in, h_out, y, c.d_inner, lay.Lc, lay.nch, bc16,
+  const RaggedScan p{device_view(*seqs), u, delta, A, Bm, Cm, ld_bc, D, z, ldz, h_in, h_out, y, c.d_inner, lay.Lc, lay.nch, bc16, lay.early,
                      reinterpret_cast<float*>(W + lay.h_end), reinterpret_cast<float*>(W + lay.h_start), reinterpret_cast<float*>(W + lay.sum_delta)};
   auto launch = c.dtype == ROM_BF16 ? (c.disc_mode == 0 ? launch_scan_ragged<__nv_bfloat16, true> : launch_scan_ragged<__nv_bfloat16, false>)
                                     : (c.disc_mode == 0 ? launch_scan_ragged<float, true> : launch_scan_ragged<float, false>);
