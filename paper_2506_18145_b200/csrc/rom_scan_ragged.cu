@@ -387,7 +387,7 @@ scan_ragged_chunks(const RaggedScan p) {
 
 // Chunks of the packed rows: the count with the smallest time by what the kernels were measured to take.  A block of four warps takes
 // 155 / 235 / 330 ns a row with one / two / three of them on an SM, 128 / 188 / 255 ns states only; rounds of three overlap to 268 and 200.  fp32:
-// two on an SM, about twice as long.  A warp takes 2 us before its first row, 0.15 us for every chunk that it chains, 0.4 us from one sequence to
+// two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains, 0.4 us from one sequence to
 // the next.  The first launch walks the rows of sequences that reach over a chunk's end, of one of length `mean` about
 // mean (1 - exp(-Lc / mean)).  A function of the sizes alone, so that workspace sizing and the launch agree.
 int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
@@ -399,13 +399,13 @@ int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
     const int k = (int)((blocks + 147.0) / 148.0);
     const double slow = fp32 ? 2.0 : 1.0;
     if (k <= most) return fixed + rows_each * pace[k - 1] * slow;
-    return (blocks / (148.0 * most) + 0.25) * (fixed + rows_each * pace[fp32 ? 1 : 3] * slow);
+    return (blocks / (148.0 * most) + 0.3) * (fixed + rows_each * pace[fp32 ? 1 : 3] * slow);
   };
   int best = 1;
   double best_t = 0.0;
   for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); ++n) {
     const double blocks = ((double)n * (De / 32) + RWARPS - 1) / RWARPS, Lc = (double)rows / n, chained = mean < Lc ? 0.0 : mean / Lc < n ? mean / Lc : n;
-    double t = time(blocks, full, Lc, 2000.0 + 150.0 * chained + 400.0 * Lc / mean);
+    double t = time(blocks, full, Lc, 3000.0 + 100.0 * chained + 400.0 * Lc / mean);
     if (n > 1) t += time(blocks, state, mean * (1.0 - exp(-Lc / mean)), 2000.0) + 3000.0;
     if (n == 1 || t < best_t) { best = n; best_t = t; }
   }
