@@ -385,28 +385,33 @@ scan_ragged_chunks(const RaggedScan p) {
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
+// Rows of a chunk when there are n of them.
+int chunk_rows(int rows, int n) { return n == 1 ? (rows > 0 ? rows : 1) : (int)align_up((size_t)(rows + n - 1) / n, RR); }
 // Chunks of the packed rows: the count with the smallest time by what the kernels were measured to take.  A block of four warps takes
-// 155 / 235 / 330 ns a row with one / two / three of them on an SM, 128 / 188 / 255 ns states only; rounds of three overlap to 268 and 200.  fp32:
-// two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains, 0.4 us from one sequence to
-// the next.  The first launch walks the rows of sequences that reach over a chunk's end, of one of length `mean` about
-// mean (1 - exp(-Lc / mean)).  A function of the sizes alone, so that workspace sizing and the launch agree.
+// 155 / 235 / 330 ns a row with one / two / three of them on an SM, 128 / 188 / 255 ns states only; more than three come in rounds, of which the last
+// may be of one or two.  fp32: two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains,
+// 0.4 us from one sequence to the next.  The first launch walks the rows of sequences that reach over a chunk's end, of one of length `mean` about
+// mean (1 - exp(-Lc / mean)) on average over rounds, twice the mean at most where all blocks run at once.  A function of the sizes alone, so that workspace sizing and the launch agree.
 int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
-  const double full[4] = {155.0, 235.0, 330.0, 268.0}, state[4] = {128.0, 188.0, 255.0, 200.0};
+  const double full[3] = {155.0, 235.0, 330.0}, state[3] = {128.0, 188.0, 255.0};
   const double mean = rows > 0 && n_seq > 0 ? (double)rows / n_seq : 1.0;
   const int most = fp32 ? 2 : 3;
   // blocks that each take fixed + rows_each * pace ns
-  auto time = [&](double blocks, const double (&pace)[4], double rows_each, double fixed) {
-    const int k = (int)((blocks + 147.0) / 148.0);
+  auto time = [&](double blocks, const double (&pace)[3], double rows_each, double fixed) {
     const double slow = fp32 ? 2.0 : 1.0;
-    if (k <= most) return fixed + rows_each * pace[k - 1] * slow;
-    return (blocks / (148.0 * most) + 0.3) * (fixed + rows_each * pace[fp32 ? 1 : 3] * slow);
+    const int per_sm = (int)ceil(blocks / 148.0), last = per_sm % most;
+    return per_sm / most * (fixed + rows_each * pace[most - 1] * slow) + (last ? fixed + rows_each * pace[last - 1] * slow : 0.0);
   };
   int best = 1;
   double best_t = 0.0;
   for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); ++n) {
-    const double blocks = ((double)n * (De / 32) + RWARPS - 1) / RWARPS, Lc = (double)rows / n, chained = mean < Lc ? 0.0 : mean / Lc < n ? mean / Lc : n;
-    double t = time(blocks, full, Lc, 3000.0 + 100.0 * chained + 400.0 * Lc / mean);
-    if (n > 1) t += time(blocks, state, mean * (1.0 - exp(-Lc / mean)), 2000.0) + 3000.0;
+    const double Lc = chunk_rows(rows, n), nch = rows > 0 ? ceil(rows / Lc) : 1.0;
+    const double chained = mean < Lc ? 0.0 : mean / Lc < nch ? mean / Lc : nch;
+    double t = time(nch * (De / 32) / RWARPS, full, Lc, 3000.0 + 100.0 * chained + 400.0 * Lc / mean);
+    if (n > 1) {
+      const double blocks = (nch - 1.0) * (De / 32) / RWARPS, longest = 2.0 * mean < Lc ? 2.0 * mean : Lc;
+      t += time(blocks, state, blocks <= 148.0 * most ? longest : mean * (1.0 - exp(-Lc / mean)), 2000.0) + 3000.0;
+    }
     if (n == 1 || t < best_t) { best = n; best_t = t; }
   }
   return best;
@@ -416,7 +421,7 @@ RaggedWs ragged_ws(const rom_config& c, int n_seq, int rows) {
   const int De = c.d_inner;
   RaggedWs l{};
   const int n = ragged_chunks(De, n_seq, rows, c.dtype == ROM_F32);
-  l.Lc = n == 1 ? (rows > 0 ? rows : 1) : (int)align_up((size_t)(rows + n - 1) / n, RR);
+  l.Lc = chunk_rows(rows, n);
   l.nch = rows > 0 ? (rows + l.Lc - 1) / l.Lc : 1;
   l.early = 2ll * l.nch * (De / 32) <= 148ll * RWARPS * (c.dtype == ROM_F32 ? 2 : 3);
   size_t o = 0;
