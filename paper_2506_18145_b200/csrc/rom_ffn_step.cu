@@ -358,7 +358,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     // ---------------------------------------------------------------- TMA producer of the weights (nothing here depends on the launch before)
     if (leader) {
       int stage = 0, issued = 0; uint32_t phase = 0;
-      bool ok = true, ready = false;                 // ready: the next stage was free when it was looked at
+      bool ok = true, ready = true;                  // ready: the next stage was free when it was looked at (all are at first)
       for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
         const Item it = item(w);
         const int row = it.e * p.w_rows + it.tile * p.h, m = by.off[it.e + 1] - by.off[it.e];
