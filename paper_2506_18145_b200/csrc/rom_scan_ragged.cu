@@ -321,8 +321,7 @@ scan_ragged_chunks(const RaggedScan p) {
           const float2 uB = __fmul2_rn(uu[j], pair(bb[n]));
           if (FINE) {
             float2 a, e;
-            decay(x.x, a.x, e.x);
-            decay(x.y, a.y, e.y);
+            decay(x, a, e);
             h[n][j] = __ffma2_rn(a, h[n][j], ZOH ? __fmul2_rn(e, __fmul2_rn(uB, kin[n][j])) : uB);
           } else {
             const float2 a = make_float2(ex2_ftz(x.x), ex2_ftz(x.y));

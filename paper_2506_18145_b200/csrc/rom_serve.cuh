@@ -71,17 +71,19 @@ constexpr float kLog2eServe = 1.4426950408889634f;
 // a = exp(x), e = exp(x) - 1 for x <= 0.  Near zero e comes from its power series (x^8/8! left out: below 2^-25 of e for |x| < 0.35) and a from e,
 // so that both keep fp32 accuracy however small the step: the input of a zero-order hold is e / A, and a state that decays by 1e-3 a step
 // adds up the errors of a thousand decays.
-__device__ __forceinline__ void decay(float x, float& a, float& e) {
-  float p = fmaf(x, 1.0f / 5040.0f, 1.0f / 720.0f);
-  p = fmaf(p, x, 1.0f / 120.0f);
-  p = fmaf(p, x, 1.0f / 24.0f);
-  p = fmaf(p, x, 1.0f / 6.0f);
-  p = fmaf(p, x, 0.5f);
-  p = fmaf(p, x, 1.0f);
-  const float es = p * x, al = ex2_ftz(x * kLog2eServe);
-  const bool small = x > -0.35f;
-  e = small ? es : al - 1.0f;
-  a = small ? es + 1.0f : al;
+__device__ __forceinline__ void decay(float2 x, float2& a, float2& e) {
+  auto both = [](float v) { return make_float2(v, v); };
+  float2 p = __ffma2_rn(x, both(1.0f / 5040.0f), both(1.0f / 720.0f));
+  p = __ffma2_rn(p, x, both(1.0f / 120.0f));
+  p = __ffma2_rn(p, x, both(1.0f / 24.0f));
+  p = __ffma2_rn(p, x, both(1.0f / 6.0f));
+  p = __ffma2_rn(p, x, both(0.5f));
+  p = __ffma2_rn(p, x, both(1.0f));
+  const float2 es = __fmul2_rn(p, x), xl = __fmul2_rn(x, both(kLog2eServe)), al = make_float2(ex2_ftz(xl.x), ex2_ftz(xl.y));
+  const float2 el = __fadd2_rn(al, both(-1.0f)), as = __fadd2_rn(es, both(1.0f));
+  const bool s0 = x.x > -0.35f, s1 = x.y > -0.35f;
+  e = make_float2(s0 ? es.x : el.x, s1 ? es.y : el.y);
+  a = make_float2(s0 ? as.x : al.x, s1 ? as.y : al.y);
 }
 
 }  // namespace

@@ -111,11 +111,12 @@ scan_slot_step(const T* __restrict__ u, const float* __restrict__ delta, const f
       const float av[4] = {a4[i].x, a4[i].y, a4[i].z, a4[i].w};
       float hv[4] = {h4[k][i].x, h4[k][i].y, h4[k][i].z, h4[k][i].w}, p = 0.0f;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        float a, e;
-        decay(di * av[n], a, e);
-        hv[n] = fmaf(a, hv[n], (ZOH ? __fdividef(e, av[n]) : di) * (ui * bb[n]));
-        p = fmaf(cc[n], hv[n], p);
+      for (int n = 0; n < 4; n += 2) {
+        float2 a, e;
+        decay(make_float2(di * av[n], di * av[n + 1]), a, e);
+        hv[n] = fmaf(a.x, hv[n], (ZOH ? __fdividef(e.x, av[n]) : di) * (ui * bb[n]));
+        hv[n + 1] = fmaf(a.y, hv[n + 1], (ZOH ? __fdividef(e.y, av[n + 1]) : di) * (ui * bb[n + 1]));
+        p = fmaf(cc[n + 1], hv[n + 1], fmaf(cc[n], hv[n], p));
       }
       __stcs(reinterpret_cast<float4*>(h_out + ((size_t)sl[k] * De + c0 + 8 * i + g) * 16 + 4 * t), make_float4(hv[0], hv[1], hv[2], hv[3]));
       part[i] = p;
