@@ -340,8 +340,16 @@ def _rows_at(t: Optional[torch.Tensor], device: int):
     return t.data_ptr(), pitch[0] if rows > 1 else width      # (a single row has no pitch: torch may say anything)
 
 
-def _slots(a: torch.Tensor, b: torch.Tensor) -> int:
-    """Slots of the state pools of a call."""
+def _sequences(seqs: RomRagged, device: int):
+    if getattr(seqs, "device", device) != device:
+        raise ValueError(f"the sequences are on cuda:{seqs.device}, the call runs on cuda:{device}")
+    return ctypes.byref(seqs)
+
+
+def _slots(a: Optional[torch.Tensor], b: Optional[torch.Tensor]) -> int:
+    """Slots of the state pools of a call (0 without both, which the library refuses)."""
+    if a is None or b is None:
+        return 0
     n = a.size(0)
     if b is not a and b.size(0) != n:
         raise ValueError("the pools differ in their slots")
@@ -364,6 +372,10 @@ def make_ragged(rows: int, n_slots: int, seq_start, slot=None, resume=None) -> R
             raise ValueError("expected int32 tensors: n_seq + 1 offsets, n_seq slots, n_seq flags")
     r = RomRagged(n_seq, rows, n_slots, _ptr(seq_start), _ptr(slot), _ptr(resume))
     r.tensors = (seq_start, slot, resume)      # (they live as long as the addresses do)
+    r.device = seq_start.get_device()
+    for t in (slot, resume):
+        if t is not None and t.get_device() != r.device:
+            raise ValueError("the sequences' tensors are on different devices")
     return r
 
 
@@ -371,7 +383,7 @@ def rom_conv_ragged(cfg, seqs: RomRagged, x, w_conv, b_conv, win_in, win_out, y,
     """x: [rows, d_inner], rows may be a column slice of wider ones."""
     d = torch.cuda.current_device()
     px, ldx = _rows_at(x, d)
-    rc = lib().rom_conv_ragged(ctypes.byref(cfg), ctypes.byref(seqs), px, ldx, _at(w_conv, d), _at(b_conv, d), _at(win_in, d), _at(win_out, d),
+    rc = lib().rom_conv_ragged(ctypes.byref(cfg), _sequences(seqs, d), px, ldx, _at(w_conv, d), _at(b_conv, d), _at(win_in, d), _at(win_out, d),
                                _at(y, d), _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_conv_ragged")
@@ -390,7 +402,7 @@ def rom_scan_ragged(cfg, seqs: RomRagged, u, delta, A, Bm, Cm, D, z, h_in, h_out
     """Bm, Cm: [rows, d_state] of one pitch; z: [rows, d_inner]; both may be column slices of wider rows."""
     d = torch.cuda.current_device()
     (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm, d), _rows_at(z, d)
-    rc = lib().rom_scan_ragged(ctypes.byref(cfg), ctypes.byref(seqs), _at(u, d), _at(delta, d), _at(A, d), pb, pc, ld, _at(D, d), pz, ldz, _at(h_in, d),
+    rc = lib().rom_scan_ragged(ctypes.byref(cfg), _sequences(seqs, d), _at(u, d), _at(delta, d), _at(A, d), pb, pc, ld, _at(D, d), pz, ldz, _at(h_in, d),
                                _at(h_out, d), _at(y, d), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_scan_ragged")

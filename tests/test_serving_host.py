@@ -160,3 +160,8 @@ def test_binding_refuses_what_it_cannot_describe():
         rb.make_ragged(10, 4, i32, slot=i32)                                  # three sequences, four slots
     with pytest.raises(ValueError):
         rb._slots(torch.zeros(3, 2), torch.zeros(4, 2))
+    assert rb._slots(None, torch.zeros(4, 2)) == 0
+    elsewhere = ragged()
+    elsewhere.device = 1
+    with pytest.raises(ValueError, match="cuda:1"):
+        rb._sequences(elsewhere, 0)
