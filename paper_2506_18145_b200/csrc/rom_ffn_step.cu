@@ -636,7 +636,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   }
 }
 
-cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaStream_t st) {
+cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32_t* arrived, cudaStream_t st) {
   int sms = 0;
   cudaError_t e = current_device_sm_count(&sms);
   if (e != cudaSuccess) return e;
@@ -644,7 +644,7 @@ cudaError_t launch_ffn_tc(const FfnStep& s, float* part, int32_t* arrived, cudaS
   p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
   p.T = s.T; p.K = s.K; p.E = s.E;
   p.cols_cap = ffn_columns(s.T, s.K, s.E);
-  const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true), cd = cut_tiles(s.T, s.K, s.E, s.Dm, s.F, false);
+  const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true);
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
     const int rows = (up ? 2 : 1) * p.h;
@@ -677,7 +677,7 @@ int check_ffn_step(const rom_config* c, int d_ff) {
   if (c->d_model > 32 * kFfnMaxTiles || (int64_t)c->E * 2 * d_ff >= (int64_t)1 << 31 || (int64_t)c->E * c->d_model >= (int64_t)1 << 31) return ROM_ERR_UNSUPPORTED;
   return ROM_OK;
 }
-struct FfnStepWs { size_t status, arrived, hid, part, total; };
+struct FfnStepWs { size_t status, arrived, hid, part, total; FfnCut down; };
 FfnStepWs ffn_step_ws(const rom_config& c, int d_ff) {
   FfnStepWs l{};
   size_t o = 0;
@@ -687,8 +687,8 @@ FfnStepWs ffn_step_ws(const rom_config& c, int d_ff) {
   const size_t A = (size_t)c.B * c.L * c.K;
   l.arrived = take(tc ? sizeof(int32_t) * kFfnMaxTiles : 0);
   l.hid = take((tc ? 2 : 4) * A * d_ff);
-  const FfnCut cd = cut_tiles(c.B * c.L, c.K, c.E, c.d_model, d_ff, false);
-  l.part = take(tc && !(c.K == 1 && cd.splits == 1) ? sizeof(float) * cd.splits * A * c.d_model : 0);
+  if (tc) l.down = cut_tiles(c.B * c.L, c.K, c.E, c.d_model, d_ff, false);
+  l.part = take(tc && !(c.K == 1 && l.down.splits == 1) ? sizeof(float) * l.down.splits * A * c.d_model : 0);
   l.total = o;
   return l;
 }
@@ -725,7 +725,7 @@ int rom_ffn_moe_step(const rom_config* cfg, int32_t d_ff, const void* W_gu, cons
   char* W = static_cast<char*>(ws);
   const FfnStep p{x, W_gu, W_down, topk_idx, gates, out, W + lay.hid, reinterpret_cast<int32_t*>(W + lay.status), c.B * c.L, c.K, c.E, c.d_model, d_ff};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = c.dtype == ROM_BF16 ? launch_ffn_tc(p, reinterpret_cast<float*>(W + lay.part), reinterpret_cast<int32_t*>(W + lay.arrived), st)
+  const cudaError_t e = c.dtype == ROM_BF16 ? launch_ffn_tc(p, lay.down, reinterpret_cast<float*>(W + lay.part), reinterpret_cast<int32_t*>(W + lay.arrived), st)
                                             : launch_ffn_rows(p, st);
   return e == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }

@@ -407,7 +407,7 @@ int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
   };
   int best = 1;
   double best_t = 0.0;
-  for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); ++n) {
+  for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); n += 1 + n / 16) {      // (a few us on the host at most)
     const double Lc = chunk_rows(rows, n), nch = rows > 0 ? ceil(rows / Lc) : 1.0;
     const double chained = mean < Lc ? 0.0 : mean / Lc < nch ? mean / Lc : nch;
     double t = time(nch * (De / 32) / RWARPS, full, Lc, 3000.0 + 100.0 * chained + 400.0 * Lc / mean);
