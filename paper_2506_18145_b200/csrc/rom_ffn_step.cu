@@ -99,20 +99,26 @@ __device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const floa
   float acc[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
-  for (int k = k0 + lane * V; k < k1; k += 32 * V) {
-    V16<float> wq[4];
+  V16<float> next[4];                  // the weights a round ahead
+  int k = k0 + lane * V;
+  if (k < k1)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) wq[r].load(w[r] + k);
+    for (int r = 0; r < 4; ++r) next[r].load(w[r] + k);
+  for (; k < k1; k += 32 * V) {
     float wv[4][V];
+    float4 xq[8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) wq[r].get(wv[r]);
+    for (int r = 0; r < 4; ++r) next[r].get(wv[r]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) xq[j] = *reinterpret_cast<const float4*>(x[j] + k);
+    if (k + 32 * V < k1)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) next[r].load(w[r] + k + 32 * V);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j >= n) break;
-      float xv[V];
-      V16<float> xq;
-      xq.q = *reinterpret_cast<const float4*>(x[j] + k);
-      xq.get(xv);
+      const float xv[V] = {xq[j].x, xq[j].y, xq[j].z, xq[j].w};
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -122,7 +128,7 @@ __device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const floa
   return sum_to_lane(acc);
 }
 
-// A warp has two hidden columns of one expert.
+// A warp has two hidden columns of one expert at a time.
 constexpr int FR_UP_WARPS = 4;
 __global__ void __launch_bounds__(FR_UP_WARPS * 32)
 ffn_step_up(const FfnStep p) {
@@ -130,27 +136,29 @@ ffn_step_up(const FfnStep p) {
   pdl_sync();
   if (blockIdx.x == 0 && blockIdx.y == 0) ffn_status(p);
   by.build(p.idx, p.T * p.K, p.E);
-  const int lane = threadIdx.x & 31, j = lane & 7;
-  const int f = (blockIdx.x * FR_UP_WARPS + (threadIdx.x >> 5)) * 2, e = by.chosen(blockIdx.y, p.E);
+  const int lane = threadIdx.x & 31, j = lane & 7, e = by.chosen(blockIdx.y, p.E);
   if (e < 0) return;
-  const float* g = static_cast<const float*>(p.W_gu) + ((size_t)e * 2 * p.F + f) * p.Dm;
-  const float* u = g + (size_t)p.F * p.Dm;
-  const float* const w[4] = {g, g + p.Dm, u, u + p.Dm};
-  for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
-    const int n = min(8, by.off[e + 1] - a0);
-    const float* x[8];
+  for (int f = (blockIdx.x * FR_UP_WARPS + (threadIdx.x >> 5)) * 2; f < p.F; f += gridDim.x * FR_UP_WARPS * 2) {
+    const float* g = static_cast<const float*>(p.W_gu) + ((size_t)e * 2 * p.F + f) * p.Dm;
+    const float* u = g + (size_t)p.F * p.Dm;
+    const float* const w[4] = {g, g + p.Dm, u, u + p.Dm};
+    for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
+      const int n = min(8, by.off[e + 1] - a0);
+      const float* x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.x) + (size_t)(by.list[a0 + min(i, n - 1)] / p.K) * p.Dm;
-    const float v = rows_4x8(w, x, n, 0, p.Dm);
-    const float up = __shfl_down_sync(0xffffffffu, v, 16);
-    if (lane < 16 && j < n) {
-      const int a = by.list[a0 + j];
-      static_cast<float*>(p.hid)[(size_t)a * p.F + f + (lane >> 3)] = silu_f(v) * up * __ldg(p.gates + a);
+      for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(p.x) + (size_t)(by.list[a0 + min(i, n - 1)] / p.K) * p.Dm;
+      const float v = rows_4x8(w, x, n, 0, p.Dm);
+      const float up = __shfl_down_sync(0xffffffffu, v, 16);
+      if (lane < 16 && j < n) {
+        const int a = by.list[a0 + j];
+        static_cast<float*>(p.hid)[(size_t)a * p.F + f + (lane >> 3)] = silu_f(v) * up * __ldg(p.gates + a);
+      }
     }
   }
 }
-// A block has four rows of the output; its warps share the contracted index of every expert and add their sums at the end, in order.
-constexpr int FR_DOWN_WARPS = 8;
+// A block has four rows of the output; its warps share the contracted index of every expert, two sets of them the experts, and add their sums at the
+// end, in order.
+constexpr int FR_PARTS = 8, FR_DOWN_WARPS = 2 * FR_PARTS;
 __global__ void __launch_bounds__(FR_DOWN_WARPS * 32)
 ffn_step_down(const FfnStep p) {
   __shared__ ByExpert by;
@@ -158,11 +166,13 @@ ffn_step_down(const FfnStep p) {
   by.build(p.idx, p.T * p.K, p.E);
   pdl_sync();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 4;
-  const int part = (p.F / 128 + FR_DOWN_WARPS - 1) / FR_DOWN_WARPS * 128, k0 = min(warp * part, p.F), k1 = min(k0 + part, p.F);
+  const int part = (p.F / 128 + FR_PARTS - 1) / FR_PARTS * 128, k0 = min(warp % FR_PARTS * part, p.F), k1 = min(k0 + part, p.F);
   float (*s)[4] = sum[warp];
   for (int t = lane; t < p.T * 4; t += 32) s[t >> 2][t & 3] = 0.0f;
   __syncwarp();
+  int turn = warp / FR_PARTS;
   for (int e = 0; e < p.E && k0 < k1; ++e) {
+    if (by.off[e] == by.off[e + 1] || (turn++ & 1)) continue;      // (every second chosen expert)
     const float* w0 = static_cast<const float*>(p.W_down) + ((size_t)e * p.Dm + d) * p.F;
     const float* const w[4] = {w0, w0 + p.F, w0 + 2 * (size_t)p.F, w0 + 3 * (size_t)p.F};
     for (int a0 = by.off[e]; a0 < by.off[e + 1]; a0 += 8) {
@@ -188,7 +198,9 @@ ffn_step_down(const FfnStep p) {
 
 cudaError_t launch_ffn_rows(const FfnStep& p, cudaStream_t st) {
   const int A = p.T * p.K;
-  cudaError_t e = launch_k(ffn_step_up, dim3(p.F / (2 * FR_UP_WARPS), A < p.E ? A : p.E), FR_UP_WARPS * 32, 0, st, p);
+  // (about eight blocks an SM at most: each makes its lists first)
+  const int experts = A < p.E ? A : p.E, blocks = std::min(p.F / (2 * FR_UP_WARPS), std::max(148 * 8 / experts, 1));
+  cudaError_t e = launch_k(ffn_step_up, dim3(blocks, experts), FR_UP_WARPS * 32, 0, st, p);
   if (e != cudaSuccess) return e;
   count_launch();
   e = launch_k(ffn_step_down, dim3(p.Dm / 4), FR_DOWN_WARPS * 32, 0, st, p);
