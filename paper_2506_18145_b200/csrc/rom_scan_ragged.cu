@@ -35,7 +35,7 @@ struct RaggedScan {
   const void* z; long long ldz; const float* h_in; float* h_out; void* y; int De;
   int Lc, nch;                    // rows per chunk, chunks
   int bc16;                       // rows of B and C on 16-byte boundaries
-  int early;                      // both launches' blocks fit the GPU together: the second is let in at once
+  int early;                      // the first launch's blocks all run at once: the second's may take the room they leave (1 to 2 % of calls of a few thousand rows)
   float* h_end;                   // [nch, De, 16]: state at the end of a chunk that a sequence reaches over
   float* h_start;                 // [nch, De, 16]: initial state of the sequence that starts in the chunk and reaches on
   float* sum_delta;               // [nch, De]
@@ -426,7 +426,7 @@ RaggedWs ragged_ws(const rom_config& c, int n_seq, int rows) {
   const int n = ragged_chunks(De, n_seq, rows, c.dtype == ROM_F32);
   l.Lc = chunk_rows(rows, n);
   l.nch = rows > 0 ? (rows + l.Lc - 1) / l.Lc : 1;
-  l.early = 2ll * l.nch * (De / 32) <= 148ll * RWARPS * (c.dtype == ROM_F32 ? 2 : 3);
+  l.early = (long long)l.nch * (De / 32) <= 148ll * RWARPS * (c.dtype == ROM_F32 ? 2 : 3);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
   const size_t keep = l.nch > 1 ? l.nch : 0;
