@@ -8,8 +8,8 @@
 // put the tokens' rows beside them, warp 1 issues the MMAs, warps 2..5 take the accumulators (two, so that a tile's end runs beside the next tile).  The
 // down projection, of few rows and a long contracted index, is cut along that index too: the parts go to the workspace and whoever brings
 // a tile's last one adds them all, in the order of slots and parts, so that results do not depend on who came when.
-// Measured (us a call, GB/s of the chosen experts' weights): one token of 2048 x 8192 26.7 (3770), 64 tokens with two of sixteen experts 254 (6330: 97 % of the
-// measured copy), 16 tokens with two of eight 128 (6250), 8 tokens with one of eight of 1280 x 5120 44.8 (4610).  Small calls: about 10 us of launches, lists and
+// Measured (us a call, GB/s of the chosen experts' weights): one token of 2048 x 8192 25.3 (3980), 64 tokens with two of sixteen experts 254 (6330: 97 % of the
+// measured copy), 16 tokens with two of eight 127 (6290), 8 tokens with one of eight of 1280 x 5120 43.2 (4780).  Small calls: about 10 us of launches, lists and
 // first loads.  Tried: rings of half the size, so that both launches share the SMs and the second has its first weights when the first ends, no gain (the MMAs
 // of short tiles bound it then); stages of 64 elements 264 and 29 us, of one 64-wide block a warp's turn each 0.37 us a stage.
 //

@@ -14,10 +14,12 @@
 //
 // bf16: what bounds it is one exponential per state update on the special-function unit, 4.65 T a second: the first launch keeps it 81 to 98 %
 // busy, the second 70 to 75 % (then the fp32 pipe and the latency of twelve warps).  fp32: decay() keeps fp32 accuracy, about ten operations more an update.
-// Measured: one sequence of 16384 rows x 4096 channels 660 us (231 us of exponentials, once; they are evaluated twice here), 23 prompts of 8186 x 2048 164 us (58),
-// 64 prompts of 16384 x 2048 303 us, 512 one-row sequences x 4096 53 us (4.9 TB/s: states in and out), fp32 531 rows of 37 sequences x 512 21 us.
+// Measured: one sequence of 16384 rows x 4096 channels 664 us (231 us of exponentials, once; they are evaluated twice here), 23 prompts of 8186 x 2048 164 us (58),
+// 64 prompts of 16384 x 2048 303 to 316 us by their lengths, 512 one-row sequences x 4096 53 us (4.9 TB/s: states in and out), fp32 531 rows of 37
+// sequences x 512 20.1 us.
 // Tried: a tile that ends with its sequence (512 one-row sequences 70 us, waiting for every one's rows), one initial state ahead, chunk starts moved to a
-// sequence's start a third of a chunk away (fewer rows in the first launch, uneven chunks: no gain), one warp per sequence (16384 rows: 21 ms).
+// sequence's start a third of a chunk away (fewer rows in the first launch, uneven chunks: no gain), one warp per sequence (16384 rows: 21 ms),
+// an eighth of the exponentials, or a quarter of the first launch's, as polynomials on the fp32 pipe (2 % less where the work is most, up to 7 % more elsewhere).
 #include <cmath>
 
 #include "rom_serve.cuh"
