@@ -68,7 +68,7 @@ inline Ragged device_view(const rom_ragged& r) { return Ragged{r.n_seq, r.rows, 
 
 constexpr float kLog2eServe = 1.4426950408889634f;
 
-// a = exp(x), e = exp(x) - 1 for x <= 0.  Near zero e comes from its power series (x^8/8! left out: below 2^-25 of e for |x| < 0.35) and a from e,
+// a = exp(x), e = exp(x) - 1.  Near zero e comes from its power series (x^8/8! left out: below 2^-25 of e for |x| < 0.35) and a from e,
 // so that both keep fp32 accuracy however small the step: the input of a zero-order hold is e / A, and a state that decays by 1e-3 a step
 // adds up the errors of a thousand decays.
 __device__ __forceinline__ void decay(float2 x, float2& a, float2& e) {
@@ -81,7 +81,7 @@ __device__ __forceinline__ void decay(float2 x, float2& a, float2& e) {
   p = __ffma2_rn(p, x, both(1.0f));
   const float2 es = __fmul2_rn(p, x), xl = __fmul2_rn(x, both(kLog2eServe)), al = make_float2(ex2_ftz(xl.x), ex2_ftz(xl.y));
   const float2 el = __fadd2_rn(al, both(-1.0f)), as = __fadd2_rn(es, both(1.0f));
-  const bool s0 = x.x > -0.35f, s1 = x.y > -0.35f;
+  const bool s0 = fabsf(x.x) < 0.35f, s1 = fabsf(x.y) < 0.35f;
   e = make_float2(s0 ? es.x : el.x, s1 ? es.y : el.y);
   a = make_float2(s0 ? as.x : al.x, s1 ? as.y : al.y);
 }

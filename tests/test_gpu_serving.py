@@ -227,6 +227,38 @@ def test_scan_step(B, De, disc_mode, skip, gate, padded, in_place, dtype):
         assert same_bits(dst[q], before[q])
 
 
+@pytest.mark.parametrize("disc_mode", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scans_of_a_state_that_grows(dtype, disc_mode):
+    """Negative steps: the state grows, by up to e here, which makes every error of a step up to e times the one that the bound counts."""
+    B, De = 6, 64
+    p = Packed([1] * B, seed=51, resume=[1] * B)
+    s = scan_inputs(B, De, dtype, seed=51)
+    g = torch.Generator()
+    g.manual_seed(52)
+    s["delta"] = -torch.rand((B, De), generator=g)
+    s["A"] = -(0.5 + 0.5 * torch.rand((De, 16), generator=g))
+    cfg = config(De, dtype, disc_mode=disc_mode, B=B)
+    h0 = randn(53, (p.n_slots, De, 16), 0.3)
+    d = {n: v.cuda() for n, v in s.items()}
+    outs = []
+    for step in (True, False):
+        h, y = h0.cuda(), torch.empty(B, De, dtype=TORCH[dtype], device="cuda")
+        if step:
+            rb.rom_scan_step(cfg, d["u"], d["delta"], d["A"], d["Bm"], d["Cm"], d["D"], d["z"], p.dev[1], h, h, y)
+        else:
+            ws = torch.empty(rb.scan_ragged_workspace_size(cfg, B, B), dtype=torch.uint8, device="cuda")
+            rb.rom_scan_ragged(cfg, p.ragged, d["u"], d["delta"], d["A"], d["Bm"], d["Cm"], d["D"], d["z"], h, h, y, ws)
+        outs.append((y, h))
+    torch.cuda.synchronize()
+    for y, h in outs:
+        for i in range(B):
+            ref, bound, last, G = scan_reference(np64(s["u"][i:i + 1]), np64(s["delta"][i:i + 1]), np64(s["A"]), np64(s["Bm"][i:i + 1]), np64(s["Cm"][i:i + 1]),
+                                                 np64(s["D"]), np64(s["z"][i:i + 1]), np64(h0[p.slots[i]]), disc_mode)
+            check(y[i:i + 1], ref, np.e * bound, dtype, f"token {i}")
+            check(h[p.slots[i]], last, np.e * G, "f32", f"state {i}")
+
+
 def test_steps_in_slot_order_without_a_table():
     B, De = 5, 64
     cfg = config(De, "f32", B=B)
