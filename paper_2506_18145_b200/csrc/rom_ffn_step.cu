@@ -13,7 +13,10 @@
 // first loads.  Tried: rings of half the size, so that both launches share the SMs and the second has its first weights when the first ends, no gain (the MMAs
 // of short tiles bound it then); stages of 64 elements 264 and 29 us, of one 64-wide block a warp's turn each 0.37 us a stage.
 //
-// fp32: a warp has four weight rows and up to eight tokens, products over its lanes; the plain form for a small model in full precision.
+// fp32: a warp has four weight rows and up to eight tokens, products over its lanes; the plain form for a small model in full precision.  Bound by the latency
+// of the loads (activations from the L1 and L2 as often as weights): 5 tokens of 256 x 1024 9.4 us, 40 with two of sixteen of 512 x 2048 88 (2270 GB/s of weights).
+// Tried: weights by cp.async three steps ahead through shared memory 79 to 85 for the second but 10.2 to 10.9 for the first and 5 to 14 % more at sixteen tokens an
+// expert (less L1 for the activations); activations a step ahead 135; the down projection's weights asked for before the wait, 1 %.
 #include <algorithm>
 #include <type_traits>
 
@@ -128,9 +131,9 @@ __device__ __forceinline__ float rows_4x8(const float* const (&w)[4], const floa
   return sum_to_lane(acc);
 }
 
-// A warp has two hidden columns of one expert at a time.
+// A warp has two hidden columns of one expert at a time.  Four blocks an SM for the loads' latency, though a few registers are spilled (three: 6 to 17 % longer).
 constexpr int FR_UP_WARPS = 4;
-__global__ void __launch_bounds__(FR_UP_WARPS * 32)
+__global__ void __launch_bounds__(FR_UP_WARPS * 32, 4)
 ffn_step_up(const FfnStep p) {
   __shared__ ByExpert by;
   pdl_sync();
