@@ -1,6 +1,7 @@
 // FFN-MoE of the few tokens of a generation step (rom_ffn_moe_step): out_t = sum_k g_tk W_down,e (SiLU(W_gate,e x_t) * (W_up,e x_t)), e = topk_idx[t, k].
-// Two launches: hidden rows g SiLU(gate) up of every assignment (token, slot), rounded to the storage type with their gate in them, then the down
-// projection with the sum over the slots in fp32.
+// Two launches: hidden rows g SiLU(gate) up of every assignment (token, slot), then the down projection with the sum over the slots in fp32.  In bf16
+// a hidden row is kept as the sum of two bf16 numbers, high and low, 2^-16 off at most: rounded to one it added as much to the error as the output's own
+// rounding (2.4e-3 of the outputs against 1.7e-3).  Both are columns of the same MMA, which takes as long for 32 columns as for 16.
 //
 // What bounds it: the chosen experts' weights, 6 d_model d_ff bytes each (bf16), read once.  rom_ffn_moe_forward takes five launches and pads every
 // expert's tokens to 128 rows.  Here the weights are the M = 128 operand of tcgen05 and an expert's tokens its 16, 32 or 64 columns: one CTA per SM
@@ -33,7 +34,7 @@ constexpr int kFfnMaxSplits = 16;
 
 struct FfnStep {
   const void* x; const void* W_gu; const void* W_down; const int32_t* idx; const float* gates; void* out;
-  void* hid;                // [B K, d_ff] storage type
+  void* hid;                // fp32: [B K, d_ff]; bf16: [B K, 2, d_ff], high and low halves
   int32_t* status;
   int T, K, E, Dm, F;
 };
@@ -220,7 +221,9 @@ int chosen_experts(int T, int K, int E) {
   return n < 1 ? 1 : n;
 }
 constexpr int kSizingSms = 148;      // (workspace sizing and the launch agree)
-constexpr int FT_COLS = 64;                          // token columns per pass at most
+constexpr int FT_TOKENS = 64;                        // tokens per pass at most
+// Columns of a token: the down projection has the high and the low half of a hidden row, which add up to it within 2^-16, as two columns of the same MMA.
+__host__ __device__ constexpr int ffn_per_token(bool up) { return up ? 1 : 2; }
 constexpr int FT_MIN_STAGES = 4, FT_MAX_STAGES = 12;      // (a stage for each of the four warps that bring token rows)
 constexpr int FT_KB = 2, FT_K = FT_KB * BLOCK_K;     // contracted elements per stage: two swizzled rows
 constexpr int FT_SMEM = 208 * 1024;                  // operand ring
@@ -232,9 +235,9 @@ constexpr int ffn_ring(int rows, int cols, int stages) {
 constexpr int ffn_stages(int rows, int cols) {
   return std::min((FT_SMEM - ffn_ring(rows, cols, 0)) / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES);
 }
-// Token columns of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights again (from the
+// Tokens of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights again (from the
 // L2 mostly), the others have deeper rings.
-int ffn_columns(int T, int K, int E) {
+int ffn_tokens(int T, int K, int E) {
   const int want = std::min(T, 2 * (T * K / chosen_experts(T, K, E)) + 8);
   return want > 32 ? 64 : want > 16 ? 32 : 16;
 }
@@ -244,14 +247,14 @@ int ffn_columns(int T, int K, int E) {
 struct FfnCut { int h, splits; };
 FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
   const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Kd + FT_K - 1) / FT_K, per = up ? 2 : 1;
-  const int cols = ffn_columns(T, K, E);
+  const int per_token = ffn_per_token(up), cols = per_token * ffn_tokens(T, K, E);
   FfnCut best{8, 1};
   long long least = -1;
   for (int s = 1; s <= (up ? 1 : kFfnMaxSplits) && s <= kb; ++s)
     for (int h = up ? 64 : 128; h >= (up ? 8 : 32); h -= 8) {
       if (ffn_stages((int)per * h, cols) < FT_MIN_STAGES) continue;
       const long long rounds = (n * s * ((rows_out + h - 1) / h) + kSizingSms - 1) / kSizingSms;
-      const long long stage = std::max(460ll, 60 + 2 * FT_K * (per * h + m) / 44), parts = up || (K == 1 && s == 1) ? 0 : 4 * m * h * rounds / 100 + 4ll * T * K * s * h / 20;
+      const long long stage = std::max(460ll, 60 + 2 * FT_K * (per * h + per_token * m) / 44), parts = up || (K == 1 && s == 1) ? 0 : 4 * m * h * rounds / 100 + 4ll * T * K * s * h / 20;
       const long long cost = rounds * ((kb + s - 1) / s * stage + 1000) + parts;
       if (least < 0 || cost < least) { least = cost; best.h = h; best.splits = s; }
     }
@@ -259,12 +262,12 @@ FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
 }
 
 struct FfnTc {
-  const bf16* x; int ldx;                            // rows of activations: up: x of the token; down: hid of the assignment
+  const bf16* x; int ldx;                            // rows of activations: up: x of the token; down: hid of the assignment, two rows
   int Kd, w_rows, out_rows;                          // contracted length; weight rows per expert; rows of the product (up: pairs of them)
   const int32_t* idx; const float* gates;
   bf16* hid; float* part; bf16* out; int32_t* arrived; int32_t* status;
   int T, K, E;
-  int h, tiles, splits, stages, cols_cap;            // rows per tile, tiles per expert, parts of the contracted index, ring, columns of a stage
+  int h, tiles, splits, stages, tokens_cap;          // rows per tile, tiles per expert, parts of the contracted index, ring, tokens of a stage
   int direct;                                        // down: one expert and one part a token: written at once
 };
 
@@ -294,6 +297,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 template <bool UP, int FLIGHT>
 __global__ void __launch_bounds__(FT_THREADS, 1)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
+  constexpr int PT = ffn_per_token(UP), COLS = PT * FT_TOKENS;      // columns of a token, of an accumulator
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   __shared__ ByExpert by;
@@ -323,7 +327,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   }
   if (tid == 32 * 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * FT_COLS) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (UP) { pdl_wait(); pdl_trigger(); }             // (down: the choice of experts is older than the launch before)
@@ -348,8 +352,8 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   const uint32_t tmem_base = tmem_s;
   const int n_act = n_act_s, per_expert = p.tiles * p.splits, total = n_act * per_expert;
   const int num_kb = (p.Kd + FT_K - 1) / FT_K;
-  const uint32_t w_bytes = (UP ? 2 : 1) * p.h * 128, x_bytes = p.cols_cap * 128, stage_bytes = FT_KB * (w_bytes + x_bytes);
-  auto cols = [](int m) { return m > 32 ? 64 : m > 16 ? 32 : 16; };      // N of a pass over m tokens
+  const uint32_t w_bytes = (UP ? 2 : 1) * p.h * 128, x_bytes = PT * p.tokens_cap * 128, stage_bytes = FT_KB * (w_bytes + x_bytes);
+  auto cols = [](int m) { return PT * (m > 32 ? 64 : m > 16 ? 32 : m > 16 / PT ? 16 : 16 / PT); };      // N of a pass over m tokens
   // item w: expert, first row, stages [kb0, kb0 + n) of the contracted index, walked from a start of the tile's own: in step all CTAs
   // would read the same columns of rows that are a power of two apart
   struct Item { int e, tile, part, kb0, n, rot; };
@@ -377,7 +381,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
         const Item it = item(w);
         const int row = it.e * p.w_rows + it.tile * p.h, m = by.off[it.e + 1] - by.off[it.e];
-        for (int n0 = 0; n0 < m && ok; n0 += p.cols_cap)
+        for (int n0 = 0; n0 < m && ok; n0 += p.tokens_cap)
           for (int q = 0; q < it.n; ++q) {
             if (!ready && !mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
             const int k0 = k_of(it, q), next = stage + 1 == p.stages ? 0 : stage + 1;
@@ -414,9 +418,9 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
         const Item it = item(w);
         const int m = by.off[it.e + 1] - by.off[it.e];
-        for (int n0 = 0; n0 < m && ok; n0 += p.cols_cap) {
-          const int n16 = cols(min(m - n0, p.cols_cap));
-          const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n16 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+        for (int n0 = 0; n0 < m && ok; n0 += p.tokens_cap) {
+          const int nc = cols(min(m - n0, p.tokens_cap));
+          const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(nc >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
           if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, wait_limit)) { ok = false; break; }
           tc_fence_after();
           for (int q = 0; q < it.n; ++q) {
@@ -429,9 +433,9 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
               const uint64_t adesc = make_smem_desc(base + stage * stage_bytes + b * w_bytes), bdesc = make_smem_desc(base + stage * stage_bytes + FT_KB * w_bytes + b * x_bytes);
 #pragma unroll
               for (int k = 0; k < BLOCK_K / UMMA_K; ++k)
-                // few columns: into 64 / n16 accumulators in turns, so that an MMA does not wait for the one before
-                umma_bf16(tmem_base + acc * FT_COLS + k * n16 % FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc,
-                          (q | b) != 0 || k * n16 >= FT_COLS ? 1u : 0u);
+                // few columns: into 64 / nc accumulators in turns, so that an MMA does not wait for the one before
+                umma_bf16(tmem_base + acc * COLS + k * nc % 64, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc,
+                          (q | b) != 0 || k * nc >= 64 ? 1u : 0u);
             }
             umma_commit(empty_bar(stage));
             issued_any = true;
@@ -470,8 +474,8 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
       const Item it = item(w);
       const int m_all = by.off[it.e + 1] - by.off[it.e];
-      for (int n0 = 0; n0 < m_all && ok; n0 += p.cols_cap) {
-        const int m = min(m_all - n0, p.cols_cap);
+      for (int n0 = 0; n0 < m_all && ok; n0 += p.tokens_cap) {
+        const int m = min(m_all - n0, p.tokens_cap);
         const short* mine = by.list + by.off[it.e] + n0;
         for (int kb = 0; kb < it.n; ++kb) {
           if (turn == xw) {
@@ -479,9 +483,10 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
             if (!ok) break;
             const uint32_t dst = base + stage * stage_bytes + FT_KB * w_bytes;
             const int k0 = k_of(it, kb), blocks = min(FT_KB, (p.Kd - k0) / BLOCK_K);
-            for (int r = lrow; r < m; r += 4) {      // (columns past the last token hold whatever the stage held: nobody reads their sums)
-              const int a = mine[r];
-              const bf16* src = p.x + (size_t)(UP ? a / p.K : a) * p.ldx + k0 + chunk * 8;
+            for (int i = lrow; i < PT * m; i += 4) { // (columns past the last token hold whatever the stage held: nobody reads their sums)
+              // down: the high halves, then the low ones, each in half of the pass's columns
+              const int a = mine[i / PT], r = UP ? i : (i >> 1) + (i & 1) * (cols(m) / 2);
+              const bf16* src = p.x + (size_t)(UP ? a / p.K : 2 * a + (i & 1)) * p.ldx + k0 + chunk * 8;
               for (int b = 0; b < blocks; ++b)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + b * x_bytes + r * 128 + ((chunk ^ (r & 7)) << 4)), "l"(src + b * BLOCK_K) : "memory");
             }
@@ -520,8 +525,8 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
       const Item it = item(w);
       const int row0 = it.tile * p.h, rows = min(p.h, p.out_rows - row0), m_all = by.off[it.e + 1] - by.off[it.e];
-      for (int n0 = 0; n0 < m_all && ok; n0 += p.cols_cap) {
-        const int m = min(m_all - n0, p.cols_cap), n16 = cols(m);
+      for (int n0 = 0; n0 < m_all && ok; n0 += p.tokens_cap) {
+        const int m = min(m_all - n0, p.tokens_cap), nc = cols(m);
         const short* mine = by.list + by.off[it.e] + n0;
         ok = warp_wait(tfull_bar(acc), acc_phase, abort_flag, wait_limit);
         if (UP) {                                    // (the four warps meet in the exchange below: they leave together)
@@ -531,20 +536,23 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
         }
         if (!ok) break;
         tc_fence_after();
-        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * FT_COLS;
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * COLS;
         for (int c0 = 0; c0 < m; c0 += 32) {
           uint32_t r[32];
           tmem_ld32_issue(taddr + c0, r);
           tmem_ld_wait(r);
-          if (n16 < FT_COLS) {                       // the sums of the turns
+          if (!UP || nc < COLS) {                    // the sums of the turns and of the halves: columns 32 further on, then 16, then 8
             uint32_t r2[32];
-            tmem_ld32_issue(taddr + 32, r2);
+            tmem_ld32_issue(taddr + (!UP && nc == COLS ? c0 + COLS / 2 : 32), r2);
             tmem_ld_wait(r2);
 #pragma unroll
             for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r2[j]));
-            if (n16 == 16)
+            if (nc <= 16 * PT)
 #pragma unroll
               for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r[16 + j]));
+            if (!UP && nc == 16)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r[8 + j]));
           }
           if (UP) {
 #pragma unroll
@@ -563,8 +571,14 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
                   const int a = mine[c0 + jb + j];
                   const float2 g = *reinterpret_cast<const float2*>(&exch[j][rr]), u = *reinterpret_cast<const float2*>(&exch[j][p.h + rr]);
                   const float gate = __ldg(p.gates + a);
-                  *reinterpret_cast<__nv_bfloat162*>(p.hid + (size_t)a * p.out_rows + row0 + rr) =
-                      __floats2bfloat162_rn(silu_fast(g.x) * u.x * gate, silu_fast(g.y) * u.y * gate);
+                  // high and low half; one that is not finite has no low half
+                  const float v0 = silu_fast(g.x) * u.x * gate, v1 = silu_fast(g.y) * u.y * gate;
+                  const __nv_bfloat162 hi = __floats2bfloat162_rn(v0, v1);
+                  const float h0 = __low2float(hi), h1 = __high2float(hi);
+                  bf16* to = p.hid + (size_t)a * 2 * p.out_rows + row0 + rr;
+                  *reinterpret_cast<__nv_bfloat162*>(to) = hi;
+                  *reinterpret_cast<__nv_bfloat162*>(to + p.out_rows) =
+                      __floats2bfloat162_rn(isfinite(h0) ? v0 - h0 : 0.0f, isfinite(h1) ? v1 - h1 : 0.0f);
                 }
               }
               together();
@@ -647,7 +661,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * FT_COLS) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * COLS) : "memory");
   }
 }
 
@@ -658,12 +672,12 @@ cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32
   FfnTc p{};
   p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
   p.T = s.T; p.K = s.K; p.E = s.E;
-  p.cols_cap = ffn_columns(s.T, s.K, s.E);
+  p.tokens_cap = ffn_tokens(s.T, s.K, s.E);
   const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true);
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
-    const int rows = (up ? 2 : 1) * p.h;
-    p.stages = ffn_stages(rows, p.cols_cap);
+    const int rows = (up ? 2 : 1) * p.h, cols = ffn_per_token(up) * p.tokens_cap;
+    p.stages = ffn_stages(rows, cols);
     if (p.stages < FT_MIN_STAGES) return cudaErrorInvalidValue;      // (cut_tiles takes no such tile)
     CUtensorMap tw;
     if (!make_tmap(&tw, W, (uint64_t)s.E * p.w_rows, (uint64_t)p.Kd, (uint64_t)p.Kd, p.h)) return cudaErrorInvalidValue;
@@ -671,7 +685,7 @@ cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32
     cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
     if (rc != cudaSuccess) return rc;
     count_launch();
-    return launch_k(kern, dim3(sms), FT_THREADS, ffn_ring(rows, p.cols_cap, p.stages), st, tw, p, WAIT_LIMIT);
+    return launch_k(kern, dim3(sms), FT_THREADS, ffn_ring(rows, cols, p.stages), st, tw, p, WAIT_LIMIT);
   };
   p.x = static_cast<const bf16*>(s.x); p.ldx = s.Dm; p.Kd = s.Dm; p.w_rows = 2 * s.F; p.out_rows = s.F;
   p.h = cu.h; p.tiles = (s.F + cu.h - 1) / cu.h; p.splits = 1;
@@ -701,7 +715,7 @@ FfnStepWs ffn_step_ws(const rom_config& c, int d_ff) {
   const bool tc = c.dtype == ROM_BF16;
   const size_t A = (size_t)c.B * c.L * c.K;
   l.arrived = take(tc ? sizeof(int32_t) * kFfnMaxTiles : 0);
-  l.hid = take((tc ? 2 : 4) * A * d_ff);
+  l.hid = take(4 * A * d_ff);      // (bf16: two halves)
   if (tc) l.down = cut_tiles(c.B * c.L, c.K, c.E, c.d_model, d_ff, false);
   l.part = take(tc && !(c.K == 1 && l.down.splits == 1) ? sizeof(float) * l.down.splits * A * c.d_model : 0);
   l.total = o;
