@@ -363,7 +363,8 @@ ROM_API int rom_conv_ragged(const rom_config *cfg, const rom_ragged *seqs, const
  *   h_in (NULL: every sequence starts from zeros), h_out (NULL: not kept).  y is none of the inputs.
  *   ws : rom_scan_ragged_workspace_size(cfg, n_seq, rows) bytes (host out); scratch of this call alone: overlapping calls, captured graphs
  *        that may run at the same time among them, need one each.
- * State and arithmetic are fp32.  Uses cfg->d_inner, d_state, dtype, disc_mode (B and L are not used).             */
+ * State and arithmetic are fp32; in bf16 with zero-order hold a step's input may be 2^-10 of itself off (2^-19 in fp32), however small the step.
+ * Uses cfg->d_inner, d_state, dtype, disc_mode (B and L are not used).                                              */
 ROM_API int rom_scan_ragged_workspace_size(const rom_config *cfg, int32_t n_seq, int32_t rows, size_t *bytes);
 ROM_API int rom_scan_ragged(const rom_config *cfg, const rom_ragged *seqs, const void *u, const float *delta, const float *A,
                     const float *Bm, const float *Cm, int64_t ld_bc, const float *D, const void *z, int64_t ldz, const float *h_in,

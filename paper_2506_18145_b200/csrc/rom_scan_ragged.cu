@@ -21,6 +21,7 @@
 // sequence's start a third of a chunk away (fewer rows in the first launch, uneven chunks: no gain), one warp per sequence (16384 rows: 21 ms),
 // an eighth of the exponentials, or a quarter of the first launch's, as polynomials on the fp32 pipe (2 % less where the work is most, up to 7 % more elsewhere).
 #include <cmath>
+#include <type_traits>
 
 #include "rom_serve.cuh"
 
@@ -53,6 +54,21 @@ struct RaggedTile {
 };
 
 __device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
+
+// bf16, zero-order hold: with w = -B u / A a step is h <- a (h - w) + w, of which 1 - a is taken of w.  a is up to 2^-22 off, so the input (1 - a) w is off by
+// that over |Delta A|: below kSmallStep, where it could be more than 2^-10, and for an infinite w (inf - inf) a row of the warp's
+// channels is run with 1 - a by itself.  16384 rows x 4096 channels: 926 us when all rows are, 675 when none is, 10 of them for the look at the rows.
+// (A growing state, Delta < 0, has no such steps.)
+constexpr float kSmallStep = 1.0f / 4096.0f, kLargeInput = 0x1p62f;
+// a = 2^t, d = 1 - a for t <= 0, within 2^-14 of itself: the larger of the first two terms of its power series, which stay below it, and 1 - a less
+// the 2^-22 that a may be off, which does too.  Up to |t| of about 2^-6 it is the series, then the difference.
+__device__ __forceinline__ void decay_of_small_steps(float2 t, float2& a, float2& d) {
+  constexpr float ln2 = 0.6931471805599453f;
+  const float2 ds = __fmul2_rn(__ffma2_rn(t, pair(-ln2 * ln2 / 2.0f), pair(-ln2)), t);
+  a = make_float2(ex2_ftz(t.x), ex2_ftz(t.y));
+  const float2 dl = __ffma2_rn(a, pair(-1.0f), pair(1.0f - 0x1p-22f));
+  d = make_float2(fmaxf(ds.x, dl.x), fmaxf(ds.y, dl.y));
+}
 // Slot of lane l's partial sums of row r: conflict-free for a quarter-warp of writers (eight lanes, one row) and of readers (lanes 8 g + const, two rows).
 __device__ __forceinline__ int y_slot(int l, int r) { return l ^ (2 * (l >> 3) + (r & 1)); }
 
@@ -151,6 +167,19 @@ scan_ragged_chunks(const RaggedScan p) {
       a2[n][j] = make_float2(av[2 * j][n] * a, av[2 * j + 1][n] * a);
       kin[n][j] = make_float2(k / av[2 * j][n], k / av[2 * j + 1][n]);
     }
+  // the smallest Delta whose steps are not small, whatever the channel and state
+  constexpr bool CAREFUL = ZOH && !FINE;
+  float d_small = 0.0f;
+  if (CAREFUL) {
+    float least = fabsf(av[0][0]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) least = fminf(least, fabsf(av[i][n]));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+    d_small = kSmallStep / least;
+  }
   if (second) pdl_wait();
   {
     float4 v[4] = {zero4, zero4, zero4, zero4};
@@ -288,9 +317,16 @@ scan_ragged_chunks(const RaggedScan p) {
   if (t < hi) fetch(t, min(RR, hi - t));
   while (t < hi) {
     const int m = min(RR, hi - t), t_next = t + m;
+    unsigned careful = 0;         // four bits a row
     {
       float d[8], uu[8];
       r_d.get(d); r_u.get(uu);
+      if (CAREFUL) {
+        float least = d[0], most = fmaxf(fmaxf(fabsf(r_b.x), fabsf(r_b.y)), fmaxf(fabsf(r_b.z), fabsf(r_b.w)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { least = fminf(least, d[i]); most = fmaxf(most, fabsf(uu[i])); }
+        careful = __ballot_sync(0xffffffffu, lt < m && least >= 0.0f && (least < d_small || most >= kLargeInput));
+      }
       if (!ZOH) {                 // B-bar = Delta B: the input enters as Delta u
 #pragma unroll
         for (int i = 0; i < 8; ++i) uu[i] *= d[i];
@@ -308,7 +344,7 @@ scan_ragged_chunks(const RaggedScan p) {
     // one row; its operands have been requested, those of row `ahead` are before this row's arithmetic: a load issued behind a row's exponentials
     // waits for all of them
     float4 nd = s.dl[0][cg], nu = s.u[0][cg], nb = s.b[0][q], nc = STATE ? zero4 : s.c[0][q];
-    auto row = [&](int r, int ahead) {
+    auto row = [&](int r, int ahead, auto careful_tag) {
       const float4 d4 = nd, u4 = nu, b4 = nb, c4 = nc;
       nd = s.dl[ahead][cg ^ ahead]; nu = s.u[ahead][cg ^ ahead]; nb = s.b[ahead][q];
       if (!STATE) nc = s.c[ahead][q];
@@ -325,6 +361,10 @@ scan_ragged_chunks(const RaggedScan p) {
             float2 a, e;
             decay(x, a, e);
             h[n][j] = __ffma2_rn(a, h[n][j], ZOH ? __fmul2_rn(e, __fmul2_rn(uB, kin[n][j])) : uB);
+          } else if (decltype(careful_tag)::value) {
+            float2 a, d;
+            decay_of_small_steps(x, a, d);
+            h[n][j] = __ffma2_rn(a, h[n][j], __fmul2_rn(d, __fmul2_rn(uB, kin[n][j])));
           } else {
             const float2 a = make_float2(ex2_ftz(x.x), ex2_ftz(x.y));
             if (ZOH) {            // w = -B u / A, h <- a (h - w) + w
@@ -339,15 +379,22 @@ scan_ragged_chunks(const RaggedScan p) {
       if (STATE) { sdel[0] = __fadd2_rn(sdel[0], dl[0]); sdel[1] = __fadd2_rn(sdel[1], dl[1]); }
       else s.y[r][y_slot(lane, r)] = make_float4(acc[0].x, acc[0].y, acc[1].x, acc[1].y);
     };
-    constexpr int UF = FINE ? 2 : STATE ? 4 : RR;
-    if (m == RR && (STATE || cur_end >= t_next)) {
+    constexpr int UF = FINE ? 2 : STATE ? 4 : RR, UC = 4;
+    const bool whole = m == RR && (STATE || cur_end >= t_next);
+    unsigned each = careful | careful >> 2;
+    each = (each | each >> 1) & 0x11111111u;
+    if (whole && !careful) {
 #pragma unroll UF
-      for (int r = 0; r < RR; ++r) row(r, min(r + 1, RR - 1));
-    } else {                      // the chunk's last rows, or sequences that end here
+      for (int r = 0; r < RR; ++r) row(r, min(r + 1, RR - 1), std::false_type{});
+    } else if (CAREFUL && whole && each == 0x11111111u) {
+#pragma unroll UC
+      for (int r = 0; r < RR; ++r) row(r, min(r + 1, RR - 1), std::bool_constant<CAREFUL>{});
+    } else {                      // the chunk's last rows, sequences that end here, rows that need care
 #pragma unroll 1
       for (int r = 0; r < m; ++r) {
         if (!STATE && t + r >= cur_end) enter();
-        row(r, min(r + 1, RR - 1));
+        if (CAREFUL && ((each >> (4 * r)) & 1u)) row(r, min(r + 1, RR - 1), std::bool_constant<CAREFUL>{});
+        else row(r, min(r + 1, RR - 1), std::false_type{});
       }
     }
     __syncwarp();
