@@ -61,12 +61,12 @@ __device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
 // (A growing state, Delta < 0, has no such steps.)
 constexpr float kSmallStep = 1.0f / 4096.0f, kLargeInput = 0x1p62f;
 // a = 2^t, d = 1 - a for t <= 0, within 2^-14 of itself: the larger of the first two terms of its power series, which stay below it, and 1 - a less
-// the 2^-22 that a may be off, which does too.  Up to |t| of about 2^-6 it is the series, then the difference.
+// the 2^-22 that a may be off, and its rounding, which does too.  Up to |t| of about 2^-6 it is the series, then the difference.
 __device__ __forceinline__ void decay_of_small_steps(float2 t, float2& a, float2& d) {
   constexpr float ln2 = 0.6931471805599453f;
   const float2 ds = __fmul2_rn(__ffma2_rn(t, pair(-ln2 * ln2 / 2.0f), pair(-ln2)), t);
   a = make_float2(ex2_ftz(t.x), ex2_ftz(t.y));
-  const float2 dl = __ffma2_rn(a, pair(-1.0f), pair(1.0f - 0x1p-22f));
+  const float2 dl = __ffma2_rn(a, pair(-1.0f), pair(1.0f - 0x1.4p-22f));
   d = make_float2(fmaxf(ds.x, dl.x), fmaxf(ds.y, dl.y));
 }
 // Slot of lane l's partial sums of row r: conflict-free for a quarter-warp of writers (eight lanes, one row) and of readers (lanes 8 g + const, two rows).
