@@ -91,6 +91,28 @@ struct SeqWindow {
   __device__ __forceinline__ int out_of(int i) const { return __shfl_sync(0xffffffffu, out, i - base); }
 };
 
+// The chained states of a warp, h <- 2^(a sum Delta) h + h_end over the chunks [k0, k1), where the plain product has given a NaN: none of a chunk's decays may be
+// zero where their product is, and an infinite state then stays infinite, as it does step by step; nor does a state of zero
+// become one by a product past the largest number.  The chunk's largest Delta tells whether a decay is zero.
+__device__ __noinline__ void chain_not_finite(const float* h_end, const float* sum_delta, const float* delta, const float* A, int Lc, int De, int c0, int q, int k0, int k1,
+                                              float4* v) {
+  for (int k = k0; k < k1; ++k)
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(A + (size_t)(c0 + i) * 16) + q);
+      const float4 e = *reinterpret_cast<const float4*>(h_end + ((size_t)k * De + c0 + i) * 16 + 4 * q);
+      const float sum = sum_delta[(size_t)k * De + c0 + i];
+      float most = -INFINITY;
+#pragma unroll 8
+      for (int r = 0; r < Lc; ++r) most = fmaxf(most, __ldg(delta + ((size_t)k * Lc + r) * De + c0 + i));
+      auto factor = [&](float av) {
+        const float al = av * kLog2eServe, x = al * sum, P = ex2_ftz(x);
+        return x < -126.0f && al * most >= -126.0f ? __int_as_float(1) : fminf(P, 3.402823466e38f);
+      };
+      v[i] = make_float4(fmaf(factor(a.x), v[i].x, e.x), fmaf(factor(a.y), v[i].y, e.y), fmaf(factor(a.z), v[i].z, e.z), fmaf(factor(a.w), v[i].w, e.w));
+    }
+}
+
 // STATE: the first launch.
 template <typename T, bool ZOH, bool STATE>
 __global__ void __launch_bounds__(RWARPS * 32, sizeof(T) == 2 ? 3 : 2)
@@ -215,6 +237,17 @@ scan_ragged_chunks(const RaggedScan p) {
             v[i].w = fmaf(ex2_ftz(al[3] * dk[i]), v[i].w, e4[k][i].w);
           }
         }
+      }
+      float any = 0.0f;                                          // (a NaN is there to the end)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) any += (v[i].x + v[i].y) + (v[i].z + v[i].w);
+      if (any != any) {
+        float4 again[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) again[i] = *reinterpret_cast<const float4*>(p.h_end + (size_t)first_chunk * De * 16 + state_at(i));
+        chain_not_finite(p.h_end, p.sum_delta, p.delta, p.A, p.Lc, De, c0, q, first_chunk + 1, chunk, again);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = again[i];
       }
     }
     set_state(v);

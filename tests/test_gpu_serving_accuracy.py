@@ -169,3 +169,42 @@ def test_scan_ragged_input_that_is_infinite(dtype, disc_mode):
         sign = torch.sign(s["Cm"][a + at:e, n])[:, None] * torch.sign(s["z"][a + at:e].float())
         want = (sign * float("inf")).cuda()
         assert torch.equal(y[a + at:e].float(), want) and torch.all(torch.isfinite(y[a:a + at]))
+
+
+@pytest.mark.parametrize("lens", [[1500], [700, 0, 3, 900, 40], [9, 30, 1100]])
+@pytest.mark.parametrize("disc_mode", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scan_ragged_infinite_state_stays_infinite(dtype, disc_mode, lens):
+    """An initial state of infinity, of one channel and state: no step's decay is zero, the product of ten of them is.  However the rows are cut into chunks,
+    that state is infinite at the end of its sequence, and nothing else differs from a call with a zero in its place."""
+    De, c, n = 64, 37, 11
+    p = Packed(lens, seed=41, resume=[1] * len(lens))
+    s = one_sign(p.rows, De, dtype, (1.0, 2.0), seed=3)
+    s["A"] = -(3.0 + torch.rand((De, 16), generator=torch.Generator().manual_seed(42)) * 8.0)
+    h0 = randn(43, (p.n_slots, De, 16), 0.3)
+    h0[:, c, n] = 0.0
+    y0, rest = scan_run(p, De, dtype, disc_mode, s, h0)
+    h0[:, c, n] = -float("inf")
+    y, h = scan_run(p, De, dtype, disc_mode, s, h0)
+    others = torch.ones(De, dtype=torch.bool)
+    others[c] = False
+    for i, (a, e) in enumerate(zip(p.start, p.start[1:])):
+        q = int(p.slots[i])
+        assert torch.isneginf(h[q, c, n]) and same_bits(h[q][others], rest[q][others]) and same_bits(h[q, c, :n], rest[q, c, :n]) and same_bits(h[q, c, n + 1:], rest[q, c, n + 1:])
+        want = -torch.sign(s["Cm"][a:e, n]) * torch.sign(s["z"][a:e, c].float()) * float("inf")
+        assert torch.equal(y[a:e, c].float(), want.cuda()) and same_bits(y[a:e][:, others], y0[a:e][:, others])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scan_ragged_state_of_zero_that_grows(dtype):
+    """Steps backwards: no input before the last row, and decays whose product over ten rows is past the largest number.  A state of zero stays zero."""
+    De = 64
+    p = Packed([900], seed=44, resume=[0])
+    s = one_sign(p.rows, De, dtype, (0.2, 0.5), seed=4)
+    s["delta"] = -s["delta"]
+    s["A"] = -(20.0 + 20.0 * torch.rand((De, 16), generator=torch.Generator().manual_seed(45)))
+    s["u"][:-1] = 0.0
+    y, h = scan_run(p, De, dtype, 1, s, torch.zeros((p.n_slots, De, 16)))
+    want = (s["delta"][-1] * s["u"][-1].float())[:, None] * s["Bm"][-1][None]
+    torch.testing.assert_close(h[int(p.slots[0])].cpu(), want, rtol=1e-6, atol=0.0)
+    assert torch.all(y[:-1] == 0)
