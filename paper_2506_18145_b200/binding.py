@@ -316,27 +316,39 @@ def rom_layer_step(cfg, weights: RomWeights, x, conv_state, ssm_state, out, topk
     return rc
 
 
-def _at(t: Optional[torch.Tensor], device: int) -> Optional[int]:
-    """Address of a contiguous tensor of a serving call.  These launch on the current device: what lies on another one (or on the host) is refused."""
+_STORAGE = {ROM_F32: torch.float32, ROM_BF16: torch.bfloat16}
+
+
+def _elsewhere(t: torch.Tensor, device: int) -> ValueError:
+    return ValueError(f"a tensor is on device {t.device}, the call runs on cuda:{device}")
+
+
+def _at(t: Optional[torch.Tensor], device: int, n: int = 0, dtype: Optional[torch.dtype] = None) -> Optional[int]:
+    """Address of a contiguous tensor of a serving call, of which the call reads or writes n elements of the given type.  These launch on the current device: what
+    lies on another one (or on the host) is refused."""
     if t is None:
         return None
     if t.get_device() != device:
-        raise ValueError(f"a tensor is on device {t.device}, the call runs on cuda:{device}")
+        raise _elsewhere(t, device)
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
+    if t.numel() < n or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"a tensor of {t.numel()} elements of {t.dtype} where the call needs {n} of {dtype}")
     return t.data_ptr()
 
 
-def _rows_at(t: Optional[torch.Tensor], device: int):
+def _rows_at(t: Optional[torch.Tensor], device: int, n_rows: int = 0, n_columns: int = 0, dtype: Optional[torch.dtype] = None):
     """(address, elements between rows) of a [rows, width] tensor whose rows are contiguous; a column slice of wider rows is one."""
     if t is None:
         return None, 0
     if t.get_device() != device:
-        raise ValueError(f"a tensor is on device {t.device}, the call runs on cuda:{device}")
+        raise _elsewhere(t, device)
     pitch = t.stride()
     if len(pitch) != 2 or pitch[1] != 1:
         raise ValueError("expected a tensor [rows, width] with contiguous rows")
     rows, width = t.shape
+    if rows < n_rows or width < n_columns or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"a tensor [{rows}, {width}] of {t.dtype} where the call needs [{n_rows}, {n_columns}] of {dtype}")
     return t.data_ptr(), pitch[0] if rows > 1 else width      # (a single row has no pitch: torch may say anything)
 
 
@@ -350,15 +362,15 @@ def _slots(a: Optional[torch.Tensor], b: Optional[torch.Tensor]) -> int:
     """Slots of the state pools of a call (0 without both, which the library refuses)."""
     if a is None or b is None:
         return 0
-    n = a.size(0)
-    if b is not a and b.size(0) != n:
+    n = a.shape[0]
+    if b is not a and b.shape[0] != n:
         raise ValueError("the pools differ in their slots")
     return n
 
 
-def _bc(Bm, Cm, device: int):
+def _bc(Bm, Cm, device: int, n_rows: int, d_state: int):
     """Addresses of B and C and their common pitch."""
-    (pb, ldb), (pc, ldc) = _rows_at(Bm, device), _rows_at(Cm, device)
+    (pb, ldb), (pc, ldc) = _rows_at(Bm, device, n_rows, d_state, torch.float32), _rows_at(Cm, device, n_rows, d_state, torch.float32)
     if ldb != ldc:
         raise ValueError("Bm and Cm differ in their pitch")
     return pb, pc, ldb
@@ -380,11 +392,13 @@ def make_ragged(rows: int, n_slots: int, seq_start, slot=None, resume=None) -> R
 
 
 def rom_conv_ragged(cfg, seqs: RomRagged, x, w_conv, b_conv, win_in, win_out, y, stream=None, check=True) -> int:
-    """x: [rows, d_inner], rows may be a column slice of wider ones."""
-    d = torch.cuda.current_device()
-    px, ldx = _rows_at(x, d)
-    rc = lib().rom_conv_ragged(ctypes.byref(cfg), _sequences(seqs, d), px, ldx, _at(w_conv, d), _at(b_conv, d), _at(win_in, d), _at(win_out, d),
-                               _at(y, d), _stream(stream, d))
+    """x: [rows, d_inner], rows may be a column slice of wider ones; y is not x."""
+    d, De, rows, k, T, f32 = torch.cuda.current_device(), cfg.d_inner, seqs.rows, cfg.d_conv, _STORAGE.get(cfg.dtype), torch.float32
+    (px, ldx), py, pool = _rows_at(x, d, rows, De, T), _at(y, d, rows * De, T), seqs.n_slots * (k - 1) * De
+    if px == py and px:
+        raise ValueError("y is x")
+    rc = lib().rom_conv_ragged(ctypes.byref(cfg), _sequences(seqs, d), px, ldx, _at(w_conv, d, k * De, T), _at(b_conv, d, De, f32), _at(win_in, d, pool, f32),
+                               _at(win_out, d, pool, f32), py, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_conv_ragged")
     return rc
@@ -400,30 +414,33 @@ def scan_ragged_workspace_size(cfg: RomConfig, n_seq: int, rows: int) -> int:
 
 def rom_scan_ragged(cfg, seqs: RomRagged, u, delta, A, Bm, Cm, D, z, h_in, h_out, y, ws, stream=None, check=True) -> int:
     """Bm, Cm: [rows, d_state] of one pitch; z: [rows, d_inner]; both may be column slices of wider rows."""
-    d = torch.cuda.current_device()
-    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm, d), _rows_at(z, d)
-    rc = lib().rom_scan_ragged(ctypes.byref(cfg), _sequences(seqs, d), _at(u, d), _at(delta, d), _at(A, d), pb, pc, ld, _at(D, d), pz, ldz, _at(h_in, d),
-                               _at(h_out, d), _at(y, d), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
+    d, De, N, rows, T, f32 = torch.cuda.current_device(), cfg.d_inner, cfg.d_state, seqs.rows, _STORAGE.get(cfg.dtype), torch.float32
+    n, pool = rows * De, seqs.n_slots * De * N
+    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm, d, rows, N), _rows_at(z, d, rows, De, T)
+    rc = lib().rom_scan_ragged(ctypes.byref(cfg), _sequences(seqs, d), _at(u, d, n, T), _at(delta, d, n, f32), _at(A, d, De * N, f32), pb, pc, ld, _at(D, d, De, f32), pz, ldz,
+                               _at(h_in, d, pool, f32), _at(h_out, d, pool, f32), _at(y, d, n, T), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_scan_ragged")
     return rc
 
 
 def rom_conv_step(cfg, x, w_conv, b_conv, slot, win_in, win_out, y, stream=None, check=True) -> int:
-    d = torch.cuda.current_device()
-    px, ldx = _rows_at(x, d)
-    rc = lib().rom_conv_step(ctypes.byref(cfg), px, ldx, _at(w_conv, d), _at(b_conv, d), _at(slot, d), _slots(win_in, win_out), _at(win_in, d),
-                             _at(win_out, d), _at(y, d), _stream(stream, d))
+    d, B, De, k, T, f32 = torch.cuda.current_device(), cfg.B, cfg.d_inner, cfg.d_conv, _STORAGE.get(cfg.dtype), torch.float32
+    (px, ldx), n_slots = _rows_at(x, d, B, De, T), _slots(win_in, win_out)
+    pool = n_slots * (k - 1) * De
+    rc = lib().rom_conv_step(ctypes.byref(cfg), px, ldx, _at(w_conv, d, k * De, T), _at(b_conv, d, De, f32), _at(slot, d, B, torch.int32), n_slots, _at(win_in, d, pool, f32),
+                             _at(win_out, d, pool, f32), _at(y, d, B * De, T), _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_conv_step")
     return rc
 
 
 def rom_scan_step(cfg, u, delta, A, Bm, Cm, D, z, slot, h_in, h_out, y, stream=None, check=True) -> int:
-    d = torch.cuda.current_device()
-    (pb, pc, ld), (pz, ldz) = _bc(Bm, Cm, d), _rows_at(z, d)
-    rc = lib().rom_scan_step(ctypes.byref(cfg), _at(u, d), _at(delta, d), _at(A, d), pb, pc, ld, _at(D, d), pz, ldz, _at(slot, d), _slots(h_in, h_out),
-                             _at(h_in, d), _at(h_out, d), _at(y, d), _stream(stream, d))
+    d, B, De, N, T, f32 = torch.cuda.current_device(), cfg.B, cfg.d_inner, cfg.d_state, _STORAGE.get(cfg.dtype), torch.float32
+    (pb, pc, ld), (pz, ldz), n_slots = _bc(Bm, Cm, d, B, N), _rows_at(z, d, B, De, T), _slots(h_in, h_out)
+    n, pool = B * De, n_slots * De * N
+    rc = lib().rom_scan_step(ctypes.byref(cfg), _at(u, d, n, T), _at(delta, d, n, f32), _at(A, d, De * N, f32), pb, pc, ld, _at(D, d, De, f32), pz, ldz, _at(slot, d, B, torch.int32),
+                             n_slots, _at(h_in, d, pool, f32), _at(h_out, d, pool, f32), _at(y, d, n, T), _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_scan_step")
     return rc
@@ -438,9 +455,12 @@ def ffn_moe_step_workspace_size(cfg: RomConfig, d_ff: int) -> int:
 
 
 def rom_ffn_moe_step(cfg, d_ff, W_gu, W_down, x, topk_idx, gates, out, ws, stream=None, check=True) -> int:
-    d = torch.cuda.current_device()
-    rc = lib().rom_ffn_moe_step(ctypes.byref(cfg), int(d_ff), _at(W_gu, d), _at(W_down, d), _at(x, d), _at(topk_idx, d), _at(gates, d), _at(out, d),
-                                _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
+    d, T, f32, F = torch.cuda.current_device(), _STORAGE.get(cfg.dtype), torch.float32, int(d_ff)
+    tokens, Dm, E = cfg.B * cfg.L, cfg.d_model, cfg.E
+    n, w = tokens * Dm, E * F * Dm
+    chosen = tokens * cfg.K
+    rc = lib().rom_ffn_moe_step(ctypes.byref(cfg), F, _at(W_gu, d, 2 * w, T), _at(W_down, d, w, T), _at(x, d, n, T), _at(topk_idx, d, chosen, torch.int32),
+                                _at(gates, d, chosen, f32), _at(out, d, n, T), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_ffn_moe_step")
     return rc
