@@ -362,7 +362,7 @@ ROM_API int rom_conv_ragged(const rom_config *cfg, const rom_ragged *seqs, const
  *   A, D as in rom_scan;  z : [rows, d_inner] dtype, pitch ldz, or NULL (no gate);
  *   h_in (NULL: every sequence starts from zeros), h_out (NULL: not kept).  y is none of the inputs.
  *   ws : rom_scan_ragged_workspace_size(cfg, n_seq, rows) bytes (host out); scratch of this call alone: overlapping calls, captured graphs
- *        that may run at the same time among them, need one each.
+ *        that may run at the same time among them, need one each.  A buffer sized for some n_seq and rows does for all calls of no more of both.
  * State and arithmetic are fp32; in bf16 with zero-order hold a step's input may be 2^-10 of itself off (2^-19 in fp32), however small the step.
  * Uses cfg->d_inner, d_state, dtype, disc_mode (B and L are not used).                                              */
 ROM_API int rom_scan_ragged_workspace_size(const rom_config *cfg, int32_t n_seq, int32_t rows, size_t *bytes);
@@ -382,7 +382,8 @@ ROM_API int rom_scan_step(const rom_config *cfg, const void *u, const float *del
  * each chosen expert's weights once.  An expert index outside [0, E) contributes nothing; negative ones are the padding of a fixed
  * batch (a token with none but those gets a row of zeros), others are reported by rom_get_status as ROM_ERR_INVALID_ARG.  An expert that a
  * token names twice counts twice.
- *   ws : rom_ffn_moe_step_workspace_size(cfg, d_ff) bytes (host out); overlapping calls need one each.
+ *   ws : rom_ffn_moe_step_workspace_size(cfg, d_ff) bytes (host out); overlapping calls need one each.  A buffer sized for some
+ *        B*L does for calls of fewer tokens (the rest of cfg and d_ff as they are).
  * Uses cfg->B, L, d_model, E, K, dtype (flags must be 0).                                                          */
 ROM_API int rom_ffn_moe_step_workspace_size(const rom_config *cfg, int32_t d_ff, size_t *bytes);
 ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_gu, const void *W_down, const void *x,

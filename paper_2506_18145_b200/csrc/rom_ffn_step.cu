@@ -717,7 +717,8 @@ FfnStepWs ffn_step_ws(const rom_config& c, int d_ff) {
   l.arrived = take(tc ? sizeof(int32_t) * kFfnMaxTiles : 0);
   l.hid = take(4 * A * d_ff);      // (bf16: two halves)
   if (tc) l.down = cut_tiles(c.B * c.L, c.K, c.E, c.d_model, d_ff, false);
-  l.part = take(tc && !(c.K == 1 && l.down.splits == 1) ? sizeof(float) * l.down.splits * A * c.d_model : 0);
+  // (as many parts as any number of tokens up to these may take: a buffer for the largest batch does for all smaller ones, which are cut into more)
+  l.part = take(tc ? sizeof(float) * std::min(kFfnMaxSplits, (d_ff + FT_K - 1) / FT_K) * A * c.d_model : 0);
   l.total = o;
   return l;
 }

@@ -472,6 +472,13 @@ scan_ragged_chunks(const RaggedScan p) {
 
 // Rows of a chunk when there are n of them.
 int chunk_rows(int rows, int n) { return n == 1 ? (rows > 0 ? rows : 1) : (int)align_up((size_t)(rows + n - 1) / n, RR); }
+// Chunks that packed rows may be cut into.
+int most_chunks(int De, int rows) {
+  int n = 148 * 12 * 6 / (De / 32);
+  if (n > 512) n = 512;
+  if (n > rows / 8) n = rows / 8;
+  return n > 1 ? n : 1;
+}
 // Chunks of the packed rows: the count with the smallest time by what the kernels were measured to take.  A block of four warps takes
 // 155 / 235 / 330 ns a row with one / two / three of them on an SM, 128 / 188 / 255 ns states only; more than three come in rounds, of which the last
 // may be of one or two.  fp32: two on an SM, about twice as long.  A warp takes 3 us before its first row, 0.1 us for every chunk that it chains,
@@ -489,7 +496,7 @@ int ragged_chunks(int De, int n_seq, int rows, bool fp32) {
   };
   int best = 1;
   double best_t = 0.0;
-  for (int n = 1; n == 1 || (rows >= 8 * n && n <= 512 && (long long)n * (De / 32) <= 148 * 12 * 6); n += 1 + n / 16) {      // (a few us on the host at most)
+  for (int n = 1; n <= most_chunks(De, rows); n += 1 + n / 16) {      // (a few us on the host at most)
     const double Lc = chunk_rows(rows, n), nch = rows > 0 ? ceil(rows / Lc) : 1.0;
     const double chained = mean < Lc ? 0.0 : mean / Lc < nch ? mean / Lc : nch;
     double t = time(nch * (De / 32) / RWARPS, full, Lc, 3000.0 + 100.0 * chained + 400.0 * Lc / mean);
@@ -510,12 +517,14 @@ RaggedWs ragged_ws(const rom_config& c, int n_seq, int rows) {
   l.nch = rows > 0 ? (rows + l.Lc - 1) / l.Lc : 1;
   l.early = (long long)l.nch * (De / 32) <= 148ll * RWARPS * (c.dtype == ROM_F32 ? 2 : 3);
   size_t o = 0;
-  auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
+  auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };      // (within total: nch is most_chunks at most)
   const size_t keep = l.nch > 1 ? l.nch : 0;
   l.h_end = take(keep * De * 16 * sizeof(float));
   l.h_start = take(keep * De * 16 * sizeof(float));
   l.sum_delta = take(keep * De * sizeof(float));
-  l.total = o > 256 ? o : 256;
+  // What any number of sequences and rows up to these may take: a buffer for the largest batch does for all smaller ones, whose chunks may be more.
+  const size_t most = most_chunks(De, rows);
+  l.total = most > 1 ? 2 * align_up(most * De * 16 * sizeof(float), 256) + align_up(most * De * sizeof(float), 256) : 256;
   return l;
 }
 

@@ -87,3 +87,23 @@ def test_packed_conv_in_place_is_refused(calls):
     with pytest.raises(ValueError, match="y is x"):
         rb.rom_conv_ragged(cfg, **fixed, **{**t, "y": t["x"]})
     assert calls == []
+
+
+# ---------------------------------------------------------------------------------------------- workspaces
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d_inner", [64, 256, 1024, 2048, 4096, 8192])
+def test_scan_workspace_of_the_largest_batch_does_for_all_smaller_ones(d_inner, dtype):
+    cfg = rb.make_config(1, 1, 64, d_inner, 16, 4, 16, 1, 1, dtype)
+    size = lambda n, r: rb.scan_ragged_workspace_size(cfg, n, r)
+    rows = [0, 1, 7, 8, 15, 16, 17, 100, 500, 777, 1024, 2000, 4096, 8000, 8192, 16384, 30000, 1 << 20]
+    seqs = [0, 1, 2, 5, 8, 23, 64, 500, 5000]
+    for i, r in enumerate(rows):
+        for j, n in enumerate(seqs):
+            assert all(size(n, r) >= size(m, q) for q in rows[:i + 1] for m in seqs[:j + 1][-2:]), (n, r)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d_model,d_ff,experts,K", [(2048, 8192, 16, 2), (1280, 5120, 8, 1), (256, 1024, 4, 2), (4096, 4096, 64, 8), (64, 128, 1, 1), (512, 2048, 16, 2)])
+def test_ffn_step_workspace_of_the_largest_batch_does_for_all_smaller_ones(d_model, d_ff, experts, K, dtype):
+    sizes = [rb.ffn_moe_step_workspace_size(rb.make_config(n, 1, d_model, 64, 16, 4, 16, experts, K, dtype), d_ff) for n in range(1, 65)]
+    assert sizes == sorted(sizes)
