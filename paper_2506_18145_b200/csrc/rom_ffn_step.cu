@@ -221,7 +221,7 @@ int chosen_experts(int T, int K, int E) {
   return n < 1 ? 1 : n;
 }
 constexpr int kSizingSms = 148;      // (workspace sizing and the launch agree)
-constexpr int FT_TOKENS = 64;                        // tokens per pass at most
+constexpr int FT_COLS = 64;                          // columns per pass at most
 // Columns of a token: the down projection has the high and the low half of a hidden row, which add up to it within 2^-16, as two columns of the same MMA.
 __host__ __device__ constexpr int ffn_per_token(bool up) { return up ? 1 : 2; }
 constexpr int FT_MIN_STAGES = 4, FT_MAX_STAGES = 12;      // (a stage for each of the four warps that bring token rows)
@@ -235,11 +235,12 @@ constexpr int ffn_ring(int rows, int cols, int stages) {
 constexpr int ffn_stages(int rows, int cols) {
   return std::min((FT_SMEM - ffn_ring(rows, cols, 0)) / (FT_KB * (rows + cols) * 128), FT_MAX_STAGES);
 }
-// Tokens of a stage: room for twice an expert's mean and eight more; whoever has more than that many streams its weights again (from the
-// L2 mostly), the others have deeper rings.
-int ffn_tokens(int T, int K, int E) {
-  const int want = std::min(T, 2 * (T * K / chosen_experts(T, K, E)) + 8);
-  return want > 32 ? 64 : want > 16 ? 32 : 16;
+// Tokens of a stage: room for twice an expert's mean and eight more (down, where a token is two columns: half as much again and four more, at most 32);
+// whoever has more than that many streams its weights again (from the L2 mostly), the others have deeper rings.  Down, 64 tokens of 2048 x 8192: with room for 64 tokens
+// and twice the mean one of four experts each 88 us instead of 78, two of four 118 instead of 106, two of sixteen 259 instead of 255.
+int ffn_tokens(int T, int K, int E, bool up) {
+  const int mean = T * K / chosen_experts(T, K, E), want = std::min(T, up ? 2 * mean + 8 : mean + mean / 2 + 4);
+  return want > 32 && up ? 64 : want > 16 ? 32 : 16;
 }
 // How the weights are cut into tiles: rows per tile and, of the down projection, parts of the contracted index.  The cheapest by the time that the
 // fullest SM takes, in ns: rounds of tiles times stages of 60 ns and their bytes at 44 a ns (an SM's share of HBM), but at least 460 ns (eight MMAs of
@@ -247,7 +248,7 @@ int ffn_tokens(int T, int K, int E) {
 struct FfnCut { int h, splits; };
 FfnCut cut_tiles(int T, int K, int E, int rows_out, int Kd, bool up) {
   const long long n = chosen_experts(T, K, E), m = (T * K + n - 1) / n, kb = (Kd + FT_K - 1) / FT_K, per = up ? 2 : 1;
-  const int per_token = ffn_per_token(up), cols = per_token * ffn_tokens(T, K, E);
+  const int per_token = ffn_per_token(up), cols = per_token * ffn_tokens(T, K, E, up);
   FfnCut best{8, 1};
   long long least = -1;
   for (int s = 1; s <= (up ? 1 : kFfnMaxSplits) && s <= kb; ++s)
@@ -297,7 +298,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 template <bool UP, int FLIGHT>
 __global__ void __launch_bounds__(FT_THREADS, 1)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
-  constexpr int PT = ffn_per_token(UP), COLS = PT * FT_TOKENS;      // columns of a token, of an accumulator
+  constexpr int PT = ffn_per_token(UP);
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   __shared__ ByExpert by;
@@ -327,7 +328,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   }
   if (tid == 32 * 9) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * COLS) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * FT_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (UP) { pdl_wait(); pdl_trigger(); }             // (down: the choice of experts is older than the launch before)
@@ -353,7 +354,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   const int n_act = n_act_s, per_expert = p.tiles * p.splits, total = n_act * per_expert;
   const int num_kb = (p.Kd + FT_K - 1) / FT_K;
   const uint32_t w_bytes = (UP ? 2 : 1) * p.h * 128, x_bytes = PT * p.tokens_cap * 128, stage_bytes = FT_KB * (w_bytes + x_bytes);
-  auto cols = [](int m) { return PT * (m > 32 ? 64 : m > 16 ? 32 : m > 16 / PT ? 16 : 16 / PT); };      // N of a pass over m tokens
+  auto cols = [](int m) { return PT * m > 32 ? 64 : PT * m > 16 ? 32 : 16; };      // N of a pass over m tokens
   // item w: expert, first row, stages [kb0, kb0 + n) of the contracted index, walked from a start of the tile's own: in step all CTAs
   // would read the same columns of rows that are a power of two apart
   struct Item { int e, tile, part, kb0, n, rot; };
@@ -433,9 +434,9 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
               const uint64_t adesc = make_smem_desc(base + stage * stage_bytes + b * w_bytes), bdesc = make_smem_desc(base + stage * stage_bytes + FT_KB * w_bytes + b * x_bytes);
 #pragma unroll
               for (int k = 0; k < BLOCK_K / UMMA_K; ++k)
-                // few columns: into 64 / nc accumulators in turns, so that an MMA does not wait for the one before
-                umma_bf16(tmem_base + acc * COLS + k * nc % 64, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc,
-                          (q | b) != 0 || k * nc >= 64 ? 1u : 0u);
+                // few columns: into FT_COLS / nc accumulators in turns, so that an MMA does not wait for the one before
+                umma_bf16(tmem_base + acc * FT_COLS + k * nc % FT_COLS, adesc + (uint64_t)(2 * k), bdesc + (uint64_t)(2 * k), idesc,
+                          (q | b) != 0 || k * nc >= FT_COLS ? 1u : 0u);
             }
             umma_commit(empty_bar(stage));
             issued_any = true;
@@ -536,14 +537,14 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
         }
         if (!ok) break;
         tc_fence_after();
-        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * COLS;
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * FT_COLS;
         for (int c0 = 0; c0 < m; c0 += 32) {
           uint32_t r[32];
           tmem_ld32_issue(taddr + c0, r);
           tmem_ld_wait(r);
-          if (!UP || nc < COLS) {                    // the sums of the turns and of the halves: columns 32 further on, then 16, then 8
+          if (!UP || nc < FT_COLS) {                 // the sums of the turns and of the halves: columns 32 further on, then 16, then 8
             uint32_t r2[32];
-            tmem_ld32_issue(taddr + (!UP && nc == COLS ? c0 + COLS / 2 : 32), r2);
+            tmem_ld32_issue(taddr + 32, r2);
             tmem_ld_wait(r2);
 #pragma unroll
             for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r2[j]));
@@ -661,7 +662,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * COLS) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * FT_COLS) : "memory");
   }
 }
 
@@ -672,10 +673,10 @@ cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32
   FfnTc p{};
   p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
   p.T = s.T; p.K = s.K; p.E = s.E;
-  p.tokens_cap = ffn_tokens(s.T, s.K, s.E);
   const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true);
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
+    p.tokens_cap = ffn_tokens(s.T, s.K, s.E, up);
     const int rows = (up ? 2 : 1) * p.h, cols = ffn_per_token(up) * p.tokens_cap;
     p.stages = ffn_stages(rows, cols);
     if (p.stages < FT_MIN_STAGES) return cudaErrorInvalidValue;      // (cut_tiles takes no such tile)
