@@ -331,7 +331,10 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * FT_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (UP) { pdl_wait(); pdl_trigger(); }             // (down: the choice of experts is older than the launch before)
+  if (UP) {                                          // (down: the choice of experts is older than the launch before)
+    pdl_wait();
+    if (warp == 1) pdl_trigger();                    // (the warp that has the block's tensor memory by now: the successor takes some before it waits)
+  }
   by.build(p.idx, A, p.E);
   if (warp == 0) {                                   // the experts that somebody chose
     const bool lo = lane < p.E && by.off[lane + 1] > by.off[lane], hi = 32 + lane < p.E && by.off[33 + lane] > by.off[32 + lane];
