@@ -514,7 +514,14 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   } else {
     // ---------------------------------------------------------------- output: lane = weight row, column = token
     const int quarter = warp & 3, r_acc = quarter * 32 + lane, ct = tid - 64;      // ct: thread of the 128 here
-    auto together = [&]() { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    // (barriers and tensor-memory loads take whole warps: after branches by lane a warp is brought together first)
+    auto together = [&]() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    auto all_warps = [&](bool mine) {
+      int all;
+      __syncwarp();
+      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.and.pred p, 2, 128, q;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(all) : "r"((int)mine) : "memory");
+      return all != 0;
+    };
     if (!UP) {
       pdl_wait();
       for (int t = blockIdx.x; t < p.T; t += gridDim.x) {      // tokens without an expert
@@ -533,16 +540,13 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
         const int m = min(m_all - n0, p.tokens_cap), nc = cols(m);
         const short* mine = by.list + by.off[it.e] + n0;
         ok = warp_wait(tfull_bar(acc), acc_phase, abort_flag, wait_limit);
-        if (UP) {                                    // (the four warps meet in the exchange below: they leave together)
-          int all;
-          asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.and.pred p, 2, 128, q;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(all) : "r"((int)ok) : "memory");
-          ok = all != 0;
-        }
+        if (UP) ok = all_warps(ok);                  // (the four warps meet in the exchange below: they leave together)
         if (!ok) break;
         tc_fence_after();
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)acc * FT_COLS;
         for (int c0 = 0; c0 < m; c0 += 32) {
           uint32_t r[32];
+          __syncwarp();
           tmem_ld32_issue(taddr + c0, r);
           tmem_ld_wait(r);
           if (!UP || nc < FT_COLS) {                 // the sums of the turns and of the halves: columns 32 further on, then 16, then 8
@@ -605,9 +609,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
       if (!UP && !p.direct) {
         // whoever brings the last part of these rows adds them all, in the order of slots and parts
         __threadfence();
-        int all;
-        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.and.pred p, 2, 128, q;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(all) : "r"((int)ok) : "memory");
-        ok = all != 0;
+        ok = all_warps(ok);
         if (!ok) break;
         if (ct == 0) last_s = atomicAdd(p.arrived + it.tile, 1) == n_act * p.splits - 1;
         together();
@@ -664,6 +666,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
+    __syncwarp();                                    // (the leader comes from its own branch; before the barrier, for all warps, this cost 1 to 30 %)
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * FT_COLS) : "memory");
   }

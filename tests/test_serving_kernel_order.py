@@ -21,3 +21,13 @@ def test_the_successor_comes_in_behind_the_tensor_memory_of_the_block(body):
     first = re.search(r"pdl_trigger\(\)", body)
     assert alloc.start() < first.start() < body.index("__syncthreads();\n  tc_fence_after();")
     assert f"if (warp == {alloc.group(1)}) pdl_trigger();" in body[first.start() - 20:first.end() + 1]
+
+
+@pytest.mark.parametrize("what", [r'asm volatile\("bar\.sync', r"bar\.red", r"tmem_ld32_issue\(taddr \+ c0", r"tc_fence_after\(\);\s*asm volatile\(\"tcgen05\.dealloc"])
+def test_warps_meet_before_aligned_instructions(body, what):
+    """The statement before is the one that brings the lanes of a warp together."""
+    found = list(re.finditer(what, body))
+    assert found
+    for m in found:
+        before = body[:body.rindex("asm volatile", 0, m.end())] if "bar" in what else body[:m.start()]
+        assert before.rstrip().endswith("__syncwarp();")
