@@ -294,7 +294,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, abort_flag, limit);
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
-// FLIGHT: stages of token rows that each of the four warps has in flight besides the one it asks for: 4 (FLIGHT + 1) + 1 stages at least.
+// FLIGHT: stages of token rows that each of the four warps has in flight besides the one it asks for: 4 FLIGHT + 1 stages at least, and one for each warp.
 template <bool UP, int FLIGHT>
 __global__ void __launch_bounds__(FT_THREADS, 1)
 ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t wait_limit) {
