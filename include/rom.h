@@ -90,7 +90,8 @@ typedef struct {
                                  operand stage per CTA (or, on CTA pairs, in the x Proj and dt Proj kernels and
                                  in rom_layer_step, wait for more bytes than are copied) and every wait of them gives up after 2^14 polls
                                  instead of 2^22, so the call returns normally, produces no valid output, and rom_get_status reports
-                                 ROM_ERR_DEVICE_TIMEOUT.  The workspace stays usable for the next call.          */
+                                 ROM_ERR_DEVICE_TIMEOUT.  The workspace stays usable for the next call.  rom_ffn_moe_step in bf16: all stages
+                                 of a block behind its first wait for more bytes than are copied, in both launches    */
 
 typedef struct {                /* all read-only device pointers                                   */
   const void  *W_r;             /* [E, d_model]              dtype  router, W_r of Section 4.2 transposed */
@@ -384,7 +385,7 @@ ROM_API int rom_scan_step(const rom_config *cfg, const void *u, const float *del
  * token names twice counts twice.
  *   ws : rom_ffn_moe_step_workspace_size(cfg, d_ff) bytes (host out); overlapping calls need one each.  A buffer sized for some
  *        B*L does for calls of fewer tokens (the rest of cfg and d_ff as they are).
- * Uses cfg->B, L, d_model, E, K, dtype (flags must be 0).                                                          */
+ * Uses cfg->B, L, d_model, E, K, dtype (flags must be 0 but for ROM_FLAG_TEST_STALL).                               */
 ROM_API int rom_ffn_moe_step_workspace_size(const rom_config *cfg, int32_t d_ff, size_t *bytes);
 ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_gu, const void *W_down, const void *x,
                      const int32_t *topk_idx, const float *gates, void *out, void *ws, size_t ws_bytes, void *stream);

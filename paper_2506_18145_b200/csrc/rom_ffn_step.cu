@@ -270,6 +270,7 @@ struct FfnTc {
   int T, K, E;
   int h, tiles, splits, stages, tokens_cap;          // rows per tile, tiles per expert, parts of the contracted index, ring, tokens of a stage
   int direct;                                        // down: one expert and one part a token: written at once
+  uint32_t stall;                                    // fault injection: bytes that a block's stages behind its first wait for in vain
 };
 
 // Whether a phase is over; does not wait.  A wait takes 200 to 250 cycles even then, as long as three MMAs: the producer and the issuer look at
@@ -380,7 +381,7 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA producer of the weights (nothing here depends on the launch before)
     if (leader) {
-      int stage = 0, issued = 0; uint32_t phase = 0;
+      int stage = 0, issued = 0; uint32_t phase = 0, tx = FT_KB * w_bytes;
       bool ok = true, ready = true;                  // ready: the next stage was free when it was looked at (all are at first)
       for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
         const Item it = item(w);
@@ -391,7 +392,8 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
             const int k0 = k_of(it, q), next = stage + 1 == p.stages ? 0 : stage + 1;
             const uint32_t dst = base + stage * stage_bytes;
             ready = mbar_ready(empty_bar(next), (next ? phase : phase ^ 1u) ^ 1u);
-            mbar_expect_tx(full_bar(stage), FT_KB * w_bytes);
+            mbar_expect_tx(full_bar(stage), tx);
+            tx = FT_KB * w_bytes + p.stall;
 #pragma unroll
             for (int b = 0; b < FT_KB; ++b) {
               tma_load_2d(dst + b * w_bytes, &tmap_w, full_bar(stage), k0 + b * BLOCK_K, row);
@@ -672,13 +674,13 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
   }
 }
 
-cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32_t* arrived, cudaStream_t st) {
+cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32_t* arrived, bool test_stall, cudaStream_t st) {
   int sms = 0;
   cudaError_t e = current_device_sm_count(&sms);
   if (e != cudaSuccess) return e;
   FfnTc p{};
   p.idx = s.idx; p.gates = s.gates; p.hid = static_cast<bf16*>(s.hid); p.part = part; p.out = static_cast<bf16*>(s.out); p.arrived = arrived; p.status = s.status;
-  p.T = s.T; p.K = s.K; p.E = s.E;
+  p.T = s.T; p.K = s.K; p.E = s.E; p.stall = test_stall ? 16 : 0;
   const FfnCut cu = cut_tiles(s.T, s.K, s.E, s.F, s.Dm, true);
   auto launch = [&](auto up_tag, const void* W) {
     constexpr bool up = decltype(up_tag)::value;
@@ -692,7 +694,7 @@ cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32
     cudaError_t rc = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FT_SMEM);
     if (rc != cudaSuccess) return rc;
     count_launch();
-    return launch_k(kern, dim3(sms), FT_THREADS, ffn_ring(rows, cols, p.stages), st, tw, p, WAIT_LIMIT);
+    return launch_k(kern, dim3(sms), FT_THREADS, ffn_ring(rows, cols, p.stages), st, tw, p, p.stall ? WAIT_LIMIT_TEST : WAIT_LIMIT);
   };
   p.x = static_cast<const bf16*>(s.x); p.ldx = s.Dm; p.Kd = s.Dm; p.w_rows = 2 * s.F; p.out_rows = s.F;
   p.h = cu.h; p.tiles = (s.F + cu.h - 1) / cu.h; p.splits = 1;
@@ -705,7 +707,7 @@ cudaError_t launch_ffn_tc(const FfnStep& s, const FfnCut& cd, float* part, int32
 int check_ffn_step(const rom_config* c, int d_ff) {
   if (!c) return ROM_ERR_INVALID_ARG;
   if (c->dtype != ROM_F32 && c->dtype != ROM_BF16) return ROM_ERR_INVALID_ARG;
-  if (c->B < 1 || c->L < 1 || c->E < 1 || c->K < 1 || c->K > c->E || c->flags != 0) return ROM_ERR_INVALID_ARG;
+  if (c->B < 1 || c->L < 1 || c->E < 1 || c->K < 1 || c->K > c->E || (c->flags & ~ROM_FLAG_TEST_STALL) != 0) return ROM_ERR_INVALID_ARG;
   if (c->E > kMaxE || c->K > kMaxK) return ROM_ERR_UNSUPPORTED;
   if (c->d_model < 64 || c->d_model % 64 != 0) return ROM_ERR_INVALID_ARG;
   if (d_ff < 128 || d_ff % 128 != 0) return d_ff < 1 ? ROM_ERR_INVALID_ARG : ROM_ERR_UNSUPPORTED;
@@ -762,7 +764,7 @@ int rom_ffn_moe_step(const rom_config* cfg, int32_t d_ff, const void* W_gu, cons
   char* W = static_cast<char*>(ws);
   const FfnStep p{x, W_gu, W_down, topk_idx, gates, out, W + lay.hid, reinterpret_cast<int32_t*>(W + lay.status), c.B * c.L, c.K, c.E, c.d_model, d_ff};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = c.dtype == ROM_BF16 ? launch_ffn_tc(p, lay.down, reinterpret_cast<float*>(W + lay.part), reinterpret_cast<int32_t*>(W + lay.arrived), st)
+  const cudaError_t e = c.dtype == ROM_BF16 ? launch_ffn_tc(p, lay.down, reinterpret_cast<float*>(W + lay.part), reinterpret_cast<int32_t*>(W + lay.arrived), c.flags != 0, st)
                                             : launch_ffn_rows(p, st);
   return e == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
