@@ -102,14 +102,16 @@ __device__ __noinline__ void chain_not_finite(const float* h_end, const float* s
       const float4 a = __ldg(reinterpret_cast<const float4*>(A + (size_t)(c0 + i) * 16) + q);
       const float4 e = *reinterpret_cast<const float4*>(h_end + ((size_t)k * De + c0 + i) * 16 + 4 * q);
       const float sum = sum_delta[(size_t)k * De + c0 + i];
+      auto lost = [&](float av, float h) { return av * kLog2eServe * sum < -126.0f && isinf(h); };
       float most = -INFINITY;
+      if (lost(a.x, v[i].x) || lost(a.y, v[i].y) || lost(a.z, v[i].z) || lost(a.w, v[i].w))
 #pragma unroll 8
-      for (int r = 0; r < Lc; ++r) most = fmaxf(most, __ldg(delta + ((size_t)k * Lc + r) * De + c0 + i));
-      auto factor = [&](float av) {
-        const float al = av * kLog2eServe, x = al * sum, P = ex2_ftz(x);
-        return x < -126.0f && al * most >= -126.0f ? __int_as_float(1) : fminf(P, 3.402823466e38f);
+        for (int r = 0; r < Lc; ++r) most = fmaxf(most, __ldg(delta + ((size_t)k * Lc + r) * De + c0 + i));
+      auto next = [&](float av, float h, float end) {
+        const float P = ex2_ftz(av * kLog2eServe * sum);
+        return fmaf(lost(av, h) && av * kLog2eServe * most >= -126.0f ? __int_as_float(1) : fminf(P, 3.402823466e38f), h, end);
       };
-      v[i] = make_float4(fmaf(factor(a.x), v[i].x, e.x), fmaf(factor(a.y), v[i].y, e.y), fmaf(factor(a.z), v[i].z, e.z), fmaf(factor(a.w), v[i].w, e.w));
+      v[i] = make_float4(next(a.x, v[i].x, e.x), next(a.y, v[i].y, e.y), next(a.z, v[i].z, e.z), next(a.w, v[i].w, e.w));
     }
 }
 
