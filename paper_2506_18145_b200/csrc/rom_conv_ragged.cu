@@ -5,7 +5,7 @@
 // the next RB are on their way; the rows before a tile are read again, from the L2 mostly.  The first rows are requested before the
 // search for the tile's sequences, which takes two dependent loads.
 //
-// Measured: 16384 rows x 4096 channels (bf16) 53.8 us, 4.98 TB/s = 76 % of the measured copy; half its issue slots, 58 % of the special-function unit (profiles);
+// Measured: 16384 rows x 4096 channels (bf16) 55.4 us, 4.84 TB/s = 74 % of the measured copy (53.8 replayed from a graph); half its issue slots, 58 % of the special-function unit (profiles);
 // 531 rows of 37 sequences x 512 (fp32) 4.3 us.  Tried: 8 bytes a lane 57 us, eight rows in flight 55 to 60, two 61, whole sequences a warp (serial).
 //
 // A tile takes the sequences that start in it and what reaches into it from before.  The first k-1 rows of a sequence need its old window, so they all

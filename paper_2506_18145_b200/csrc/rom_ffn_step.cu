@@ -4,18 +4,19 @@
 // rounding (2.4e-3 of the outputs against 1.7e-3).  Both are columns of the same MMA, which takes as long for 32 columns as for 16.
 //
 // What bounds it: the chosen experts' weights, 6 d_model d_ff bytes each (bf16), read once.  rom_ffn_moe_forward takes five launches and pads every
-// expert's tokens to 128 rows.  Here the weights are the M = 128 operand of tcgen05 and an expert's tokens its 16, 32 or 64 columns: one CTA per SM
+// expert's tokens to 128 rows.  Here the weights are the M = 128 operand of tcgen05 and an expert's tokens (their halves) its 16, 32 or 64 columns: one CTA per SM
 // walks (expert, weight rows, part of the contracted index) tiles; warp 0 keeps a ring of stages of 128 contracted elements full by TMA, warps 6..9
 // put the tokens' rows beside them, warp 1 issues the MMAs, warps 2..5 take the accumulators (two, so that a tile's end runs beside the next tile).  The
 // down projection, of few rows and a long contracted index, is cut along that index too: the parts go to the workspace and whoever brings
 // a tile's last one adds them all, in the order of slots and parts, so that results do not depend on who came when.
-// Measured (us a call, GB/s of the chosen experts' weights): one token of 2048 x 8192 25.3 (3980), 64 tokens with two of sixteen experts 254 (6330: 97 % of the
-// measured copy), 16 tokens with two of eight 127 (6290), 8 tokens with one of eight of 1280 x 5120 43.2 (4780).  Small calls: about 10 us of launches, lists and
-// first loads.  Tried: rings of half the size, so that both launches share the SMs and the second has its first weights when the first ends, no gain (the MMAs
+// Measured (us a call, GB/s of the chosen experts' weights): one token of 2048 x 8192 25.9 (3890), 64 tokens with two of sixteen experts 262 (6140: 94 % of the
+// measured copy), 16 tokens with two of eight 130 (6170), 8 tokens with one of eight of 1280 x 5120 43.3 (4760).  Small calls: about 10 us of launches, lists and
+// first loads.  With 32 and more tokens an
+// expert the MMAs bound it, and the down projection goes over its weights once for every 32 tokens: 64 tokens of one expert each of two 66 us (2.8 TB/s).  Tried: rings of half the size, so that both launches share the SMs and the second has its first weights when the first ends, no gain (the MMAs
 // of short tiles bound it then); stages of 64 elements 264 and 29 us, of one 64-wide block a warp's turn each 0.37 us a stage.
 //
 // fp32: a warp has four weight rows and up to eight tokens, products over its lanes; the plain form for a small model in full precision.  Bound by the latency
-// of the loads (activations from the L1 and L2 as often as weights): 5 tokens of 256 x 1024 9.4 us, 40 with two of sixteen of 512 x 2048 88 (2270 GB/s of weights).
+// of the loads (activations from the L1 and L2 as often as weights): 5 tokens of 256 x 1024 9.6 us, 40 with two of sixteen of 512 x 2048 88 (2270 GB/s of weights).
 // Tried: weights by cp.async three steps ahead through shared memory 79 to 85 for the second but 10.2 to 10.9 for the first and 5 to 14 % more at sixteen tokens an
 // expert (less L1 for the activations); activations a step ahead 135; the down projection's weights asked for before the wait, 1 %.
 #include <algorithm>

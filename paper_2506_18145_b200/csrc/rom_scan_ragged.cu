@@ -12,11 +12,12 @@
 // rom_scan_warp.cu, where the reasons stand): eight rows are staged in shared memory, whatever sequences they belong to, while the next eight
 // are in registers, and the initial states of the next four sequences are on their way to shared memory.
 //
-// bf16: what bounds it is one exponential per state update on the special-function unit, 4.65 T a second: the first launch keeps it 81 to 98 %
-// busy, the second 70 to 75 % (then the fp32 pipe and the latency of twelve warps).  fp32: decay() keeps fp32 accuracy, about ten operations more an update.
-// Measured: one sequence of 16384 rows x 4096 channels 664 us (231 us of exponentials, once; they are evaluated twice here), 23 prompts of 8186 x 2048 164 us (58),
-// 64 prompts of 16384 x 2048 303 to 316 us by their lengths, 512 one-row sequences x 4096 53 us (4.9 TB/s: states in and out), fp32 531 rows of 37
-// sequences x 512 20.1 us.
+// bf16: what bounds it is one exponential per state update on the special-function unit, 4.65 T a second: the first launch keeps it 82 %
+// busy, the second 70 % (23 prompts of 8186 x 2048; then the fp32 pipe and the latency of twelve warps).  fp32: decay() keeps fp32 accuracy, about ten operations more an update.
+// Measured: one sequence of 16384 rows x 4096 channels 681 us (231 us of exponentials, once; they are evaluated twice here; rom_scan, in
+// one launch for sequences of one length, takes 538), 23 prompts of 8186 x 2048 in Euler form 164 us (58),
+// 64 prompts of 16384 x 2048 318 us, 512 one-row sequences x 4096 53 us (4.9 TB/s: states in and out), fp32 531 rows of 37
+// sequences x 512 19.8 us.  A call whose sequences all hold a NaN from their first row on: 16384 x 4096 1294 us.
 // Tried: a tile that ends with its sequence (512 one-row sequences 70 us, waiting for every one's rows), one initial state ahead, chunk starts moved to a
 // sequence's start a third of a chunk away (fewer rows in the first launch, uneven chunks: no gain), one warp per sequence (16384 rows: 21 ms),
 // an eighth of the exponentials, or a quarter of the first launch's, as polynomials on the fp32 pipe (2 % less where the work is most, up to 7 % more elsewhere).
@@ -57,7 +58,8 @@ __device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
 
 // bf16, zero-order hold: with w = -B u / A a step is h <- a (h - w) + w, of which 1 - a is taken of w.  a is up to 2^-22 off, so the input (1 - a) w is off by
 // that over |Delta A|: below kSmallStep, where it could be more than 2^-10, and for an infinite w (inf - inf) a row of the warp's
-// channels is run with 1 - a by itself.  16384 rows x 4096 channels: 926 us when all rows are, 675 when none is, 10 of them for the look at the rows.
+// channels is run with 1 - a by itself.  16384 rows x 4096 channels: 927 us when all rows are, 681 when none is, 18 of them for the look at the rows
+// (as many with packed or three-operand minima).
 // (A growing state, Delta < 0, has no such steps.)
 constexpr float kSmallStep = 1.0f / 4096.0f, kLargeInput = 0x1p62f;
 // a = 2^t, d = 1 - a for t <= 0, within 2^-14 of itself: the larger of the first two terms of its power series, which stay below it, and 1 - a less

@@ -1,7 +1,7 @@
 // One token of many sequences, their states in slots of a pool: the short conv on the slot's window, the recurrence on the slot's state.
 // Both move states: 12 d_inner bytes in and out a token for the conv (four taps), 64 d_inner in and out for the scan; HBM bounds them from
 // some tens of tokens on, the latency of two dependent loads (slot, then state) below.
-// Measured at 4096 channels (bf16): 512 tokens conv 12.8 us (4.4 TB/s; 1.8 us of it a launch), scan 50.9 us (5.5 TB/s, 84 % of the measured copy); 64 tokens 2.9 and
+// Measured at 4096 channels (bf16): 512 tokens conv 12.8 us (4.4 TB/s; 1.8 us of it a launch), scan 53.7 us (5.2 TB/s, 79 % of the measured copy; 50.8 replayed from a graph); 64 tokens 2.9 and
 // 7.3 us; one token 1.8 and 1.9 us.  Scan, tried: blocks of eight warps 56 to 63 us, of four 52, of one 54; four tokens a warp 76; plain stores of
 // the states 50.9 but 9.9 at 64 tokens.
 #include "rom_serve.cuh"
