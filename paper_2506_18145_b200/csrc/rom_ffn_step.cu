@@ -556,14 +556,19 @@ ffn_step_tc(const __grid_constant__ CUtensorMap tmap_w, const FfnTc p, uint32_t 
             uint32_t r2[32];
             tmem_ld32_issue(taddr + 32, r2);
             tmem_ld_wait(r2);
+            // (the last step down adds the halves: an infinite weight makes the low one's sum infinite of either sign or NaN)
+            auto add = [&](uint32_t x, uint32_t y, bool halves) {
+              const float u = __uint_as_float(x), v = __uint_as_float(y);
+              return __float_as_uint(halves && isinf(u) ? u : u + v);
+            };
 #pragma unroll
-            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r2[j]));
+            for (int j = 0; j < 32; ++j) r[j] = add(r[j], r2[j], !UP && nc == 64);
             if (nc <= 16 * PT)
 #pragma unroll
-              for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r[16 + j]));
+              for (int j = 0; j < 16; ++j) r[j] = add(r[j], r[16 + j], !UP && nc == 32);
             if (!UP && nc == 16)
 #pragma unroll
-              for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(r[8 + j]));
+              for (int j = 0; j < 8; ++j) r[j] = add(r[j], r[8 + j], true);
           }
           if (UP) {
 #pragma unroll

@@ -208,3 +208,24 @@ def test_scan_ragged_state_of_zero_that_grows(dtype):
     want = (s["delta"][-1] * s["u"][-1].float())[:, None] * s["Bm"][-1][None]
     torch.testing.assert_close(h[int(p.slots[0])].cpu(), want, rtol=1e-6, atol=0.0)
     assert torch.all(y[:-1] == 0)
+
+
+@pytest.mark.parametrize("B", [1, 5, 13, 30, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ffn_step_infinite_weight(dtype, B):
+    """An infinite weight of the down projection makes its output infinite, of the sign of weight and hidden value, and no other output differs."""
+    Dm, F, d, f = 64, 256, 37, 201
+    x, W_gu, W_down = randn(261, (B, Dm), dtype=TORCH[dtype]), randn(262, (1, 2 * F, Dm), Dm ** -0.5, TORCH[dtype]), randn(263, (1, Dm, F), F ** -0.5, TORCH[dtype])
+    cfg = rb.make_config(B, 1, Dm, 64, 16, 4, 16, 1, 1, dtype)
+    idx, gates = torch.zeros((B, 1), dtype=torch.int32, device="cuda"), torch.ones((B, 1), device="cuda")
+    outs = []
+    for w in (0.0, -float("inf")):
+        W_down[0, d, f] = w
+        ws = torch.empty(rb.ffn_moe_step_workspace_size(cfg, F), dtype=torch.uint8, device="cuda")
+        outs.append(torch.empty((B, Dm), dtype=TORCH[dtype], device="cuda"))
+        rb.rom_ffn_moe_step(cfg, F, W_gu.cuda(), W_down.cuda(), x.cuda(), idx, gates, outs[-1], ws)
+    gu = np64(W_gu)[0] @ np64(x).T
+    h = (O.silu(gu[:F]) * gu[F:])[f]
+    assert torch.equal(outs[1][:, d].cpu().float(), torch.from_numpy(-np.sign(h) * np.inf).float())
+    others = torch.arange(Dm) != d
+    assert same_bits(outs[0][:, others], outs[1][:, others])
