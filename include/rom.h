@@ -390,6 +390,82 @@ ROM_API int rom_ffn_moe_step_workspace_size(const rom_config *cfg, int32_t d_ff,
 ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_gu, const void *W_down, const void *x,
                      const int32_t *topk_idx, const float *gates, void *out, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------------------
+ * Linear attention with a decay for each head: the linear recurrence of Section 3.1 with a matrix state per head instead of d_state numbers per
+ * channel (Section 5.2: other linear recurrent architectures).  Per value head h,
+ *   S_t = lambda_h S_{t-1} + k_t v_t^T   [d_k, d_v],     o_t = scale * q_t S_t,     lambda_h = exp(log_decay[h]).
+ * Value head h uses head h / (n_heads / n_qk_heads) of q and k.  Values wider than d_v = 128 are several heads that share q and k and their decay.
+ *   q, k : [rows, n_qk_heads, d_k] dtype, pitches ldq, ldk;   v : [rows, n_heads, d_v] dtype, pitch ldv;   o : [rows, n_heads, d_v] dtype, contiguous;
+ *   log_decay : [n_heads] fp32, finite and at most 0 (0: no decay; others are in bounds, their results unspecified);  a constant of the model: it has no gradient.
+ *   State pools: [n_slots, n_heads, d_k, d_v] fp32, slots as in the serving calls above (rom_ragged; in place, or two that do not overlap).
+ * Pitches: elements, at least the row's width and a multiple of 16 bytes.  log_decay needs the alignment of its elements, everything else 16 bytes.
+ * States and sums are fp32.  In bf16 the scores (after their decay) and the state that a chunk of rows meets are rounded to bf16 as operands of the matrix
+ * instructions; the keys that enter the state are the sum of two bf16 numbers (2^-16 of each).
+ * A value that is not finite shows in its own row and later ones of its sequence and head, in earlier rows never. */
+typedef struct {
+  int32_t n_heads;            /* value heads, 1..1024: one state and one decay each                            */
+  int32_t n_qk_heads;         /* heads of q and k, a divisor of n_heads                                        */
+  int32_t d_k, d_v;           /* multiples of 8, 8..128                                                        */
+  int32_t dtype;              /* rom_dtype                                                                     */
+  int32_t flags;              /* ROM_FLAG_SIMT_GEMM (bf16 on the plain fp32-FMA kernels), ROM_FLAG_TEST_STALL   */
+  float scale;                /* of the outputs, d_k^-1/2 as a rule; finite                                    */
+} rom_linattn_config;
+
+/* Packed sequences.  s_in (NULL: every sequence starts from zeros), s_out (NULL: not kept).  o is none of the inputs.
+ *   ws : rom_linattn_ragged_workspace_size(cfg, n_seq, rows) bytes (host out); scratch of this call alone: overlapping calls, captured graphs that may run at
+ *        the same time among them, need one each.  A buffer sized for some n_seq and rows does for all calls of no more of both.  rom_get_status(ws) tells
+ *        whether a device-side wait ran out.                                                                    */
+ROM_API int rom_linattn_ragged_workspace_size(const rom_linattn_config *cfg, int32_t n_seq, int32_t rows, size_t *bytes);
+ROM_API int rom_linattn_ragged(const rom_linattn_config *cfg, const rom_ragged *seqs, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v,
+                       int64_t ldv, const float *log_decay, const float *s_in, float *s_out, void *o, void *ws, size_t ws_bytes, void *stream);
+
+/* One token of B sequences: row b continues the sequence of slot[b] (NULL: slot b).  A row whose slot is outside [0, n_slots) is padding: its output and all
+ * slots are left as they are.  Both pools are required.                                                                 */
+ROM_API int rom_linattn_step(const rom_linattn_config *cfg, int32_t B, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                     const float *log_decay, const int32_t *slot, int32_t n_slots, const float *s_in, float *s_out, void *o, void *stream);
+
+/* Backward of rom_linattn_ragged on the same sequences and inputs: given dout = dLoss/do and ds_out = dLoss/d(s_out) (NULL: zeros),
+ *   dq_t = scale * S_t dout_t,   R_t = lambda R_{t+1} + scale * q_t dout_t^T  (+ ds_out at a sequence's last row),   dk_t = R_t v_t,   dv_t = R_t^T k_t,
+ * dq and dk summed over the value heads that share them, and ds_in = lambda R at a sequence's first row (of an empty one: ds_out), zeros for a sequence that
+ * started from zeros.  The states are recomputed, not kept by the forward.
+ *   dout : [rows, n_heads, d_v] contiguous;  dq, dk : [rows, n_qk_heads, d_k] contiguous;  dv : [rows, n_heads, d_v], pitch lddv;  all dtype, rows outside the
+ *   sequences are left as they are;  ds_in (NULL: not produced): [n_slots, n_heads, d_k, d_v] fp32, slots that no sequence names are left as they are; does not
+ *   overlap ds_out or s_in.  No output is an input.  Sums are taken in a fixed order: results are the same from run to run.
+ *   ws : rom_linattn_backward_workspace_size(cfg, n_seq, rows) bytes, as above.                                         */
+ROM_API int rom_linattn_backward_workspace_size(const rom_linattn_config *cfg, int32_t n_seq, int32_t rows, size_t *bytes);
+ROM_API int rom_linattn_backward(const rom_linattn_config *cfg, const rom_ragged *seqs, const void *dout, const void *q, int64_t ldq, const void *k, int64_t ldk,
+                         const void *v, int64_t ldv, const float *log_decay, const float *s_in, const float *ds_out, void *dq, void *dk, void *dv, int64_t lddv,
+                         float *ds_in, void *ws, size_t ws_bytes, void *stream);
+
+/* What prepares q and k of that recurrence: the RMS norm of every head and its rotation by the row's position, in one pass.
+ *   n = x * (mean_c x_c^2 + eps)^-1/2 * w;   for the pair i of the first rot_dim places, with the angle pos[row] * inv_freq[i],
+ *   (y_a, y_b) = (n_a cos - n_b sin, n_b cos + n_a sin),   (a, b) = (i, i + rot_dim/2), or (2i, 2i + 1) when interleaved;   the other places: y = n.
+ * Prompts, training batches and single tokens are all rows of one call.
+ *   q : [rows, n_q_heads, d_head] dtype, pitch ldq;  k : [rows, n_k_heads, d_head], pitch ldk;  q_out, k_out alike, with their own pitches; each output may be its
+ *   input (same address and pitch), otherwise no output overlaps an input;
+ *   w_q, w_k : [d_head] fp32, or NULL (ones);  pos : [rows] int32;  inv_freq : [rot_dim/2] fp32 (both NULL when rot_dim is 0).
+ * The angle is the exact product of the two, reduced before it is rounded: positions up to 2^31 keep fp32 accuracy.  Norm and rotation are fp32, rounded once.
+ * Pitches as above; w, pos and inv_freq need the alignment of their elements, everything else 16 bytes.                  */
+typedef struct {
+  int32_t n_q_heads, n_k_heads;   /* 1..1024                                                      */
+  int32_t d_head;                 /* a multiple of 8, 8..256                                      */
+  int32_t rot_dim;                /* places that are rotated: a multiple of 16, 0..d_head         */
+  int32_t interleaved;            /* 0 or 1                                                       */
+  int32_t dtype;                  /* rom_dtype                                                    */
+  float eps;                      /* positive and finite                                          */
+} rom_qk_config;
+ROM_API int rom_qk_norm_rope(const rom_qk_config *cfg, int32_t rows, const void *q, int64_t ldq, const void *k, int64_t ldk, const float *w_q, const float *w_k,
+                     const int32_t *pos, const float *inv_freq, void *q_out, int64_t ldq_out, void *k_out, int64_t ldk_out, void *stream);
+
+/* Its backward, from the inputs of the forward and the gradients dq_out, dk_out of its outputs (contiguous):
+ *   dn = the rotation back of dy;   dx = r (dn w - xhat mean_c(dn w xhat)),  r = (mean_c x_c^2 + eps)^-1/2, xhat = x r;   dw = sum over rows and heads of dn xhat.
+ *   dq, dk : like q and k, pitches lddq, lddk, none of the inputs;  dw_q, dw_k : [d_head] fp32, NULL exactly when w_q, w_k are.  Sums in a fixed order.
+ *   ws : rom_qk_norm_rope_backward_workspace_size(cfg, rows) bytes; one sized for more rows does for fewer.             */
+ROM_API int rom_qk_norm_rope_backward_workspace_size(const rom_qk_config *cfg, int32_t rows, size_t *bytes);
+ROM_API int rom_qk_norm_rope_backward(const rom_qk_config *cfg, int32_t rows, const void *dq_out, const void *dk_out, const void *q, int64_t ldq, const void *k,
+                              int64_t ldk, const float *w_q, const float *w_k, const int32_t *pos, const float *inv_freq, void *dq, int64_t lddq, void *dk,
+                              int64_t lddk, float *dw_q, float *dw_k, void *ws, size_t ws_bytes, void *stream);
+
 /* Profiling aid: the same launch sequence as rom_layer_forward with a CUDA event recorded on
  * `stream` between stages; synchronises the stream and writes the device time of each stage in
  * milliseconds to stage_ms (host out, at least rom_num_stages() floats).  Stage i is named

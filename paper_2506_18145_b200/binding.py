@@ -29,7 +29,9 @@ EXPORTS = ("rom_workspace_size", "rom_route", "rom_scan", "rom_layer_forward", "
            "rom_scan_workspace_size", "rom_debug_check", "rom_scan_backward_workspace_size", "rom_scan_backward",
            "rom_layer_backward_workspace_size", "rom_layer_backward", "rom_mamba2_workspace_size", "rom_mamba2_layer_forward",
            "rom_conv_ragged", "rom_scan_ragged_workspace_size", "rom_scan_ragged", "rom_conv_step", "rom_scan_step",
-           "rom_ffn_moe_step_workspace_size", "rom_ffn_moe_step")
+           "rom_ffn_moe_step_workspace_size", "rom_ffn_moe_step",
+           "rom_linattn_ragged_workspace_size", "rom_linattn_ragged", "rom_linattn_step", "rom_linattn_backward_workspace_size", "rom_linattn_backward",
+           "rom_qk_norm_rope", "rom_qk_norm_rope_backward_workspace_size", "rom_qk_norm_rope_backward")
 
 
 class RomConfig(ctypes.Structure):
@@ -55,6 +57,14 @@ class RomMamba2Weights(ctypes.Structure):
 
 class RomRagged(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "rows", "n_slots")] + [(n, ctypes.c_void_p) for n in ("seq_start", "slot", "resume")]
+
+
+class RomLinattnConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_qk_heads", "d_k", "d_v", "dtype", "flags")] + [("scale", ctypes.c_float)]
+
+
+class RomQkConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_k_heads", "d_head", "rot_dim", "interleaved", "dtype")] + [("eps", ctypes.c_float)]
 
 
 class RomError(RuntimeError):
@@ -109,6 +119,14 @@ def lib() -> ctypes.CDLL:
         L.rom_scan_step.argtypes = [cfgp, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, i32, vp, vp, vp, vp]
         L.rom_ffn_moe_step_workspace_size.argtypes = [cfgp, i32, szp]
         L.rom_ffn_moe_step.argtypes = [cfgp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        linp, qkp, size_t = ctypes.POINTER(RomLinattnConfig), ctypes.POINTER(RomQkConfig), ctypes.c_size_t
+        L.rom_linattn_ragged_workspace_size.argtypes = L.rom_linattn_backward_workspace_size.argtypes = [linp, i32, i32, szp]
+        L.rom_linattn_ragged.argtypes = [linp, ragp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, size_t, vp]
+        L.rom_linattn_step.argtypes = [linp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp, vp]
+        L.rom_linattn_backward.argtypes = [linp, ragp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, size_t, vp]
+        L.rom_qk_norm_rope.argtypes = [qkp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+        L.rom_qk_norm_rope_backward_workspace_size.argtypes = [qkp, i32, szp]
+        L.rom_qk_norm_rope_backward.argtypes = [qkp, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, size_t, vp]
         L.rom_num_stages.argtypes = []
         L.rom_stage_name.argtypes = [ctypes.c_int]
         L.rom_stage_name.restype = ctypes.c_char_p
@@ -463,6 +481,117 @@ def rom_ffn_moe_step(cfg, d_ff, W_gu, W_down, x, topk_idx, gates, out, ws, strea
                                 _at(gates, d, chosen, f32), _at(out, d, n, T), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
     if check and rc != ROM_OK:
         raise RomError(rc, "rom_ffn_moe_step")
+    return rc
+
+
+_DTYPES = {"f32": ROM_F32, "bf16": ROM_BF16, torch.float32: ROM_F32, torch.bfloat16: ROM_BF16}
+
+
+def make_linattn_config(n_heads, n_qk_heads, d_k, d_v, dtype, scale: Optional[float] = None, flags=0) -> RomLinattnConfig:
+    """scale: None = d_k ** -0.5."""
+    return RomLinattnConfig(n_heads, n_qk_heads, d_k, d_v, _DTYPES[dtype], flags, d_k ** -0.5 if scale is None else scale)
+
+
+def _linattn_size(name: str, cfg: RomLinattnConfig, n_seq: int, rows: int) -> int:
+    n = ctypes.c_size_t(0)
+    rc = getattr(lib(), name)(ctypes.byref(cfg), int(n_seq), int(rows), ctypes.byref(n))
+    if rc != ROM_OK:
+        raise RomError(rc, name)
+    return int(n.value)
+
+
+def linattn_ragged_workspace_size(cfg: RomLinattnConfig, n_seq: int, rows: int) -> int:
+    return _linattn_size("rom_linattn_ragged_workspace_size", cfg, n_seq, rows)
+
+
+def linattn_backward_workspace_size(cfg: RomLinattnConfig, n_seq: int, rows: int) -> int:
+    return _linattn_size("rom_linattn_backward_workspace_size", cfg, n_seq, rows)
+
+
+def rom_linattn_ragged(cfg, seqs: RomRagged, q, k, v, log_decay, s_in, s_out, o, ws, stream=None, check=True) -> int:
+    """q, k: [rows, n_qk_heads * d_k], v: [rows, n_heads * d_v], each may be a column slice of wider rows; o: [rows, n_heads * d_v], contiguous, none of them."""
+    d, rows, T, f32 = torch.cuda.current_device(), seqs.rows, _STORAGE.get(cfg.dtype), torch.float32
+    wqk, wv, pool = cfg.n_qk_heads * cfg.d_k, cfg.n_heads * cfg.d_v, seqs.n_slots * cfg.n_heads * cfg.d_k * cfg.d_v
+    (pq, ldq), (pk, ldk), (pv, ldv) = _rows_at(q, d, rows, wqk, T), _rows_at(k, d, rows, wqk, T), _rows_at(v, d, rows, wv, T)
+    rc = lib().rom_linattn_ragged(ctypes.byref(cfg), _sequences(seqs, d), pq, ldq, pk, ldk, pv, ldv, _at(log_decay, d, cfg.n_heads, f32), _at(s_in, d, pool, f32),
+                                  _at(s_out, d, pool, f32), _at(o, d, rows * wv, T), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_linattn_ragged")
+    return rc
+
+
+def rom_linattn_step(cfg, q, k, v, log_decay, slot, s_in, s_out, o, stream=None, check=True) -> int:
+    """One token of q.shape[0] sequences; slot: int32 [B] or None."""
+    if q is None or q.dim() != 2:
+        raise ValueError("expected q [B, n_qk_heads * d_k]")
+    d, B, T, f32, n_slots = torch.cuda.current_device(), q.shape[0], _STORAGE.get(cfg.dtype), torch.float32, _slots(s_in, s_out)
+    wqk, wv, pool = cfg.n_qk_heads * cfg.d_k, cfg.n_heads * cfg.d_v, n_slots * cfg.n_heads * cfg.d_k * cfg.d_v
+    (pq, ldq), (pk, ldk), (pv, ldv) = _rows_at(q, d, B, wqk, T), _rows_at(k, d, B, wqk, T), _rows_at(v, d, B, wv, T)
+    rc = lib().rom_linattn_step(ctypes.byref(cfg), B, pq, ldq, pk, ldk, pv, ldv, _at(log_decay, d, cfg.n_heads, f32), _at(slot, d, B, torch.int32), n_slots,
+                                _at(s_in, d, pool, f32), _at(s_out, d, pool, f32), _at(o, d, B * wv, T), _stream(stream, d))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_linattn_step")
+    return rc
+
+
+def rom_linattn_backward(cfg, seqs: RomRagged, dout, q, k, v, log_decay, s_in, ds_out, dq, dk, dv, ds_in, ws, stream=None, check=True) -> int:
+    """dout: [rows, n_heads * d_v], dq, dk: [rows, n_qk_heads * d_k], contiguous; dv: [rows, n_heads * d_v], may be a column slice of wider rows."""
+    d, rows, T, f32 = torch.cuda.current_device(), seqs.rows, _STORAGE.get(cfg.dtype), torch.float32
+    wqk, wv, pool = cfg.n_qk_heads * cfg.d_k, cfg.n_heads * cfg.d_v, seqs.n_slots * cfg.n_heads * cfg.d_k * cfg.d_v
+    (pq, ldq), (pk, ldk), (pv, ldv), (pdv, lddv) = _rows_at(q, d, rows, wqk, T), _rows_at(k, d, rows, wqk, T), _rows_at(v, d, rows, wv, T), _rows_at(dv, d, rows, wv, T)
+    rc = lib().rom_linattn_backward(ctypes.byref(cfg), _sequences(seqs, d), _at(dout, d, rows * wv, T), pq, ldq, pk, ldk, pv, ldv, _at(log_decay, d, cfg.n_heads, f32),
+                                    _at(s_in, d, pool, f32), _at(ds_out, d, pool, f32), _at(dq, d, rows * wqk, T), _at(dk, d, rows * wqk, T), pdv, lddv,
+                                    _at(ds_in, d, pool, f32), _at(ws, d), ws.numel() if ws is not None else 0, _stream(stream, d))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_linattn_backward")
+    return rc
+
+
+def make_qk_config(n_q_heads, n_k_heads, d_head, rot_dim, dtype, eps=1e-6, interleaved=False) -> RomQkConfig:
+    return RomQkConfig(n_q_heads, n_k_heads, d_head, rot_dim, int(interleaved), _DTYPES[dtype], eps)
+
+
+def _rotation(cfg, pos, inv_freq, d: int, rows: int):
+    n = rows if cfg.rot_dim else 0
+    return _at(pos, d, n, torch.int32), _at(inv_freq, d, cfg.rot_dim // 2, torch.float32)
+
+
+def rom_qk_norm_rope(cfg, q, k, w_q, w_k, pos, inv_freq, q_out, k_out, stream=None, check=True) -> int:
+    """q, q_out: [rows, n_q_heads * d_head]; k, k_out: [rows, n_k_heads * d_head]; each may be a column slice of wider rows, an output may be its input."""
+    if q is None or q.dim() != 2:
+        raise ValueError("expected q [rows, n_q_heads * d_head]")
+    d, rows, T, f32 = torch.cuda.current_device(), q.shape[0], _STORAGE.get(cfg.dtype), torch.float32
+    wq, wk = cfg.n_q_heads * cfg.d_head, cfg.n_k_heads * cfg.d_head
+    (pq, ldq), (pk, ldk), (pyq, ldyq), (pyk, ldyk) = _rows_at(q, d, rows, wq, T), _rows_at(k, d, rows, wk, T), _rows_at(q_out, d, rows, wq, T), _rows_at(k_out, d, rows, wk, T)
+    ppos, pfreq = _rotation(cfg, pos, inv_freq, d, rows)
+    rc = lib().rom_qk_norm_rope(ctypes.byref(cfg), rows, pq, ldq, pk, ldk, _at(w_q, d, cfg.d_head, f32), _at(w_k, d, cfg.d_head, f32), ppos, pfreq, pyq, ldyq, pyk, ldyk,
+                                _stream(stream, d))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_qk_norm_rope")
+    return rc
+
+
+def qk_norm_rope_backward_workspace_size(cfg: RomQkConfig, rows: int) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().rom_qk_norm_rope_backward_workspace_size(ctypes.byref(cfg), int(rows), ctypes.byref(n))
+    if rc != ROM_OK:
+        raise RomError(rc, "rom_qk_norm_rope_backward_workspace_size")
+    return int(n.value)
+
+
+def rom_qk_norm_rope_backward(cfg, dq_out, dk_out, q, k, w_q, w_k, pos, inv_freq, dq, dk, dw_q, dw_k, ws, stream=None, check=True) -> int:
+    """dq_out, dk_out: contiguous; q, k, dq, dk: as q and k of rom_qk_norm_rope; dw_q, dw_k: None exactly where w_q, w_k are."""
+    if q is None or q.dim() != 2:
+        raise ValueError("expected q [rows, n_q_heads * d_head]")
+    d, rows, T, f32 = torch.cuda.current_device(), q.shape[0], _STORAGE.get(cfg.dtype), torch.float32
+    wq, wk, w = cfg.n_q_heads * cfg.d_head, cfg.n_k_heads * cfg.d_head, cfg.d_head
+    (pq, ldq), (pk, ldk), (pyq, ldyq), (pyk, ldyk) = _rows_at(q, d, rows, wq, T), _rows_at(k, d, rows, wk, T), _rows_at(dq, d, rows, wq, T), _rows_at(dk, d, rows, wk, T)
+    ppos, pfreq = _rotation(cfg, pos, inv_freq, d, rows)
+    rc = lib().rom_qk_norm_rope_backward(ctypes.byref(cfg), rows, _at(dq_out, d, rows * wq, T), _at(dk_out, d, rows * wk, T), pq, ldq, pk, ldk, _at(w_q, d, w, f32),
+                                         _at(w_k, d, w, f32), ppos, pfreq, pyq, ldyq, pyk, ldyk, _at(dw_q, d, w, f32), _at(dw_k, d, w, f32), _at(ws, d),
+                                         ws.numel() if ws is not None else 0, _stream(stream, d))
+    if check and rc != ROM_OK:
+        raise RomError(rc, "rom_qk_norm_rope_backward")
     return rc
 
 

@@ -1,0 +1,560 @@
+// Linear attention with a decay per head: the calls, the plain fp32-FMA walk (fp32 storage; bf16 as a bisecting aid), the chain of segment states, the
+// sums over heads that share q and k, the single-token step.  (The bf16 walk on the tensor cores: rom_linattn_tc.cu.)
+//
+// Walk in chunks of C rows, i and j places in the chunk:
+//   out_i = inter lambda^{i+1} q_i S + sum_{j <= i} p lambda^{i-j} (q_i . k_j) v_j,    S <- lambda^C S + sum_j lambda^{C-1-j} ks k_j v_j^T.
+// Powers of lambda come from exp in 64 bits, lambda^C as two floats: a state that decays by 2^-11 a row meets the same factor every chunk, and its
+// rounding would add up.
+#include <math.h>
+
+#include "rom_linattn.cuh"
+
+namespace rom {
+namespace {
+
+constexpr int SIMT_THREADS = 256;
+constexpr int SIMT_C = 32;           // rows of a chunk
+constexpr int SIMT_DV = 64;          // columns of the state a block owns
+constexpr int SIMT_SPITCH = SIMT_DV + 4;
+
+__device__ __forceinline__ float2 ffma2(float a, float2 b, float2 c) { return __ffma2_rn(make_float2(a, a), b, c); }
+
+// One chunk's rows of one head into shared memory as fp32 (rows from `row0` on, or down from it), zeros beyond `len` and `width`.
+template <typename T>
+__device__ __forceinline__ void load_tile(float* dst, int pitch, const T* src, int64_t ld, int row0, int step, int len, int width, int fill_to) {
+  const int pieces = fill_to / 8;
+  for (int i = threadIdx.x; i < SIMT_C * pieces; i += SIMT_THREADS) {
+    const int r = i / pieces, c = (i - r * pieces) * 8;
+    float v[8];
+    if (r < len && c < width) {
+      Raw8<T> raw;
+      raw.load(src + (int64_t)(row0 + step * r) * ld + c);
+      raw.get(v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    }
+    *reinterpret_cast<float4*>(dst + r * pitch + c) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(dst + r * pitch + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// A block owns up to 64 columns of one head's state and walks one segment.  256 threads: 16 x 16, each 2 rows x 4 columns of the outputs and
+// 8 x 4 of the state.  What bounds it: shared-memory reads of the operands (10 wavefronts for 16 packed FMAs in q S).
+template <typename T, bool STATE>
+__global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged seqs, int seg_rows, int n_seg) {
+  extern __shared__ float sm[];
+  const int qp = p.dk + 4;
+  float* S = sm;                              // [dk][SIMT_SPITCH]
+  float* K = S + p.dk * SIMT_SPITCH;          // [C][qp]
+  float* V = K + SIMT_C * qp;                 // [C][SIMT_SPITCH]
+  float* Q = V + SIMT_C * SIMT_SPITCH;        // [C][qp]
+  float* P = Q + (STATE ? 0 : SIMT_C * qp);   // [C][C + 1]
+  __shared__ float lam[SIMT_C + 1], lam_lo[SIMT_C + 1];
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int seg = STATE && p.reverse ? (int)blockIdx.x + 1 : (int)blockIdx.x, head = blockIdx.y, c0 = blockIdx.z * SIMT_DV, wv = min(SIMT_DV, p.dv - c0);
+  if (tid <= SIMT_C) {
+    const double l = exp((double)__ldg(p.log_decay + head) * tid);
+    lam[tid] = (float)l;
+    lam_lo[tid] = (float)(l - (double)lam[tid]);
+  }
+  pdl_sync();
+  const size_t state = (size_t)p.dk * p.dv;
+  const T* q = static_cast<const T*>(p.q) + (size_t)(head / p.qdiv) * p.dk;
+  const T* k = static_cast<const T*>(p.k) + (size_t)(head / p.kdiv) * p.dk;
+  const T* v = static_cast<const T*>(p.v) + (size_t)(head / p.vdiv) * p.dv + c0;
+  const int a = seg * seg_rows, b = min(a + seg_rows, seqs.rows);
+  auto place = [&](int i, int& r, int& c) {      // i-th element of the block's columns, in the order of the memory's rows
+    if (p.transposed) { c = i / p.dk; r = i - c * p.dk; } else { r = i / wv; c = i - r * wv; }
+  };
+  auto at = [&](int r, int c) { return p.transposed ? (size_t)(c0 + c) * p.dk + r : (size_t)r * p.dv + c0 + c; };
+  auto load_state = [&](const float* from) {
+    __syncthreads();
+    for (int i = tid; i < p.dk * SIMT_SPITCH; i += SIMT_THREADS) S[i] = 0.0f;
+    __syncthreads();
+    if (from)
+      for (int i = tid; i < p.dk * wv; i += SIMT_THREADS) { int r, c; place(i, r, c); S[r * SIMT_SPITCH + c] = from[at(r, c)]; }
+  };
+  auto store_state = [&](float* to, float factor) {
+    __syncthreads();
+    for (int i = tid; i < p.dk * wv; i += SIMT_THREADS) { int r, c; place(i, r, c); to[at(r, c)] = factor * S[r * SIMT_SPITCH + c]; }
+  };
+  // rows [r0, r1) of one sequence; pool_init: the state they meet is a sequence's initial one
+  auto walk = [&](int r0, int r1, bool pool_init) {
+    int early = pool_init && p.early ? 1 : 0;
+    for (int done = 0, n = r1 - r0; done < n; done += SIMT_C) {
+      const int len = min(SIMT_C, n - done), row0 = p.reverse ? r1 - 1 - done : r0 + done, step = p.reverse ? -1 : 1;
+      __syncthreads();
+      load_tile(K, qp, k, p.ldk, row0, step, len, p.dk, p.dk);
+      load_tile(V, SIMT_SPITCH, v, p.ldv, row0, step, len, wv, SIMT_DV);
+      if (!STATE) load_tile(Q, qp, q, p.ldq, row0, step, len, p.dk, p.dk);
+      __syncthreads();
+      if constexpr (!STATE) {
+        float s[2][2] = {};
+        for (int d = 0; d < p.dk; d += 4) {
+          float4 qv[2], kv[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) { qv[i] = *reinterpret_cast<const float4*>(Q + (2 * ty + i) * qp + d); kv[i] = *reinterpret_cast<const float4*>(K + (tx + 16 * i) * qp + d); }
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s[i][j] = fmaf(qv[i].x, kv[j].x, fmaf(qv[i].y, kv[j].y, fmaf(qv[i].z, kv[j].z, fmaf(qv[i].w, kv[j].w, s[i][j]))));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int gap = 2 * ty + i - (tx + 16 * j);
+            P[(2 * ty + i) * (SIMT_C + 1) + tx + 16 * j] = gap >= 0 ? s[i][j] * (p.p_scale * lam[gap]) : 0.0f;
+          }
+        __syncthreads();
+        float2 o[2][2] = {};
+        for (int d = 0; d < p.dk; d += 4) {
+          float4 qv[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) qv[i] = *reinterpret_cast<const float4*>(Q + (2 * ty + i) * qp + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float4 sv = *reinterpret_cast<const float4*>(S + (d + e) * SIMT_SPITCH + 4 * tx);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float w = e == 0 ? qv[i].x : e == 1 ? qv[i].y : e == 2 ? qv[i].z : qv[i].w;
+              o[i][0] = ffma2(w, make_float2(sv.x, sv.y), o[i][0]);
+              o[i][1] = ffma2(w, make_float2(sv.z, sv.w), o[i][1]);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float f = p.inter_scale * lam[2 * ty + i + 1 - early];
+          o[i][0] = __fmul2_rn(o[i][0], make_float2(f, f));
+          o[i][1] = __fmul2_rn(o[i][1], make_float2(f, f));
+        }
+        for (int j = 0; j <= 2 * ty + 1; ++j) {      // (a row's own and earlier ones alone: a later value may be anything)
+          const float4 vv = *reinterpret_cast<const float4*>(V + j * SIMT_SPITCH + 4 * tx);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (j <= 2 * ty + i) {
+              const float w = P[(2 * ty + i) * (SIMT_C + 1) + j];
+              o[i][0] = ffma2(w, make_float2(vv.x, vv.y), o[i][0]);
+              o[i][1] = ffma2(w, make_float2(vv.z, vv.w), o[i][1]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (2 * ty + i < len && 4 * tx < wv) {
+            const size_t to = (size_t)(row0 + step * (2 * ty + i)) * p.ldo + (size_t)head * p.dv + c0 + 4 * tx;
+            const float r[4] = {o[i][0].x, o[i][0].y, o[i][1].x, o[i][1].y};
+            if (sizeof(T) == 4 || p.out_f32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = make_float4(r[0], r[1], r[2], r[3]);
+            else {
+              const __nv_bfloat162 lo = __floats2bfloat162_rn(r[0], r[1]), hi = __floats2bfloat162_rn(r[2], r[3]);
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + to) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            }
+          }
+        __syncthreads();
+      }
+      // state
+      if (8 * ty < p.dk) {
+        float2 s[8][2];
+        const float f = lam[len - early], fl = lam_lo[len - early];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float4 sv = *reinterpret_cast<const float4*>(S + (8 * ty + e) * SIMT_SPITCH + 4 * tx);
+          const float2 x = make_float2(sv.x, sv.y), y = make_float2(sv.z, sv.w);
+          s[e][0] = __ffma2_rn(x, make_float2(f, f), __fmul2_rn(x, make_float2(fl, fl)));
+          s[e][1] = __ffma2_rn(y, make_float2(f, f), __fmul2_rn(y, make_float2(fl, fl)));
+        }
+        for (int j = 0; j < len; ++j) {
+          const float w = p.k_scale * lam[len - 1 - j];
+          const float4 ka = *reinterpret_cast<const float4*>(K + j * qp + 8 * ty), kb = *reinterpret_cast<const float4*>(K + j * qp + 8 * ty + 4);
+          const float4 vv = *reinterpret_cast<const float4*>(V + j * SIMT_SPITCH + 4 * tx);
+          const float2 v0 = make_float2(w * vv.x, w * vv.y), v1 = make_float2(w * vv.z, w * vv.w);
+          const float kk[8] = {ka.x, ka.y, ka.z, ka.w, kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { s[e][0] = ffma2(kk[e], v0, s[e][0]); s[e][1] = ffma2(kk[e], v1, s[e][1]); }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) *reinterpret_cast<float4*>(S + (8 * ty + e) * SIMT_SPITCH + 4 * tx) = make_float4(s[e][0].x, s[e][0].y, s[e][1].x, s[e][1].y);
+      }
+      early = 0;
+    }
+  };
+
+  if constexpr (STATE) {
+    const int cut = p.reverse ? a : b, s = lin_spanning(seqs, cut);
+    if (s < 0) return;
+    load_state(nullptr);
+    if (p.reverse) walk(a, min(seqs.end_of(s), b), false);
+    else walk(max(seqs.start_of(s), a), b, false);
+    store_state(p.seg_state + ((size_t)(p.reverse ? seg - 1 : seg) * p.H + head) * state, 1.0f);
+  } else {
+    int s = seqs.first_from(a);
+    if (s > 0 && seqs.end_of(s - 1) > a) --s;
+    for (; s < seqs.n_seq; ++s) {
+      const int st = seqs.start_of(s), en = seqs.end_of(s), r0 = max(st, a), r1 = min(en, b);
+      if (st >= b && seg + 1 < n_seg) break;
+      const int slot = seqs.slot_of(s);
+      const bool empty = en <= st, over = !empty && (p.reverse ? en > b : st < a);      // its state comes over a cut
+      if (!empty && r0 >= r1) continue;
+      if (over) load_state(p.seg_state + ((size_t)(p.reverse ? seg : seg - 1) * p.H + head) * state);
+      else if (!empty && !p.reverse && p.init_copy && en > b && lin_init_of(p, seqs, s, head)) load_state(p.init_copy + ((size_t)seg * p.H + head) * state);
+      else load_state(lin_init_of(p, seqs, s, head));
+      if (!empty) walk(r0, r1, !over);
+      if (p.last && slot >= 0 && (empty || (p.reverse ? st >= a : en <= b)))
+        store_state(p.last + ((size_t)slot * p.H + head) * state, p.init_all && !seqs.resumes(s) ? 0.0f : !empty && p.early ? lam[1] : 1.0f);
+    }
+  }
+}
+
+size_t simt_smem(int dk, bool state) { return sizeof(float) * (size_t)(dk * SIMT_SPITCH + SIMT_C * ((state ? 1 : 2) * (dk + 4) + SIMT_SPITCH) + (state ? 0 : SIMT_C * (SIMT_C + 1))); }
+
+template <typename T, bool STATE>
+cudaError_t launch_simt(const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
+  const size_t smem = simt_smem(p.dk, STATE);
+  auto kern = lin_walk_simt<T, STATE>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)simt_smem(kLinMaxDim, STATE));
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return launch_k(kern, dim3(STATE ? cut.n_seg - 1 : cut.n_seg, p.H, (p.dv + SIMT_DV - 1) / SIMT_DV), SIMT_THREADS, smem, st, p, device_view(seqs), cut.seg_rows, cut.n_seg);
+}
+
+// Launch 2: the states that reach every cut, element by element.  A thread owns four adjacent elements of one head.
+constexpr int CHAIN_THREADS = 128;
+__global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seqs, int seg_rows, int n_seg) {
+  __shared__ int how[kLinMaxSegs];              // at the cut before segment b: -2 nobody reaches over it; -1 the state comes over a cut; else a sequence starts here
+  __shared__ float weight[kLinMaxSegs];         // its initial state decayed up to the cut
+  const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const double g = (double)__ldg(p.log_decay + head);
+  pdl_sync();
+  for (int b = 1 + warp; b < n_seg; b += CHAIN_THREADS / 32) {
+    const int r = b * seg_rows, s = lin_spanning(seqs, r);
+    if (lane == 0) {
+      int h = -2;
+      float w = 0.0f;
+      if (s >= 0) {
+        const int away = p.reverse ? seqs.end_of(s) - r : r - seqs.start_of(s);
+        h = away > (p.reverse ? min(seqs.rows - r, seg_rows) : seg_rows) ? -1 : s;
+        w = (float)exp(g * (h < 0 ? seg_rows : away - (p.early ? 1 : 0)));
+      }
+      how[b] = h;
+      weight[b] = w;
+    }
+  }
+  __syncthreads();
+  const size_t state = (size_t)p.dk * p.dv, e = ((size_t)blockIdx.x * CHAIN_THREADS + threadIdx.x) * 4;
+  if (e >= state) return;
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i = 1; i < n_seg; ++i) {
+    const int b = p.reverse ? n_seg - i : i, h = how[b];
+    if (h == -2) continue;
+    float4* here = reinterpret_cast<float4*>(p.seg_state + ((size_t)(b - 1) * p.H + head) * state + e);
+    const float4 add = *here;
+    const float w = weight[b];
+    bool from = true;
+    if (h >= 0) {
+      const float* init = lin_init_of(p, seqs, h, head);
+      from = init != nullptr;
+      if (from) {
+        x = *reinterpret_cast<const float4*>(init + e);
+        if (p.init_copy) *reinterpret_cast<float4*>(p.init_copy + ((size_t)(b - 1) * p.H + head) * state + e) = x;
+      }
+    }
+    x = from ? make_float4(fmaf(w, x.x, add.x), fmaf(w, x.y, add.y), fmaf(w, x.z, add.z), fmaf(w, x.w, add.w)) : add;
+    *here = x;
+  }
+}
+
+// dst[row, g, :] = sum over the value heads of group g of part[row, h, :], rows that belong to a sequence.
+template <typename T>
+__global__ void __launch_bounds__(256) lin_sum_heads(const float* part, T* dst, Ragged seqs, int H, int G, int d) {
+  pdl_sync();
+  const int first = seqs.start_of(0), end = seqs.end_of(seqs.n_seq - 1), share = H / G;
+  const size_t per_row = (size_t)G * d / 4, n = (size_t)seqs.rows * per_row;
+  for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (size_t)gridDim.x * blockDim.x) {
+    const int row = (int)(i / per_row);
+    if (row < first || row >= end) continue;
+    const int c = (int)(i - (size_t)row * per_row) * 4, g = c / d;
+    const float* from = part + ((size_t)row * H + (size_t)g * share) * d + (c - g * d);
+    float4 s = *reinterpret_cast<const float4*>(from);
+    for (int h = 1; h < share; ++h) {
+      const float4 a = *reinterpret_cast<const float4*>(from + (size_t)h * d);
+      s = make_float4(s.x + a.x, s.y + a.y, s.z + a.z, s.w + a.w);
+    }
+    T* to = dst + (size_t)row * G * d + c;
+    to[0] = from_f32<T>(s.x); to[1] = from_f32<T>(s.y); to[2] = from_f32<T>(s.z); to[3] = from_f32<T>(s.w);
+  }
+}
+
+// ---------------------------------------------------------------- one token
+// A block updates 32 columns of one token's and head's state: 4 warps x 4 rows x 8 column quads, every load of the state in flight at once.
+// S e^g is S + S (e^g - 1) for slow decays: a factor rounded to fp32 would be off by the same 2^-25 in every one of thousands of steps.
+constexpr int STEP_THREADS = 128, STEP_COLS = 32;
+template <typename T>
+__global__ void __launch_bounds__(STEP_THREADS) lin_step(const T* q, const T* k, const T* v, long long ldq, long long ldk, long long ldv, const float* log_decay,
+                                                         const int32_t* slot, int n_slots, const float* s_in, float* s_out, T* o, int H, int share, int dk, int dv,
+                                                         int slices, float scale) {
+  __shared__ float part[STEP_THREADS / 32][STEP_COLS];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int slice = blockIdx.x % slices, bh = blockIdx.x / slices, head = bh % H, b = bh / H;
+  const int c = slice * STEP_COLS + (lane & 7) * 4, r0 = warp * 4 + (lane >> 3);
+  pdl_sync();
+  const int sl = slot ? __ldg(slot + b) : b;
+  if (sl < 0 || sl >= n_slots) return;
+  const size_t base = ((size_t)sl * H + head) * ((size_t)dk * dv);
+  const bool mine = c < dv;
+  float4 S[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 16 * i;
+    if (mine && r < dk) S[i] = *reinterpret_cast<const float4*>(s_in + base + (size_t)r * dv + c);
+  }
+  const T* qr = q + (size_t)b * ldq + (size_t)(head / share) * dk;
+  const T* kr = k + (size_t)b * ldk + (size_t)(head / share) * dk;
+  const T* vr = v + (size_t)b * ldv + (size_t)head * dv;
+  float vv[4] = {};
+  if (mine) { vv[0] = to_f32(vr[c]); vv[1] = to_f32(vr[c + 1]); vv[2] = to_f32(vr[c + 2]); vv[3] = to_f32(vr[c + 3]); }
+  const float g = __ldg(log_decay + head), lam = expf(g), em1 = expm1f(g);
+  const bool slow = g > -0.5f;
+  const float f = slow ? em1 : lam;
+  float acc[4] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 16 * i;
+    if (mine && r < dk) {
+      const float kk = to_f32(kr[r]), qq = to_f32(qr[r]);
+      float s[4] = {S[i].x, S[i].y, S[i].z, S[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] = fmaf(kk, vv[e], slow ? fmaf(s[e], f, s[e]) : s[e] * f);
+        acc[e] = fmaf(qq, s[e], acc[e]);
+      }
+      __stcs(reinterpret_cast<float4*>(s_out + base + (size_t)r * dv + c), make_float4(s[0], s[1], s[2], s[3]));
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 8);
+    acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 16);
+  }
+  if (lane < 8)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[warp][lane * 4 + e] = acc[e];
+  __syncthreads();
+  const int col = slice * STEP_COLS + tid;
+  if (tid < STEP_COLS && col < dv) o[((size_t)b * H + head) * dv + col] = from_f32<T>(scale * (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]));
+}
+
+// ---------------------------------------------------------------- host
+int check_lin(const rom_linattn_config* c) {
+  if (!c || c->n_heads < 1 || c->n_qk_heads < 1 || c->d_k < 1 || c->d_v < 1 || c->n_heads % c->n_qk_heads != 0) return ROM_ERR_INVALID_ARG;
+  if (c->dtype != ROM_F32 && c->dtype != ROM_BF16) return ROM_ERR_INVALID_ARG;
+  if ((c->flags & ~(ROM_FLAG_SIMT_GEMM | ROM_FLAG_TEST_STALL)) != 0 || !isfinite(c->scale)) return ROM_ERR_INVALID_ARG;
+  if (c->d_k % 8 != 0 || c->d_v % 8 != 0 || c->d_k > kLinMaxDim || c->d_v > kLinMaxDim || c->n_heads > 1024) return ROM_ERR_UNSUPPORTED;
+  return ROM_OK;
+}
+bool on_tensor_cores(const rom_linattn_config&) { return false; }
+
+// Segments of the packed rows: enough that the walks of all heads fill the SMs, none shorter than `least` rows.
+int max_segments(const rom_linattn_config& c, int rows) {
+  const bool tc = on_tensor_cores(c);
+  const int per = c.n_heads * (tc ? 1 : (c.d_v + SIMT_DV - 1) / SIMT_DV), blocks = tc ? 148 : 296, least = tc ? 256 : 64;
+  const int want = (blocks + per - 1) / per, most = rows / least;
+  return want < most ? want : most < 1 ? 1 : most;
+}
+LinCut cut_rows(const rom_linattn_config& c, int rows) {
+  const int n = max_segments(c, rows), unit = on_tensor_cores(c) ? 128 : SIMT_C;
+  const int seg_rows = (int)align_up((size_t)(rows + n - 1) / n, unit);
+  return LinCut{seg_rows, (rows + seg_rows - 1) / seg_rows};
+}
+struct LinWs { size_t status, seg_a, seg_b, part, total; };
+LinWs lin_ws(const rom_linattn_config& c, int rows, bool backward) {
+  LinWs l{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
+  const int n = max_segments(c, rows);
+  const size_t state = n > 1 ? (size_t)n * c.n_heads * c.d_k * c.d_v * sizeof(float) : 0;
+  l.status = take(sizeof(int32_t) * kStatusInts);
+  l.seg_a = take(state);
+  l.seg_b = take(state);
+  l.part = take(backward && c.n_qk_heads < c.n_heads ? (size_t)rows * c.n_heads * c.d_k * sizeof(float) : 0);
+  l.total = off;
+  return l;
+}
+int lin_ws_size(const rom_linattn_config* c, int32_t n_seq, int32_t rows, size_t* bytes, bool backward) {
+  const int rc = check_lin(c);
+  if (rc != ROM_OK) return rc;
+  if (!bytes || n_seq < 0 || rows < 0) return ROM_ERR_INVALID_ARG;
+  if (n_seq > kMaxRaggedSeqs || rows >= 1 << 30) return ROM_ERR_UNSUPPORTED;
+  *bytes = lin_ws(*c, rows, backward).total;
+  return ROM_OK;
+}
+
+template <bool STATE>
+cudaError_t launch_walk(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
+  if (c.dtype == ROM_F32) return launch_simt<float, STATE>(p, seqs, cut, st);
+  return launch_simt<__nv_bfloat16, STATE>(p, seqs, cut, st);
+}
+// Launches 1 and 2: the states at the cuts.
+cudaError_t launch_states(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
+  if (cut.n_seg < 2) return cudaSuccess;
+  const cudaError_t e = launch_walk<true>(c, p, seqs, cut, st);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return launch_k(lin_chain, dim3((p.dk * p.dv / 4 + CHAIN_THREADS - 1) / CHAIN_THREADS, p.H), CHAIN_THREADS, 0, st, p, device_view(seqs), cut.seg_rows, cut.n_seg);
+}
+cudaError_t launch_sum(const rom_linattn_config& c, const float* part, void* dst, const rom_ragged& seqs, cudaStream_t st) {
+  int sms = 0;
+  const cudaError_t e = current_device_sm_count(&sms);
+  if (e != cudaSuccess) return e;
+  const size_t n = (size_t)seqs.rows * c.n_qk_heads * c.d_k / 4, blocks = (n + 255) / 256;
+  const dim3 grid((unsigned)(blocks < (size_t)sms * 8 ? blocks : (size_t)sms * 8));
+  count_launch();
+  if (c.dtype == ROM_F32) return launch_k(lin_sum_heads<float>, grid, 256, 0, st, part, (float*)dst, device_view(seqs), c.n_heads, c.n_qk_heads, c.d_k);
+  return launch_k(lin_sum_heads<__nv_bfloat16>, grid, 256, 0, st, part, (__nv_bfloat16*)dst, device_view(seqs), c.n_heads, c.n_qk_heads, c.d_k);
+}
+
+bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + nb && y < x + na;
+}
+
+}  // namespace
+}  // namespace rom
+
+using namespace rom;
+
+extern "C" {
+
+int rom_linattn_ragged_workspace_size(const rom_linattn_config* cfg, int32_t n_seq, int32_t rows, size_t* bytes) { return lin_ws_size(cfg, n_seq, rows, bytes, false); }
+int rom_linattn_backward_workspace_size(const rom_linattn_config* cfg, int32_t n_seq, int32_t rows, size_t* bytes) { return lin_ws_size(cfg, n_seq, rows, bytes, true); }
+
+int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                       const float* log_decay, const float* s_in, float* s_out, void* o, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_lin(cfg);
+  if (rc != ROM_OK || (rc = check_ragged(seqs)) != ROM_OK) return rc;
+  if (seqs->n_seq == 0) return ROM_OK;
+  const rom_linattn_config& c = *cfg;
+  const size_t esz = c.dtype == ROM_BF16 ? 2 : 4, pool = (size_t)seqs->n_slots * c.n_heads * c.d_k * c.d_v;
+  if (!q || !k || !v || !log_decay || !o || !ws || !aligned4(log_decay)) return ROM_ERR_INVALID_ARG;
+  const void* ptrs[] = {q, k, v, o, ws};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
+  if (!pitch_ok(ldq, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldk, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldv, c.n_heads * c.d_v, esz)) return ROM_ERR_INVALID_ARG;
+  if (o == q || o == k || o == v || !pools_ok(s_in, s_out, pool)) return ROM_ERR_INVALID_ARG;
+  const LinWs lay = lin_ws(c, seqs->rows, false);
+  if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
+  if ((rc = check_device()) != ROM_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  LaunchCounter::count = 0;
+  char* W = static_cast<char*>(ws);
+  const LinCut cut = cut_rows(c, seqs->rows > 0 ? seqs->rows : 1);
+  LinPass p{};
+  p.q = q; p.k = k; p.v = v; p.ldq = ldq; p.ldk = ldk; p.ldv = ldv;
+  p.qdiv = p.kdiv = c.n_heads / c.n_qk_heads; p.vdiv = 1;
+  p.H = c.n_heads; p.dk = c.d_k; p.dv = c.d_v; p.log_decay = log_decay;
+  p.p_scale = p.inter_scale = c.scale; p.k_scale = 1.0f;
+  p.init = s_in; p.last = s_out;
+  p.seg_state = reinterpret_cast<float*>(W + lay.seg_a);
+  p.init_copy = s_in && s_in == s_out ? reinterpret_cast<float*>(W + lay.seg_b) : nullptr;
+  p.out = o; p.ldo = (int64_t)c.n_heads * c.d_v;
+  p.status = reinterpret_cast<int32_t*>(W + lay.status);
+  if (launch_init_status(p.status, st) != cudaSuccess) return ROM_ERR_CUDA;
+  if (launch_states(c, p, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  return launch_walk<false>(c, p, *seqs, cut, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
+}
+
+int rom_linattn_step(const rom_linattn_config* cfg, int32_t B, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const float* log_decay,
+                     const int32_t* slot, int32_t n_slots, const float* s_in, float* s_out, void* o, void* stream) {
+  int rc = check_lin(cfg);
+  if (rc != ROM_OK) return rc;
+  const rom_linattn_config& c = *cfg;
+  const size_t esz = c.dtype == ROM_BF16 ? 2 : 4;
+  if (B < 0 || n_slots < 0 || (c.flags & ROM_FLAG_TEST_STALL)) return ROM_ERR_INVALID_ARG;
+  if (B == 0) return ROM_OK;
+  if (!q || !k || !v || !log_decay || !s_in || !s_out || !o) return ROM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned4(log_decay) || !aligned4(slot)) return ROM_ERR_INVALID_ARG;
+  if (!pitch_ok(ldq, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldk, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldv, c.n_heads * c.d_v, esz)) return ROM_ERR_INVALID_ARG;
+  if (o == q || o == k || o == v || !pools_ok(s_in, s_out, (size_t)n_slots * c.n_heads * c.d_k * c.d_v)) return ROM_ERR_INVALID_ARG;
+  const int slices = (c.d_v + STEP_COLS - 1) / STEP_COLS;
+  const long long blocks = (long long)B * c.n_heads * slices;
+  if (blocks > INT32_MAX) return ROM_ERR_UNSUPPORTED;
+  if ((rc = check_device()) != ROM_OK) return rc;
+  LaunchCounter::count = 0;
+  count_launch();
+  const dim3 grid((unsigned)blocks);
+  const int share = c.n_heads / c.n_qk_heads;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto go = [&](auto zero) {
+    using T = decltype(zero);
+    return launch_k(lin_step<T>, grid, STEP_THREADS, 0, st, (const T*)q, (const T*)k, (const T*)v, (long long)ldq, (long long)ldk, (long long)ldv, log_decay, slot, n_slots,
+                    s_in, s_out, (T*)o, c.n_heads, share, c.d_k, c.d_v, slices, c.scale);
+  };
+  return (c.dtype == ROM_BF16 ? go(__nv_bfloat16()) : go(0.0f)) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
+}
+
+int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, const void* dout, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                         int64_t ldv, const float* log_decay, const float* s_in, const float* ds_out, void* dq, void* dk, void* dv, int64_t lddv, float* ds_in, void* ws,
+                         size_t ws_bytes, void* stream) {
+  int rc = check_lin(cfg);
+  if (rc != ROM_OK || (rc = check_ragged(seqs)) != ROM_OK) return rc;
+  if (seqs->n_seq == 0) return ROM_OK;
+  const rom_linattn_config& c = *cfg;
+  const size_t esz = c.dtype == ROM_BF16 ? 2 : 4, pool = (size_t)seqs->n_slots * c.n_heads * c.d_k * c.d_v * sizeof(float);
+  if (!dout || !q || !k || !v || !log_decay || !dq || !dk || !dv || !ws || !aligned4(log_decay)) return ROM_ERR_INVALID_ARG;
+  const void* ptrs[] = {dout, q, k, v, s_in, ds_out, dq, dk, dv, ds_in, ws};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
+  if (!pitch_ok(ldq, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldk, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldv, c.n_heads * c.d_v, esz) || !pitch_ok(lddv, c.n_heads * c.d_v, esz))
+    return ROM_ERR_INVALID_ARG;
+  const void *ins[] = {dout, q, k, v}, *outs[] = {dq, dk, dv};
+  for (int i = 0; i < 3; ++i) {
+    for (const void* a : ins)
+      if (a == outs[i]) return ROM_ERR_INVALID_ARG;
+    if (outs[i] == outs[(i + 1) % 3]) return ROM_ERR_INVALID_ARG;
+  }
+  if (overlaps(ds_in, pool, ds_out, pool) || overlaps(ds_in, pool, s_in, pool)) return ROM_ERR_INVALID_ARG;
+  const LinWs lay = lin_ws(c, seqs->rows, true);
+  if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
+  if ((rc = check_device()) != ROM_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  LaunchCounter::count = 0;
+  char* W = static_cast<char*>(ws);
+  const LinCut cut = cut_rows(c, seqs->rows > 0 ? seqs->rows : 1);
+  const int share = c.n_heads / c.n_qk_heads;
+  float* part = share > 1 ? reinterpret_cast<float*>(W + lay.part) : nullptr;
+  LinPass base{};
+  base.H = c.n_heads; base.log_decay = log_decay; base.p_scale = c.scale;
+  base.status = reinterpret_cast<int32_t*>(W + lay.status);
+  if (launch_init_status(base.status, st) != cudaSuccess) return ROM_ERR_CUDA;
+  // the states S of the forward at the cuts
+  LinPass s = base;
+  s.k = k; s.v = v; s.ldk = ldk; s.ldv = ldv; s.q = k; s.ldq = ldk;
+  s.qdiv = s.kdiv = share; s.vdiv = 1; s.dk = c.d_k; s.dv = c.d_v;
+  s.k_scale = 1.0f; s.init = s_in; s.seg_state = reinterpret_cast<float*>(W + lay.seg_a);
+  if (launch_states(c, s, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  // dq
+  LinPass w = base;
+  w.q = dout; w.k = v; w.v = k; w.ldq = (int64_t)c.n_heads * c.d_v; w.ldk = ldv; w.ldv = ldk;
+  w.qdiv = w.kdiv = 1; w.vdiv = share; w.dk = c.d_v; w.dv = c.d_k;
+  w.inter_scale = c.scale; w.k_scale = 1.0f; w.transposed = true; w.init = s_in; w.seg_state = s.seg_state;
+  w.out = part ? part : dq; w.ldo = (int64_t)c.n_heads * c.d_k; w.out_f32 = part != nullptr;
+  if (launch_walk<false>(c, w, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  if (part && launch_sum(c, part, dq, *seqs, st) != cudaSuccess) return ROM_ERR_CUDA;
+  // the states R behind the cuts, and dv from them
+  LinPass r = base;
+  r.q = k; r.k = q; r.v = dout; r.ldq = ldk; r.ldk = ldq; r.ldv = (int64_t)c.n_heads * c.d_v;
+  r.qdiv = r.kdiv = share; r.vdiv = 1; r.dk = c.d_k; r.dv = c.d_v;
+  r.inter_scale = 1.0f; r.k_scale = c.scale; r.reverse = true; r.init = ds_out; r.init_all = true; r.early = true; r.last = ds_in;
+  r.seg_state = reinterpret_cast<float*>(W + lay.seg_b);
+  r.out = dv; r.ldo = lddv;
+  if (launch_states(c, r, *seqs, cut, st) != cudaSuccess || launch_walk<false>(c, r, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  // dk
+  LinPass d = r;
+  d.q = v; d.k = dout; d.v = q; d.ldq = ldv; d.ldk = r.ldv; d.ldv = ldq;
+  d.qdiv = d.kdiv = 1; d.vdiv = share; d.dk = c.d_v; d.dv = c.d_k; d.transposed = true; d.last = nullptr;
+  d.out = part ? part : dk; d.ldo = (int64_t)c.n_heads * c.d_k; d.out_f32 = part != nullptr;
+  if (launch_walk<false>(c, d, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  return !part || launch_sum(c, part, dk, *seqs, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
+}
+
+}  // extern "C"
