@@ -352,26 +352,34 @@ int check_lin(const rom_linattn_config* c) {
   if (c->d_k % 8 != 0 || c->d_v % 8 != 0 || c->d_k > kLinMaxDim || c->d_v > kLinMaxDim || c->n_heads > 1024) return ROM_ERR_UNSUPPORTED;
   return ROM_OK;
 }
-bool on_tensor_cores(const rom_linattn_config&) { return false; }
+bool on_tensor_cores(const rom_linattn_config& c) { return c.dtype == ROM_BF16 && !(c.flags & ROM_FLAG_SIMT_GEMM); }
 
-// Segments of the packed rows: enough that the walks of all heads fill the SMs, none shorter than `least` rows.
-int max_segments(const rom_linattn_config& c, int rows) {
+// Segments of the packed rows.  A segment of a head is one block of launch 3 (on the tensor cores one to an SM), and rows in a segment are walked in turn: the
+// count with the fewest chunks one after the other, each wave of blocks counted with two chunks more for its start.  A function of the sizes only (148 SMs assumed).
+int most_segments(const rom_linattn_config& c, int rows) {
   const bool tc = on_tensor_cores(c);
-  const int per = c.n_heads * (tc ? 1 : (c.d_v + SIMT_DV - 1) / SIMT_DV), blocks = tc ? 148 : 296, least = tc ? 256 : 64;
-  const int want = (blocks + per - 1) / per, most = rows / least;
-  return want < most ? want : most < 1 ? 1 : most;
+  const int per = c.n_heads * (tc ? 1 : (c.d_v + SIMT_DV - 1) / SIMT_DV), slots = tc ? 148 : 296, least = tc ? 256 : 64;
+  const int want = (2 * slots + per - 1) / per, most = rows / least, n = want < most ? want : most;
+  return n < 1 ? 1 : n < kLinMaxSegs ? n : kLinMaxSegs;
 }
 LinCut cut_rows(const rom_linattn_config& c, int rows) {
-  const int n = max_segments(c, rows), unit = on_tensor_cores(c) ? 128 : SIMT_C;
-  const int seg_rows = (int)align_up((size_t)(rows + n - 1) / n, unit);
-  return LinCut{seg_rows, (rows + seg_rows - 1) / seg_rows};
+  const bool tc = on_tensor_cores(c);
+  const int per = c.n_heads * (tc ? 1 : (c.d_v + SIMT_DV - 1) / SIMT_DV), slots = tc ? 148 : 296, unit = tc ? 128 : SIMT_C;
+  LinCut best{0, 0};
+  long long least = 0;
+  for (int n = 1, most = most_segments(c, rows); n <= most; ++n) {
+    const int seg_rows = (int)align_up((size_t)(rows + n - 1) / n, unit), segs = (rows + seg_rows - 1) / seg_rows;
+    const long long waves = ((long long)per * segs + slots - 1) / slots, time = waves * (seg_rows / unit + 2);
+    if (best.n_seg == 0 || time < least) { best = LinCut{seg_rows, segs}; least = time; }
+  }
+  return best;
 }
 struct LinWs { size_t status, seg_a, seg_b, part, total; };
 LinWs lin_ws(const rom_linattn_config& c, int rows, bool backward) {
   LinWs l{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
-  const int n = max_segments(c, rows);
+  const int n = most_segments(c, rows);
   const size_t state = n > 1 ? (size_t)n * c.n_heads * c.d_k * c.d_v * sizeof(float) : 0;
   l.status = take(sizeof(int32_t) * kStatusInts);
   l.seg_a = take(state);
@@ -391,6 +399,7 @@ int lin_ws_size(const rom_linattn_config* c, int32_t n_seq, int32_t rows, size_t
 
 template <bool STATE>
 cudaError_t launch_walk(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
+  if (on_tensor_cores(c) && seqs.rows > 0) return launch_lin_tc(p, seqs, cut, STATE, (c.flags & ROM_FLAG_TEST_STALL) != 0, st);
   if (c.dtype == ROM_F32) return launch_simt<float, STATE>(p, seqs, cut, st);
   return launch_simt<__nv_bfloat16, STATE>(p, seqs, cut, st);
 }
@@ -435,12 +444,12 @@ int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, co
   if (seqs->n_seq == 0) return ROM_OK;
   const rom_linattn_config& c = *cfg;
   const size_t esz = c.dtype == ROM_BF16 ? 2 : 4, pool = (size_t)seqs->n_slots * c.n_heads * c.d_k * c.d_v;
-  if (!q || !k || !v || !log_decay || !o || !ws || !aligned4(log_decay)) return ROM_ERR_INVALID_ARG;
+  if (!log_decay || !ws || (seqs->rows > 0 && (!q || !k || !v || !o)) || !aligned4(log_decay)) return ROM_ERR_INVALID_ARG;
   const void* ptrs[] = {q, k, v, o, ws};
   for (const void* p : ptrs)
     if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
   if (!pitch_ok(ldq, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldk, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldv, c.n_heads * c.d_v, esz)) return ROM_ERR_INVALID_ARG;
-  if (o == q || o == k || o == v || !pools_ok(s_in, s_out, pool)) return ROM_ERR_INVALID_ARG;
+  if ((o && (o == q || o == k || o == v)) || !pools_ok(s_in, s_out, pool)) return ROM_ERR_INVALID_ARG;
   const LinWs lay = lin_ws(c, seqs->rows, false);
   if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
   if ((rc = check_device()) != ROM_OK) return rc;
@@ -500,7 +509,7 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   if (seqs->n_seq == 0) return ROM_OK;
   const rom_linattn_config& c = *cfg;
   const size_t esz = c.dtype == ROM_BF16 ? 2 : 4, pool = (size_t)seqs->n_slots * c.n_heads * c.d_k * c.d_v * sizeof(float);
-  if (!dout || !q || !k || !v || !log_decay || !dq || !dk || !dv || !ws || !aligned4(log_decay)) return ROM_ERR_INVALID_ARG;
+  if (!log_decay || !ws || (seqs->rows > 0 && (!dout || !q || !k || !v || !dq || !dk || !dv)) || !aligned4(log_decay)) return ROM_ERR_INVALID_ARG;
   const void* ptrs[] = {dout, q, k, v, s_in, ds_out, dq, dk, dv, ds_in, ws};
   for (const void* p : ptrs)
     if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
@@ -509,8 +518,8 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   const void *ins[] = {dout, q, k, v}, *outs[] = {dq, dk, dv};
   for (int i = 0; i < 3; ++i) {
     for (const void* a : ins)
-      if (a == outs[i]) return ROM_ERR_INVALID_ARG;
-    if (outs[i] == outs[(i + 1) % 3]) return ROM_ERR_INVALID_ARG;
+      if (a && a == outs[i]) return ROM_ERR_INVALID_ARG;
+    if (outs[i] && outs[i] == outs[(i + 1) % 3]) return ROM_ERR_INVALID_ARG;
   }
   if (overlaps(ds_in, pool, ds_out, pool) || overlaps(ds_in, pool, s_in, pool)) return ROM_ERR_INVALID_ARG;
   const LinWs lay = lin_ws(c, seqs->rows, true);

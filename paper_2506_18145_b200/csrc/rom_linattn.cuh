@@ -52,4 +52,7 @@ __device__ __forceinline__ const float* lin_init_of(const LinPass& p, const Ragg
 }
 
 
+// The walk (or launch 1 alone) on the tensor cores, bf16 (rom_linattn_tc.cu).
+cudaError_t launch_lin_tc(const LinPass& p, const rom_ragged& seqs, LinCut cut, bool state_only, bool test_stall, cudaStream_t st);
+
 }  // namespace rom

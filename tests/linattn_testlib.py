@@ -131,7 +131,9 @@ def near(got, ref, size, unit, store, what):
         # Three independent roundings of half a step 2^-8 at most (scores or state, stored partial sum, output), each of a variance of at most a third of its square: together
         # 2^-8 of the norm.  fp32: sums of up to 1000 random terms, sqrt(1000) 2^-24 / 2, twice.
         rel = float((got - ref).norm() / ref.norm().clamp(min=1e-30))
-        most = HALF_STEP["bf16"] if store == "bf16" else 2.0 ** -15 if unit > 2.0 ** -14 else 2.0 ** -19
+        # A state of keys that are the sum of two bf16 numbers: hi is off by 2^-8 of the key at most, lo by 2^-8 of that, so each term by 2^-16 and independent ones together by
+        # 2^-16 of the norm; `unit` holds that 2^-16 exactly where it applies, and without it stays below 2^-16 (its 2^-24 are counted, at most 250 of them here).
+        most = HALF_STEP["bf16"] if store == "bf16" else 2.0 ** -16 if unit > 2.0 ** -16 else 2.0 ** -19
         assert rel <= most, f"{what}: {rel:.2e} of the norm"
 
 

@@ -321,3 +321,21 @@ def test_binding_refuses(what):
         with pytest.raises(ValueError):
             rb.rom_linattn_ragged(cfg, seqs, *{**a, name: t}.values())
     rb.rom_linattn_ragged(cfg, seqs, *a.values())
+
+
+@pytest.mark.parametrize("H,G,dk,dv,lens", [(2, 2, 128, 128, [700]), (4, 2, 64, 64, [100, 300]), (1, 1, 64, 128, [2000])])
+def test_stalled_call_is_reported(H, G, dk, dv, lens):
+    """The timeout path: more bytes are expected than are copied, every wait gives up, the call returns and says so, the workspace stays usable."""
+    from test_gpu_parity import _status_detail
+    pr = Problem(lens, H, G, dk, dv, "bf16", seed=1, backward=True)
+    ref = pr.run()
+    good, stalled = pr.cfg, rb.make_linattn_config(H, G, dk, dv, "bf16", flags=rb.ROM_FLAG_TEST_STALL)
+    for call in (pr.run, pr.run_backward):
+        pr.cfg = stalled
+        call()
+        torch.cuda.synchronize()
+        assert 51 <= _status_detail(pr.ws)[1] <= 57
+        assert rb.rom_get_status(pr.ws) == -6
+        pr.cfg = good
+        again = pr.run()
+        assert same_bits(ref[0], again[0]) and same_bits(ref[1], again[1]) and rb.rom_get_status(pr.ws) == 0
