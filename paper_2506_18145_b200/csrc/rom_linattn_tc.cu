@@ -8,9 +8,9 @@
 // Roundings: P and the S that a chunk meets are bf16 (half a step each, of separate parts of the sum); K~ is hi + lo, two bf16 numbers, in two matrix products, since
 // the state is an fp32 result that many chunks add up in.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
 //
-// One CTA per SM walks one head of one segment of the packed rows.  320 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
-// width), warp 1 the matrix products, warps 2..5 turn scores into P and O1, O2 into output rows, warps 6..9 scale K in place (K~ hi; lo beside it), and keep S.  K and V
-// are double-buffered; the scores' tensor memory is reused for P.
+// One CTA per SM walks one head of one segment of the packed rows.  640 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
+// width), warp 1 the matrix products, warps 4..11 turn scores into P and O1, O2 into output rows, warps 12..19 scale K in place (K~ hi; lo beside it), and keep S; two
+// warps share each 32-lane quarter of tensor memory and take half of the columns each.  The scores' tensor memory is reused for P.
 //
 // Values that are not finite: a masked P is 0 by selection, but 0 * V is not 0 for a V of a later row that is not finite.  Rows whose O2 is not finite are summed
 // again over their own and earlier rows alone (slow_rows).  Rows behind the chunk's last one are never part of a sum: K~ and P are selected 0, V rows in the last
@@ -27,7 +27,11 @@ namespace {
 using bf16 = __nv_bfloat16;
 constexpr int LT_C = 128;                     // rows of a chunk
 constexpr int LT_BOX = 64 * LT_C * 2;         // bytes of one TMA box
-constexpr int LT_THREADS = 320;
+constexpr int LT_WALK_THREADS = 640, LT_STATE_THREADS = 320;
+// Registers of the walk's threads: 640 x 96 at launch; the copies' and products' warps give theirs to those that keep S: 128 x 48 + 256 x 96 + 256 x 120 = 640 x 96.
+constexpr int LT_FEW = 48, LT_MANY = 120;
+template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 constexpr uint32_t LT_TMEM = 512;
 
 __device__ __forceinline__ bool elect_one() {
@@ -35,12 +39,18 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
   return e != 0;
 }
-// A warp's wait, polled by one lane.
+// A warp's wait; the outcome is the same in all lanes.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
-  int ok = 1;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, abort_flag, limit);
-  ok = __shfl_sync(0xffffffffu, ok, 0);
-  __syncwarp();
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
+}
+// Several barriers at once: a wait takes about 200 cycles even when it is over, one after the other the issuer's took 600 a chunk.
+__device__ __forceinline__ bool mbar_ready(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
@@ -62,6 +72,18 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
                "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                : "memory");
+}
+__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+                 "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t (&r)[16]) {      // (the registers pass through: nothing that reads them moves ahead)
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
+                 "+r"(r[14]), "+r"(r[15])
+               :: "memory");
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -86,35 +108,66 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3ffffu) >> 4) | (uint64_t)(LT_BOX >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
-// One row of K (128 bytes of one box, 16-byte pieces swizzled by the row) times w: hi in place, lo beside it; zeros where the row is not part of the sum.
+__device__ __forceinline__ float ld_state(const float* p) { float v; asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p)); return v; }
+__device__ __forceinline__ float4 ld_state4(const float* p) {
+  float4 v;
+  asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+  return v;
+}
+// Part of one row of K (16-byte pieces of a 128-byte row of one box, swizzled by the row) times w: hi in place, lo beside it; zeros where the row is not part of the
+// sum.  Some pieces at a time: one after the other, a piece's load, conversions and stores took 230 cycles.
+template <int AT_ONCE>
 __device__ __forceinline__ void scale_row(uint32_t khi, uint32_t klo, int row, float w, bool live, int piece0, int pieces) {
-#pragma unroll 4
-  for (int i = 0; i < pieces; ++i) {
-    const uint32_t off = row * 128 + (((piece0 + i) ^ (row & 7)) << 4);
-    uint4 hi = make_uint4(0, 0, 0, 0), lo = hi;
-    if (live) {
-      const uint4 x = lds128(khi + off);
-      const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+  const float2 ww = make_float2(w, w);
+#pragma unroll 1
+  for (int i = 0; i < pieces; i += AT_ONCE) {
+    uint4 x[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      x[u] = lds128(khi + row * 128 + (((piece0 + i + u) ^ (row & 7)) << 4));
+      if (!live) x[u] = make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const uint32_t off = row * 128 + (((piece0 + i + u) ^ (row & 7)) << 4), in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
       uint32_t h[4], l[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float a = lo_of(in[e]), b = hi_of(in[e]);
-        h[e] = pack2(a * w, b * w);
-        l[e] = pack2(fmaf(a, w, -lo_of(h[e])), fmaf(b, w, -hi_of(h[e])));      // (of an infinite product NaN: not finite either way)
+        const float2 a = make_float2(lo_of(in[e]), hi_of(in[e])), y = __fmul2_rn(a, ww);
+        h[e] = pack2(y.x, y.y);
+        const float2 rest = __ffma2_rn(a, ww, make_float2(-lo_of(h[e]), -hi_of(h[e])));      // (of an infinite product NaN: not finite either way)
+        l[e] = pack2(rest.x, rest.y);
       }
-      hi = make_uint4(h[0], h[1], h[2], h[3]);
-      lo = make_uint4(l[0], l[1], l[2], l[3]);
+      sts128(khi + off, make_uint4(h[0], h[1], h[2], h[3]));
+      sts128(klo + off, make_uint4(l[0], l[1], l[2], l[3]));
     }
-    sts128(khi + off, hi);
-    sts128(klo + off, lo);
   }
 }
-template <int BOXES>
-__device__ __forceinline__ void clear_row(uint32_t tile, int row) {
+__device__ __forceinline__ void clear_row(uint32_t box, int row) {
 #pragma unroll
-  for (int b = 0; b < BOXES; ++b)
+  for (int i = 0; i < 8; ++i) sts128(box + row * 128 + i * 16, make_uint4(0, 0, 0, 0));
+}
+// A lane holds 128 bytes of its row, eight 16-byte pieces; they are exchanged among eight lanes so that a store instruction of the warp writes four whole runs of 128
+// bytes.  Straight from the lanes it would touch 32 rows with 16 bytes each: eight times the accesses of the LSU, which the loads and stores of K~ and S share (an output
+// tile took 5200 cycles, everything beside it twice its time).  row_at: byte offset of the lane's first row (8 (lane / 8)) and piece; rows: valid rows from there on.
+__device__ __forceinline__ void store_rows128(char* row_at, int64_t pitch, int rows, bool piece_ok, uint32_t (&w)[32], int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sts128(tile + b * LT_BOX + row * 128 + i * 16, make_uint4(0, 0, 0, 0));
+  for (int m = 1; m < 8; m *= 2) {
+    const bool up = (lane & m) != 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (q & m) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t a = w[4 * q + e], b = w[4 * (q | m) + e], got = __shfl_xor_sync(0xffffffffu, up ? a : b, m);
+        w[4 * q + e] = up ? got : a;
+        w[4 * (q | m) + e] = up ? b : got;
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 8; ++t)
+    if (piece_ok && t < rows) *reinterpret_cast<uint4*>(row_at + t * pitch) = make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
 }
 // V^T K~: hi and lo, the first ks steps of 16 rows.
 __device__ __forceinline__ void issue_state(uint32_t tmem_d, uint32_t v, uint32_t khi, uint32_t klo, uint32_t idesc, int ks, bool accumulate) {
@@ -175,16 +228,17 @@ struct LinSegment {
 template <int KP, int VP>
 struct WalkShape {
   static constexpr int KB = KP / 64, VB = VP / 64;
-  static constexpr int QST = KP + VP < 256 ? 2 : 1;                 // stages of Q: one where 227 KB leave no room
-  static constexpr int Q = 0, K = Q + QST * KB * LT_BOX, V = K + 2 * KB * LT_BOX, LO = V + 2 * VB * LT_BOX, S = LO + KB * LT_BOX, BYTES = S + KB * VP * 128;
+  // stages, as many as 227 KB hold: a copy takes up to 2 us when memory is busy, a chunk of two heads' widths of 64 half of that
+  static constexpr int KVST = KP == 128 ? 2 : VP == 128 ? 3 : 4, QST = KP == 128 ? (VP == 128 ? 1 : 2) : KVST;
+  static constexpr int Q = 0, K = Q + QST * KB * LT_BOX, V = K + KVST * KB * LT_BOX, LO = V + KVST * VB * LT_BOX, S = LO + KB * LT_BOX, BYTES = S + KB * VP * 128;
   static constexpr int SC = 0, O1 = 128, KV = O1 + VP, O2 = KV + KP;      // tensor-memory columns (P over the scores' first 64)
 };
 
 // Rows of O2 that are not finite, summed again: out = f O1 + sum over their own and earlier rows.  Rare; all lanes of the warp call it.
 template <bool REV>
 __device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf16* k, const bf16* v, bf16* out, uint32_t taddr_o1, const float* lam, int i, int row0, int len, float f,
-                                       bool mine, int head) {
-  for (int c0 = 0; c0 < p.dv; c0 += 32) {
+                                       bool mine, int head, int c_from, int c_to) {
+  for (int c0 = c_from; c0 < c_to; c0 += 32) {
     uint32_t r[32];
     __syncwarp();
     tmem_ld32_issue(taddr_o1 + c0, r);
@@ -215,14 +269,15 @@ __device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf
 }
 
 template <int KP, int VP, bool REV>
-__global__ void __launch_bounds__(LT_THREADS, 1)
+__global__ void __launch_bounds__(LT_WALK_THREADS, 1)
 lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs,
             int seg_rows, int n_seg, uint32_t wait_limit, uint32_t stall) {
   using W = WalkShape<KP, VP>;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(16) float lam[LT_C + 4], lam_lo[LT_C + 4];
-  __shared__ __align__(8) unsigned long long bars[16];
+  __shared__ __align__(16) float lam_pad[32 + LT_C + 4], lam_lo[LT_C + 4];      // lambda^0.. behind 32 zeros; what each lost to fp32
+  float* const lam = lam_pad + 32;
+  __shared__ __align__(8) unsigned long long bars[24];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
@@ -230,12 +285,12 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
   // full: copies have landed; empty: the matrix products that read them are done; the others by name
   auto q_full = [&](int s) { return bar(s); };
-  auto q_empty = [&](int s) { return bar(2 + s); };
-  auto kv_full = [&](int s) { return bar(4 + s); };
-  auto kv_empty = [&](int s) { return bar(6 + s); };
-  const uint32_t sc_full = bar(8), p_ready = bar(9), k_ready = bar(10), s_ready = bar(11), pv_full = bar(12), o_free = bar(13), state_full = bar(14), drain = bar(15);
+  auto q_empty = [&](int s) { return bar(4 + s); };
+  auto kv_full = [&](int s) { return bar(8 + s); };
+  auto kv_empty = [&](int s) { return bar(12 + s); };
+  const uint32_t sc_full = bar(16), pv_full = bar(17), state_full = bar(18), drain = bar(19), p_ready = bar(20), k_ready = bar(21), s_ready = bar(22), o_free = bar(23);
   if (tid == 0) {
-    for (int i = 0; i < 16; ++i) mbar_init(bar(i), i == 9 || i == 10 || i == 11 || i == 13 ? 4 : 1);
+    for (int i = 0; i < 24; ++i) mbar_init(bar(i), i >= 20 ? 8 : 1);
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -250,6 +305,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     lam[tid] = (float)l;
     lam_lo[tid] = (float)(l - (double)lam[tid]);
   }
+  if (tid < 32) lam_pad[tid] = 0.0f;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -260,7 +316,9 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
   LinPiece x;
   int n = 0;                           // chunks so far
 
+  // (setmaxnreg inside each role's branch: behind a join the compiler would hold every role to the fewest)
   if (warp == 0) {
+    registers_down<LT_FEW>();
     // ---------------------------------------------------------------- copies
     if (elect_one()) {
       bool ok = true;
@@ -268,8 +326,8 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
-          const int st = n & 1, qs = n % W::QST;
-          if (!mbar_wait(kv_empty(st), (n >> 1 & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
+          const int st = n % W::KVST, qs = n % W::QST;
+          if (!mbar_wait(kv_empty(st), (n / W::KVST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
           mbar_expect_tx(kv_full(st), (W::KB + W::VB) * LT_BOX + stall);
           load_tile<W::KB>(base + W::K + st * W::KB * LT_BOX, &tmap_k, kv_full(st), head / p.kdiv, row0);
           load_tile<W::VB>(base + W::V + st * W::VB * LT_BOX, &tmap_v, kv_full(st), head / p.vdiv, row0);
@@ -279,14 +337,15 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         }
       if (!ok) latch(p, abort_flag, 51);
       if (*abort_flag)                 // the copies still in flight land (bounded) before the block ends
-        for (int i = 1; i <= 2 && i <= n; ++i) {
+        for (int i = 1; i <= W::KVST && i <= n; ++i) {
           const int c = n - i;
-          for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(kv_full(c & 1), c >> 1 & 1); ++it) {}
+          for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(kv_full(c % W::KVST), c / W::KVST & 1); ++it) {}
           for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(q_full(c % W::QST), c / W::QST & 1); ++it) {}
         }
     }
     __syncwarp();
   } else if (warp == 1) {
+    registers_down<LT_FEW>();
     // ---------------------------------------------------------------- matrix products
     if (elect_one()) {
       constexpr uint32_t d_sc = lt_idesc(LT_C, false, false), d_o1 = lt_idesc(VP, false, false), d_o2 = lt_idesc(VP, false, true), d_kv = lt_idesc(KP, true, true);
@@ -296,10 +355,12 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
-          const int st = n & 1, qs = n % W::QST, ks = (len + 15) / 16;
+          const int st = n % W::KVST, qs = n % W::QST, ks = (len + 15) / 16;
           const uint32_t ph = n & 1, q = base + W::Q + qs * W::KB * LT_BOX, k = base + W::K + st * W::KB * LT_BOX, v = base + W::V + st * W::VB * LT_BOX;
           // scores, once the P that lies over them has been used
-          if (!wait(kv_full(st), n >> 1 & 1) || !wait(q_full(qs), n / W::QST & 1) || (n > 0 && !wait(pv_full, ph ^ 1))) break;
+          const uint32_t kv_ph = n / W::KVST & 1, q_ph = n / W::QST & 1;
+          const bool kv_in = mbar_ready(kv_full(st), kv_ph), q_in = mbar_ready(q_full(qs), q_ph), pv_in = n == 0 || mbar_ready(pv_full, ph ^ 1);
+          if (!(kv_in && q_in && pv_in) && (!wait(kv_full(st), kv_ph) || !wait(q_full(qs), q_ph) || (n > 0 && !wait(pv_full, ph ^ 1)))) break;
           tc_fence_after();
 #pragma unroll
           for (int b = 0; b < W::KB; ++b)
@@ -309,7 +370,8 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           umma_commit(sc_full);
           issued = true;
           // Q S, once the output before has been read and S written
-          if (!wait(s_ready, ph) || (n > 0 && !wait(o_free, ph ^ 1))) break;
+          const bool s_in = mbar_ready(s_ready, ph), o_in = n == 0 || mbar_ready(o_free, ph ^ 1);
+          if (!(s_in && o_in) && (!wait(s_ready, ph) || (n > 0 && !wait(o_free, ph ^ 1)))) break;
           tc_fence_after();
 #pragma unroll
           for (int b = 0; b < W::KB; ++b)
@@ -317,7 +379,8 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
             for (int e = 0; e < 4; ++e)
               umma_bf16(tmem + W::O1, make_smem_desc(q + b * LT_BOX) + 2 * e, make_smem_desc(base + W::S + b * VP * 128) + 2 * e, d_o1, b + e > 0 ? 1u : 0u);
           umma_commit(q_empty(qs));
-          if (!wait(p_ready, ph) || !wait(k_ready, ph)) break;
+          const bool p_in = mbar_ready(p_ready, ph), k_in = mbar_ready(k_ready, ph);
+          if (!(p_in && k_in) && (!wait(p_ready, ph) || !wait(k_ready, ph))) break;
           tc_fence_after();
           for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 8 * e, desc_mn(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
           umma_commit(pv_full);
@@ -332,9 +395,9 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
       }
     }
     __syncwarp();
-  } else if (warp < 6) {
+  } else if (warp >= 4 && warp < 12) {
     // ---------------------------------------------------------------- scores to P, outputs
-    const int quarter = warp & 3, i = quarter * 32 + lane;
+    const int quarter = warp & 3, half = (warp - 4) >> 2, i = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     bf16* out = static_cast<bf16*>(p.out);
     bool ok = true;
@@ -346,45 +409,50 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         const int early = m == 0 && !x.over && p.early ? 1 : 0, blocks = (len + 31) / 32;
         if (!(ok = warp_wait(sc_full, ph, abort_flag, wait_limit))) break;
         tc_fence_after();
-        for (int b = 0; b < blocks; ++b) {
-          uint32_t w[16];
-          if (REV ? b < quarter : b > quarter) {
+        // blocks half and half + 2 of 32 columns; P lies over the scores, so both warps of the quarter have read theirs before either writes
+        uint32_t w[2][16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = 0;
+        for (int t = 0; t < 2; ++t) {
+          const int b = half + 2 * t;
+          if (b >= blocks || (REV ? b < quarter : b > quarter)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[t][e] = 0;
+            continue;
+          }
+          uint32_t r[32];
+          tmem_ld32_issue(lanes + W::SC + 32 * b, r);
+          tmem_ld_wait(r);
+          if (b == quarter) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float* l = REV ? lam - lane + e : lam + lane - e;
+              const bool on0 = REV ? e >= lane && 32 * b + e < len : lane >= e, on1 = REV ? e + 1 >= lane && 32 * b + e + 1 < len : lane >= e + 1;
+              const float2 x = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(make_float2(l[0], l[REV ? 1 : -1]), make_float2(p.p_scale, p.p_scale)));
+              w[t][e / 2] = pack2(on0 ? x.x : 0.0f, on1 ? x.y : 0.0f);
+            }
           } else {
-            uint32_t r[32];
-            tmem_ld32_issue(lanes + W::SC + 32 * b, r);
-            tmem_ld_wait(r);
-            if (b == quarter) {
+            // lambda^{i-j} = lambda^{i - last of the block} lambda^{last - j}
+            const float f = p.p_scale * lam[REV ? 32 * b - i : i - 32 * b - 31];
+            const bool whole = !REV || 32 * b + 32 <= len;
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                const int g0 = REV ? e - lane : lane - e, g1 = REV ? e + 1 - lane : lane - e - 1;
-                const bool on0 = g0 >= 0 && (!REV || 32 * b + e < len), on1 = g1 >= 0 && (!REV || 32 * b + e + 1 < len);
-                const float p0 = __uint_as_float(r[e]) * (p.p_scale * lam[max(g0, 0)]), p1 = __uint_as_float(r[e + 1]) * (p.p_scale * lam[max(g1, 0)]);
-                w[e / 2] = pack2(on0 ? p0 : 0.0f, on1 ? p1 : 0.0f);
+            for (int e = 0; e < 32; e += 4) {
+              const float4 u = *reinterpret_cast<const float4*>(lam + (REV ? e : 28 - e));
+              const float2 u0 = REV ? make_float2(u.x, u.y) : make_float2(u.w, u.z), u1 = REV ? make_float2(u.z, u.w) : make_float2(u.y, u.x);
+              float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(f, f)));
+              float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(f, f)));
+              if (REV && !whole) {
+                const int j = 32 * b + e;
+                p0 = make_float2(j < len ? p0.x : 0.0f, j + 1 < len ? p0.y : 0.0f);
+                p1 = make_float2(j + 2 < len ? p1.x : 0.0f, j + 3 < len ? p1.y : 0.0f);
               }
-            } else {
-              // lambda^{i-j} = lambda^{i - last of the block} lambda^{last - j}
-              const float f = p.p_scale * lam[REV ? 32 * b - i : i - 32 * b - 31];
-              const bool whole = !REV || 32 * b + 32 <= len;
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 u = *reinterpret_cast<const float4*>(lam + (REV ? e : 28 - e));
-                const float2 u0 = REV ? make_float2(u.x, u.y) : make_float2(u.w, u.z), u1 = REV ? make_float2(u.z, u.w) : make_float2(u.y, u.x);
-                float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(f, f)));
-                float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(f, f)));
-                if (REV && !whole) {
-                  const int j = 32 * b + e;
-                  p0 = make_float2(j < len ? p0.x : 0.0f, j + 1 < len ? p0.y : 0.0f);
-                  p1 = make_float2(j + 2 < len ? p1.x : 0.0f, j + 3 < len ? p1.y : 0.0f);
-                }
-                w[e / 2] = pack2(p0.x, p0.y);
-                w[e / 2 + 1] = pack2(p1.x, p1.y);
-              }
+              w[t][e / 2] = pack2(p0.x, p0.y);
+              w[t][e / 2 + 1] = pack2(p1.x, p1.y);
             }
           }
-          tmem_st16(lanes + W::SC + 16 * b, w);
         }
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+        tmem_st16(lanes + W::SC + 16 * half, w[0]);
+        if (half + 2 < blocks) tmem_st16(lanes + W::SC + 16 * (half + 2), w[1]);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         warp_arrive(p_ready);
@@ -392,56 +460,71 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         tc_fence_after();
         const bool mine = i < len;
         const float f = p.inter_scale * lam[REV ? max(len - i - early, 0) : i + 1 - early];
-        const int64_t to = (int64_t)(row0 + i) * p.ldo + (int64_t)head * p.dv;
         float2 odd = make_float2(0.0f, 0.0f);
-#pragma unroll 1
-        for (int c = 0; c < p.dv; c += 32) {
-          uint32_t r1[32], r2[32];
+        const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + (lane & 24), rows = len - first;      // (rows that the lane stores)
+        // 16 columns: f O1 + O2, noting what is not finite
+        auto columns = [&](int c, float2 (&o)[8]) {
+          uint32_t r1[16], r2[16];
           __syncwarp();
-          tmem_ld32_issue(lanes + W::O1 + c, r1);
-          tmem_ld32_issue(lanes + W::O2 + c, r2);
-          tmem_ld_wait(r1);
-          tmem_ld_wait(r2);
+          tmem_ld16_issue(lanes + W::O1 + c, r1);
+          tmem_ld16_issue(lanes + W::O2 + c, r2);
+          tmem_ld16_wait(r1);
+          tmem_ld16_wait(r2);
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            float2 o[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              const float2 b2 = make_float2(__uint_as_float(r2[e + 2 * h]), __uint_as_float(r2[e + 2 * h + 1]));
-              odd = __ffma2_rn(b2, make_float2(0.0f, 0.0f), odd);
-              o[h] = __ffma2_rn(make_float2(__uint_as_float(r1[e + 2 * h]), __uint_as_float(r1[e + 2 * h + 1])), make_float2(f, f), b2);
-            }
-            if (mine && c + e < p.dv) {
-              if (p.out_f32) {
-                float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.out) + to + c + e);
-                dst[0] = make_float4(o[0].x, o[0].y, o[1].x, o[1].y);
-                dst[1] = make_float4(o[2].x, o[2].y, o[3].x, o[3].y);
-              } else {
-                *reinterpret_cast<uint4*>(out + to + c + e) = make_uint4(pack2(o[0].x, o[0].y), pack2(o[1].x, o[1].y), pack2(o[2].x, o[2].y), pack2(o[3].x, o[3].y));
-              }
-            }
+          for (int e = 0; e < 8; ++e) {
+            const float2 b2 = make_float2(__uint_as_float(r2[2 * e]), __uint_as_float(r2[2 * e + 1]));
+            odd = __ffma2_rn(b2, make_float2(0.0f, 0.0f), odd);
+            o[e] = __ffma2_rn(make_float2(__uint_as_float(r1[2 * e]), __uint_as_float(r1[2 * e + 1])), make_float2(f, f), b2);
           }
+        };
+        if (p.out_f32) {
+#pragma unroll 1
+          for (int c = c_from; c < c_to; c += 32) {
+            uint32_t w[32];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              float2 o[8];
+              columns(c + 16 * u, o);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) { w[16 * u + 2 * e] = __float_as_uint(o[e].x); w[16 * u + 2 * e + 1] = __float_as_uint(o[e].y); }
+            }
+            const int col = c + 4 * (lane & 7);
+            store_rows128(reinterpret_cast<char*>(static_cast<float*>(p.out) + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 4, rows, col < p.dv, w, lane);
+          }
+        } else if (c_from < c_to) {
+          uint32_t w[32];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            float2 o[8];
+            if (VP == 128 || u < 2) columns(c_from + 16 * u, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[8 * u + e] = VP == 128 || u < 2 ? pack2(o[e].x, o[e].y) : 0;
+          }
+          const int col = c_from + 8 * (lane & 7);
+          store_rows128(reinterpret_cast<char*>(out + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 2, rows, (VP == 128 || (lane & 7) < 4) && col < p.dv, w, lane);
         }
         const bool again = mine && !(odd.x == 0.0f && odd.y == 0.0f);
         if (__any_sync(0xffffffffu, again))
           slow_rows<REV>(p, static_cast<const bf16*>(p.q) + (int64_t)(head / p.qdiv) * p.dk, static_cast<const bf16*>(p.k) + (int64_t)(head / p.kdiv) * p.dk,
-                         static_cast<const bf16*>(p.v) + (int64_t)(head / p.vdiv) * p.dv, out, lanes + W::O1, lam, i, row0, len, f, again, head);
+                         static_cast<const bf16*>(p.v) + (int64_t)(head / p.vdiv) * p.dv, out, lanes + W::O1, lam, i, row0, len, f, again, head, c_from, c_to);
         tc_fence_before();
         warp_arrive(o_free);
       }
     if (!ok) latch(p, abort_flag, 53);
-  } else {
-    // ---------------------------------------------------------------- K~ and the state: thread c keeps column c of S
-    const int quarter = warp & 3, c = quarter * 32 + lane;
+  } else if (warp >= 12) {
+    registers_up<LT_MANY>();
+    // ---------------------------------------------------------------- K~ and the state: two threads keep column c of S, half of its rows each
+    constexpr int KH = KP / 2;
+    const int quarter = warp & 3, half = (warp - 12) >> 2, c = quarter * 32 + lane, a0 = half * KH;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     const size_t state = (size_t)p.dk * p.dv;
-    float S[KP];
+    float S[KH];
     bool ok = true;
     auto write_s = [&]() {      // bf16 rows of S^T, K-major
       if (c < VP)
 #pragma unroll
-        for (int a = 0; a < KP; a += 8)
-          sts128(base + W::S + (a / 64) * VP * 128 + c * 128 + (((a / 8 & 7) ^ (c & 7)) << 4),
+        for (int a = 0; a < KH; a += 8)
+          sts128(base + W::S + (KP == 128 ? half : 0) * VP * 128 + c * 128 + ((((KP == 128 ? 0 : 4 * half) + a / 8) ^ (c & 7)) << 4),
                  make_uint4(pack2(S[a], S[a + 1]), pack2(S[a + 2], S[a + 3]), pack2(S[a + 4], S[a + 5]), pack2(S[a + 6], S[a + 7])));
       fence_async();
       warp_arrive(s_ready);
@@ -452,28 +535,38 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
       if (x.over) from = p.seg_state + ((size_t)(REV ? seg.seg : seg.seg - 1) * p.H + head) * state;
       else if (!REV && mm > 0 && from && p.init_copy && !x.ends) from = p.init_copy + ((size_t)seg.seg * p.H + head) * state;
       if (mm == 0 && !x.ends) continue;
+      // (every load at a valid address and selected afterwards: one by one behind branches they took 10000 cycles)
+      const bool mine = from != nullptr && c < p.dv;
+      if (from) {
+        const int col = min(c, p.dv - 1);
+        if (p.transposed) {
+          float4 v[KH / 4];
 #pragma unroll
-      for (int a = 0; a < KP; a += 4) {
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (from && c < p.dv && a < p.dk) {
-          if (p.transposed) v = *reinterpret_cast<const float4*>(from + (size_t)c * p.dk + a);
-          else v = make_float4(from[(size_t)a * p.dv + c], from[(size_t)(a + 1) * p.dv + c], from[(size_t)(a + 2) * p.dv + c], from[(size_t)(a + 3) * p.dv + c]);
+          for (int a = 0; a < KH; a += 4) v[a / 4] = ld_state4(from + (size_t)col * p.dk + min(a0 + a, p.dk - 4));
+#pragma unroll
+          for (int a = 0; a < KH; a += 4) { S[a] = v[a / 4].x; S[a + 1] = v[a / 4].y; S[a + 2] = v[a / 4].z; S[a + 3] = v[a / 4].w; }
+        } else {
+#pragma unroll
+          for (int a = 0; a < KH; ++a) S[a] = ld_state(from + (size_t)min(a0 + a, p.dk - 1) * p.dv + col);
         }
-        S[a] = v.x; S[a + 1] = v.y; S[a + 2] = v.z; S[a + 3] = v.w;
       }
+#pragma unroll
+      for (int a = 0; a < KH; ++a)
+        if (!mine || a0 + a >= p.dk) S[a] = 0.0f;
       if (mm > 0) write_s();
       for (int m = 0; m < mm; ++m, ++n) {
         int row0, len;
         x.chunk<REV>(m, row0, len);
-        const int st = n & 1, early = m == 0 && !x.over && p.early ? 1 : 0, rows16 = (len + 15) / 16 * 16;
-        const uint32_t ph = n & 1, k = base + W::K + st * W::KB * LT_BOX;
-        if (!(ok = warp_wait(kv_full(st), n >> 1 & 1, abort_flag, wait_limit) && warp_wait(sc_full, ph, abort_flag, wait_limit))) break;
+        const int st = n % W::KVST, early = m == 0 && !x.over && p.early ? 1 : 0, rows16 = (len + 15) / 16 * 16;
+        const uint32_t ph = n & 1, k = base + W::K + st * W::KB * LT_BOX, box = KP == 128 ? half * LT_BOX : 0;
+        // (the scores are made of this K: sc_full says that it has landed, but the copies' own barrier makes them visible)
+        if (!(ok = warp_wait(sc_full, ph, abort_flag, wait_limit) && (__all_sync(0xffffffffu, mbar_ready(kv_full(st), n / W::KVST & 1)) || warp_wait(kv_full(st), n / W::KVST & 1, abort_flag, wait_limit))))
+          break;
         if (c < rows16) {
           const bool live = c < len;
           const float w = live ? p.k_scale * lam[REV ? c : len - 1 - c] : 0.0f;
-#pragma unroll
-          for (int b = 0; b < W::KB; ++b) scale_row(k + b * LT_BOX, base + W::LO + b * LT_BOX, c, w, live, 0, 8);
-          if (!live) clear_row<W::VB>(base + W::V + st * W::VB * LT_BOX, c);
+          scale_row<4>(k + box, base + W::LO + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
+          if (!live && half < W::VB) clear_row(base + W::V + (st * W::VB + half) * LT_BOX, c);
         }
         fence_async();
         warp_arrive(k_ready);
@@ -481,12 +574,12 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         tc_fence_after();
         const float f = lam[len - early], fl = lam_lo[len - early];
 #pragma unroll
-        for (int a = 0; a < KP; a += 32) {
-          uint32_t r[32];
-          tmem_ld32_issue(lanes + W::KV + a, r);
-          tmem_ld_wait(r);
+        for (int a = 0; a < KH; a += 16) {
+          uint32_t r[16];
+          tmem_ld16_issue(lanes + W::KV + a0 + a, r);
+          tmem_ld16_wait(r);
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
+          for (int e = 0; e < 16; e += 2) {
             float2 v = __ffma2_rn(make_float2(S[a + e], S[a + e + 1]), make_float2(fl, fl), make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
             v = __ffma2_rn(make_float2(S[a + e], S[a + e + 1]), make_float2(f, f), v);
             S[a + e] = v.x;
@@ -498,15 +591,19 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
       }
       if (!ok) break;
       if (p.last && slot >= 0 && x.ends && c < p.dv) {
-        const float f = p.init_all && !seqs.resumes(s) ? 0.0f : mm > 0 && p.early ? lam[1] : 1.0f;
-        float* to = p.last + ((size_t)slot * p.H + head) * state + c;
         const bool none = p.init_all && !seqs.resumes(s);
+        const float f = mm > 0 && p.early ? lam[1] : 1.0f;
+        float* to = p.last + ((size_t)slot * p.H + head) * state + c;
 #pragma unroll
-        for (int a = 0; a < KP; ++a)
-          if (a < p.dk) to[(size_t)a * p.dv] = none ? 0.0f : f * S[a];
+        for (int a = 0; a < KH; a += 8)
+          if (a0 + a < p.dk)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[(size_t)(a0 + a + e) * p.dv] = none ? 0.0f : f * S[a + e];
       }
     }
     if (!ok) latch(p, abort_flag, 54);
+  } else {
+    registers_down<LT_FEW>();
   }
   tc_fence_before();
   __syncthreads();
@@ -523,12 +620,12 @@ struct StateShape {
   static constexpr int STAGE = (2 * KB + VB) * LT_BOX, LO = KB * LT_BOX, V = 2 * KB * LT_BOX;      // K (hi) | lo | V
   static constexpr int STAGES = KP == 128 ? 2 : 3, BYTES = STAGES * STAGE + (VB == 1 ? LT_BOX : 0);      // (see desc_mn: one box behind the last V)
 };
-constexpr int kLtMaxSmem = 232448 - 4096;      // what a block may ask for, less its static variables
-static_assert(WalkShape<128, 128>::BYTES + 1024 <= kLtMaxSmem + 2048 && WalkShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && WalkShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
+constexpr int kLtMaxSmem = 232448 - 2048;      // what a block may ask for, less its static variables
+static_assert(WalkShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && WalkShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && WalkShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
 static_assert(StateShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && StateShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && StateShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
 
 template <int KP, int VP, bool REV>
-__global__ void __launch_bounds__(LT_THREADS, 1)
+__global__ void __launch_bounds__(LT_STATE_THREADS, 1)
 lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs, int seg_rows, uint32_t wait_limit, uint32_t stall) {
   using W = StateShape<KP, VP>;
   extern __shared__ unsigned char smem_raw[];
@@ -613,9 +710,9 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
       if (!(ok = warp_wait(full(st), n / W::STAGES & 1, abort_flag, wait_limit))) break;
       if (j < rows16) {
         const bool live = j < len;
-        if (KP == 128) scale_row(at + half * LT_BOX, at + W::LO + half * LT_BOX, j, w, live, 0, 8);
-        else scale_row(at, at + W::LO, j, w, live, 4 * half, 4);
-        if (!live && half == 0) clear_row<W::VB>(at + W::V, j);
+        if (KP == 128) scale_row<4>(at + half * LT_BOX, at + W::LO + half * LT_BOX, j, w, live, 0, 8);
+        else scale_row<4>(at, at + W::LO, j, w, live, 4 * half, 4);
+        if (!live && half < W::VB) clear_row(at + W::V + half * LT_BOX, j);
       }
       fence_async();
       warp_arrive(scaled(st));
@@ -665,14 +762,14 @@ cudaError_t launch_shape(const LinPass& p, const rom_ragged& seqs, LinCut cut, b
     auto kern = lin_state_tc<KP, VP, REV>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_k(kern, dim3(p.H, cut.n_seg - 1), LT_THREADS, smem, st, tk, tv, p, device_view(seqs), cut.seg_rows, limit, stall);
+    return launch_k(kern, dim3(p.H, cut.n_seg - 1), LT_STATE_THREADS, smem, st, tk, tv, p, device_view(seqs), cut.seg_rows, limit, stall);
   }
   if (!make_tmap_heads(&tq, p.q, seqs.rows, p.H / p.qdiv, p.dk, p.ldq)) return cudaErrorInvalidValue;
   constexpr int smem = WalkShape<KP, VP>::BYTES + 1024;
   auto kern = lin_walk_tc<KP, VP, REV>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_k(kern, dim3(p.H, cut.n_seg), LT_THREADS, smem, st, tq, tk, tv, p, device_view(seqs), cut.seg_rows, cut.n_seg, limit, stall);
+  return launch_k(kern, dim3(p.H, cut.n_seg), LT_WALK_THREADS, smem, st, tq, tk, tv, p, device_view(seqs), cut.seg_rows, cut.n_seg, limit, stall);
 }
 
 }  // namespace
