@@ -39,10 +39,10 @@ __device__ __forceinline__ void load_tile(float* dst, int pitch, const T* src, i
   }
 }
 
-// A block owns up to 64 columns of one head's state and walks one segment.  256 threads: 16 x 16, each 2 rows x 4 columns of the outputs and
+// A block owns up to 64 columns of a state and walks one run.  256 threads: 16 x 16, each 2 rows x 4 columns of the outputs and
 // 8 x 4 of the state.  What bounds it: shared-memory reads of the operands (10 wavefronts for 16 packed FMAs in q S).
 template <typename T, bool STATE>
-__global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged seqs, int seg_rows, int n_seg) {
+__global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged seqs, LinCut cut) {
   extern __shared__ float sm[];
   const int qp = p.dk + 4;
   float* S = sm;                              // [dk][SIMT_SPITCH]
@@ -52,18 +52,23 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
   float* P = Q + (STATE ? 0 : SIMT_C * qp);   // [C][C + 1]
   __shared__ float lam[SIMT_C + 1], lam_lo[SIMT_C + 1];
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int seg = STATE && p.reverse ? (int)blockIdx.x + 1 : (int)blockIdx.x, head = blockIdx.y, c0 = blockIdx.z * SIMT_DV, wv = min(SIMT_DV, p.dv - c0);
-  if (tid <= SIMT_C) {
-    const double l = exp((double)__ldg(p.log_decay + head) * tid);
-    lam[tid] = (float)l;
-    lam_lo[tid] = (float)(l - (double)lam[tid]);
-  }
+  const int run = blockIdx.x, c0 = blockIdx.y * SIMT_DV, wv = min(SIMT_DV, p.dv - c0);
   pdl_sync();
   const size_t state = (size_t)p.dk * p.dv;
-  const T* q = static_cast<const T*>(p.q) + (size_t)(head / p.qdiv) * p.dk;
-  const T* k = static_cast<const T*>(p.k) + (size_t)(head / p.kdiv) * p.dk;
-  const T* v = static_cast<const T*>(p.v) + (size_t)(head / p.vdiv) * p.dv + c0;
-  const int a = seg * seg_rows, b = min(a + seg_rows, seqs.rows);
+  int head = 0;
+  const T *q = nullptr, *k = nullptr, *v = nullptr;
+  auto enter = [&](int h) {
+    head = h;
+    q = static_cast<const T*>(p.q) + (size_t)(head / p.qdiv) * p.dk;
+    k = static_cast<const T*>(p.k) + (size_t)(head / p.kdiv) * p.dk;
+    v = static_cast<const T*>(p.v) + (size_t)(head / p.vdiv) * p.dv + c0;
+    __syncthreads();
+    if (tid <= SIMT_C) {
+      lam[tid] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + tid);
+      lam_lo[tid] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + kLinPowers + tid);
+    }
+    __syncthreads();
+  };
   auto place = [&](int i, int& r, int& c) {      // i-th element of the block's columns, in the order of the memory's rows
     if (p.transposed) { c = i / p.dk; r = i - c * p.dk; } else { r = i / wv; c = i - r * wv; }
   };
@@ -181,27 +186,31 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
   };
 
   if constexpr (STATE) {
-    const int cut = p.reverse ? a : b, s = lin_spanning(seqs, cut);
-    if (s < 0) return;
+    int h, r0, r1;
+    if (!lin_cut_rows(cut, run + 1, p.reverse, seqs, h, r0, r1)) return;
+    enter(h);
     load_state(nullptr);
-    if (p.reverse) walk(a, min(seqs.end_of(s), b), false);
-    else walk(max(seqs.start_of(s), a), b, false);
-    store_state(p.seg_state + ((size_t)(p.reverse ? seg - 1 : seg) * p.H + head) * state, 1.0f);
+    walk(r0, r1, false);
+    store_state(p.cut_state + (size_t)run * state, 1.0f);
   } else {
-    int s = seqs.first_from(a);
-    if (s > 0 && seqs.end_of(s - 1) > a) --s;
-    for (; s < seqs.n_seq; ++s) {
-      const int st = seqs.start_of(s), en = seqs.end_of(s), r0 = max(st, a), r1 = min(en, b);
-      if (st >= b && seg + 1 < n_seg) break;
-      const int slot = seqs.slot_of(s);
-      const bool empty = en <= st, over = !empty && (p.reverse ? en > b : st < a);      // its state comes over a cut
-      if (!empty && r0 >= r1) continue;
-      if (over) load_state(p.seg_state + ((size_t)(p.reverse ? seg : seg - 1) * p.H + head) * state);
-      else if (!empty && !p.reverse && p.init_copy && en > b && lin_init_of(p, seqs, s, head)) load_state(p.init_copy + ((size_t)seg * p.H + head) * state);
-      else load_state(lin_init_of(p, seqs, s, head));
-      if (!empty) walk(r0, r1, !over);
-      if (p.last && slot >= 0 && (empty || (p.reverse ? st >= a : en <= b)))
-        store_state(p.last + ((size_t)slot * p.H + head) * state, p.init_all && !seqs.resumes(s) ? 0.0f : !empty && p.early ? lam[1] : 1.0f);
+    for (LinItem it(cut, run); it.next(cut, seqs.rows);) {
+      enter(it.head);
+      const int a = it.a, b = it.b;
+      int s = seqs.first_from(a);
+      if (s > 0 && seqs.end_of(s - 1) > a) --s;
+      for (; s < seqs.n_seq; ++s) {
+        const int st = seqs.start_of(s), en = seqs.end_of(s), r0 = max(st, a), r1 = min(en, b);
+        if (st >= b && !it.last) break;
+        const int slot = seqs.slot_of(s);
+        const bool empty = en <= st, over = !empty && (p.reverse ? en > b : st < a);      // its state comes over a cut
+        if (!empty && r0 >= r1) continue;
+        if (over) load_state(p.cut_state + (size_t)(p.reverse ? run : run - 1) * state);
+        else if (!empty && !p.reverse && p.init_copy && en > b && lin_init_of(p, seqs, s, head)) load_state(p.init_copy + (size_t)run * state);
+        else load_state(lin_init_of(p, seqs, s, head));
+        if (!empty) walk(r0, r1, !over);
+        if (p.last && slot >= 0 && (empty || (p.reverse ? st >= a : en <= b)))
+          store_state(p.last + ((size_t)slot * p.H + head) * state, p.init_all && !seqs.resumes(s) ? 0.0f : !empty && p.early ? lam[1] : 1.0f);
+      }
     }
   }
 }
@@ -215,52 +224,77 @@ cudaError_t launch_simt(const LinPass& p, const rom_ragged& seqs, LinCut cut, cu
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)simt_smem(kLinMaxDim, STATE));
   if (e != cudaSuccess) return e;
   count_launch();
-  return launch_k(kern, dim3(STATE ? cut.n_seg - 1 : cut.n_seg, p.H, (p.dv + SIMT_DV - 1) / SIMT_DV), SIMT_THREADS, smem, st, p, device_view(seqs), cut.seg_rows, cut.n_seg);
+  return launch_k(kern, dim3(STATE ? cut.blocks - 1 : cut.blocks, (p.dv + SIMT_DV - 1) / SIMT_DV), SIMT_THREADS, smem, st, p, device_view(seqs), cut);
+}
+
+// Before launch 1: the status block cleared, and the powers of every head's decay.
+__global__ void __launch_bounds__(256) lin_powers(const float* log_decay, int H, float* powers, int32_t* status) {
+  pdl_sync();
+  if (blockIdx.x == 0 && threadIdx.x < kStatusInts) status[threadIdx.x] = 0;
+  const int i = blockIdx.x * 256 + threadIdx.x, head = i / kLinPowers, n = i - head * kLinPowers;
+  if (head >= H) return;
+  const double l = exp((double)__ldg(log_decay + head) * n);
+  const float hi = (float)l;
+  powers[(size_t)head * 2 * kLinPowers + n] = hi;
+  powers[(size_t)head * 2 * kLinPowers + kLinPowers + n] = (float)(l - (double)hi);
 }
 
 // Launch 2: the states that reach every cut, element by element.  A thread owns four adjacent elements of one head.
 constexpr int CHAIN_THREADS = 128;
-__global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seqs, int seg_rows, int n_seg) {
-  __shared__ int how[kLinMaxSegs];              // at the cut before segment b: -2 nobody reaches over it; -1 the state comes over a cut; else a sequence starts here
-  __shared__ float weight[kLinMaxSegs];         // its initial state decayed up to the cut
+__global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seqs, LinCut cut) {
+  __shared__ int how[kLinMaxBlocks];            // at the head's cuts: -2 nobody reaches over it; -1 the state comes over a cut; else a sequence starts here
+  __shared__ float weight[kLinMaxBlocks];       // of the state at the cut before, or of the sequence's initial state
   const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const double g = (double)__ldg(p.log_decay + head);
-  pdl_sync();
-  for (int b = 1 + warp; b < n_seg; b += CHAIN_THREADS / 32) {
-    const int r = b * seg_rows, s = lin_spanning(seqs, r);
+  const long long u0 = (long long)head * cut.per_head, u1 = u0 + cut.per_head;
+  int first = (int)(u0 * cut.blocks / cut.units), n = 0;      // the head's cuts: first .. first + n - 1
+  while (cut.bound(first) <= u0) ++first;
+  while (cut.bound(first + n) < u1) ++n;
+  auto row_of = [&](int j) { return j < 0 ? 0 : j >= n ? seqs.rows : (int)(cut.bound(first + j) - u0) * cut.chunk; };
+  for (int j = warp; j < n; j += CHAIN_THREADS / 32) {
+    const int r = row_of(j), s = lin_spanning(seqs, r), far = row_of(p.reverse ? j + 1 : j - 1);
     if (lane == 0) {
       int h = -2;
       float w = 0.0f;
       if (s >= 0) {
-        const int away = p.reverse ? seqs.end_of(s) - r : r - seqs.start_of(s);
-        h = away > (p.reverse ? min(seqs.rows - r, seg_rows) : seg_rows) ? -1 : s;
-        w = (float)exp(g * (h < 0 ? seg_rows : away - (p.early ? 1 : 0)));
+        const int away = p.reverse ? seqs.end_of(s) - r : r - seqs.start_of(s), seg = p.reverse ? far - r : r - far;
+        h = away > seg ? -1 : s;
+        w = (float)exp(g * (h < 0 ? seg : away - (p.early ? 1 : 0)));
       }
-      how[b] = h;
-      weight[b] = w;
+      how[j] = h;
+      weight[j] = w;
     }
   }
+  pdl_sync();                           // (the tables above come from inputs, which are older than launch 1)
   __syncthreads();
   const size_t state = (size_t)p.dk * p.dv, e = ((size_t)blockIdx.x * CHAIN_THREADS + threadIdx.x) * 4;
   if (e >= state) return;
   float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int i = 1; i < n_seg; ++i) {
-    const int b = p.reverse ? n_seg - i : i, h = how[b];
-    if (h == -2) continue;
-    float4* here = reinterpret_cast<float4*>(p.seg_state + ((size_t)(b - 1) * p.H + head) * state + e);
-    const float4 add = *here;
-    const float w = weight[b];
-    bool from = true;
-    if (h >= 0) {
-      const float* init = lin_init_of(p, seqs, h, head);
-      from = init != nullptr;
-      if (from) {
-        x = *reinterpret_cast<const float4*>(init + e);
-        if (p.init_copy) *reinterpret_cast<float4*>(p.init_copy + ((size_t)(b - 1) * p.H + head) * state + e) = x;
-      }
+  for (int i0 = 0; i0 < n; i0 += 4) {
+    float4 add[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {      // (loads of four cuts at a time: nothing of theirs depends on the chain)
+      const int j = p.reverse ? n - 1 - (i0 + u) : i0 + u;
+      if (i0 + u < n && how[j] != -2) add[u] = *reinterpret_cast<const float4*>(p.cut_state + (size_t)(first + j - 1) * state + e);
     }
-    x = from ? make_float4(fmaf(w, x.x, add.x), fmaf(w, x.y, add.y), fmaf(w, x.z, add.z), fmaf(w, x.w, add.w)) : add;
-    *here = x;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i0 + u >= n) break;
+      const int j = p.reverse ? n - 1 - (i0 + u) : i0 + u, h = how[j];
+      if (h == -2) continue;
+      const float w = weight[j];
+      bool from = true;
+      if (h >= 0) {
+        const float* init = lin_init_of(p, seqs, h, head);
+        from = init != nullptr;
+        if (from) {
+          x = *reinterpret_cast<const float4*>(init + e);
+          if (p.init_copy) *reinterpret_cast<float4*>(p.init_copy + (size_t)(first + j - 1) * state + e) = x;
+        }
+      }
+      x = from ? make_float4(fmaf(w, x.x, add[u].x), fmaf(w, x.y, add[u].y), fmaf(w, x.z, add[u].z), fmaf(w, x.w, add[u].w)) : add[u];
+      *reinterpret_cast<float4*>(p.cut_state + (size_t)(first + j - 1) * state + e) = x;
+    }
   }
 }
 
@@ -354,36 +388,42 @@ int check_lin(const rom_linattn_config* c) {
 }
 bool on_tensor_cores(const rom_linattn_config& c) { return c.dtype == ROM_BF16 && !(c.flags & ROM_FLAG_SIMT_GEMM); }
 
-// Segments of the packed rows.  A segment of a head is one block of launch 3 (on the tensor cores one to an SM), and rows in a segment are walked in turn: the
-// count with the fewest chunks one after the other, each wave of blocks counted with two chunks more for its start.  A function of the sizes only (148 SMs assumed).
-int most_segments(const rom_linattn_config& c, int rows) {
-  const bool tc = on_tensor_cores(c);
-  const int per = c.n_heads * (tc ? 1 : (c.d_v + SIMT_DV - 1) / SIMT_DV), slots = tc ? 148 : 296, least = tc ? 256 : 64;
-  const int want = (2 * slots + per - 1) / per, most = rows / least, n = want < most ? want : most;
-  return n < 1 ? 1 : n < kLinMaxSegs ? n : kLinMaxSegs;
+// Runs: one head each, or, where that leaves SMs idle for longer than launches 1 and 2 take, equal runs of all heads' chunks on as many blocks as the GPU holds
+// (on the tensor cores one to an SM).  Launch 1 takes about 0.6 of a chunk's time, launches 1 and 2 about six chunks of one block besides.  A function of the sizes only
+// (148 SMs assumed).
+struct LinSlots { int blocks, chunk, least; };
+LinSlots slots_of(const rom_linattn_config& c) {
+  if (on_tensor_cores(c)) return LinSlots{148, 128, 2};
+  return LinSlots{kLinMaxBlocks / ((c.d_v + SIMT_DV - 1) / SIMT_DV), SIMT_C, 2};
+}
+int most_runs(const rom_linattn_config& c, int rows) {      // with cuts inside heads
+  const LinSlots s = slots_of(c);
+  const long long units = (long long)c.n_heads * ((rows + s.chunk - 1) / s.chunk), n = units / s.least;
+  return (int)(n < 1 ? 1 : n < s.blocks ? n : s.blocks);
 }
 LinCut cut_rows(const rom_linattn_config& c, int rows) {
-  const bool tc = on_tensor_cores(c);
-  const int per = c.n_heads * (tc ? 1 : (c.d_v + SIMT_DV - 1) / SIMT_DV), slots = tc ? 148 : 296, unit = tc ? 128 : SIMT_C;
-  LinCut best{0, 0};
-  long long least = 0;
-  for (int n = 1, most = most_segments(c, rows); n <= most; ++n) {
-    const int seg_rows = (int)align_up((size_t)(rows + n - 1) / n, unit), segs = (rows + seg_rows - 1) / seg_rows;
-    const long long waves = ((long long)per * segs + slots - 1) / slots, time = waves * (seg_rows / unit + 2);
-    if (best.n_seg == 0 || time < least) { best = LinCut{seg_rows, segs}; least = time; }
-  }
-  return best;
+  const LinSlots s = slots_of(c);
+  LinCut cut{s.chunk, rows > 0 ? (rows + s.chunk - 1) / s.chunk : 1, c.n_heads, 0, false};
+  cut.units = (long long)c.n_heads * cut.per_head;
+  // A run inside one head starts once, and heads that are cut at the same rows read memory side by side: a whole number of runs a head, where that leaves no more than a
+  // fifth of the blocks out (32 heads of 64, 23 prompts of 8186 rows: 128 runs 81 us, 148 of them 106; 16384 rows of 32 heads of 128: 173 and 175).
+  int n = most_runs(c, rows);
+  const int aligned = n / c.n_heads * c.n_heads;
+  if (aligned * 5 >= n * 4) n = aligned;
+  const double whole = (double)((c.n_heads + s.blocks - 1) / s.blocks) * cut.per_head, even = 1.6 * (double)cut.units / n + 6.0;
+  if (even < whole) { cut.blocks = n; cut.inside = true; }
+  return cut;
 }
-struct LinWs { size_t status, seg_a, seg_b, part, total; };
+struct LinWs { size_t status, powers, cut_a, cut_b, part, total; };
 LinWs lin_ws(const rom_linattn_config& c, int rows, bool backward) {
   LinWs l{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
-  const int n = most_segments(c, rows);
-  const size_t state = n > 1 ? (size_t)n * c.n_heads * c.d_k * c.d_v * sizeof(float) : 0;
+  const size_t state = (size_t)most_runs(c, rows) * c.d_k * c.d_v * sizeof(float);
   l.status = take(sizeof(int32_t) * kStatusInts);
-  l.seg_a = take(state);
-  l.seg_b = take(state);
+  l.powers = take((size_t)c.n_heads * 2 * kLinPowers * sizeof(float));
+  l.cut_a = take(state);
+  l.cut_b = take(state);
   l.part = take(backward && c.n_qk_heads < c.n_heads ? (size_t)rows * c.n_heads * c.d_k * sizeof(float) : 0);
   l.total = off;
   return l;
@@ -403,13 +443,17 @@ cudaError_t launch_walk(const rom_linattn_config& c, const LinPass& p, const rom
   if (c.dtype == ROM_F32) return launch_simt<float, STATE>(p, seqs, cut, st);
   return launch_simt<__nv_bfloat16, STATE>(p, seqs, cut, st);
 }
+cudaError_t launch_powers(const LinPass& p, float* powers, cudaStream_t st) {
+  count_launch();
+  return launch_k(lin_powers, dim3((p.H * kLinPowers + 255) / 256), 256, 0, st, p.log_decay, p.H, powers, p.status);
+}
 // Launches 1 and 2: the states at the cuts.
 cudaError_t launch_states(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
-  if (cut.n_seg < 2) return cudaSuccess;
+  if (!cut.inside) return cudaSuccess;
   const cudaError_t e = launch_walk<true>(c, p, seqs, cut, st);
   if (e != cudaSuccess) return e;
   count_launch();
-  return launch_k(lin_chain, dim3((p.dk * p.dv / 4 + CHAIN_THREADS - 1) / CHAIN_THREADS, p.H), CHAIN_THREADS, 0, st, p, device_view(seqs), cut.seg_rows, cut.n_seg);
+  return launch_k(lin_chain, dim3((p.dk * p.dv / 4 + CHAIN_THREADS - 1) / CHAIN_THREADS, p.H), CHAIN_THREADS, 0, st, p, device_view(seqs), cut);
 }
 cudaError_t launch_sum(const rom_linattn_config& c, const float* part, void* dst, const rom_ragged& seqs, cudaStream_t st) {
   int sms = 0;
@@ -456,18 +500,20 @@ int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, co
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
-  const LinCut cut = cut_rows(c, seqs->rows > 0 ? seqs->rows : 1);
+  const LinCut cut = cut_rows(c, seqs->rows);
   LinPass p{};
   p.q = q; p.k = k; p.v = v; p.ldq = ldq; p.ldk = ldk; p.ldv = ldv;
   p.qdiv = p.kdiv = c.n_heads / c.n_qk_heads; p.vdiv = 1;
   p.H = c.n_heads; p.dk = c.d_k; p.dv = c.d_v; p.log_decay = log_decay;
   p.p_scale = p.inter_scale = c.scale; p.k_scale = 1.0f;
   p.init = s_in; p.last = s_out;
-  p.seg_state = reinterpret_cast<float*>(W + lay.seg_a);
-  p.init_copy = s_in && s_in == s_out ? reinterpret_cast<float*>(W + lay.seg_b) : nullptr;
+  float* powers = reinterpret_cast<float*>(W + lay.powers);
+  p.powers = powers;
+  p.cut_state = reinterpret_cast<float*>(W + lay.cut_a);
+  p.init_copy = cut.inside && s_in && s_in == s_out ? reinterpret_cast<float*>(W + lay.cut_b) : nullptr;
   p.out = o; p.ldo = (int64_t)c.n_heads * c.d_v;
   p.status = reinterpret_cast<int32_t*>(W + lay.status);
-  if (launch_init_status(p.status, st) != cudaSuccess) return ROM_ERR_CUDA;
+  if (launch_powers(p, powers, st) != cudaSuccess) return ROM_ERR_CUDA;
   if (launch_states(c, p, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
   return launch_walk<false>(c, p, *seqs, cut, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
@@ -528,24 +574,26 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
-  const LinCut cut = cut_rows(c, seqs->rows > 0 ? seqs->rows : 1);
+  const LinCut cut = cut_rows(c, seqs->rows);
   const int share = c.n_heads / c.n_qk_heads;
   float* part = share > 1 ? reinterpret_cast<float*>(W + lay.part) : nullptr;
   LinPass base{};
   base.H = c.n_heads; base.log_decay = log_decay; base.p_scale = c.scale;
   base.status = reinterpret_cast<int32_t*>(W + lay.status);
-  if (launch_init_status(base.status, st) != cudaSuccess) return ROM_ERR_CUDA;
+  float* powers = reinterpret_cast<float*>(W + lay.powers);
+  base.powers = powers;
+  if (launch_powers(base, powers, st) != cudaSuccess) return ROM_ERR_CUDA;
   // the states S of the forward at the cuts
   LinPass s = base;
   s.k = k; s.v = v; s.ldk = ldk; s.ldv = ldv; s.q = k; s.ldq = ldk;
   s.qdiv = s.kdiv = share; s.vdiv = 1; s.dk = c.d_k; s.dv = c.d_v;
-  s.k_scale = 1.0f; s.init = s_in; s.seg_state = reinterpret_cast<float*>(W + lay.seg_a);
+  s.k_scale = 1.0f; s.init = s_in; s.cut_state = reinterpret_cast<float*>(W + lay.cut_a);
   if (launch_states(c, s, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
   // dq
   LinPass w = base;
   w.q = dout; w.k = v; w.v = k; w.ldq = (int64_t)c.n_heads * c.d_v; w.ldk = ldv; w.ldv = ldk;
   w.qdiv = w.kdiv = 1; w.vdiv = share; w.dk = c.d_v; w.dv = c.d_k;
-  w.inter_scale = c.scale; w.k_scale = 1.0f; w.transposed = true; w.init = s_in; w.seg_state = s.seg_state;
+  w.inter_scale = c.scale; w.k_scale = 1.0f; w.transposed = true; w.init = s_in; w.cut_state = s.cut_state;
   w.out = part ? part : dq; w.ldo = (int64_t)c.n_heads * c.d_k; w.out_f32 = part != nullptr;
   if (launch_walk<false>(c, w, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
   if (part && launch_sum(c, part, dq, *seqs, st) != cudaSuccess) return ROM_ERR_CUDA;
@@ -554,7 +602,7 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   r.q = k; r.k = q; r.v = dout; r.ldq = ldk; r.ldk = ldq; r.ldv = (int64_t)c.n_heads * c.d_v;
   r.qdiv = r.kdiv = share; r.vdiv = 1; r.dk = c.d_k; r.dv = c.d_v;
   r.inter_scale = 1.0f; r.k_scale = c.scale; r.reverse = true; r.init = ds_out; r.init_all = true; r.early = true; r.last = ds_in;
-  r.seg_state = reinterpret_cast<float*>(W + lay.seg_b);
+  r.cut_state = reinterpret_cast<float*>(W + lay.cut_b);
   r.out = dv; r.ldo = lddv;
   if (launch_states(c, r, *seqs, cut, st) != cudaSuccess || launch_walk<false>(c, r, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
   // dk

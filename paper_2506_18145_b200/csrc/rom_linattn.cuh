@@ -5,17 +5,18 @@
 //   dq        (q, k, v) = (dout, v, k)        out = dq   (scaled on output; its state is the forward's, transposed)
 //   dv        (q, k, v) = (k, q, dout)        out = dv   backwards, ks = scale; the state starts from ds_out, which meets the last row undecayed
 //   dk        (q, k, v) = (v, dout, q)        out = dk   backwards; the state of dv's walk, transposed
-// The packed rows are cut into segments of equal length whatever sequences they hold.  Launch 1 (state only) walks in each segment the rows of the
-// sequence that reaches over its far end, launch 2 chains those states from segment to segment, launch 3 walks every segment's rows from the states
-// that reach it.
+// The packed rows of all heads, one head behind the other, are cut into equal runs of chunks, one per block, whatever sequences they hold.  Launch 1 (state only)
+// walks for each cut inside a head the rows of the sequence that reaches over it, up to the cut before; launch 2 chains those states from cut to cut; launch 3
+// walks every run from the states that reach it.
 #pragma once
 
 #include "rom_serve.cuh"
 
 namespace rom {
 
-constexpr int kLinMaxDim = 128;      // of q, k, v and the state, each way
-constexpr int kLinMaxSegs = 512;
+constexpr int kLinMaxDim = 128;        // of q, k, v and the state, each way
+constexpr int kLinMaxBlocks = 296;     // runs, where there are cuts inside heads
+constexpr int kLinPowers = 132;        // lambda^0 .. lambda^128 of a head as fp32, and as many of what each lost (two rows of a table in the workspace)
 
 struct LinPass {
   const void *q, *k, *v;
@@ -30,20 +31,67 @@ struct LinPass {
   bool init_all;                   // every sequence starts from it (else: those that resume)
   bool early;                      // it meets the first row undecayed, and the state left at the end is decayed once more
   float* last;                     // pool of the states left at the end (a sequence that does not resume leaves zeros when init_all), or null
-  float* seg_state;                // [segments, H, state]: launch 1 writes, launch 2 chains in place, launch 3 reads; [b - 1] belongs to the cut before segment b
-  float* init_copy;                // [segments, H, state] or null: initial states of sequences that start in a segment and reach over its end (pools in place)
+  const float* powers;             // [H][2][kLinPowers]
+  float* cut_state;                // [cuts, state]: launch 1 writes, launch 2 chains in place, launch 3 reads; [i - 1] belongs to the cut before run i
+  float* init_copy;                // [cuts, state] or null: initial states of sequences that start in run i - 1 and reach over the cut before run i (pools in place)
   void* out;
   int64_t ldo;
   bool out_f32;                    // out is fp32 whatever the storage type
   int32_t* status;
 };
 
-struct LinCut { int seg_rows, n_seg; };
-
+// Run i of `blocks` is the chunks [units i / blocks, units (i + 1) / blocks) of all heads' chunks.
+struct LinCut {
+  int chunk, per_head;             // rows of a chunk; chunks of a head
+  int blocks;
+  long long units;                 // heads * per_head
+  bool inside;                     // there are cuts inside heads
+  __host__ __device__ __forceinline__ long long bound(int i) const { return units * i / blocks; }
+};
+// What a run has of one head: rows [a, b).
+struct LinItem {
+  long long u, u1;                 // next chunk, end of the run
+  int head, a, b;
+  bool last;                       // b is the head's end
+  __device__ __forceinline__ LinItem(const LinCut& c, int run) : u(c.bound(run)), u1(c.bound(run + 1)) {}
+  __device__ __forceinline__ bool next(const LinCut& c, int rows) {
+    if (u >= u1) return false;
+    head = (int)(u / c.per_head);
+    const int c0 = (int)(u - (long long)head * c.per_head), c1 = (int)min((long long)c.per_head, c0 + (u1 - u));
+    a = c0 * c.chunk;
+    last = c1 == c.per_head;
+    b = last ? rows : c1 * c.chunk;
+    u += c1 - c0;
+    return true;
+  }
+};
+// The cut before run i: its head and row; row 0: it lies between two heads.
+__device__ __forceinline__ void lin_cut_at(const LinCut& c, int i, int& head, int& row) {
+  const long long u = c.bound(i);
+  head = (int)(u / c.per_head);
+  row = (int)(u - (long long)head * c.per_head) * c.chunk;
+}
 // Whether a sequence reaches over the cut before row r (0 < r < rows), and which.  All lanes of a warp call it.
 __device__ __forceinline__ int lin_spanning(const Ragged& seqs, int r) {
   const int s = seqs.first_from(r) - 1;
   return s >= 0 && seqs.end_of(s) > r ? s : -1;
+}
+// The rows that launch 1 walks for the cut before run i (1 <= i < blocks): those of the sequence that reaches over it, back to the cut before or, backwards, on to
+// the next one.  False: nothing reaches over it.  All lanes of a warp call it.
+__device__ __forceinline__ bool lin_cut_rows(const LinCut& c, int i, bool reverse, const Ragged& seqs, int& head, int& r0, int& r1) {
+  int row, h2, near;
+  lin_cut_at(c, i, head, row);
+  const int s = row > 0 ? lin_spanning(seqs, row) : -1;
+  if (s < 0) return false;
+  lin_cut_at(c, reverse ? i + 1 : i - 1, h2, near);
+  if (reverse) {
+    r0 = row;
+    r1 = min(seqs.end_of(s), h2 == head ? near : seqs.rows);
+  } else {
+    r0 = max(seqs.start_of(s), h2 == head ? near : 0);
+    r1 = row;
+  }
+  return r1 > r0;
 }
 __device__ __forceinline__ const float* lin_init_of(const LinPass& p, const Ragged& seqs, int s, int head) {
   const int slot = seqs.slot_of(s);

@@ -8,7 +8,7 @@
 // Roundings: P and the S that a chunk meets are bf16 (half a step each, of separate parts of the sum); K~ is hi + lo, two bf16 numbers, in two matrix products, since
 // the state is an fp32 result that many chunks add up in.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
 //
-// One CTA per SM walks one head of one segment of the packed rows.  640 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
+// One CTA per SM walks one run of chunks.  640 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
 // width), warp 1 the matrix products, warps 4..11 turn scores into P and O1, O2 into output rows, warps 12..19 scale K in place (K~ hi; lo beside it), and keep S; two
 // warps share each 32-lane quarter of tensor memory and take half of the columns each.  The scores' tensor memory is reused for P.
 //
@@ -102,10 +102,11 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) { asm volatile("st.s
 __host__ __device__ constexpr uint32_t lt_idesc(int n, bool a_mn, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
-// An MN-major tile of 64-column boxes of 128 rows: as make_smem_desc_mn, the next 64 columns one box further.  (An operand of 128 columns that has one box alone reads
-// the 16 KB behind it, which are other tiles of this block, into accumulator lanes that nobody reads.)
+// An MN-major tile of 64-column boxes: as make_smem_desc_mn, the next 64 columns one box further.  (An operand of 128 columns that has one box alone reads
+// the box behind it, which is other tiles of this block, into accumulator lanes that nobody reads.)
+template <int BOX>
 __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
-  return (uint64_t)((saddr & 0x3ffffu) >> 4) | (uint64_t)(LT_BOX >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+  return (uint64_t)((saddr & 0x3ffffu) >> 4) | (uint64_t)(BOX >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
 __device__ __forceinline__ float ld_state(const float* p) { float v; asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p)); return v; }
@@ -170,15 +171,16 @@ __device__ __forceinline__ void store_rows128(char* row_at, int64_t pitch, int r
     if (piece_ok && t < rows) *reinterpret_cast<uint4*>(row_at + t * pitch) = make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
 }
 // V^T K~: hi and lo, the first ks steps of 16 rows.
+template <int BOX>
 __device__ __forceinline__ void issue_state(uint32_t tmem_d, uint32_t v, uint32_t khi, uint32_t klo, uint32_t idesc, int ks, bool accumulate) {
-  const uint64_t a = desc_mn(v), h = desc_mn(khi), l = desc_mn(klo);
+  const uint64_t a = desc_mn<BOX>(v), h = desc_mn<BOX>(khi), l = desc_mn<BOX>(klo);
   for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), h + (uint64_t)(MN_KSTEP * k), idesc, accumulate || k > 0 ? 1u : 0u);
   for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), l + (uint64_t)(MN_KSTEP * k), idesc, 1u);
 }
-template <int BOXES>
+template <int BOXES, int BOX = LT_BOX>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
 #pragma unroll
-  for (int b = 0; b < BOXES; ++b) tma_load_3d(dst + b * LT_BOX, map, bar, 64 * b, head, row);
+  for (int b = 0; b < BOXES; ++b) tma_load_3d(dst + b * BOX, map, bar, 64 * b, head, row);
 }
 __device__ __forceinline__ void latch(const LinPass& p, volatile int* abort_flag, int where) {
   if (!*abort_flag) {
@@ -188,7 +190,7 @@ __device__ __forceinline__ void latch(const LinPass& p, volatile int* abort_flag
   *abort_flag = 1;
 }
 
-// The rows [r0, r1) of one sequence in one segment, in chunks.
+// The rows [r0, r1) of one sequence in one run, in chunks.
 struct LinPiece {
   int s, r0, r1;
   bool over;             // the state comes over a cut
@@ -200,31 +202,28 @@ struct LinPiece {
     else { row0 = r0 + LT_C * m; len = min(LT_C, r1 - row0); }
   }
 };
-struct LinSegment {
-  int a, b, seg;
-  bool last;
-  __device__ __forceinline__ LinSegment(const Ragged& q, int seg_, int seg_rows, int n_seg) : a(seg_ * seg_rows), b(min(a + seg_rows, q.rows)), seg(seg_), last(seg_ + 1 == n_seg) {}
-  __device__ __forceinline__ int first(const Ragged& q) const {      // all lanes of a warp
-    const int s = q.first_from(a);
-    return s > 0 && q.end_of(s - 1) > a ? s - 1 : s;
-  }
-  // false: no sequence from s on is of this segment
-  template <bool REV>
-  __device__ __forceinline__ bool piece(const Ragged& q, int s, LinPiece& x) const {
-    if (s >= q.n_seq) return false;
-    const int st = q.start_of(s), en = q.end_of(s);
-    if (st >= b && !last) return false;
-    const bool empty = en <= st;
-    x.s = s;
-    x.r0 = max(st, a);
-    x.r1 = empty ? x.r0 : max(min(en, b), x.r0);
-    x.over = !empty && (REV ? en > b : st < a);
-    x.ends = empty || (x.r1 > x.r0 && (REV ? st >= a : en <= b));
-    return true;
-  }
-};
+// The pieces of a run's rows of one head.
+__device__ __forceinline__ int first_piece(const LinItem& it, const Ragged& q) {      // all lanes of a warp
+  const int s = q.first_from(it.a);
+  return s > 0 && q.end_of(s - 1) > it.a ? s - 1 : s;
+}
+template <bool REV>
+__device__ __forceinline__ bool get_piece(const LinItem& it, const Ragged& q, int s, LinPiece& x) {      // false: no sequence from s on has to do with these rows
+  if (s >= q.n_seq) return false;
+  const int st = q.start_of(s), en = q.end_of(s);
+  if (st >= it.b && !it.last) return false;
+  const bool empty = en <= st;
+  x.s = s;
+  x.r0 = max(st, it.a);
+  x.r1 = empty ? x.r0 : max(min(en, it.b), x.r0);
+  x.over = !empty && (REV ? en > it.b : st < it.a);
+  x.ends = empty || (x.r1 > x.r0 && (REV ? st >= it.a : en <= it.b));
+  return true;
+}
 
 // ------------------------------------------------------------------------------------------------------------------------------ the walk
+// A wait that gives up ends the waits of its warp, not its loop: the warps that meet at named barriers (a quarter's two, each role's eight) all come to every one of
+// them, and only the results are left out.
 template <int KP, int VP>
 struct WalkShape {
   static constexpr int KB = KP / 64, VB = VP / 64;
@@ -234,7 +233,7 @@ struct WalkShape {
   static constexpr int SC = 0, O1 = 128, KV = O1 + VP, O2 = KV + KP;      // tensor-memory columns (P over the scores' first 64)
 };
 
-// Rows of O2 that are not finite, summed again: out = f O1 + sum over their own and earlier rows.  Rare; all lanes of the warp call it.
+// Rows of O2 that are not finite, summed again over their own and earlier rows.  Rare; all lanes of the warp call it.
 template <bool REV>
 __device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf16* k, const bf16* v, bf16* out, uint32_t taddr_o1, const float* lam, int i, int row0, int len, float f,
                                        bool mine, int head, int c_from, int c_to) {
@@ -246,13 +245,13 @@ __device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf
     if (!mine) continue;
     float acc[32];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) acc[e] = f * __uint_as_float(r[e]);
+    for (int e = 0; e < 32; ++e) acc[e] = 0.0f;
     const bf16* qi = q + (int64_t)(row0 + i) * p.ldq;
     for (int j = REV ? i : 0; j < (REV ? len : i + 1); ++j) {
       const bf16* kj = k + (int64_t)(row0 + j) * p.ldk;
       float s = 0.0f;
       for (int d = 0; d < p.dk; ++d) s = fmaf(to_f32(qi[d]), to_f32(kj[d]), s);
-      const float w = to_f32(__float2bfloat16_rn(s * p.p_scale * lam[REV ? j - i : i - j]));
+      const float w = to_f32(__float2bfloat16_rn(s * lam[REV ? j - i : i - j]));
       const bf16* vj = v + (int64_t)(row0 + j) * p.ldv + c0;
 #pragma unroll
       for (int e = 0; e < 32; ++e)
@@ -262,8 +261,9 @@ __device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf
 #pragma unroll
     for (int e = 0; e < 32; ++e)
       if (c0 + e < p.dv) {
-        if (p.out_f32) reinterpret_cast<float*>(out)[to + e] = acc[e];
-        else out[to + e] = __float2bfloat16_rn(acc[e]);
+        const float o = fmaf(f, __uint_as_float(r[e]), p.p_scale * acc[e]);
+        if (p.out_f32) reinterpret_cast<float*>(out)[to + e] = o;
+        else out[to + e] = __float2bfloat16_rn(o);
       }
   }
 }
@@ -271,17 +271,17 @@ __device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf
 template <int KP, int VP, bool REV>
 __global__ void __launch_bounds__(LT_WALK_THREADS, 1)
 lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs,
-            int seg_rows, int n_seg, uint32_t wait_limit, uint32_t stall) {
+            const LinCut cut, uint32_t wait_limit, uint32_t stall) {
   using W = WalkShape<KP, VP>;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(16) float lam_pad[32 + LT_C + 4], lam_lo[LT_C + 4];      // lambda^0.. behind 32 zeros; what each lost to fp32
-  float* const lam = lam_pad + 32;
+  // powers of lambda: of the warps that make P (behind 32 zeros), of those that keep S, with what each lost to fp32
+  __shared__ __align__(16) float p_pad[32 + kLinPowers], s_lam[kLinPowers], s_lo[kLinPowers];
   __shared__ __align__(8) unsigned long long bars[24];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), head = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), run = blockIdx.x;
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
   // full: copies have landed; empty: the matrix products that read them are done; the others by name
   auto q_full = [&](int s) { return bar(s); };
@@ -299,30 +299,34 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(LT_TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
-  if (tid <= LT_C) {
-    const double l = exp((double)__ldg(p.log_decay + head) * tid);
-    lam[tid] = (float)l;
-    lam_lo[tid] = (float)(l - (double)lam[tid]);
-  }
-  if (tid < 32) lam_pad[tid] = 0.0f;
+  if (tid < 32) p_pad[tid] = 0.0f;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  pdl_trigger();                       // (behind the block's tensor memory: the successor takes its own before it waits)
   const uint32_t tmem = tmem_s;
-  const LinSegment seg(seqs, blockIdx.y, seg_rows, n_seg);
-  const int s_first = seg.first(seqs);
+  // Here the launch before may still run (launch 2, or the powers): inputs and the sequences' tables are older than it.  What it writes (states, powers) is read, and what
+  // it may read or what its own predecessors may write (pools, outputs) is written, by warps that have waited for it.
+  LinItem it(cut, run);
   LinPiece x;
   int n = 0;                           // chunks so far
 
+  // Rows of the last quarter (backwards: the first) have four blocks of scores to turn into P, those of the first one: the copies' and products' warps poll on the
+  // schedulers of the light quarters.
+  constexpr int COPIES = REV ? 3 : 0, PRODUCTS = REV ? 2 : 1;
   // (setmaxnreg inside each role's branch: behind a join the compiler would hold every role to the fewest)
-  if (warp == 0) {
+  if (warp == COPIES) {
     registers_down<LT_FEW>();
     // ---------------------------------------------------------------- copies
-    if (elect_one()) {
-      bool ok = true;
-      for (int s = s_first; ok && seg.piece<REV>(seqs, s, x); ++s)
+    const bool leader = elect_one();
+    bool ok = true;
+    while (it.next(cut, seqs.rows)) {
+      const int head = it.head, s_first = first_piece(it, seqs);
+      if (leader)
+      for (int s = s_first; ok && get_piece<REV>(it, seqs, s, x); ++s) {
+        if (!x.over) {                 // the state that the piece starts from, into L2 while the pieces before are walked
+          const float* from = lin_init_of(p, seqs, s, head);
+          if (from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(p.dk * p.dv * sizeof(float))) : "memory");
+        }
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
@@ -335,6 +339,10 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           mbar_expect_tx(q_full(qs), W::KB * LT_BOX);
           load_tile<W::KB>(base + W::Q + qs * W::KB * LT_BOX, &tmap_q, q_full(qs), head / p.qdiv, row0);
         }
+      }
+      __syncwarp();
+    }
+    if (leader) {
       if (!ok) latch(p, abort_flag, 51);
       if (*abort_flag)                 // the copies still in flight land (bounded) before the block ends
         for (int i = 1; i <= W::KVST && i <= n; ++i) {
@@ -344,14 +352,17 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         }
     }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp == PRODUCTS) {
     registers_down<LT_FEW>();
     // ---------------------------------------------------------------- matrix products
-    if (elect_one()) {
+    const bool leader = elect_one();
+    bool ok = true, issued = false;
+    while (it.next(cut, seqs.rows)) {
+      const int s_first = first_piece(it, seqs);
       constexpr uint32_t d_sc = lt_idesc(LT_C, false, false), d_o1 = lt_idesc(VP, false, false), d_o2 = lt_idesc(VP, false, true), d_kv = lt_idesc(KP, true, true);
-      bool ok = true, issued = false;
       auto wait = [&](uint32_t b, uint32_t parity) { ok = ok && mbar_wait(b, parity, abort_flag, wait_limit); return ok; };
-      for (int s = s_first; ok && seg.piece<REV>(seqs, s, x); ++s)
+      if (leader)
+      for (int s = s_first; ok && get_piece<REV>(it, seqs, s, x); ++s)
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
@@ -382,12 +393,15 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           const bool p_in = mbar_ready(p_ready, ph), k_in = mbar_ready(k_ready, ph);
           if (!(p_in && k_in) && (!wait(p_ready, ph) || !wait(k_ready, ph))) break;
           tc_fence_after();
-          for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 8 * e, desc_mn(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
+          for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 8 * e, desc_mn<LT_BOX>(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
           umma_commit(pv_full);
-          issue_state(tmem + W::KV, v, k, base + W::LO, d_kv, ks, false);
+          issue_state<LT_BOX>(tmem + W::KV, v, k, base + W::LO, d_kv, ks, false);
           umma_commit(state_full);
           umma_commit(kv_empty(st));
         }
+      __syncwarp();
+    }
+    if (leader) {
       if (!ok) latch(p, abort_flag, 52);
       if (*abort_flag && issued) {     // what has been issued may still read shared memory and write tensor memory
         umma_commit(drain);
@@ -400,14 +414,21 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     const int quarter = warp & 3, half = (warp - 4) >> 2, i = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     bf16* out = static_cast<bf16*>(p.out);
+    const float* lam = p_pad + 32;
+    pdl_wait();
     bool ok = true;
-    for (int s = s_first; ok && seg.piece<REV>(seqs, s, x); ++s)
+    while (it.next(cut, seqs.rows)) {
+    const int head = it.head, s_first = first_piece(it, seqs);
+    asm volatile("bar.sync 5, 256;" ::: "memory");      // (all of these warps are done with the powers of the head before)
+    for (int e = tid - 128; e < kLinPowers; e += 256) p_pad[32 + e] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + e);
+    asm volatile("bar.sync 5, 256;" ::: "memory");
+    for (int s = s_first; get_piece<REV>(it, seqs, s, x); ++s)
       for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
         int row0, len;
         x.chunk<REV>(m, row0, len);
         const uint32_t ph = n & 1;
         const int early = m == 0 && !x.over && p.early ? 1 : 0, blocks = (len + 31) / 32;
-        if (!(ok = warp_wait(sc_full, ph, abort_flag, wait_limit))) break;
+        ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit);
         tc_fence_after();
         // blocks half and half + 2 of 32 columns; P lies over the scores, so both warps of the quarter have read theirs before either writes
         uint32_t w[2][16];
@@ -422,29 +443,31 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           uint32_t r[32];
           tmem_ld32_issue(lanes + W::SC + 32 * b, r);
           tmem_ld_wait(r);
+          // a masked score is times 0; in the last chunk, whose other rows are not the sequence's, it is selected 0 (elsewhere, where it is not finite, the row is
+          // summed again below).  A pass of its own: tests among the loads of the powers left each to wait for its own, 75 cycles a place.
+          if (len < LT_C) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int j = 32 * b + e;
+              if (REV ? j < i || j >= len : j > i) r[e] = 0;
+            }
+          }
           if (b == quarter) {
+            const float* l = REV ? lam - lane : lam + lane;
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float* l = REV ? lam - lane + e : lam + lane - e;
-              const bool on0 = REV ? e >= lane && 32 * b + e < len : lane >= e, on1 = REV ? e + 1 >= lane && 32 * b + e + 1 < len : lane >= e + 1;
-              const float2 x = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(make_float2(l[0], l[REV ? 1 : -1]), make_float2(p.p_scale, p.p_scale)));
-              w[t][e / 2] = pack2(on0 ? x.x : 0.0f, on1 ? x.y : 0.0f);
+              const float2 y = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), REV ? make_float2(l[e], l[e + 1]) : make_float2(l[-e], l[-e - 1]));
+              w[t][e / 2] = pack2(y.x, y.y);
             }
           } else {
             // lambda^{i-j} = lambda^{i - last of the block} lambda^{last - j}
-            const float f = p.p_scale * lam[REV ? 32 * b - i : i - 32 * b - 31];
-            const bool whole = !REV || 32 * b + 32 <= len;
+            const float f = lam[REV ? 32 * b - i : i - 32 * b - 31];
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const float4 u = *reinterpret_cast<const float4*>(lam + (REV ? e : 28 - e));
               const float2 u0 = REV ? make_float2(u.x, u.y) : make_float2(u.w, u.z), u1 = REV ? make_float2(u.z, u.w) : make_float2(u.y, u.x);
-              float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(f, f)));
-              float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(f, f)));
-              if (REV && !whole) {
-                const int j = 32 * b + e;
-                p0 = make_float2(j < len ? p0.x : 0.0f, j + 1 < len ? p0.y : 0.0f);
-                p1 = make_float2(j + 2 < len ? p1.x : 0.0f, j + 3 < len ? p1.y : 0.0f);
-              }
+              const float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(f, f)));
+              const float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(f, f)));
               w[t][e / 2] = pack2(p0.x, p0.y);
               w[t][e / 2 + 1] = pack2(p1.x, p1.y);
             }
@@ -456,13 +479,13 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         warp_arrive(p_ready);
-        if (!(ok = warp_wait(pv_full, ph, abort_flag, wait_limit))) break;
+        ok = ok && warp_wait(pv_full, ph, abort_flag, wait_limit);
         tc_fence_after();
         const bool mine = i < len;
         const float f = p.inter_scale * lam[REV ? max(len - i - early, 0) : i + 1 - early];
         float2 odd = make_float2(0.0f, 0.0f);
-        const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + (lane & 24), rows = len - first;      // (rows that the lane stores)
-        // 16 columns: f O1 + O2, noting what is not finite
+        const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + (lane & 24), rows = ok ? len - first : 0;      // (rows that the lane stores)
+        // 16 columns: f O1 + p O2, noting what is not finite
         auto columns = [&](int c, float2 (&o)[8]) {
           uint32_t r1[16], r2[16];
           __syncwarp();
@@ -474,7 +497,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           for (int e = 0; e < 8; ++e) {
             const float2 b2 = make_float2(__uint_as_float(r2[2 * e]), __uint_as_float(r2[2 * e + 1]));
             odd = __ffma2_rn(b2, make_float2(0.0f, 0.0f), odd);
-            o[e] = __ffma2_rn(make_float2(__uint_as_float(r1[2 * e]), __uint_as_float(r1[2 * e + 1])), make_float2(f, f), b2);
+            o[e] = __ffma2_rn(make_float2(__uint_as_float(r1[2 * e]), __uint_as_float(r1[2 * e + 1])), make_float2(f, f), __fmul2_rn(b2, make_float2(p.p_scale, p.p_scale)));
           }
         };
         if (p.out_f32) {
@@ -503,13 +526,14 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           const int col = c_from + 8 * (lane & 7);
           store_rows128(reinterpret_cast<char*>(out + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 2, rows, (VP == 128 || (lane & 7) < 4) && col < p.dv, w, lane);
         }
-        const bool again = mine && !(odd.x == 0.0f && odd.y == 0.0f);
+        const bool again = ok && mine && !(odd.x == 0.0f && odd.y == 0.0f);
         if (__any_sync(0xffffffffu, again))
           slow_rows<REV>(p, static_cast<const bf16*>(p.q) + (int64_t)(head / p.qdiv) * p.dk, static_cast<const bf16*>(p.k) + (int64_t)(head / p.kdiv) * p.dk,
                          static_cast<const bf16*>(p.v) + (int64_t)(head / p.vdiv) * p.dv, out, lanes + W::O1, lam, i, row0, len, f, again, head, c_from, c_to);
         tc_fence_before();
         warp_arrive(o_free);
       }
+    }
     if (!ok) latch(p, abort_flag, 53);
   } else if (warp >= 12) {
     registers_up<LT_MANY>();
@@ -519,6 +543,9 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     const size_t state = (size_t)p.dk * p.dv;
     float S[KH];
+    const float *lam = s_lam, *lam_lo = s_lo;
+    pdl_wait();
+    pdl_trigger();                     // (behind the block's tensor memory: the successor takes its own before it waits)
     bool ok = true;
     auto write_s = [&]() {      // bf16 rows of S^T, K-major
       if (c < VP)
@@ -529,22 +556,47 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
       fence_async();
       warp_arrive(s_ready);
     };
-    for (int s = s_first; ok && seg.piece<REV>(seqs, s, x); ++s) {
+    while (it.next(cut, seqs.rows)) {
+    const int head = it.head, s_first = first_piece(it, seqs);
+    asm volatile("bar.sync 6, 256;" ::: "memory");
+    for (int e = tid - 384; e < 2 * kLinPowers; e += 256) (e < kLinPowers ? s_lam : s_lo - kLinPowers)[e] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + e);
+    asm volatile("bar.sync 6, 256;" ::: "memory");
+    for (int s = s_first; get_piece<REV>(it, seqs, s, x); ++s) {
       const int mm = x.chunks(), slot = seqs.slot_of(s);
       const float* from = lin_init_of(p, seqs, s, head);
-      if (x.over) from = p.seg_state + ((size_t)(REV ? seg.seg : seg.seg - 1) * p.H + head) * state;
-      else if (!REV && mm > 0 && from && p.init_copy && !x.ends) from = p.init_copy + ((size_t)seg.seg * p.H + head) * state;
+      if (x.over) from = p.cut_state + (size_t)(REV ? run : run - 1) * state;
+      else if (!REV && mm > 0 && from && p.init_copy && !x.ends) from = p.init_copy + (size_t)run * state;
       if (mm == 0 && !x.ends) continue;
       // (every load at a valid address and selected afterwards: one by one behind branches they took 10000 cycles)
       const bool mine = from != nullptr && c < p.dv;
       if (from) {
         const int col = min(c, p.dv - 1);
         if (p.transposed) {
+          // rows of the memory are columns of S^T's rows: 32 rows x 16 columns at a time are read whole and change lanes through the (idle) space of K~'s low halves
           float4 v[KH / 4];
 #pragma unroll
-          for (int a = 0; a < KH; a += 4) v[a / 4] = ld_state4(from + (size_t)col * p.dk + min(a0 + a, p.dk - 4));
+          for (int g = 0; g < KH / 16; ++g)
 #pragma unroll
-          for (int a = 0; a < KH; a += 4) { S[a] = v[a / 4].x; S[a + 1] = v[a / 4].y; S[a + 2] = v[a / 4].z; S[a + 3] = v[a / 4].w; }
+            for (int u = 0; u < 4; ++u)
+              v[4 * g + u] = ld_state4(from + (size_t)min(quarter * 32 + 8 * u + lane / 4, p.dv - 1) * p.dk + min(a0 + 16 * g + 4 * (lane & 3), p.dk - 4));
+          const uint32_t mine_at = base + W::LO + (warp - 12) * 2048;
+#pragma unroll
+          for (int g = 0; g < KH / 16; ++g) {
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int row = 8 * u + lane / 4;
+              const float4 x4 = v[4 * g + u];
+              sts128(mine_at + row * 64 + (((lane & 3) ^ (row >> 1 & 3)) << 4), make_uint4(__float_as_uint(x4.x), __float_as_uint(x4.y), __float_as_uint(x4.z), __float_as_uint(x4.w)));
+            }
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const uint4 x4 = lds128(mine_at + lane * 64 + ((u ^ (lane >> 1 & 3)) << 4));
+              S[16 * g + 4 * u] = __uint_as_float(x4.x); S[16 * g + 4 * u + 1] = __uint_as_float(x4.y);
+              S[16 * g + 4 * u + 2] = __uint_as_float(x4.z); S[16 * g + 4 * u + 3] = __uint_as_float(x4.w);
+            }
+          }
         } else {
 #pragma unroll
           for (int a = 0; a < KH; ++a) S[a] = ld_state(from + (size_t)min(a0 + a, p.dk - 1) * p.dv + col);
@@ -560,8 +612,8 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         const int st = n % W::KVST, early = m == 0 && !x.over && p.early ? 1 : 0, rows16 = (len + 15) / 16 * 16;
         const uint32_t ph = n & 1, k = base + W::K + st * W::KB * LT_BOX, box = KP == 128 ? half * LT_BOX : 0;
         // (the scores are made of this K: sc_full says that it has landed, but the copies' own barrier makes them visible)
-        if (!(ok = warp_wait(sc_full, ph, abort_flag, wait_limit) && (__all_sync(0xffffffffu, mbar_ready(kv_full(st), n / W::KVST & 1)) || warp_wait(kv_full(st), n / W::KVST & 1, abort_flag, wait_limit))))
-          break;
+        ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit) &&
+             (__all_sync(0xffffffffu, mbar_ready(kv_full(st), n / W::KVST & 1)) || warp_wait(kv_full(st), n / W::KVST & 1, abort_flag, wait_limit));
         if (c < rows16) {
           const bool live = c < len;
           const float w = live ? p.k_scale * lam[REV ? c : len - 1 - c] : 0.0f;
@@ -570,7 +622,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         }
         fence_async();
         warp_arrive(k_ready);
-        if (!(ok = warp_wait(state_full, ph, abort_flag, wait_limit))) break;
+        ok = ok && warp_wait(state_full, ph, abort_flag, wait_limit);
         tc_fence_after();
         const float f = lam[len - early], fl = lam_lo[len - early];
 #pragma unroll
@@ -589,8 +641,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         tc_fence_before();
         if (m + 1 < mm) write_s();
       }
-      if (!ok) break;
-      if (p.last && slot >= 0 && x.ends && c < p.dv) {
+      if (ok && p.last && slot >= 0 && x.ends && c < p.dv) {
         const bool none = p.init_all && !seqs.resumes(s);
         const float f = mm > 0 && p.early ? lam[1] : 1.0f;
         float* to = p.last + ((size_t)slot * p.H + head) * state + c;
@@ -600,6 +651,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
 #pragma unroll
             for (int e = 0; e < 8; ++e) to[(size_t)(a0 + a + e) * p.dv] = none ? 0.0f : f * S[a + e];
       }
+    }
     }
     if (!ok) latch(p, abort_flag, 54);
   } else {
@@ -612,13 +664,13 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
 }
 
 // ------------------------------------------------------------------------------------------------------------------------------ launch 1: states at the cuts
-// sum over a segment's rows of the sequence that reaches over its far end, lambda^{distance to that end} ks k_j v_j^T: every row's weight is known, so all chunks add
-// up in tensor memory.  Warps 2..9 scale K, two to a row.
+// sum over the rows between two cuts of the sequence that reaches over the far one, lambda^{distance to that cut} ks k_j v_j^T: every row's weight is known, so all of
+// them add up in tensor memory, in steps of 64 rows.  Warps 2..9 scale K, four threads to a row.
 template <int KP, int VP>
 struct StateShape {
-  static constexpr int KB = KP / 64, VB = VP / 64;
-  static constexpr int STAGE = (2 * KB + VB) * LT_BOX, LO = KB * LT_BOX, V = 2 * KB * LT_BOX;      // K (hi) | lo | V
-  static constexpr int STAGES = KP == 128 ? 2 : 3, BYTES = STAGES * STAGE + (VB == 1 ? LT_BOX : 0);      // (see desc_mn: one box behind the last V)
+  static constexpr int KB = KP / 64, VB = VP / 64, ROWS = 64, BOX = 64 * ROWS * 2;
+  static constexpr int STAGE = (2 * KB + VB) * BOX, LO = KB * BOX, V = 2 * KB * BOX;      // K (hi) | lo | V
+  static constexpr int STAGES = 196608 / STAGE, BYTES = STAGES * STAGE + (VB == 1 ? BOX : 0);      // (see desc_mn: one box behind the last V)
 };
 constexpr int kLtMaxSmem = 232448 - 2048;      // what a block may ask for, less its static variables
 static_assert(WalkShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && WalkShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && WalkShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
@@ -626,26 +678,29 @@ static_assert(StateShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && StateShape<128
 
 template <int KP, int VP, bool REV>
 __global__ void __launch_bounds__(LT_STATE_THREADS, 1)
-lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs, int seg_rows, uint32_t wait_limit, uint32_t stall) {
+lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs, const LinCut cut, uint32_t wait_limit, uint32_t stall) {
   using W = StateShape<KP, VP>;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(8) unsigned long long bars[3 * 3 + 2];
+  __shared__ __align__(8) unsigned long long bars[3 * 8 + 2];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), head = blockIdx.x, seg = REV ? blockIdx.y + 1 : blockIdx.y;
-  pdl_wait();
-  const int a = seg * seg_rows, b = min(a + seg_rows, seqs.rows), s = lin_spanning(seqs, REV ? a : b);
-  if (s < 0) return;
-  const int r0 = REV ? a : max(seqs.start_of(s), a), r1 = REV ? min(seqs.end_of(s), b) : b, chunks = (r1 - r0 + LT_C - 1) / LT_C;
-  if (r1 <= r0) return;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  // The launch before may still run.  It (the powers, or a walk of the backward pass before this one) writes no input and reads none of what this one writes (its
+  // own predecessors, which may have, are complete); only the launches behind this one count on it being complete once this one is: every block waits before it ends.
+  int head, r0, r1;
+  if (!lin_cut_rows(cut, blockIdx.x + 1, REV, seqs, head, r0, r1)) { pdl_wait(); return; }
+  const int chunks = (r1 - r0 + W::ROWS - 1) / W::ROWS;
+  static_assert(W::STAGES <= 8, "barriers");
+  // the rows that launch 3 begins with last: they are still in L2 when it comes
+  auto step = [&](int n) { return REV ? n : chunks - 1 - n; };
   auto full = [&](int i) { return smem_u32(&bars[i]); };
-  auto empty = [&](int i) { return smem_u32(&bars[3 + i]); };
-  auto scaled = [&](int i) { return smem_u32(&bars[6 + i]); };
-  const uint32_t done = smem_u32(&bars[9]), drain = smem_u32(&bars[10]);
+  auto empty = [&](int i) { return smem_u32(&bars[8 + i]); };
+  auto scaled = [&](int i) { return smem_u32(&bars[16 + i]); };
+  const uint32_t done = smem_u32(&bars[24]), drain = smem_u32(&bars[25]);
   if (tid == 0) {
-    for (int i = 0; i < 3; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); mbar_init(scaled(i), 8); }
+    for (int i = 0; i < 8; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); mbar_init(scaled(i), 8); }
     mbar_init(done, 1);
     mbar_init(drain, 1);
     abort_s = 0;
@@ -669,9 +724,9 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
         const int st = n % W::STAGES;
         const uint32_t at = base + st * W::STAGE;
         if (!mbar_wait(empty(st), (n / W::STAGES & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
-        mbar_expect_tx(full(st), (W::KB + W::VB) * LT_BOX + stall);
-        load_tile<W::KB>(at, &tmap_k, full(st), head / p.kdiv, r0 + LT_C * n);
-        load_tile<W::VB>(at + W::V, &tmap_v, full(st), head / p.vdiv, r0 + LT_C * n);
+        mbar_expect_tx(full(st), (W::KB + W::VB) * W::BOX + stall);
+        load_tile<W::KB, W::BOX>(at, &tmap_k, full(st), head / p.kdiv, r0 + W::ROWS * step(n));
+        load_tile<W::VB, W::BOX>(at + W::V, &tmap_v, full(st), head / p.vdiv, r0 + W::ROWS * step(n));
       }
       if (!ok) latch(p, abort_flag, 55);
       if (*abort_flag)
@@ -687,7 +742,7 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
         const uint32_t at = base + st * W::STAGE;
         if (!mbar_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
         tc_fence_after();
-        issue_state(tmem, at + W::V, at, at + W::LO, lt_idesc(KP, true, true), (min(LT_C, r1 - r0 - LT_C * n) + 15) / 16, n > 0);
+        issue_state<W::BOX>(tmem, at + W::V, at, at + W::LO, lt_idesc(KP, true, true), (min(W::ROWS, r1 - r0 - W::ROWS * step(n)) + 15) / 16, n > 0);
         umma_commit(empty(st));
         issued = true;
       }
@@ -700,26 +755,29 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
     }
     __syncwarp();
   } else {
-    const int half = (warp - 2) >> 2, quarter = warp & 3, j = quarter * 32 + lane;
-    const double g = (double)__ldg(p.log_decay + head);
+    const int half = (warp - 2) >> 2, quarter = warp & 3, j = quarter * 32 + lane, row = (tid - 64) & 63, part = (tid - 64) >> 6;
+    const double g2 = (double)__ldg(p.log_decay + head) * 1.4426950408889634;
     bool ok = true;
     for (int n = 0; n < chunks; ++n) {
-      const int st = n % W::STAGES, row0 = r0 + LT_C * n, len = min(LT_C, r1 - row0), rows16 = (len + 15) / 16 * 16;
+      const int st = n % W::STAGES, row0 = r0 + W::ROWS * step(n), len = min(W::ROWS, r1 - row0), rows16 = (len + 15) / 16 * 16;
       const uint32_t at = base + st * W::STAGE;
-      const float w = p.k_scale * (float)exp(g * max(REV ? row0 + j - r0 : r1 - 1 - row0 - j, 0));
+      // lambda^{distance}: the exponent in 64 bits, its fraction alone through fp32
+      const double t = fmax(g2 * max(REV ? row0 + row - r0 : r1 - 1 - row0 - row, 0), -400.0), whole = rint(t);
+      const float w = p.k_scale * ldexpf(exp2f((float)(t - whole)), (int)whole);
       if (!(ok = warp_wait(full(st), n / W::STAGES & 1, abort_flag, wait_limit))) break;
-      if (j < rows16) {
-        const bool live = j < len;
-        if (KP == 128) scale_row<4>(at + half * LT_BOX, at + W::LO + half * LT_BOX, j, w, live, 0, 8);
-        else scale_row<4>(at, at + W::LO, j, w, live, 4 * half, 4);
-        if (!live && half < W::VB) clear_row(at + W::V + half * LT_BOX, j);
+      if (row < rows16) {
+        const bool live = row < len;
+        if (KP == 128) scale_row<4>(at + (part >> 1) * W::BOX, at + W::LO + (part >> 1) * W::BOX, row, w, live, 4 * (part & 1), 4);
+        else scale_row<2>(at, at + W::LO, row, w, live, 2 * part, 2);
+        if (!live && part < W::VB) clear_row(at + W::V + part * W::BOX, row);
       }
       fence_async();
       warp_arrive(scaled(st));
     }
+    pdl_wait();
     if (ok && (ok = warp_wait(done, 0, abort_flag, wait_limit))) {
       tc_fence_after();
-      float* to = p.seg_state + ((size_t)(REV ? seg - 1 : seg) * p.H + head) * ((size_t)p.dk * p.dv) + j;
+      float* to = p.cut_state + (size_t)blockIdx.x * ((size_t)p.dk * p.dv) + j;
       for (int c = half * (KP / 2); c < (half + 1) * (KP / 2); c += 32) {
         uint32_t r[32];
         __syncwarp();
@@ -739,13 +797,13 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------------- host
-// bf16 [rows, heads, d] with row pitch ld as a 3-D tensor: a box is 64 columns of one head in 128 rows, zeros beyond the head's width and the last row.
-bool make_tmap_heads(CUtensorMap* map, const void* ptr, int rows, int heads, int d, int64_t ld) {
+// bf16 [rows, heads, d] with row pitch ld as a 3-D tensor: a box is 64 columns of one head in box_rows rows, zeros beyond the head's width and the last row.
+bool make_tmap_heads(CUtensorMap* map, const void* ptr, int rows, int heads, int d, int64_t ld, int box_rows) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)rows};
   cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)ld * 2};
-  cuuint32_t box[3] = {64, 1, LT_C};
+  cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -754,7 +812,8 @@ bool make_tmap_heads(CUtensorMap* map, const void* ptr, int rows, int heads, int
 template <int KP, int VP, bool REV>
 cudaError_t launch_shape(const LinPass& p, const rom_ragged& seqs, LinCut cut, bool state_only, bool test_stall, cudaStream_t st) {
   CUtensorMap tq, tk, tv;
-  if (!make_tmap_heads(&tk, p.k, seqs.rows, p.H / p.kdiv, p.dk, p.ldk) || !make_tmap_heads(&tv, p.v, seqs.rows, p.H / p.vdiv, p.dv, p.ldv)) return cudaErrorInvalidValue;
+  const int box_rows = state_only ? StateShape<KP, VP>::ROWS : LT_C;
+  if (!make_tmap_heads(&tk, p.k, seqs.rows, p.H / p.kdiv, p.dk, p.ldk, box_rows) || !make_tmap_heads(&tv, p.v, seqs.rows, p.H / p.vdiv, p.dv, p.ldv, box_rows)) return cudaErrorInvalidValue;
   const uint32_t limit = test_stall ? WAIT_LIMIT_TEST : WAIT_LIMIT, stall = test_stall ? 16 : 0;
   count_launch();
   if (state_only) {
@@ -762,14 +821,14 @@ cudaError_t launch_shape(const LinPass& p, const rom_ragged& seqs, LinCut cut, b
     auto kern = lin_state_tc<KP, VP, REV>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_k(kern, dim3(p.H, cut.n_seg - 1), LT_STATE_THREADS, smem, st, tk, tv, p, device_view(seqs), cut.seg_rows, limit, stall);
+    return launch_k(kern, dim3(cut.blocks - 1), LT_STATE_THREADS, smem, st, tk, tv, p, device_view(seqs), cut, limit, stall);
   }
-  if (!make_tmap_heads(&tq, p.q, seqs.rows, p.H / p.qdiv, p.dk, p.ldq)) return cudaErrorInvalidValue;
+  if (!make_tmap_heads(&tq, p.q, seqs.rows, p.H / p.qdiv, p.dk, p.ldq, box_rows)) return cudaErrorInvalidValue;
   constexpr int smem = WalkShape<KP, VP>::BYTES + 1024;
   auto kern = lin_walk_tc<KP, VP, REV>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_k(kern, dim3(p.H, cut.n_seg), LT_WALK_THREADS, smem, st, tq, tk, tv, p, device_view(seqs), cut.seg_rows, cut.n_seg, limit, stall);
+  return launch_k(kern, dim3(cut.blocks), LT_WALK_THREADS, smem, st, tq, tk, tv, p, device_view(seqs), cut, limit, stall);
 }
 
 }  // namespace
