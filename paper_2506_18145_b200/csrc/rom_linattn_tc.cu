@@ -39,11 +39,6 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
   return e != 0;
 }
-// A warp's wait; the outcome is the same in all lanes.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
-}
-// Several barriers at once: a wait takes about 200 cycles even when it is over, one after the other the issuer's took 600 a chunk.
 __device__ __forceinline__ bool mbar_ready(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -52,6 +47,15 @@ __device__ __forceinline__ bool mbar_ready(uint32_t bar, uint32_t parity) {
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
+}
+// A look at a barrier takes 25 cycles, a wait (mbarrier.try_wait) 200 to 400 even when it is over: one look first.  (More of them take issue slots from the warps that
+// work: with 128 a chunk took 8900 cycles instead of 6500.)  Bounded like mbar_wait.
+__device__ __forceinline__ bool lt_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  return mbar_ready(bar, parity) || mbar_wait(bar, parity, abort_flag, limit);
+}
+// A warp's wait; the outcome is the same in all lanes.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  return __all_sync(0xffffffffu, lt_wait(bar, parity, abort_flag, limit));
 }
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
   __syncwarp();
@@ -176,6 +180,12 @@ __device__ __forceinline__ void issue_state(uint32_t tmem_d, uint32_t v, uint32_
   const uint64_t a = desc_mn<BOX>(v), h = desc_mn<BOX>(khi), l = desc_mn<BOX>(klo);
   for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), h + (uint64_t)(MN_KSTEP * k), idesc, accumulate || k > 0 ? 1u : 0u);
   for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), l + (uint64_t)(MN_KSTEP * k), idesc, 1u);
+}
+template <int BOXES>
+__device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int head, int row) {
+#pragma unroll
+  for (int b = 0; b < BOXES; ++b)
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(64 * b), "r"(head), "r"(row) : "memory");
 }
 template <int BOXES, int BOX = LT_BOX>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
@@ -331,11 +341,14 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           int row0, len;
           x.chunk<REV>(m, row0, len);
           const int st = n % W::KVST, qs = n % W::QST;
-          if (!mbar_wait(kv_empty(st), (n / W::KVST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
+          if (n == 1) pdl_wait();      // (the first chunk's copies need not wait for the launch before, but no bounded wait may count its time)
+          if (!lt_wait(kv_empty(st), (n / W::KVST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
           mbar_expect_tx(kv_full(st), (W::KB + W::VB) * LT_BOX + stall);
           load_tile<W::KB>(base + W::K + st * W::KB * LT_BOX, &tmap_k, kv_full(st), head / p.kdiv, row0);
           load_tile<W::VB>(base + W::V + st * W::VB * LT_BOX, &tmap_v, kv_full(st), head / p.vdiv, row0);
-          if (!mbar_wait(q_empty(qs), (n / W::QST & 1) ^ 1, abort_flag, wait_limit)) { ++n; ok = false; break; }
+          // one stage of Q: it is asked for when Q S of the chunk before is done, 4000 cycles from memory where the chunk has 2500 left; from L2 1500
+          if (W::QST == 1) prefetch_tile<W::KB>(&tmap_q, head / p.qdiv, row0);
+          if (!lt_wait(q_empty(qs), (n / W::QST & 1) ^ 1, abort_flag, wait_limit)) { ++n; ok = false; break; }
           mbar_expect_tx(q_full(qs), W::KB * LT_BOX);
           load_tile<W::KB>(base + W::Q + qs * W::KB * LT_BOX, &tmap_q, q_full(qs), head / p.qdiv, row0);
         }
@@ -357,10 +370,11 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     // ---------------------------------------------------------------- matrix products
     const bool leader = elect_one();
     bool ok = true, issued = false;
+    pdl_wait();
     while (it.next(cut, seqs.rows)) {
       const int s_first = first_piece(it, seqs);
       constexpr uint32_t d_sc = lt_idesc(LT_C, false, false), d_o1 = lt_idesc(VP, false, false), d_o2 = lt_idesc(VP, false, true), d_kv = lt_idesc(KP, true, true);
-      auto wait = [&](uint32_t b, uint32_t parity) { ok = ok && mbar_wait(b, parity, abort_flag, wait_limit); return ok; };
+      auto wait = [&](uint32_t b, uint32_t parity) { ok = ok && lt_wait(b, parity, abort_flag, wait_limit); return ok; };
       if (leader)
       for (int s = s_first; ok && get_piece<REV>(it, seqs, s, x); ++s)
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
@@ -369,9 +383,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           const int st = n % W::KVST, qs = n % W::QST, ks = (len + 15) / 16;
           const uint32_t ph = n & 1, q = base + W::Q + qs * W::KB * LT_BOX, k = base + W::K + st * W::KB * LT_BOX, v = base + W::V + st * W::VB * LT_BOX;
           // scores, once the P that lies over them has been used
-          const uint32_t kv_ph = n / W::KVST & 1, q_ph = n / W::QST & 1;
-          const bool kv_in = mbar_ready(kv_full(st), kv_ph), q_in = mbar_ready(q_full(qs), q_ph), pv_in = n == 0 || mbar_ready(pv_full, ph ^ 1);
-          if (!(kv_in && q_in && pv_in) && (!wait(kv_full(st), kv_ph) || !wait(q_full(qs), q_ph) || (n > 0 && !wait(pv_full, ph ^ 1)))) break;
+          if (!wait(kv_full(st), n / W::KVST & 1) || !wait(q_full(qs), n / W::QST & 1) || (n > 0 && !wait(pv_full, ph ^ 1))) break;
           tc_fence_after();
 #pragma unroll
           for (int b = 0; b < W::KB; ++b)
@@ -381,8 +393,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           umma_commit(sc_full);
           issued = true;
           // Q S, once the output before has been read and S written
-          const bool s_in = mbar_ready(s_ready, ph), o_in = n == 0 || mbar_ready(o_free, ph ^ 1);
-          if (!(s_in && o_in) && (!wait(s_ready, ph) || (n > 0 && !wait(o_free, ph ^ 1)))) break;
+          if (!wait(s_ready, ph) || (n > 0 && !wait(o_free, ph ^ 1))) break;
           tc_fence_after();
 #pragma unroll
           for (int b = 0; b < W::KB; ++b)
@@ -390,8 +401,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
             for (int e = 0; e < 4; ++e)
               umma_bf16(tmem + W::O1, make_smem_desc(q + b * LT_BOX) + 2 * e, make_smem_desc(base + W::S + b * VP * 128) + 2 * e, d_o1, b + e > 0 ? 1u : 0u);
           umma_commit(q_empty(qs));
-          const bool p_in = mbar_ready(p_ready, ph), k_in = mbar_ready(k_ready, ph);
-          if (!(p_in && k_in) && (!wait(p_ready, ph) || !wait(k_ready, ph))) break;
+          if (!wait(p_ready, ph) || !wait(k_ready, ph)) break;
           tc_fence_after();
           for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 8 * e, desc_mn<LT_BOX>(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
           umma_commit(pv_full);
@@ -484,6 +494,8 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         const bool mine = i < len;
         const float f = p.inter_scale * lam[REV ? max(len - i - early, 0) : i + 1 - early];
         float2 odd = make_float2(0.0f, 0.0f);
+        const auto not_finite = [&]() { return ok && mine && !(odd.x == 0.0f && odd.y == 0.0f); };
+        bool freed = false;            // the tensor memory is given back once it has been read, ahead of the stores, unless it is read again
         const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + (lane & 24), rows = ok ? len - first : 0;      // (rows that the lane stores)
         // 16 columns: f O1 + p O2, noting what is not finite
         auto columns = [&](int c, float2 (&o)[8]) {
@@ -523,15 +535,22 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[8 * u + e] = VP == 128 || u < 2 ? pack2(o[e].x, o[e].y) : 0;
           }
+          if (!__any_sync(0xffffffffu, not_finite())) {
+            tc_fence_before();
+            warp_arrive(o_free);
+            freed = true;
+          }
           const int col = c_from + 8 * (lane & 7);
           store_rows128(reinterpret_cast<char*>(out + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 2, rows, (VP == 128 || (lane & 7) < 4) && col < p.dv, w, lane);
         }
-        const bool again = ok && mine && !(odd.x == 0.0f && odd.y == 0.0f);
-        if (__any_sync(0xffffffffu, again))
-          slow_rows<REV>(p, static_cast<const bf16*>(p.q) + (int64_t)(head / p.qdiv) * p.dk, static_cast<const bf16*>(p.k) + (int64_t)(head / p.kdiv) * p.dk,
-                         static_cast<const bf16*>(p.v) + (int64_t)(head / p.vdiv) * p.dv, out, lanes + W::O1, lam, i, row0, len, f, again, head, c_from, c_to);
-        tc_fence_before();
-        warp_arrive(o_free);
+        if (!freed) {
+          const bool again = not_finite();
+          if (__any_sync(0xffffffffu, again))
+            slow_rows<REV>(p, static_cast<const bf16*>(p.q) + (int64_t)(head / p.qdiv) * p.dk, static_cast<const bf16*>(p.k) + (int64_t)(head / p.kdiv) * p.dk,
+                           static_cast<const bf16*>(p.v) + (int64_t)(head / p.vdiv) * p.dv, out, lanes + W::O1, lam, i, row0, len, f, again, head, c_from, c_to);
+          tc_fence_before();
+          warp_arrive(o_free);
+        }
       }
     }
     if (!ok) latch(p, abort_flag, 53);
@@ -612,8 +631,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         const int st = n % W::KVST, early = m == 0 && !x.over && p.early ? 1 : 0, rows16 = (len + 15) / 16 * 16;
         const uint32_t ph = n & 1, k = base + W::K + st * W::KB * LT_BOX, box = KP == 128 ? half * LT_BOX : 0;
         // (the scores are made of this K: sc_full says that it has landed, but the copies' own barrier makes them visible)
-        ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit) &&
-             (__all_sync(0xffffffffu, mbar_ready(kv_full(st), n / W::KVST & 1)) || warp_wait(kv_full(st), n / W::KVST & 1, abort_flag, wait_limit));
+        ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit) && warp_wait(kv_full(st), n / W::KVST & 1, abort_flag, wait_limit);
         if (c < rows16) {
           const bool live = c < len;
           const float w = live ? p.k_scale * lam[REV ? c : len - 1 - c] : 0.0f;
@@ -723,7 +741,7 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
       for (; n < chunks; ++n) {
         const int st = n % W::STAGES;
         const uint32_t at = base + st * W::STAGE;
-        if (!mbar_wait(empty(st), (n / W::STAGES & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
+        if (!lt_wait(empty(st), (n / W::STAGES & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
         mbar_expect_tx(full(st), (W::KB + W::VB) * W::BOX + stall);
         load_tile<W::KB, W::BOX>(at, &tmap_k, full(st), head / p.kdiv, r0 + W::ROWS * step(n));
         load_tile<W::VB, W::BOX>(at + W::V, &tmap_v, full(st), head / p.vdiv, r0 + W::ROWS * step(n));
@@ -740,7 +758,7 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
       for (int n = 0; n < chunks; ++n) {
         const int st = n % W::STAGES;
         const uint32_t at = base + st * W::STAGE;
-        if (!mbar_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
+        if (!lt_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
         tc_fence_after();
         issue_state<W::BOX>(tmem, at + W::V, at, at + W::LO, lt_idesc(KP, true, true), (min(W::ROWS, r1 - r0 - W::ROWS * step(n)) + 15) / 16, n > 0);
         umma_commit(empty(st));
