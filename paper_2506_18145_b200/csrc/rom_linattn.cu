@@ -69,20 +69,30 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
     }
     __syncthreads();
   };
-  auto place = [&](int i, int& r, int& c) {      // i-th element of the block's columns, in the order of the memory's rows
-    if (p.transposed) { c = i / p.dk; r = i - c * p.dk; } else { r = i / wv; c = i - r * wv; }
+  // The block's columns of a state between memory and shared memory, four adjacent numbers of the memory's rows at a time (a transposed state's are a column's).
+  auto each4 = [&](auto&& f) {
+    const int wide = p.transposed ? p.dk : wv, high = p.transposed ? wv : p.dk, q4 = (wide + 3) / 4, lanes = q4 <= 16 ? 16 : 32;
+    for (int r = tid / lanes; r < high; r += SIMT_THREADS / lanes)
+      if (tid % lanes < q4) f(r, 4 * (tid % lanes), p.transposed ? (size_t)(c0 + r) * p.dk + 4 * (tid % lanes) : (size_t)r * p.dv + c0 + 4 * (tid % lanes));
   };
-  auto at = [&](int r, int c) { return p.transposed ? (size_t)(c0 + c) * p.dk + r : (size_t)r * p.dv + c0 + c; };
   auto load_state = [&](const float* from) {
     __syncthreads();
-    for (int i = tid; i < p.dk * SIMT_SPITCH; i += SIMT_THREADS) S[i] = 0.0f;
-    __syncthreads();
-    if (from)
-      for (int i = tid; i < p.dk * wv; i += SIMT_THREADS) { int r, c; place(i, r, c); S[r * SIMT_SPITCH + c] = from[at(r, c)]; }
+    if (!from || wv < SIMT_DV)
+      for (int i = tid; i < p.dk * SIMT_SPITCH / 4; i += SIMT_THREADS) reinterpret_cast<float4*>(S)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (!from) return;
+    if (wv < SIMT_DV) __syncthreads();
+    each4([&](int r, int c, size_t at) {
+      const float4 v = *reinterpret_cast<const float4*>(from + at);
+      if (p.transposed) { S[c * SIMT_SPITCH + r] = v.x; S[(c + 1) * SIMT_SPITCH + r] = v.y; S[(c + 2) * SIMT_SPITCH + r] = v.z; S[(c + 3) * SIMT_SPITCH + r] = v.w; }
+      else *reinterpret_cast<float4*>(S + r * SIMT_SPITCH + c) = v;
+    });
   };
-  auto store_state = [&](float* to, float factor) {
+  auto store_state = [&](float* to, float f) {      // (never a transposed one)
     __syncthreads();
-    for (int i = tid; i < p.dk * wv; i += SIMT_THREADS) { int r, c; place(i, r, c); to[at(r, c)] = factor * S[r * SIMT_SPITCH + c]; }
+    each4([&](int r, int c, size_t at) {
+      const float4 v = *reinterpret_cast<const float4*>(S + r * SIMT_SPITCH + c);
+      *reinterpret_cast<float4*>(to + at) = f == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(f * v.x, f * v.y, f * v.z, f * v.w);
+    });
   };
   // rows [r0, r1) of one sequence; pool_init: the state they meet is a sequence's initial one
   auto walk = [&](int r0, int r1, bool pool_init) {
@@ -95,8 +105,9 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
       if (!STATE) load_tile(Q, qp, q, p.ldq, row0, step, len, p.dk, p.dk);
       __syncthreads();
       if constexpr (!STATE) {
+        const bool mine = 2 * ty < len;        // (rows behind the last one cost nothing)
         float s[2][2] = {};
-        for (int d = 0; d < p.dk; d += 4) {
+        for (int d = 0; mine && d < p.dk; d += 4) {
           float4 qv[2], kv[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) { qv[i] = *reinterpret_cast<const float4*>(Q + (2 * ty + i) * qp + d); kv[i] = *reinterpret_cast<const float4*>(K + (tx + 16 * i) * qp + d); }
@@ -114,7 +125,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
           }
         __syncthreads();
         float2 o[2][2] = {};
-        for (int d = 0; d < p.dk; d += 4) {
+        for (int d = 0; mine && d < p.dk; d += 4) {
           float4 qv[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) qv[i] = *reinterpret_cast<const float4*>(Q + (2 * ty + i) * qp + d);
@@ -135,7 +146,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
           o[i][0] = __fmul2_rn(o[i][0], make_float2(f, f));
           o[i][1] = __fmul2_rn(o[i][1], make_float2(f, f));
         }
-        for (int j = 0; j <= 2 * ty + 1; ++j) {      // (a row's own and earlier ones alone: a later value may be anything)
+        for (int j = 0; mine && j <= 2 * ty + 1; ++j) {      // (a row's own and earlier ones alone: a later value may be anything)
           const float4 vv = *reinterpret_cast<const float4*>(V + j * SIMT_SPITCH + 4 * tx);
 #pragma unroll
           for (int i = 0; i < 2; ++i)
@@ -193,7 +204,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
     walk(r0, r1, false);
     store_state(p.cut_state + (size_t)run * state, 1.0f);
   } else {
-    for (LinItem it(cut, run); it.next(cut, seqs.rows);) {
+    for (LinItem it(cut, run); it.next(cut, seqs);) {
       enter(it.head);
       const int a = it.a, b = it.b;
       int s = seqs.first_from(a);
@@ -203,7 +214,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
         if (st >= b && !it.last) break;
         const int slot = seqs.slot_of(s);
         const bool empty = en <= st, over = !empty && (p.reverse ? en > b : st < a);      // its state comes over a cut
-        if (!empty && r0 >= r1) continue;
+        if ((!empty && r0 >= r1) || (p.skip_single && en - st == 1)) continue;
         if (over) load_state(p.cut_state + (size_t)(p.reverse ? run : run - 1) * state);
         else if (!empty && !p.reverse && p.init_copy && en > b && lin_init_of(p, seqs, s, head)) load_state(p.init_copy + (size_t)run * state);
         else load_state(lin_init_of(p, seqs, s, head));
@@ -242,28 +253,30 @@ __global__ void __launch_bounds__(256) lin_powers(const float* log_decay, int H,
 // Launch 2: the states that reach every cut, element by element.  A thread owns four adjacent elements of one head.
 constexpr int CHAIN_THREADS = 128;
 __global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seqs, LinCut cut) {
-  __shared__ int how[kLinMaxBlocks];            // at the head's cuts: -2 nobody reaches over it; -1 the state comes over a cut; else a sequence starts here
+  __shared__ int how[kLinMaxBlocks];            // at the head's cuts: -3 nobody reaches over it; -2 the state comes over a cut; else a sequence starts here: its state's slot, or -1
   __shared__ float weight[kLinMaxBlocks];       // of the state at the cut before, or of the sequence's initial state
-  const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int head = blockIdx.y;
   const double g = (double)__ldg(p.log_decay + head);
   const long long u0 = (long long)head * cut.per_head, u1 = u0 + cut.per_head;
   int first = (int)(u0 * cut.blocks / cut.units), n = 0;      // the head's cuts: first .. first + n - 1
   while (cut.bound(first) <= u0) ++first;
   while (cut.bound(first + n) < u1) ++n;
-  auto row_of = [&](int j) { return j < 0 ? 0 : j >= n ? seqs.rows : (int)(cut.bound(first + j) - u0) * cut.chunk; };
-  for (int j = warp; j < n; j += CHAIN_THREADS / 32) {
-    const int r = row_of(j), s = lin_spanning(seqs, r), far = row_of(p.reverse ? j + 1 : j - 1);
-    if (lane == 0) {
-      int h = -2;
-      float w = 0.0f;
-      if (s >= 0) {
-        const int away = p.reverse ? seqs.end_of(s) - r : r - seqs.start_of(s), seg = p.reverse ? far - r : r - far;
-        h = away > seg ? -1 : s;
-        w = (float)exp(g * (h < 0 ? seg : away - (p.early ? 1 : 0)));
-      }
-      how[j] = h;
-      weight[j] = w;
+  __shared__ int rows[kLinMaxBlocks];
+  for (int j = threadIdx.x; j < n; j += CHAIN_THREADS) rows[j] = cut.row_at<false>(seqs, (int)(cut.bound(first + j) - u0) * cut.chunk);
+  __syncthreads();
+  auto row_of = [&](int j) { return j < 0 ? 0 : j >= n ? seqs.rows : rows[j]; };
+  // a thread a cut (a warp a cut, its lanes searching together, took 0.7 us for each of a head's 37)
+  for (int j = threadIdx.x; j < n; j += CHAIN_THREADS) {
+    const int r = row_of(j), s = lin_spanning_1(seqs, r), far = row_of(p.reverse ? j + 1 : j - 1);
+    int h = -3;
+    float w = 0.0f;
+    if (s >= 0) {
+      const int away = p.reverse ? seqs.end_of(s) - r : r - seqs.start_of(s), seg = p.reverse ? far - r : r - far, slot = seqs.slot_of(s);
+      h = away > seg ? -2 : p.init && (p.init_all || seqs.resumes(s)) ? slot : -1;
+      w = (float)exp(g * (h == -2 ? seg : away - (p.early ? 1 : 0)));
     }
+    how[j] = h;
+    weight[j] = w;
   }
   pdl_sync();                           // (the tables above come from inputs, which are older than launch 1)
   __syncthreads();
@@ -271,28 +284,25 @@ __global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seq
   if (e >= state) return;
   float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (int i0 = 0; i0 < n; i0 += 4) {
-    float4 add[4];
+    float4 add[4], init[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {      // (loads of four cuts at a time: nothing of theirs depends on the chain)
       const int j = p.reverse ? n - 1 - (i0 + u) : i0 + u;
-      if (i0 + u < n && how[j] != -2) add[u] = *reinterpret_cast<const float4*>(p.cut_state + (size_t)(first + j - 1) * state + e);
+      if (i0 + u >= n || how[j] == -3) continue;
+      add[u] = *reinterpret_cast<const float4*>(p.cut_state + (size_t)(first + j - 1) * state + e);
+      if (how[j] >= 0) init[u] = *reinterpret_cast<const float4*>(p.init + ((size_t)how[j] * p.H + head) * state + e);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (i0 + u >= n) break;
       const int j = p.reverse ? n - 1 - (i0 + u) : i0 + u, h = how[j];
-      if (h == -2) continue;
+      if (h == -3) continue;
       const float w = weight[j];
-      bool from = true;
       if (h >= 0) {
-        const float* init = lin_init_of(p, seqs, h, head);
-        from = init != nullptr;
-        if (from) {
-          x = *reinterpret_cast<const float4*>(init + e);
-          if (p.init_copy) *reinterpret_cast<float4*>(p.init_copy + (size_t)(first + j - 1) * state + e) = x;
-        }
+        x = init[u];
+        if (p.init_copy) *reinterpret_cast<float4*>(p.init_copy + (size_t)(first + j - 1) * state + e) = x;
       }
-      x = from ? make_float4(fmaf(w, x.x, add[u].x), fmaf(w, x.y, add[u].y), fmaf(w, x.z, add[u].z), fmaf(w, x.w, add[u].w)) : add[u];
+      x = h != -1 ? make_float4(fmaf(w, x.x, add[u].x), fmaf(w, x.y, add[u].y), fmaf(w, x.z, add[u].z), fmaf(w, x.w, add[u].w)) : add[u];
       *reinterpret_cast<float4*>(p.cut_state + (size_t)(first + j - 1) * state + e) = x;
     }
   }
@@ -323,28 +333,41 @@ __global__ void __launch_bounds__(256) lin_sum_heads(const float* part, T* dst, 
 // A block updates 32 columns of one token's and head's state: 4 warps x 4 rows x 8 column quads, every load of the state in flight at once.
 // S e^g is S + S (e^g - 1) for slow decays: a factor rounded to fp32 would be off by the same 2^-25 in every one of thousands of steps.
 constexpr int STEP_THREADS = 128, STEP_COLS = 32;
-template <typename T>
+// PACKED: the tokens are the sequences of one row among packed ones, which a walk would load and keep a state for one by one.
+template <typename T, bool PACKED>
 __global__ void __launch_bounds__(STEP_THREADS) lin_step(const T* q, const T* k, const T* v, long long ldq, long long ldk, long long ldv, const float* log_decay,
                                                          const int32_t* slot, int n_slots, const float* s_in, float* s_out, T* o, int H, int share, int dk, int dv,
-                                                         int slices, float scale) {
+                                                         int slices, float scale, Ragged seqs) {
   __shared__ float part[STEP_THREADS / 32][STEP_COLS];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int slice = blockIdx.x % slices, bh = blockIdx.x / slices, head = bh % H, b = bh / H;
   const int c = slice * STEP_COLS + (lane & 7) * 4, r0 = warp * 4 + (lane >> 3);
   pdl_sync();
-  const int sl = slot ? __ldg(slot + b) : b;
-  if (sl < 0 || sl >= n_slots) return;
-  const size_t base = ((size_t)sl * H + head) * ((size_t)dk * dv);
+  int sl, row = b;
+  bool from, kept = true;              // the state is loaded (else it is zero), is stored
+  if (PACKED) {
+    row = seqs.start_of(b);
+    if (seqs.end_of(b) - row != 1) return;
+    sl = seqs.slot_of(b);
+    from = s_in && sl >= 0 && seqs.resumes(b);
+    kept = s_out && sl >= 0;
+  } else {
+    sl = slot ? __ldg(slot + b) : b;
+    if (sl < 0 || sl >= n_slots) return;
+    from = true;
+  }
+  const size_t base = ((size_t)max(sl, 0) * H + head) * ((size_t)dk * dv);
   const bool mine = c < dv;
   float4 S[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = r0 + 16 * i;
-    if (mine && r < dk) S[i] = *reinterpret_cast<const float4*>(s_in + base + (size_t)r * dv + c);
+    S[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (from && mine && r < dk) S[i] = *reinterpret_cast<const float4*>(s_in + base + (size_t)r * dv + c);
   }
-  const T* qr = q + (size_t)b * ldq + (size_t)(head / share) * dk;
-  const T* kr = k + (size_t)b * ldk + (size_t)(head / share) * dk;
-  const T* vr = v + (size_t)b * ldv + (size_t)head * dv;
+  const T* qr = q + (size_t)row * ldq + (size_t)(head / share) * dk;
+  const T* kr = k + (size_t)row * ldk + (size_t)(head / share) * dk;
+  const T* vr = v + (size_t)row * ldv + (size_t)head * dv;
   float vv[4] = {};
   if (mine) { vv[0] = to_f32(vr[c]); vv[1] = to_f32(vr[c + 1]); vv[2] = to_f32(vr[c + 2]); vv[3] = to_f32(vr[c + 3]); }
   const float g = __ldg(log_decay + head), lam = expf(g), em1 = expm1f(g);
@@ -362,7 +385,7 @@ __global__ void __launch_bounds__(STEP_THREADS) lin_step(const T* q, const T* k,
         s[e] = fmaf(kk, vv[e], slow ? fmaf(s[e], f, s[e]) : s[e] * f);
         acc[e] = fmaf(qq, s[e], acc[e]);
       }
-      __stcs(reinterpret_cast<float4*>(s_out + base + (size_t)r * dv + c), make_float4(s[0], s[1], s[2], s[3]));
+      if (kept) __stcs(reinterpret_cast<float4*>(s_out + base + (size_t)r * dv + c), make_float4(s[0], s[1], s[2], s[3]));
     }
   }
 #pragma unroll
@@ -375,7 +398,7 @@ __global__ void __launch_bounds__(STEP_THREADS) lin_step(const T* q, const T* k,
     for (int e = 0; e < 4; ++e) part[warp][lane * 4 + e] = acc[e];
   __syncthreads();
   const int col = slice * STEP_COLS + tid;
-  if (tid < STEP_COLS && col < dv) o[((size_t)b * H + head) * dv + col] = from_f32<T>(scale * (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]));
+  if (tid < STEP_COLS && col < dv) o[((size_t)row * H + head) * dv + col] = from_f32<T>(scale * (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]));
 }
 
 // ---------------------------------------------------------------- host
@@ -391,23 +414,24 @@ bool on_tensor_cores(const rom_linattn_config& c) { return c.dtype == ROM_BF16 &
 // Runs: one head each, or, where that leaves SMs idle for longer than launches 1 and 2 take, equal runs of all heads' chunks on as many blocks as the GPU holds
 // (on the tensor cores one to an SM).  Launch 1 takes about 0.6 of a chunk's time, launches 1 and 2 about six chunks of one block besides.  A function of the sizes only
 // (148 SMs assumed).
-struct LinSlots { int blocks, chunk, least; };
+struct LinSlots { int blocks, chunk, least, start; };
 LinSlots slots_of(const rom_linattn_config& c) {
-  if (on_tensor_cores(c)) return LinSlots{148, 128, 2};
-  return LinSlots{kLinMaxBlocks / ((c.d_v + SIMT_DV - 1) / SIMT_DV), SIMT_C, 2};
+  if (on_tensor_cores(c)) return LinSlots{148, 128, 2, 256};
+  return LinSlots{kLinMaxBlocks / ((c.d_v + SIMT_DV - 1) / SIMT_DV), SIMT_C, 1, 32};
 }
-int most_runs(const rom_linattn_config& c, int rows) {      // with cuts inside heads
+int units_per_head(const LinSlots& s, int n_seq, int rows) { return (int)(((long long)rows + (long long)s.start * n_seq + s.chunk - 1) / s.chunk); }
+int most_runs(const rom_linattn_config& c, int n_seq, int rows) {      // with cuts inside heads
   const LinSlots s = slots_of(c);
-  const long long units = (long long)c.n_heads * ((rows + s.chunk - 1) / s.chunk), n = units / s.least;
+  const long long n = (long long)c.n_heads * units_per_head(s, n_seq, rows) / s.least;
   return (int)(n < 1 ? 1 : n < s.blocks ? n : s.blocks);
 }
-LinCut cut_rows(const rom_linattn_config& c, int rows) {
+LinCut cut_rows(const rom_linattn_config& c, int n_seq, int rows) {
   const LinSlots s = slots_of(c);
-  LinCut cut{s.chunk, rows > 0 ? (rows + s.chunk - 1) / s.chunk : 1, c.n_heads, 0, false};
+  LinCut cut{s.chunk, s.start, units_per_head(s, n_seq, rows), c.n_heads, 0, false};
   cut.units = (long long)c.n_heads * cut.per_head;
   // A run inside one head starts once, and heads that are cut at the same rows read memory side by side: a whole number of runs a head, where that leaves no more than a
   // fifth of the blocks out (32 heads of 64, 23 prompts of 8186 rows: 128 runs 81 us, 148 of them 106; 16384 rows of 32 heads of 128: 173 and 175).
-  int n = most_runs(c, rows);
+  int n = most_runs(c, n_seq, rows);
   const int aligned = n / c.n_heads * c.n_heads;
   if (aligned * 5 >= n * 4) n = aligned;
   const double whole = (double)((c.n_heads + s.blocks - 1) / s.blocks) * cut.per_head, even = 1.6 * (double)cut.units / n + 6.0;
@@ -415,11 +439,11 @@ LinCut cut_rows(const rom_linattn_config& c, int rows) {
   return cut;
 }
 struct LinWs { size_t status, powers, cut_a, cut_b, part, total; };
-LinWs lin_ws(const rom_linattn_config& c, int rows, bool backward) {
+LinWs lin_ws(const rom_linattn_config& c, int n_seq, int rows, bool backward) {
   LinWs l{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
-  const size_t state = (size_t)most_runs(c, rows) * c.d_k * c.d_v * sizeof(float);
+  const size_t state = (size_t)most_runs(c, n_seq, rows) * c.d_k * c.d_v * sizeof(float);
   l.status = take(sizeof(int32_t) * kStatusInts);
   l.powers = take((size_t)c.n_heads * 2 * kLinPowers * sizeof(float));
   l.cut_a = take(state);
@@ -433,8 +457,23 @@ int lin_ws_size(const rom_linattn_config* c, int32_t n_seq, int32_t rows, size_t
   if (rc != ROM_OK) return rc;
   if (!bytes || n_seq < 0 || rows < 0) return ROM_ERR_INVALID_ARG;
   if (n_seq > kMaxRaggedSeqs || rows >= 1 << 30) return ROM_ERR_UNSUPPORTED;
-  *bytes = lin_ws(*c, rows, backward).total;
+  *bytes = lin_ws(*c, n_seq, rows, backward).total;
   return ROM_OK;
+}
+
+// Sequences of one row (continuous batching) in a launch of their own, where they may be many: fewer than 256 rows a sequence on average.  A walk takes 3 to 5 us for each of a
+// run's in turn (37 sequences of 531 rows, 8 heads of 64 fp32: 96 us), this launch 3 us for all; with none of them it costs its 2 us.
+bool singles_apart(const rom_ragged& seqs) { return seqs.n_seq > 1 && (long long)seqs.rows < 256LL * seqs.n_seq; }
+cudaError_t launch_singles(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, cudaStream_t st) {
+  const int slices = (c.d_v + STEP_COLS - 1) / STEP_COLS;
+  const long long blocks = (long long)seqs.n_seq * c.n_heads * slices;
+  auto go = [&](auto zero) {
+    using T = decltype(zero);
+    count_launch();
+    return launch_k(lin_step<T, true>, dim3((unsigned)blocks), STEP_THREADS, 0, st, (const T*)p.q, (const T*)p.k, (const T*)p.v, (long long)p.ldq, (long long)p.ldk, (long long)p.ldv,
+                    p.log_decay, nullptr, 0, p.init, p.last, (T*)p.out, c.n_heads, c.n_heads / c.n_qk_heads, c.d_k, c.d_v, slices, c.scale, device_view(seqs));
+  };
+  return c.dtype == ROM_BF16 ? go(__nv_bfloat16()) : go(0.0f);
 }
 
 template <bool STATE>
@@ -494,13 +533,13 @@ int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, co
     if (!aligned16(p)) return ROM_ERR_INVALID_ARG;
   if (!pitch_ok(ldq, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldk, c.n_qk_heads * c.d_k, esz) || !pitch_ok(ldv, c.n_heads * c.d_v, esz)) return ROM_ERR_INVALID_ARG;
   if ((o && (o == q || o == k || o == v)) || !pools_ok(s_in, s_out, pool)) return ROM_ERR_INVALID_ARG;
-  const LinWs lay = lin_ws(c, seqs->rows, false);
+  const LinWs lay = lin_ws(c, seqs->n_seq, seqs->rows, false);
   if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
   if ((rc = check_device()) != ROM_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
-  const LinCut cut = cut_rows(c, seqs->rows);
+  const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows);
   LinPass p{};
   p.q = q; p.k = k; p.v = v; p.ldq = ldq; p.ldk = ldk; p.ldv = ldv;
   p.qdiv = p.kdiv = c.n_heads / c.n_qk_heads; p.vdiv = 1;
@@ -514,8 +553,10 @@ int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, co
   p.out = o; p.ldo = (int64_t)c.n_heads * c.d_v;
   p.status = reinterpret_cast<int32_t*>(W + lay.status);
   if (launch_powers(p, powers, st) != cudaSuccess) return ROM_ERR_CUDA;
+  p.skip_single = singles_apart(*seqs);
   if (launch_states(c, p, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
-  return launch_walk<false>(c, p, *seqs, cut, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
+  if (launch_walk<false>(c, p, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  return !p.skip_single || launch_singles(c, p, *seqs, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
 
 int rom_linattn_step(const rom_linattn_config* cfg, int32_t B, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const float* log_decay,
@@ -541,8 +582,8 @@ int rom_linattn_step(const rom_linattn_config* cfg, int32_t B, const void* q, in
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto go = [&](auto zero) {
     using T = decltype(zero);
-    return launch_k(lin_step<T>, grid, STEP_THREADS, 0, st, (const T*)q, (const T*)k, (const T*)v, (long long)ldq, (long long)ldk, (long long)ldv, log_decay, slot, n_slots,
-                    s_in, s_out, (T*)o, c.n_heads, share, c.d_k, c.d_v, slices, c.scale);
+    return launch_k(lin_step<T, false>, grid, STEP_THREADS, 0, st, (const T*)q, (const T*)k, (const T*)v, (long long)ldq, (long long)ldk, (long long)ldv, log_decay, slot, n_slots,
+                    s_in, s_out, (T*)o, c.n_heads, share, c.d_k, c.d_v, slices, c.scale, Ragged{});
   };
   return (c.dtype == ROM_BF16 ? go(__nv_bfloat16()) : go(0.0f)) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
@@ -568,13 +609,13 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
     if (outs[i] && outs[i] == outs[(i + 1) % 3]) return ROM_ERR_INVALID_ARG;
   }
   if (overlaps(ds_in, pool, ds_out, pool) || overlaps(ds_in, pool, s_in, pool)) return ROM_ERR_INVALID_ARG;
-  const LinWs lay = lin_ws(c, seqs->rows, true);
+  const LinWs lay = lin_ws(c, seqs->n_seq, seqs->rows, true);
   if (ws_bytes < lay.total) return ROM_ERR_WORKSPACE;
   if ((rc = check_device()) != ROM_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
-  const LinCut cut = cut_rows(c, seqs->rows);
+  const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows);
   const int share = c.n_heads / c.n_qk_heads;
   float* part = share > 1 ? reinterpret_cast<float*>(W + lay.part) : nullptr;
   LinPass base{};

@@ -218,14 +218,14 @@ __device__ __forceinline__ int first_piece(const LinItem& it, const Ragged& q) {
   return s > 0 && q.end_of(s - 1) > it.a ? s - 1 : s;
 }
 template <bool REV>
-__device__ __forceinline__ bool get_piece(const LinItem& it, const Ragged& q, int s, LinPiece& x) {      // false: no sequence from s on has to do with these rows
+__device__ __forceinline__ bool get_piece(const LinItem& it, const Ragged& q, bool skip_single, int s, LinPiece& x) {      // false: no sequence from s on has to do with these rows
   if (s >= q.n_seq) return false;
   const int st = q.start_of(s), en = q.end_of(s);
   if (st >= it.b && !it.last) return false;
-  const bool empty = en <= st;
+  const bool empty = en <= st, skip = skip_single && en - st == 1;
   x.s = s;
   x.r0 = max(st, it.a);
-  x.r1 = empty ? x.r0 : max(min(en, it.b), x.r0);
+  x.r1 = empty || skip ? x.r0 : max(min(en, it.b), x.r0);
   x.over = !empty && (REV ? en > it.b : st < it.a);
   x.ends = empty || (x.r1 > x.r0 && (REV ? st >= it.a : en <= it.b));
   return true;
@@ -329,10 +329,10 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     // ---------------------------------------------------------------- copies
     const bool leader = elect_one();
     bool ok = true;
-    while (it.next(cut, seqs.rows)) {
+    while (it.next(cut, seqs)) {
       const int head = it.head, s_first = first_piece(it, seqs);
       if (leader)
-      for (int s = s_first; ok && get_piece<REV>(it, seqs, s, x); ++s) {
+      for (int s = s_first; ok && get_piece<REV>(it, seqs, p.skip_single, s, x); ++s) {
         if (!x.over) {                 // the state that the piece starts from, into L2 while the pieces before are walked
           const float* from = lin_init_of(p, seqs, s, head);
           if (from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(p.dk * p.dv * sizeof(float))) : "memory");
@@ -371,12 +371,12 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     const bool leader = elect_one();
     bool ok = true, issued = false;
     pdl_wait();
-    while (it.next(cut, seqs.rows)) {
+    while (it.next(cut, seqs)) {
       const int s_first = first_piece(it, seqs);
       constexpr uint32_t d_sc = lt_idesc(LT_C, false, false), d_o1 = lt_idesc(VP, false, false), d_o2 = lt_idesc(VP, false, true), d_kv = lt_idesc(KP, true, true);
       auto wait = [&](uint32_t b, uint32_t parity) { ok = ok && lt_wait(b, parity, abort_flag, wait_limit); return ok; };
       if (leader)
-      for (int s = s_first; ok && get_piece<REV>(it, seqs, s, x); ++s)
+      for (int s = s_first; ok && get_piece<REV>(it, seqs, p.skip_single, s, x); ++s)
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
@@ -427,12 +427,12 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     const float* lam = p_pad + 32;
     pdl_wait();
     bool ok = true;
-    while (it.next(cut, seqs.rows)) {
+    while (it.next(cut, seqs)) {
     const int head = it.head, s_first = first_piece(it, seqs);
     asm volatile("bar.sync 5, 256;" ::: "memory");      // (all of these warps are done with the powers of the head before)
     for (int e = tid - 128; e < kLinPowers; e += 256) p_pad[32 + e] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + e);
     asm volatile("bar.sync 5, 256;" ::: "memory");
-    for (int s = s_first; get_piece<REV>(it, seqs, s, x); ++s)
+    for (int s = s_first; get_piece<REV>(it, seqs, p.skip_single, s, x); ++s)
       for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
         int row0, len;
         x.chunk<REV>(m, row0, len);
@@ -575,12 +575,12 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
       fence_async();
       warp_arrive(s_ready);
     };
-    while (it.next(cut, seqs.rows)) {
+    while (it.next(cut, seqs)) {
     const int head = it.head, s_first = first_piece(it, seqs);
     asm volatile("bar.sync 6, 256;" ::: "memory");
     for (int e = tid - 384; e < 2 * kLinPowers; e += 256) (e < kLinPowers ? s_lam : s_lo - kLinPowers)[e] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + e);
     asm volatile("bar.sync 6, 256;" ::: "memory");
-    for (int s = s_first; get_piece<REV>(it, seqs, s, x); ++s) {
+    for (int s = s_first; get_piece<REV>(it, seqs, p.skip_single, s, x); ++s) {
       const int mm = x.chunks(), slot = seqs.slot_of(s);
       const float* from = lin_init_of(p, seqs, s, head);
       if (x.over) from = p.cut_state + (size_t)(REV ? run : run - 1) * state;
@@ -616,6 +616,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
               S[16 * g + 4 * u + 2] = __uint_as_float(x4.z); S[16 * g + 4 * u + 3] = __uint_as_float(x4.w);
             }
           }
+          asm volatile("bar.sync 6, 256;" ::: "memory");      // (another warp's K~ would come into this one's place)
         } else {
 #pragma unroll
           for (int a = 0; a < KH; ++a) S[a] = ld_state(from + (size_t)min(a0 + a, p.dk - 1) * p.dv + col);

@@ -21,7 +21,7 @@ struct QkArgs {
   const float *w_q, *w_k;
   const int32_t* pos;
   const float* inv_freq;
-  float* part;                  // backward: [blocks][q, k][d_head] sums of dn xhat
+  float* part;                  // backward: [blocks][d_head] sums of dn xhat, the blocks of q first
   int rows, nq, nk, d, rot, interleaved;
   float eps;
 };
@@ -156,7 +156,8 @@ __global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_kernel(QkArgs p, i
       load_weights(is_k ? p.w_k : p.w_q, at, wa, wb);
       factors<INTER>(f, wa, wb, c, s);
     }
-    for (int h = 0; h < per; h += U) {
+    const int most = __reduce_max_sync(0xffffffffu, n);      // of the warp's groups
+    for (int h = 0; h < most; h += U) {
       Raw8<T> ra[U], rb[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -189,20 +190,22 @@ __global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_kernel(QkArgs p, i
 }
 
 // The backward: rows in tiles of `rows_b`, walked by a fixed number of blocks; dw is summed per lane, then over the block's groups in order, and the blocks' sums by
-// qk_sum_weights: the same from run to run.  A block works on the heads of q or on those of k (blockIdx.y): one set of weights and sums in registers.
+// qk_sum_weights: the same from run to run.  A block works on the heads of q or on those of k (the blocks behind the first blocks_q): one set
+// of weights and sums in registers.
 // A lane copies what it needs of the next heads into places of its own in shared memory (AHEAD heads, of x and dy): in registers they left none for the arithmetic, and one
 // head ahead was half of what memory takes to answer.
 template <typename T> struct QkBwd {
   static constexpr int PIECES = 4 * sizeof(T) / 2, AHEAD = sizeof(T) == 2 ? 4 : 2, STAGE = PIECES * QK_THREADS * 16;      // 16-byte pieces of a head and lane: runs a, b of x, a, b of dy
 };
 template <typename T, int LANES, bool INTER>
-__global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_bwd_kernel(QkArgs p, int rows_b, int per) {
+__global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_bwd_kernel(QkArgs p, int rows_q, int rows_k, int per, int blocks_q) {
   constexpr int GROUPS = QK_THREADS / LANES;
   using B = QkBwd<T>;
   extern __shared__ __align__(16) unsigned char bwd_smem[];      // heads ahead, afterwards the sums [GROUPS][d]; then cos and sin [rows_b][rot / 2]
   float2* cs = reinterpret_cast<float2*>(bwd_smem + B::AHEAD * B::STAGE);
   const uint32_t place = (uint32_t)__cvta_generic_to_shared(bwd_smem) + threadIdx.x * 16;
-  const bool is_k = blockIdx.y != 0;
+  const bool is_k = (int)blockIdx.x >= blocks_q;
+  const int block = is_k ? blockIdx.x - blocks_q : blockIdx.x, blocks = is_k ? gridDim.x - blocks_q : blocks_q;
   const int l = threadIdx.x % LANES, heads = is_k ? p.nk : p.nq, splits = (heads + per - 1) / per;
   const QkLane at(l, p);
   pdl_sync();
@@ -214,7 +217,8 @@ __global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_bwd_kernel(QkArgs 
 #pragma unroll
   for (int e = 0; e < 4; ++e) sa[e] = sb[e] = both(0.0f);
   const float inv_d = 1.0f / (float)p.d;
-  for (int row0 = blockIdx.x * rows_b; row0 < p.rows; row0 += gridDim.x * rows_b) {
+  const int rows_b = is_k ? rows_k : rows_q;
+  for (int row0 = block * rows_b; row0 < p.rows; row0 += blocks * rows_b) {
     const int n_rows = min(rows_b, p.rows - row0), items = n_rows * splits;
     __syncthreads();
     if (p.rot) block_angles(p, row0, n_rows, cs);
@@ -240,8 +244,9 @@ __global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_bwd_kernel(QkArgs 
           }
         }
       };
+      const int most = __reduce_max_sync(0xffffffffu, n);      // of the warp's groups
       auto ask = [&](int h) {          // (an empty group behind the last head: the count of groups is the same)
-        if (h < per) {
+        if (h < most) {
           const int off = min(h, n - 1) * p.d;
           const T* from[4] = {x + off + at.oa, x + off + at.ob, g + off + at.oa, g + off + at.ob};
           const uint32_t to = place + (h % B::AHEAD) * B::STAGE;
@@ -252,7 +257,7 @@ __global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_bwd_kernel(QkArgs 
       };
 #pragma unroll
       for (int h = 0; h < B::AHEAD - 1; ++h) ask(h);
-      for (int h = 0; h < per; ++h) {
+      for (int h = 0; h < most; ++h) {
         ask(h + B::AHEAD - 1);
         copies_wait<B::AHEAD - 1>();
         const uint32_t here = place + (h % B::AHEAD) * B::STAGE;
@@ -324,20 +329,21 @@ __global__ void __launch_bounds__(QK_THREADS, 2) qk_norm_rope_bwd_kernel(QkArgs 
   for (int i = threadIdx.x; i < p.d; i += QK_THREADS) {
     float s = 0.0f;
     for (int g = 0; g < GROUPS; ++g) s += sums[(size_t)g * p.d + i];
-    p.part[((size_t)blockIdx.x * 2 + blockIdx.y) * p.d + i] = s;
+    p.part[(size_t)blockIdx.x * p.d + i] = s;
   }
 }
 // One warp a column: lanes take the blocks' sums in turn, in 64 bits, and meet in a fixed order.
-__global__ void __launch_bounds__(QK_THREADS) qk_sum_weights(const float* part, int blocks, int d, float* dw_q, float* dw_k) {
+__global__ void __launch_bounds__(QK_THREADS) qk_sum_weights(const float* part, int blocks_q, int blocks, int d, float* dw_q, float* dw_k) {
   pdl_sync();
   const int i = blockIdx.x * (QK_THREADS / 32) + threadIdx.x / 32, lane = threadIdx.x & 31;
   if (i >= 2 * d) return;
+  const int first = i < d ? 0 : blocks_q, end = i < d ? blocks_q : blocks, col = i < d ? i : i - d;
   double s = 0.0;
-  for (int b = lane; b < blocks; b += 32) s += (double)part[(size_t)b * 2 * d + i];
+  for (int b = first + lane; b < end; b += 32) s += (double)part[(size_t)b * d + col];
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
   float* to = i < d ? dw_q : dw_k;
-  if (lane == 0 && to) to[i < d ? i : i - d] = (float)s;
+  if (lane == 0 && to) to[col] = (float)s;
 }
 
 int check_qk(const rom_qk_config* c, int rows) {
@@ -358,7 +364,7 @@ int rows_per_block(int splits, int lanes) {
   const int n = QK_THREADS / lanes / splits;
   return n < 1 ? 1 : n < 32 ? n : 32;
 }
-constexpr int kBwdBlocks = 148, kBwdFew = 296;      // blocks for q and for k each: one to an SM, two where each has one tile
+constexpr int kBwdBlocks = 296;      // of q and k together, two to an SM, where each has several tiles; twice as many of one tile each
 template <typename F>
 cudaError_t by_lanes(int lanes, F&& go) {
   switch (lanes) {
@@ -383,8 +389,17 @@ cudaError_t launch_forward(const rom_qk_config& c, const QkArgs& p, cudaStream_t
 }
 template <typename T>
 cudaError_t launch_backward(const rom_qk_config& c, const QkArgs& p, float* dw_q, float* dw_k, cudaStream_t st) {
-  const int lanes = lanes_of(c.d_head), heads = p.nq > p.nk ? p.nq : p.nk, per = heads_per_group(p.rows, heads, lanes), rows_b = rows_per_block((heads + per - 1) / per, lanes);
-  const int tiles = (p.rows + rows_b - 1) / rows_b, blocks = tiles < 1 ? 1 : tiles <= kBwdFew ? tiles : kBwdBlocks;
+  const int lanes = lanes_of(c.d_head), per = heads_per_group(p.rows, p.nq + p.nk, lanes);
+  const int splits_q = (p.nq + per - 1) / per, splits_k = (p.nk + per - 1) / per, rows_q = rows_per_block(splits_q, lanes), rows_k = rows_per_block(splits_k, lanes);
+  int blocks_q = (p.rows + rows_q - 1) / rows_q, blocks_k = (p.rows + rows_k - 1) / rows_k;      // tiles
+  if (blocks_q + blocks_k > 2 * kBwdBlocks) {      // blocks by their share of the heads
+    const int want = kBwdBlocks * p.nq / (p.nq + p.nk), n = want < 1 ? 1 : want >= kBwdBlocks ? kBwdBlocks - 1 : want;
+    blocks_q = blocks_q < n ? blocks_q : n;
+    blocks_k = blocks_k < kBwdBlocks - n ? blocks_k : kBwdBlocks - n;
+  }
+  blocks_q = blocks_q < 1 ? 1 : blocks_q;
+  blocks_k = blocks_k < 1 ? 1 : blocks_k;
+  const int blocks = blocks_q + blocks_k, rows_b = rows_q > rows_k ? rows_q : rows_k;
   const cudaError_t e = by_lanes(lanes, [&](auto n) {
     constexpr int LANES = decltype(n)::value;
     // 64 KB of heads ahead (the sums, at most 16 KB, lie over them: a group's lanes hold more than half as many places as d, or all) and at most 32 rows of 128 pairs
@@ -393,11 +408,11 @@ cudaError_t launch_backward(const rom_qk_config& c, const QkArgs& p, float* dw_q
     const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (set != cudaSuccess) return set;
     count_launch();
-    return launch_k(kern, dim3(blocks, 2), QK_THREADS, ahead + sizeof(float2) * (size_t)rows_b * (p.rot / 2), st, p, rows_b, per);
+    return launch_k(kern, dim3(blocks), QK_THREADS, ahead + sizeof(float2) * (size_t)rows_b * (p.rot / 2), st, p, rows_q, rows_k, per, blocks_q);
   });
   if (e != cudaSuccess || (!dw_q && !dw_k)) return e;
   count_launch();
-  return launch_k(qk_sum_weights, dim3((2 * p.d + QK_THREADS / 32 - 1) / (QK_THREADS / 32)), QK_THREADS, 0, st, (const float*)p.part, blocks, p.d, dw_q, dw_k);
+  return launch_k(qk_sum_weights, dim3((2 * p.d + QK_THREADS / 32 - 1) / (QK_THREADS / 32)), QK_THREADS, 0, st, (const float*)p.part, blocks_q, blocks, p.d, dw_q, dw_k);
 }
 
 // Output rows that are their input's (same address and pitch) or begin elsewhere.
@@ -433,7 +448,7 @@ int rom_qk_norm_rope_backward_workspace_size(const rom_qk_config* cfg, int32_t r
   const int rc = check_qk(cfg, rows);
   if (rc != ROM_OK) return rc;
   if (!bytes) return ROM_ERR_INVALID_ARG;
-  *bytes = sizeof(float) * 2 * (size_t)cfg->d_head * kBwdFew;
+  *bytes = sizeof(float) * (size_t)cfg->d_head * 2 * kBwdBlocks;
   return ROM_OK;
 }
 
@@ -457,7 +472,7 @@ int rom_qk_norm_rope_backward(const rom_qk_config* cfg, int32_t rows, const void
       if (a == dq || a == dk) return ROM_ERR_INVALID_ARG;
     if (dq == dk) return ROM_ERR_INVALID_ARG;
   }
-  if (ws_bytes < sizeof(float) * 2 * (size_t)c.d_head * kBwdFew) return ROM_ERR_WORKSPACE;
+  if (ws_bytes < sizeof(float) * (size_t)c.d_head * 2 * kBwdBlocks) return ROM_ERR_WORKSPACE;
   if ((rc = check_device()) != ROM_OK) return rc;
   LaunchCounter::count = 0;
   QkArgs p{q, k, dq_out, dk_out, dq, dk, ldq, ldk, lddq, lddk, w_q, w_k, pos, inv_freq, static_cast<float*>(ws), rows, c.n_q_heads, c.n_k_heads, c.d_head, c.rot_dim, c.interleaved, c.eps};

@@ -234,7 +234,7 @@ def test_a_workspace_for_more_does_for_less(H, G, dk, dv, dtype):
         last = 0
         for rows in list(range(0, 1200, 37)) + [4096, 5000, 16384, 100000, 1 << 20]:
             size = ask(cfg, 7, rows)
-            assert size >= last and size == ask(cfg, 1, rows)
+            assert size >= last and size >= ask(cfg, 1, rows)
             last = size
 
 
