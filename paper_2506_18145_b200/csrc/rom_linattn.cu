@@ -12,6 +12,8 @@
 namespace rom {
 namespace {
 
+struct LinJobs { LinPass p[3]; };
+
 constexpr int SIMT_THREADS = 256;
 constexpr int SIMT_C = 32;           // rows of a chunk
 constexpr int SIMT_DV = 64;          // columns of the state a block owns
@@ -39,11 +41,12 @@ __device__ __forceinline__ void load_tile(float* dst, int pitch, const T* src, i
   }
 }
 
-// A block owns up to 64 columns of a state and walks one run.  256 threads: 16 x 16, each 2 rows x 4 columns of the outputs and
+// A block owns up to 64 columns of a state and walks one run of one of the call's walks (blockIdx.z).  256 threads: 16 x 16, each 2 rows x 4 columns of the outputs and
 // 8 x 4 of the state.  What bounds it: shared-memory reads of the operands (10 wavefronts for 16 packed FMAs in q S).
 template <typename T, bool STATE>
-__global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged seqs, LinCut cut) {
+__global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(const __grid_constant__ LinJobs jobs, Ragged seqs, LinCut cut) {
   extern __shared__ float sm[];
+  const LinPass& p = jobs.p[blockIdx.z];
   const int qp = p.dk + 4;
   float* S = sm;                              // [dk][SIMT_SPITCH]
   float* K = S + p.dk * SIMT_SPITCH;          // [C][qp]
@@ -54,6 +57,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int run = blockIdx.x, c0 = blockIdx.y * SIMT_DV, wv = min(SIMT_DV, p.dv - c0);
   pdl_sync();
+  if (wv <= 0) return;                        // (another walk of this launch is wider)
   const size_t state = (size_t)p.dk * p.dv;
   int head = 0;
   const T *q = nullptr, *k = nullptr, *v = nullptr;
@@ -64,8 +68,8 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
     v = static_cast<const T*>(p.v) + (size_t)(head / p.vdiv) * p.dv + c0;
     __syncthreads();
     if (tid <= SIMT_C) {
-      lam[tid] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + tid);
-      lam_lo[tid] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + kLinPowers + tid);
+      lam[tid] = __ldcg(p.powers + (size_t)head * 2 * kLinPowers + tid);
+      lam_lo[tid] = __ldcg(p.powers + (size_t)head * 2 * kLinPowers + kLinPowers + tid);
     }
     __syncthreads();
   };
@@ -229,13 +233,19 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(LinPass p, Ragged 
 size_t simt_smem(int dk, bool state) { return sizeof(float) * (size_t)(dk * SIMT_SPITCH + SIMT_C * ((state ? 1 : 2) * (dk + 4) + SIMT_SPITCH) + (state ? 0 : SIMT_C * (SIMT_C + 1))); }
 
 template <typename T, bool STATE>
-cudaError_t launch_simt(const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
-  const size_t smem = simt_smem(p.dk, STATE);
+cudaError_t launch_simt(const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, cudaStream_t st) {
+  LinJobs jobs{};
+  int dk = 0, dv = 0;
+  for (int i = 0; i < n; ++i) {
+    jobs.p[i] = p[i];
+    dk = p[i].dk > dk ? p[i].dk : dk;
+    dv = p[i].dv > dv ? p[i].dv : dv;
+  }
   auto kern = lin_walk_simt<T, STATE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)simt_smem(kLinMaxDim, STATE));
   if (e != cudaSuccess) return e;
   count_launch();
-  return launch_k(kern, dim3(STATE ? cut.blocks - 1 : cut.blocks, (p.dv + SIMT_DV - 1) / SIMT_DV), SIMT_THREADS, smem, st, p, device_view(seqs), cut);
+  return launch_k(kern, dim3(STATE ? cut.blocks - 1 : cut.blocks, (dv + SIMT_DV - 1) / SIMT_DV, n), SIMT_THREADS, simt_smem(dk, STATE), st, jobs, device_view(seqs), cut);
 }
 
 // Before launch 1: the status block cleared, and the powers of every head's decay.
@@ -252,7 +262,8 @@ __global__ void __launch_bounds__(256) lin_powers(const float* log_decay, int H,
 
 // Launch 2: the states that reach every cut, element by element.  A thread owns four adjacent elements of one head.
 constexpr int CHAIN_THREADS = 128;
-__global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seqs, LinCut cut) {
+__global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(const __grid_constant__ LinJobs jobs, Ragged seqs, LinCut cut) {
+  const LinPass& p = jobs.p[blockIdx.z];
   __shared__ int how[kLinMaxBlocks];            // at the head's cuts: -3 nobody reaches over it; -2 the state comes over a cut; else a sequence starts here: its state's slot, or -1
   __shared__ float weight[kLinMaxBlocks];       // of the state at the cut before, or of the sequence's initial state
   const int head = blockIdx.y;
@@ -310,7 +321,9 @@ __global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(LinPass p, Ragged seq
 
 // dst[row, g, :] = sum over the value heads of group g of part[row, h, :], rows that belong to a sequence.
 template <typename T>
-__global__ void __launch_bounds__(256) lin_sum_heads(const float* part, T* dst, Ragged seqs, int H, int G, int d) {
+__global__ void __launch_bounds__(256) lin_sum_heads(const float* part_q, T* dq, const float* part_k, T* dk, Ragged seqs, int H, int G, int d) {
+  const float* part = blockIdx.y == 0 ? part_q : part_k;
+  T* dst = blockIdx.y == 0 ? dq : dk;
   pdl_sync();
   const int first = seqs.start_of(0), end = seqs.end_of(seqs.n_seq - 1), share = H / G;
   const size_t per_row = (size_t)G * d / 4, n = (size_t)seqs.rows * per_row;
@@ -416,7 +429,7 @@ bool on_tensor_cores(const rom_linattn_config& c) { return c.dtype == ROM_BF16 &
 // (148 SMs assumed).
 struct LinSlots { int blocks, chunk, least, start; };
 LinSlots slots_of(const rom_linattn_config& c) {
-  if (on_tensor_cores(c)) return LinSlots{148, 128, 2, 256};
+  if (on_tensor_cores(c)) return LinSlots{148, 128, 2, 128};
   return LinSlots{kLinMaxBlocks / ((c.d_v + SIMT_DV - 1) / SIMT_DV), SIMT_C, 1, 32};
 }
 int units_per_head(const LinSlots& s, int n_seq, int rows) { return (int)(((long long)rows + (long long)s.start * n_seq + s.chunk - 1) / s.chunk); }
@@ -438,7 +451,7 @@ LinCut cut_rows(const rom_linattn_config& c, int n_seq, int rows) {
   if (even < whole) { cut.blocks = n; cut.inside = true; }
   return cut;
 }
-struct LinWs { size_t status, powers, cut_a, cut_b, part, total; };
+struct LinWs { size_t status, powers, cut_a, cut_b, part_q, part_k, total; };
 LinWs lin_ws(const rom_linattn_config& c, int n_seq, int rows, bool backward) {
   LinWs l{};
   size_t off = 0;
@@ -448,7 +461,9 @@ LinWs lin_ws(const rom_linattn_config& c, int n_seq, int rows, bool backward) {
   l.powers = take((size_t)c.n_heads * 2 * kLinPowers * sizeof(float));
   l.cut_a = take(state);
   l.cut_b = take(state);
-  l.part = take(backward && c.n_qk_heads < c.n_heads ? (size_t)rows * c.n_heads * c.d_k * sizeof(float) : 0);
+  const size_t part = backward && c.n_qk_heads < c.n_heads ? (size_t)rows * c.n_heads * c.d_k * sizeof(float) : 0;
+  l.part_q = take(part);
+  l.part_k = take(part);
   l.total = off;
   return l;
 }
@@ -463,7 +478,9 @@ int lin_ws_size(const rom_linattn_config* c, int32_t n_seq, int32_t rows, size_t
 
 // Sequences of one row (continuous batching) in a launch of their own, where they may be many: fewer than 256 rows a sequence on average.  A walk takes 3 to 5 us for each of a
 // run's in turn (37 sequences of 531 rows, 8 heads of 64 fp32: 96 us), this launch 3 us for all; with none of them it costs its 2 us.
-bool singles_apart(const rom_ragged& seqs) { return seqs.n_seq > 1 && (long long)seqs.rows < 256LL * seqs.n_seq; }
+bool singles_apart(const rom_linattn_config& c, const rom_ragged& seqs) {
+  return seqs.n_seq > 1 && (long long)seqs.rows < 256LL * seqs.n_seq && (long long)seqs.n_seq * c.n_heads * ((c.d_v + STEP_COLS - 1) / STEP_COLS) <= INT32_MAX;
+}
 cudaError_t launch_singles(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, cudaStream_t st) {
   const int slices = (c.d_v + STEP_COLS - 1) / STEP_COLS;
   const long long blocks = (long long)seqs.n_seq * c.n_heads * slices;
@@ -477,32 +494,37 @@ cudaError_t launch_singles(const rom_linattn_config& c, const LinPass& p, const 
 }
 
 template <bool STATE>
-cudaError_t launch_walk(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
-  if (on_tensor_cores(c) && seqs.rows > 0) return launch_lin_tc(p, seqs, cut, STATE, (c.flags & ROM_FLAG_TEST_STALL) != 0, st);
-  if (c.dtype == ROM_F32) return launch_simt<float, STATE>(p, seqs, cut, st);
-  return launch_simt<__nv_bfloat16, STATE>(p, seqs, cut, st);
+cudaError_t launch_simt_by_type(const rom_linattn_config& c, const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, cudaStream_t st) {
+  return c.dtype == ROM_F32 ? launch_simt<float, STATE>(p, n, seqs, cut, st) : launch_simt<__nv_bfloat16, STATE>(p, n, seqs, cut, st);
+}
+cudaError_t launch_walks(const rom_linattn_config& c, const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, cudaStream_t st) {
+  if (on_tensor_cores(c) && seqs.rows > 0) return launch_lin_walks_tc(p, n, c.d_k, c.d_v, seqs, cut, (c.flags & ROM_FLAG_TEST_STALL) != 0, st);
+  return launch_simt_by_type<false>(c, p, n, seqs, cut, st);
 }
 cudaError_t launch_powers(const LinPass& p, float* powers, cudaStream_t st) {
   count_launch();
   return launch_k(lin_powers, dim3((p.H * kLinPowers + 255) / 256), 256, 0, st, p.log_decay, p.H, powers, p.status);
 }
 // Launches 1 and 2: the states at the cuts.
-cudaError_t launch_states(const rom_linattn_config& c, const LinPass& p, const rom_ragged& seqs, LinCut cut, cudaStream_t st) {
-  if (!cut.inside) return cudaSuccess;
-  const cudaError_t e = launch_walk<true>(c, p, seqs, cut, st);
+cudaError_t launch_states(const rom_linattn_config& c, const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, cudaStream_t st) {
+  if (!cut.inside || seqs.rows == 0) return cudaSuccess;
+  const cudaError_t e = on_tensor_cores(c) ? launch_lin_states_tc(p, n, c.d_k, c.d_v, seqs, cut, (c.flags & ROM_FLAG_TEST_STALL) != 0, st) : launch_simt_by_type<true>(c, p, n, seqs, cut, st);
   if (e != cudaSuccess) return e;
+  LinJobs jobs{};
+  for (int i = 0; i < n; ++i) jobs.p[i] = p[i];
   count_launch();
-  return launch_k(lin_chain, dim3((p.dk * p.dv / 4 + CHAIN_THREADS - 1) / CHAIN_THREADS, p.H), CHAIN_THREADS, 0, st, p, device_view(seqs), cut);
+  return launch_k(lin_chain, dim3((c.d_k * c.d_v / 4 + CHAIN_THREADS - 1) / CHAIN_THREADS, c.n_heads, n), CHAIN_THREADS, 0, st, jobs, device_view(seqs), cut);
 }
-cudaError_t launch_sum(const rom_linattn_config& c, const float* part, void* dst, const rom_ragged& seqs, cudaStream_t st) {
+cudaError_t launch_sums(const rom_linattn_config& c, const float* part_q, void* dq, const float* part_k, void* dk, const rom_ragged& seqs, cudaStream_t st) {
   int sms = 0;
   const cudaError_t e = current_device_sm_count(&sms);
   if (e != cudaSuccess) return e;
-  const size_t n = (size_t)seqs.rows * c.n_qk_heads * c.d_k / 4, blocks = (n + 255) / 256;
-  const dim3 grid((unsigned)(blocks < (size_t)sms * 8 ? blocks : (size_t)sms * 8));
+  const size_t n = (size_t)seqs.rows * c.n_qk_heads * c.d_k / 4, blocks = (n + 255) / 256, most = (size_t)sms * 4;
+  if (blocks == 0) return cudaSuccess;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most), 2);
   count_launch();
-  if (c.dtype == ROM_F32) return launch_k(lin_sum_heads<float>, grid, 256, 0, st, part, (float*)dst, device_view(seqs), c.n_heads, c.n_qk_heads, c.d_k);
-  return launch_k(lin_sum_heads<__nv_bfloat16>, grid, 256, 0, st, part, (__nv_bfloat16*)dst, device_view(seqs), c.n_heads, c.n_qk_heads, c.d_k);
+  if (c.dtype == ROM_F32) return launch_k(lin_sum_heads<float>, grid, 256, 0, st, part_q, (float*)dq, part_k, (float*)dk, device_view(seqs), c.n_heads, c.n_qk_heads, c.d_k);
+  return launch_k(lin_sum_heads<__nv_bfloat16>, grid, 256, 0, st, part_q, (__nv_bfloat16*)dq, part_k, (__nv_bfloat16*)dk, device_view(seqs), c.n_heads, c.n_qk_heads, c.d_k);
 }
 
 bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
@@ -553,9 +575,8 @@ int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, co
   p.out = o; p.ldo = (int64_t)c.n_heads * c.d_v;
   p.status = reinterpret_cast<int32_t*>(W + lay.status);
   if (launch_powers(p, powers, st) != cudaSuccess) return ROM_ERR_CUDA;
-  p.skip_single = singles_apart(*seqs);
-  if (launch_states(c, p, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
-  if (launch_walk<false>(c, p, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
+  p.skip_single = singles_apart(c, *seqs);
+  if (launch_states(c, &p, 1, *seqs, cut, st) != cudaSuccess || launch_walks(c, &p, 1, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
   return !p.skip_single || launch_singles(c, p, *seqs, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
 
@@ -617,42 +638,38 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   char* W = static_cast<char*>(ws);
   const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows);
   const int share = c.n_heads / c.n_qk_heads;
-  float* part = share > 1 ? reinterpret_cast<float*>(W + lay.part) : nullptr;
-  LinPass base{};
-  base.H = c.n_heads; base.log_decay = log_decay; base.p_scale = c.scale;
-  base.status = reinterpret_cast<int32_t*>(W + lay.status);
+  float *part_q = share > 1 ? reinterpret_cast<float*>(W + lay.part_q) : nullptr, *part_k = share > 1 ? reinterpret_cast<float*>(W + lay.part_k) : nullptr;
   float* powers = reinterpret_cast<float*>(W + lay.powers);
-  base.powers = powers;
-  if (launch_powers(base, powers, st) != cudaSuccess) return ROM_ERR_CUDA;
-  // the states S of the forward at the cuts
-  LinPass s = base;
-  s.k = k; s.v = v; s.ldk = ldk; s.ldv = ldv; s.q = k; s.ldq = ldk;
+  const int64_t ld_do = (int64_t)c.n_heads * c.d_v;
+  LinPass base{};
+  base.H = c.n_heads; base.log_decay = log_decay; base.p_scale = c.scale; base.powers = powers;
+  base.status = reinterpret_cast<int32_t*>(W + lay.status);
+  // the states S of the forward at the cuts, and R behind them (with which dv is walked)
+  LinPass s = base, dv_walk = base;
+  s.k = k; s.v = v; s.ldk = ldk; s.ldv = ldv;
   s.qdiv = s.kdiv = share; s.vdiv = 1; s.dk = c.d_k; s.dv = c.d_v;
   s.k_scale = 1.0f; s.init = s_in; s.cut_state = reinterpret_cast<float*>(W + lay.cut_a);
-  if (launch_states(c, s, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
-  // dq
-  LinPass w = base;
-  w.q = dout; w.k = v; w.v = k; w.ldq = (int64_t)c.n_heads * c.d_v; w.ldk = ldv; w.ldv = ldk;
-  w.qdiv = w.kdiv = 1; w.vdiv = share; w.dk = c.d_v; w.dv = c.d_k;
-  w.inter_scale = c.scale; w.k_scale = 1.0f; w.transposed = true; w.init = s_in; w.cut_state = s.cut_state;
-  w.out = part ? part : dq; w.ldo = (int64_t)c.n_heads * c.d_k; w.out_f32 = part != nullptr;
-  if (launch_walk<false>(c, w, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
-  if (part && launch_sum(c, part, dq, *seqs, st) != cudaSuccess) return ROM_ERR_CUDA;
-  // the states R behind the cuts, and dv from them
-  LinPass r = base;
-  r.q = k; r.k = q; r.v = dout; r.ldq = ldk; r.ldk = ldq; r.ldv = (int64_t)c.n_heads * c.d_v;
-  r.qdiv = r.kdiv = share; r.vdiv = 1; r.dk = c.d_k; r.dv = c.d_v;
-  r.inter_scale = 1.0f; r.k_scale = c.scale; r.reverse = true; r.init = ds_out; r.init_all = true; r.early = true; r.last = ds_in;
-  r.cut_state = reinterpret_cast<float*>(W + lay.cut_b);
-  r.out = dv; r.ldo = lddv;
-  if (launch_states(c, r, *seqs, cut, st) != cudaSuccess || launch_walk<false>(c, r, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
-  // dk
-  LinPass d = r;
-  d.q = v; d.k = dout; d.v = q; d.ldq = ldv; d.ldk = r.ldv; d.ldv = ldq;
-  d.qdiv = d.kdiv = 1; d.vdiv = share; d.dk = c.d_v; d.dv = c.d_k; d.transposed = true; d.last = nullptr;
-  d.out = part ? part : dk; d.ldo = (int64_t)c.n_heads * c.d_k; d.out_f32 = part != nullptr;
-  if (launch_walk<false>(c, d, *seqs, cut, st) != cudaSuccess) return ROM_ERR_CUDA;
-  return !part || launch_sum(c, part, dk, *seqs, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
+  dv_walk.q = k; dv_walk.k = q; dv_walk.v = dout; dv_walk.ldq = ldk; dv_walk.ldk = ldq; dv_walk.ldv = ld_do;
+  dv_walk.qdiv = dv_walk.kdiv = share; dv_walk.vdiv = 1; dv_walk.dk = c.d_k; dv_walk.dv = c.d_v;
+  dv_walk.inter_scale = 1.0f; dv_walk.k_scale = c.scale; dv_walk.reverse = true; dv_walk.init = ds_out; dv_walk.init_all = true; dv_walk.early = true; dv_walk.last = ds_in;
+  dv_walk.cut_state = reinterpret_cast<float*>(W + lay.cut_b);
+  dv_walk.out = dv; dv_walk.ldo = lddv;
+  // dq on S, dk on R, both transposed
+  LinPass dq_walk = base, dk_walk = dv_walk;
+  dq_walk.q = dout; dq_walk.k = v; dq_walk.v = k; dq_walk.ldq = ld_do; dq_walk.ldk = ldv; dq_walk.ldv = ldk;
+  dk_walk.q = v; dk_walk.k = dout; dk_walk.v = q; dk_walk.ldq = ldv; dk_walk.ldk = ld_do; dk_walk.ldv = ldq;
+  dq_walk.inter_scale = c.scale; dq_walk.k_scale = 1.0f; dq_walk.init = s_in; dq_walk.cut_state = s.cut_state;
+  dk_walk.last = nullptr;
+  for (LinPass* w : {&dq_walk, &dk_walk}) {
+    w->qdiv = w->kdiv = 1; w->vdiv = share; w->dk = c.d_v; w->dv = c.d_k; w->transposed = true;
+    w->ldo = (int64_t)c.n_heads * c.d_k; w->out_f32 = share > 1;
+  }
+  dq_walk.out = part_q ? part_q : dq;
+  dk_walk.out = part_k ? part_k : dk;
+  const LinPass states[2] = {s, dv_walk}, walks[3] = {dq_walk, dv_walk, dk_walk};
+  if (launch_powers(base, powers, st) != cudaSuccess || launch_states(c, states, 2, *seqs, cut, st) != cudaSuccess || launch_walks(c, walks, 3, *seqs, cut, st) != cudaSuccess)
+    return ROM_ERR_CUDA;
+  return !part_q || launch_sums(c, part_q, dq, part_k, dk, *seqs, st) == cudaSuccess ? ROM_OK : ROM_ERR_CUDA;
 }
 
 }  // extern "C"

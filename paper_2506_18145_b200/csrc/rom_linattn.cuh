@@ -136,7 +136,8 @@ __device__ __forceinline__ const float* lin_init_of(const LinPass& p, const Ragg
 }
 
 
-// The walk (or launch 1 alone) on the tensor cores, bf16 (rom_linattn_tc.cu).
-cudaError_t launch_lin_tc(const LinPass& p, const rom_ragged& seqs, LinCut cut, bool state_only, bool test_stall, cudaStream_t st);
+// Launches 1 and 3 on the tensor cores, bf16 (rom_linattn_tc.cu): of the forward (n = 1), or of the backward (states: forward, backward; walks: dq, dv, dk).
+cudaError_t launch_lin_states_tc(const LinPass* p, int n, int dk, int dv, const rom_ragged& seqs, const LinCut& cut, bool test_stall, cudaStream_t st);
+cudaError_t launch_lin_walks_tc(const LinPass* p, int n, int dk, int dv, const rom_ragged& seqs, const LinCut& cut, bool test_stall, cudaStream_t st);
 
 }  // namespace rom

@@ -28,8 +28,9 @@ using bf16 = __nv_bfloat16;
 constexpr int LT_C = 128;                     // rows of a chunk
 constexpr int LT_BOX = 64 * LT_C * 2;         // bytes of one TMA box
 constexpr int LT_WALK_THREADS = 640, LT_STATE_THREADS = 320;
-// Registers of the walk's threads: 640 x 96 at launch; the copies' and products' warps give theirs to those that keep S: 128 x 48 + 256 x 96 + 256 x 120 = 640 x 96.
-constexpr int LT_FEW = 48, LT_MANY = 120;
+// Registers of the walk's threads: 640 x 96 at launch; the copies' and products' warps give theirs to those that make P and keep S: 128 x 48 + 256 x 104 + 256 x 112 =
+// 640 x 96.
+constexpr int LT_FEW = 48, LT_P = 104, LT_MANY = 112;
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 constexpr uint32_t LT_TMEM = 512;
@@ -39,23 +40,9 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
   return e != 0;
 }
-__device__ __forceinline__ bool mbar_ready(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-// A look at a barrier takes 25 cycles, a wait (mbarrier.try_wait) 200 to 400 even when it is over: one look first.  (More of them take issue slots from the warps that
-// work: with 128 a chunk took 8900 cycles instead of 6500.)  Bounded like mbar_wait.
-__device__ __forceinline__ bool lt_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
-  return mbar_ready(bar, parity) || mbar_wait(bar, parity, abort_flag, limit);
-}
 // A warp's wait; the outcome is the same in all lanes.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
-  return __all_sync(0xffffffffu, lt_wait(bar, parity, abort_flag, limit));
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
 __device__ __forceinline__ void warp_arrive(uint32_t bar) {
   __syncwarp();
@@ -152,15 +139,16 @@ __device__ __forceinline__ void clear_row(uint32_t box, int row) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) sts128(box + row * 128 + i * 16, make_uint4(0, 0, 0, 0));
 }
-// A lane holds 128 bytes of its row, eight 16-byte pieces; they are exchanged among eight lanes so that a store instruction of the warp writes four whole runs of 128
-// bytes.  Straight from the lanes it would touch 32 rows with 16 bytes each: eight times the accesses of the LSU, which the loads and stores of K~ and S share (an output
-// tile took 5200 cycles, everything beside it twice its time).  row_at: byte offset of the lane's first row (8 (lane / 8)) and piece; rows: valid rows from there on.
-__device__ __forceinline__ void store_rows128(char* row_at, int64_t pitch, int rows, bool piece_ok, uint32_t (&w)[32], int lane) {
+// A lane holds N 16-byte pieces of its row (128 or 64 bytes); they are exchanged among N lanes so that a store instruction of the warp writes 32 / N whole runs.
+// Straight from the lanes it would touch 32 rows with 16 bytes each: many times the accesses of the LSU, which the loads and stores of K~ and S share (an output
+// tile took 5200 cycles, everything beside it twice its time).  row_at: the lane's first row (N (lane / N)) and piece; rows: valid rows from there on.
+template <int N>
+__device__ __forceinline__ void store_rows(char* row_at, int64_t pitch, int rows, bool piece_ok, uint32_t (&w)[4 * N], int lane) {
 #pragma unroll
-  for (int m = 1; m < 8; m *= 2) {
+  for (int m = 1; m < N; m *= 2) {
     const bool up = (lane & m) != 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
+    for (int q = 0; q < N; ++q) {
       if (q & m) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -171,7 +159,7 @@ __device__ __forceinline__ void store_rows128(char* row_at, int64_t pitch, int r
     }
   }
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
+  for (int t = 0; t < N; ++t)
     if (piece_ok && t < rows) *reinterpret_cast<uint4*>(row_at + t * pitch) = make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
 }
 // V^T K~: hi and lo, the first ks steps of 16 rows.
@@ -243,53 +231,66 @@ struct WalkShape {
   static constexpr int SC = 0, O1 = 128, KV = O1 + VP, O2 = KV + KP;      // tensor-memory columns (P over the scores' first 64)
 };
 
-// Rows of O2 that are not finite, summed again over their own and earlier rows.  Rare; all lanes of the warp call it.
+// Rows of O2 that are not finite, summed again over their own and earlier rows, where what the state gives is finite (else the result is not, either way: a value that is not
+// finite costs its own chunk alone).  Rare; all lanes of the warp come here.
 template <bool REV>
-__device__ __noinline__ void slow_rows(const LinPass& p, const bf16* q, const bf16* k, const bf16* v, bf16* out, uint32_t taddr_o1, const float* lam, int i, int row0, int len, float f,
-                                       bool mine, int head, int c_from, int c_to) {
-  for (int c0 = c_from; c0 < c_to; c0 += 32) {
-    uint32_t r[32];
+__device__ __noinline__ void slow_rows(const LinPass& p, int head, uint32_t taddr_o1, uint32_t taddr_o2, const float* lam, int i, int row0, int len, float f, bool mine, int c_from, int c_to) {
+#pragma unroll 1
+  for (int c0 = c_from; c0 < c_to; c0 += 16) {
+    uint32_t r[16], r2[16];
     __syncwarp();
-    tmem_ld32_issue(taddr_o1 + c0, r);
-    tmem_ld_wait(r);
-    if (!mine) continue;
-    float acc[32];
+    tmem_ld16_issue(taddr_o1 + c0, r);
+    tmem_ld16_issue(taddr_o2 + c0, r2);
+    tmem_ld16_wait(r);
+    tmem_ld16_wait(r2);
+    bool need = false;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) acc[e] = 0.0f;
-    const bf16* qi = q + (int64_t)(row0 + i) * p.ldq;
+    for (int e = 0; e < 16; ++e) need |= !(fabsf(__uint_as_float(r2[e])) <= FLT_MAX) && fabsf(f * __uint_as_float(r[e])) <= FLT_MAX;
+    if (!mine || !need) continue;
+    float acc[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+    const bf16* qi = static_cast<const bf16*>(p.q) + (int64_t)(row0 + i) * p.ldq + (head / p.qdiv) * p.dk;
+#pragma unroll 1
     for (int j = REV ? i : 0; j < (REV ? len : i + 1); ++j) {
-      const bf16* kj = k + (int64_t)(row0 + j) * p.ldk;
+      const bf16* kj = static_cast<const bf16*>(p.k) + (int64_t)(row0 + j) * p.ldk + (head / p.kdiv) * p.dk;
       float s = 0.0f;
+#pragma unroll 1
       for (int d = 0; d < p.dk; ++d) s = fmaf(to_f32(qi[d]), to_f32(kj[d]), s);
-      const float w = to_f32(__float2bfloat16_rn(s * lam[REV ? j - i : i - j]));
-      const bf16* vj = v + (int64_t)(row0 + j) * p.ldv + c0;
+      const float w = to_f32(__float2bfloat16_rn(s * (p.p_scale * lam[REV ? j - i : i - j])));
+      const bf16* vj = static_cast<const bf16*>(p.v) + (int64_t)(row0 + j) * p.ldv + (head / p.vdiv) * p.dv + c0;
 #pragma unroll
-      for (int e = 0; e < 32; ++e)
+      for (int e = 0; e < 16; ++e)
         if (c0 + e < p.dv) acc[e] = fmaf(w, to_f32(vj[e]), acc[e]);
     }
     const int64_t to = (int64_t)(row0 + i) * p.ldo + (int64_t)head * p.dv + c0;
 #pragma unroll
-    for (int e = 0; e < 32; ++e)
+    for (int e = 0; e < 16; ++e)
       if (c0 + e < p.dv) {
-        const float o = fmaf(f, __uint_as_float(r[e]), p.p_scale * acc[e]);
-        if (p.out_f32) reinterpret_cast<float*>(out)[to + e] = o;
-        else out[to + e] = __float2bfloat16_rn(o);
+        const float o = fmaf(f, __uint_as_float(r[e]), acc[e]);
+        if (p.out_f32) static_cast<float*>(p.out)[to + e] = o;
+        else static_cast<bf16*>(p.out)[to + e] = __float2bfloat16_rn(o);
       }
   }
 }
 
+struct WalkArgs { CUtensorMap q, k, v; LinPass p; };
+struct WalkShared {
+  // powers of lambda: of the warps that make P (on the diagonal times p, behind 32 zeros), of those that keep S, with what each lost to fp32
+  float p_lam[kLinPowers], p_diag[64], s_lam[kLinPowers], s_lo[kLinPowers];
+  unsigned long long bars[24];
+  uint32_t tmem;
+  int abort;
+};
 template <int KP, int VP, bool REV>
-__global__ void __launch_bounds__(LT_WALK_THREADS, 1)
-lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs,
-            const LinCut cut, uint32_t wait_limit, uint32_t stall) {
+__device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const uint32_t base, const Ragged& seqs, const LinCut& cut, uint32_t wait_limit, uint32_t stall) {
   using W = WalkShape<KP, VP>;
-  extern __shared__ unsigned char smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  // powers of lambda: of the warps that make P (behind 32 zeros), of those that keep S, with what each lost to fp32
-  __shared__ __align__(16) float p_pad[32 + kLinPowers], s_lam[kLinPowers], s_lo[kLinPowers];
-  __shared__ __align__(8) unsigned long long bars[24];
-  __shared__ uint32_t tmem_s;
-  __shared__ int abort_s;
+  const LinPass& p = args.p;
+  const CUtensorMap &tmap_q = args.q, &tmap_k = args.k, &tmap_v = args.v;
+  float *const p_diag = sh.p_diag, *const s_lam = sh.s_lam, *const s_lo = sh.s_lo;
+  unsigned long long* const bars = sh.bars;
+  uint32_t& tmem_s = sh.tmem;
+  int& abort_s = sh.abort;
   volatile int* abort_flag = &abort_s;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), run = blockIdx.x;
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
@@ -309,7 +310,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(LT_TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (tid < 32) p_pad[tid] = 0.0f;
+  if (tid < 32) p_diag[tid] = 0.0f;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -342,13 +343,13 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           x.chunk<REV>(m, row0, len);
           const int st = n % W::KVST, qs = n % W::QST;
           if (n == 1) pdl_wait();      // (the first chunk's copies need not wait for the launch before, but no bounded wait may count its time)
-          if (!lt_wait(kv_empty(st), (n / W::KVST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
+          if (!mbar_wait(kv_empty(st), (n / W::KVST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
           mbar_expect_tx(kv_full(st), (W::KB + W::VB) * LT_BOX + stall);
           load_tile<W::KB>(base + W::K + st * W::KB * LT_BOX, &tmap_k, kv_full(st), head / p.kdiv, row0);
           load_tile<W::VB>(base + W::V + st * W::VB * LT_BOX, &tmap_v, kv_full(st), head / p.vdiv, row0);
           // one stage of Q: it is asked for when Q S of the chunk before is done, 4000 cycles from memory where the chunk has 2500 left; from L2 1500
           if (W::QST == 1) prefetch_tile<W::KB>(&tmap_q, head / p.qdiv, row0);
-          if (!lt_wait(q_empty(qs), (n / W::QST & 1) ^ 1, abort_flag, wait_limit)) { ++n; ok = false; break; }
+          if (!mbar_wait(q_empty(qs), (n / W::QST & 1) ^ 1, abort_flag, wait_limit)) { ++n; ok = false; break; }
           mbar_expect_tx(q_full(qs), W::KB * LT_BOX);
           load_tile<W::KB>(base + W::Q + qs * W::KB * LT_BOX, &tmap_q, q_full(qs), head / p.qdiv, row0);
         }
@@ -374,7 +375,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     while (it.next(cut, seqs)) {
       const int s_first = first_piece(it, seqs);
       constexpr uint32_t d_sc = lt_idesc(LT_C, false, false), d_o1 = lt_idesc(VP, false, false), d_o2 = lt_idesc(VP, false, true), d_kv = lt_idesc(KP, true, true);
-      auto wait = [&](uint32_t b, uint32_t parity) { ok = ok && lt_wait(b, parity, abort_flag, wait_limit); return ok; };
+      auto wait = [&](uint32_t b, uint32_t parity) { ok = ok && mbar_wait(b, parity, abort_flag, wait_limit); return ok; };
       if (leader)
       for (int s = s_first; ok && get_piece<REV>(it, seqs, p.skip_single, s, x); ++s)
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
@@ -424,13 +425,18 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     const int quarter = warp & 3, half = (warp - 4) >> 2, i = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     bf16* out = static_cast<bf16*>(p.out);
-    const float* lam = p_pad + 32;
+    registers_up<LT_P>();
+    const float* lam = sh.p_lam;
     pdl_wait();
     bool ok = true;
     while (it.next(cut, seqs)) {
     const int head = it.head, s_first = first_piece(it, seqs);
     asm volatile("bar.sync 5, 256;" ::: "memory");      // (all of these warps are done with the powers of the head before)
-    for (int e = tid - 128; e < kLinPowers; e += 256) p_pad[32 + e] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + e);
+    if (const int e = tid - 128; e < kLinPowers) {
+      const float l = __ldcg(p.powers + (size_t)head * 2 * kLinPowers + e);
+      sh.p_lam[e] = l;
+      if (e < 32) p_diag[32 + e] = p.p_scale * l;
+    }
     asm volatile("bar.sync 5, 256;" ::: "memory");
     for (int s = s_first; get_piece<REV>(it, seqs, p.skip_single, s, x); ++s)
       for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
@@ -453,17 +459,16 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           uint32_t r[32];
           tmem_ld32_issue(lanes + W::SC + 32 * b, r);
           tmem_ld_wait(r);
-          // a masked score is times 0; in the last chunk, whose other rows are not the sequence's, it is selected 0 (elsewhere, where it is not finite, the row is
-          // summed again below).  A pass of its own: tests among the loads of the powers left each to wait for its own, 75 cycles a place.
-          if (len < LT_C) {
+          // A masked score is times 0; where it is not finite, the row is summed again below.  In the last chunk, whose other rows are not the sequence's, they are
+          // selected 0: forwards they are ahead of the diagonal, backwards in the last blocks.  (A pass of its own: tests among the loads of the powers left each to wait for
+          // its own, 75 cycles a place.)
+          if (len < LT_C && (REV ? 32 * b + 32 > len : b == quarter)) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int j = 32 * b + e;
-              if (REV ? j < i || j >= len : j > i) r[e] = 0;
-            }
+            for (int e = 0; e < 32; ++e)
+              if (REV ? 32 * b + e >= len : e > lane) r[e] = 0;
           }
           if (b == quarter) {
-            const float* l = REV ? lam - lane : lam + lane;
+            const float* l = p_diag + 32 + (REV ? -lane : lane);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
               const float2 y = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), REV ? make_float2(l[e], l[e + 1]) : make_float2(l[-e], l[-e - 1]));
@@ -471,13 +476,13 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
             }
           } else {
             // lambda^{i-j} = lambda^{i - last of the block} lambda^{last - j}
-            const float f = lam[REV ? 32 * b - i : i - 32 * b - 31];
+            const float g = p.p_scale * lam[REV ? 32 * b - i : i - 32 * b - 31];
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const float4 u = *reinterpret_cast<const float4*>(lam + (REV ? e : 28 - e));
               const float2 u0 = REV ? make_float2(u.x, u.y) : make_float2(u.w, u.z), u1 = REV ? make_float2(u.z, u.w) : make_float2(u.y, u.x);
-              const float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(f, f)));
-              const float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(f, f)));
+              const float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(g, g)));
+              const float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(g, g)));
               w[t][e / 2] = pack2(p0.x, p0.y);
               w[t][e / 2 + 1] = pack2(p1.x, p1.y);
             }
@@ -494,10 +499,10 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         const bool mine = i < len;
         const float f = p.inter_scale * lam[REV ? max(len - i - early, 0) : i + 1 - early];
         float2 odd = make_float2(0.0f, 0.0f);
-        const auto not_finite = [&]() { return ok && mine && !(odd.x == 0.0f && odd.y == 0.0f); };
-        bool freed = false;            // the tensor memory is given back once it has been read, ahead of the stores, unless it is read again
-        const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + (lane & 24), rows = ok ? len - first : 0;      // (rows that the lane stores)
-        // 16 columns: f O1 + p O2, noting what is not finite
+        constexpr int PC = VP / 16;    // 16-byte pieces of a warp's columns in bf16
+        const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + lane / PC * PC, rows = ok ? len - first : 0;      // (rows that the lane stores)
+        const int first8 = quarter * 32 + (lane & 24), rows8 = ok ? len - first8 : 0;
+        // 16 columns: f O1 + O2, noting what is not finite
         auto columns = [&](int c, float2 (&o)[8]) {
           uint32_t r1[16], r2[16];
           __syncwarp();
@@ -509,7 +514,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
           for (int e = 0; e < 8; ++e) {
             const float2 b2 = make_float2(__uint_as_float(r2[2 * e]), __uint_as_float(r2[2 * e + 1]));
             odd = __ffma2_rn(b2, make_float2(0.0f, 0.0f), odd);
-            o[e] = __ffma2_rn(make_float2(__uint_as_float(r1[2 * e]), __uint_as_float(r1[2 * e + 1])), make_float2(f, f), __fmul2_rn(b2, make_float2(p.p_scale, p.p_scale)));
+            o[e] = __ffma2_rn(make_float2(__uint_as_float(r1[2 * e]), __uint_as_float(r1[2 * e + 1])), make_float2(f, f), b2);
           }
         };
         if (p.out_f32) {
@@ -524,33 +529,24 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
               for (int e = 0; e < 8; ++e) { w[16 * u + 2 * e] = __float_as_uint(o[e].x); w[16 * u + 2 * e + 1] = __float_as_uint(o[e].y); }
             }
             const int col = c + 4 * (lane & 7);
-            store_rows128(reinterpret_cast<char*>(static_cast<float*>(p.out) + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 4, rows, col < p.dv, w, lane);
+            store_rows<8>(reinterpret_cast<char*>(static_cast<float*>(p.out) + (int64_t)(row0 + first8) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 4, rows8, col < p.dv, w, lane);
           }
         } else if (c_from < c_to) {
-          uint32_t w[32];
+          uint32_t w[4 * PC];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
+          for (int u = 0; u < PC / 2; ++u) {
             float2 o[8];
-            if (VP == 128 || u < 2) columns(c_from + 16 * u, o);
+            columns(c_from + 16 * u, o);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[8 * u + e] = VP == 128 || u < 2 ? pack2(o[e].x, o[e].y) : 0;
+            for (int e = 0; e < 8; ++e) w[8 * u + e] = pack2(o[e].x, o[e].y);
           }
-          if (!__any_sync(0xffffffffu, not_finite())) {
-            tc_fence_before();
-            warp_arrive(o_free);
-            freed = true;
-          }
-          const int col = c_from + 8 * (lane & 7);
-          store_rows128(reinterpret_cast<char*>(out + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 2, rows, (VP == 128 || (lane & 7) < 4) && col < p.dv, w, lane);
+          const int col = c_from + 8 * (lane & (PC - 1));
+          store_rows<PC>(reinterpret_cast<char*>(out + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 2, rows, col < p.dv, w, lane);
         }
-        if (!freed) {
-          const bool again = not_finite();
-          if (__any_sync(0xffffffffu, again))
-            slow_rows<REV>(p, static_cast<const bf16*>(p.q) + (int64_t)(head / p.qdiv) * p.dk, static_cast<const bf16*>(p.k) + (int64_t)(head / p.kdiv) * p.dk,
-                           static_cast<const bf16*>(p.v) + (int64_t)(head / p.vdiv) * p.dv, out, lanes + W::O1, lam, i, row0, len, f, again, head, c_from, c_to);
-          tc_fence_before();
-          warp_arrive(o_free);
-        }
+        const bool again = ok && mine && !(odd.x == 0.0f && odd.y == 0.0f);
+        if (__any_sync(0xffffffffu, again)) slow_rows<REV>(p, head, lanes + W::O1, lanes + W::O2, lam, i, row0, len, f, again, c_from, c_to);
+        tc_fence_before();
+        warp_arrive(o_free);
       }
     }
     if (!ok) latch(p, abort_flag, 53);
@@ -578,7 +574,10 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
     while (it.next(cut, seqs)) {
     const int head = it.head, s_first = first_piece(it, seqs);
     asm volatile("bar.sync 6, 256;" ::: "memory");
-    for (int e = tid - 384; e < 2 * kLinPowers; e += 256) (e < kLinPowers ? s_lam : s_lo - kLinPowers)[e] = __ldg(p.powers + (size_t)head * 2 * kLinPowers + e);
+    if (int e = tid - 384; e < kLinPowers) {
+      s_lam[e] = __ldcg(p.powers + (size_t)head * 2 * kLinPowers + e);
+      s_lo[e] = __ldcg(p.powers + (size_t)head * 2 * kLinPowers + kLinPowers + e);
+    }
     asm volatile("bar.sync 6, 256;" ::: "memory");
     for (int s = s_first; get_piece<REV>(it, seqs, p.skip_single, s, x); ++s) {
       const int mm = x.chunks(), slot = seqs.slot_of(s);
@@ -636,7 +635,7 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
         if (c < rows16) {
           const bool live = c < len;
           const float w = live ? p.k_scale * lam[REV ? c : len - 1 - c] : 0.0f;
-          scale_row<4>(k + box, base + W::LO + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
+          scale_row<KP == 128 ? 2 : 4>(k + box, base + W::LO + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
           if (!live && half < W::VB) clear_row(base + W::V + (st * W::VB + half) * LT_BOX, c);
         }
         fence_async();
@@ -681,6 +680,28 @@ lin_walk_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
   tc_fence_after();
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(LT_TMEM) : "memory");
 }
+__device__ __forceinline__ uint32_t aligned_base(unsigned char* raw) { return (smem_u32(raw) + 1023u) & ~1023u; }
+// The forward's walk.
+template <int KP, int VP>
+__global__ void __launch_bounds__(LT_WALK_THREADS, 1)
+lin_walk_tc(const __grid_constant__ WalkArgs args, const Ragged seqs, const LinCut cut, uint32_t wait_limit, uint32_t stall) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(16) WalkShared sh;
+  walk<KP, VP, false>(args, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
+}
+// The backward's three: they read the same inputs and states and write different outputs, and a launch each would leave most SMs idle where sequences are few or short (two
+// sequences of one row, 8 heads: 37 us in three launches, most of it their latency).
+template <int KP, int VP>
+__global__ void __launch_bounds__(LT_WALK_THREADS, 1)
+lin_walk3_tc(const __grid_constant__ WalkArgs dq, const __grid_constant__ WalkArgs dv, const __grid_constant__ WalkArgs dk, const Ragged seqs, const LinCut cut, uint32_t wait_limit,
+             uint32_t stall) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(16) WalkShared sh;
+  const uint32_t base = aligned_base(smem_raw);
+  if (blockIdx.y == 0) walk<KP, VP, true>(dv, sh, base, seqs, cut, wait_limit, stall);
+  else if (blockIdx.y == 1) walk<VP, KP, true>(dk, sh, base, seqs, cut, wait_limit, stall);
+  else walk<VP, KP, false>(dq, sh, base, seqs, cut, wait_limit, stall);
+}
 
 // ------------------------------------------------------------------------------------------------------------------------------ launch 1: states at the cuts
 // sum over the rows between two cuts of the sequence that reaches over the far one, lambda^{distance to that cut} ks k_j v_j^T: every row's weight is known, so all of
@@ -695,15 +716,16 @@ constexpr int kLtMaxSmem = 232448 - 2048;      // what a block may ask for, less
 static_assert(WalkShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && WalkShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && WalkShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
 static_assert(StateShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && StateShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && StateShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
 
+struct StateArgs { CUtensorMap k, v; LinPass p; };
+struct StateShared { unsigned long long bars[3 * 8 + 2]; uint32_t tmem; int abort; };
 template <int KP, int VP, bool REV>
-__global__ void __launch_bounds__(LT_STATE_THREADS, 1)
-lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ LinPass p, const Ragged seqs, const LinCut cut, uint32_t wait_limit, uint32_t stall) {
+__device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& sh, const uint32_t base, const Ragged& seqs, const LinCut& cut, uint32_t wait_limit, uint32_t stall) {
   using W = StateShape<KP, VP>;
-  extern __shared__ unsigned char smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(8) unsigned long long bars[3 * 8 + 2];
-  __shared__ uint32_t tmem_s;
-  __shared__ int abort_s;
+  const LinPass& p = args.p;
+  const CUtensorMap &tmap_k = args.k, &tmap_v = args.v;
+  unsigned long long* const bars = sh.bars;
+  uint32_t& tmem_s = sh.tmem;
+  int& abort_s = sh.abort;
   volatile int* abort_flag = &abort_s;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   // The launch before may still run.  It (the powers, or a walk of the backward pass before this one) writes no input and reads none of what this one writes (its
@@ -742,7 +764,7 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
       for (; n < chunks; ++n) {
         const int st = n % W::STAGES;
         const uint32_t at = base + st * W::STAGE;
-        if (!lt_wait(empty(st), (n / W::STAGES & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
+        if (!mbar_wait(empty(st), (n / W::STAGES & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
         mbar_expect_tx(full(st), (W::KB + W::VB) * W::BOX + stall);
         load_tile<W::KB, W::BOX>(at, &tmap_k, full(st), head / p.kdiv, r0 + W::ROWS * step(n));
         load_tile<W::VB, W::BOX>(at + W::V, &tmap_v, full(st), head / p.vdiv, r0 + W::ROWS * step(n));
@@ -759,7 +781,7 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
       for (int n = 0; n < chunks; ++n) {
         const int st = n % W::STAGES;
         const uint32_t at = base + st * W::STAGE;
-        if (!lt_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
+        if (!mbar_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
         tc_fence_after();
         issue_state<W::BOX>(tmem, at + W::V, at, at + W::LO, lt_idesc(KP, true, true), (min(W::ROWS, r1 - r0 - W::ROWS * step(n)) + 15) / 16, n > 0);
         umma_commit(empty(st));
@@ -814,6 +836,15 @@ lin_state_tc(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__
   tc_fence_after();
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)KP) : "memory");
 }
+// blockIdx.y: the forward's states, the backward's.
+template <int KP, int VP>
+__global__ void __launch_bounds__(LT_STATE_THREADS, 1)
+lin_state_tc(const __grid_constant__ StateArgs fwd, const __grid_constant__ StateArgs rev, const Ragged seqs, const LinCut cut, uint32_t wait_limit, uint32_t stall) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) StateShared sh;
+  if (blockIdx.y == 0) cut_states<KP, VP, false>(fwd, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
+  else cut_states<KP, VP, true>(rev, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
+}
 
 // ---------------------------------------------------------------------------------------------------------------------------------------- host
 // bf16 [rows, heads, d] with row pitch ld as a 3-D tensor: a box is 64 columns of one head in box_rows rows, zeros beyond the head's width and the last row.
@@ -828,35 +859,58 @@ bool make_tmap_heads(CUtensorMap* map, const void* ptr, int rows, int heads, int
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int KP, int VP, bool REV>
-cudaError_t launch_shape(const LinPass& p, const rom_ragged& seqs, LinCut cut, bool state_only, bool test_stall, cudaStream_t st) {
-  CUtensorMap tq, tk, tv;
-  const int box_rows = state_only ? StateShape<KP, VP>::ROWS : LT_C;
-  if (!make_tmap_heads(&tk, p.k, seqs.rows, p.H / p.kdiv, p.dk, p.ldk, box_rows) || !make_tmap_heads(&tv, p.v, seqs.rows, p.H / p.vdiv, p.dv, p.ldv, box_rows)) return cudaErrorInvalidValue;
-  const uint32_t limit = test_stall ? WAIT_LIMIT_TEST : WAIT_LIMIT, stall = test_stall ? 16 : 0;
-  count_launch();
-  if (state_only) {
-    constexpr int smem = StateShape<KP, VP>::BYTES + 1024;
-    auto kern = lin_state_tc<KP, VP, REV>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    return launch_k(kern, dim3(cut.blocks - 1), LT_STATE_THREADS, smem, st, tk, tv, p, device_view(seqs), cut, limit, stall);
+bool make_walk(WalkArgs& a, const LinPass& p, const rom_ragged& seqs) {
+  a.p = p;
+  return make_tmap_heads(&a.q, p.q, seqs.rows, p.H / p.qdiv, p.dk, p.ldq, LT_C) && make_tmap_heads(&a.k, p.k, seqs.rows, p.H / p.kdiv, p.dk, p.ldk, LT_C) &&
+         make_tmap_heads(&a.v, p.v, seqs.rows, p.H / p.vdiv, p.dv, p.ldv, LT_C);
+}
+template <typename K>
+cudaError_t allow_smem(K kern, int bytes) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); }
+constexpr int more(int a, int b) { return a > b ? a : b; }
+
+template <int KP, int VP>
+cudaError_t launch_states_shape(const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, uint32_t limit, uint32_t stall, cudaStream_t st) {
+  constexpr int smem = StateShape<KP, VP>::BYTES + 1024, rows = StateShape<KP, VP>::ROWS;
+  StateArgs a[2];
+  for (int i = 0; i < n; ++i) {
+    a[i].p = p[i];
+    if (!make_tmap_heads(&a[i].k, p[i].k, seqs.rows, p[i].H / p[i].kdiv, p[i].dk, p[i].ldk, rows) || !make_tmap_heads(&a[i].v, p[i].v, seqs.rows, p[i].H / p[i].vdiv, p[i].dv, p[i].ldv, rows))
+      return cudaErrorInvalidValue;
   }
-  if (!make_tmap_heads(&tq, p.q, seqs.rows, p.H / p.qdiv, p.dk, p.ldq, box_rows)) return cudaErrorInvalidValue;
-  constexpr int smem = WalkShape<KP, VP>::BYTES + 1024;
-  auto kern = lin_walk_tc<KP, VP, REV>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  auto kern = lin_state_tc<KP, VP>;
+  const cudaError_t e = allow_smem(kern, smem);
   if (e != cudaSuccess) return e;
-  return launch_k(kern, dim3(cut.blocks), LT_WALK_THREADS, smem, st, tq, tk, tv, p, device_view(seqs), cut, limit, stall);
+  count_launch();
+  return launch_k(kern, dim3(cut.blocks - 1, n), LT_STATE_THREADS, smem, st, a[0], a[n - 1], device_view(seqs), cut, limit, stall);
+}
+template <int KP, int VP>
+cudaError_t launch_walks_shape(const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, uint32_t limit, uint32_t stall, cudaStream_t st) {
+  WalkArgs a[3];
+  for (int i = 0; i < n; ++i)
+    if (!make_walk(a[i], p[i], seqs)) return cudaErrorInvalidValue;
+  count_launch();
+  if (n == 1) {
+    constexpr int smem = WalkShape<KP, VP>::BYTES + 1024;
+    auto kern = lin_walk_tc<KP, VP>;
+    const cudaError_t e = allow_smem(kern, smem);
+    return e != cudaSuccess ? e : launch_k(kern, dim3(cut.blocks), LT_WALK_THREADS, smem, st, a[0], device_view(seqs), cut, limit, stall);
+  }
+  constexpr int smem = more(WalkShape<KP, VP>::BYTES, WalkShape<VP, KP>::BYTES) + 1024;
+  auto kern = lin_walk3_tc<KP, VP>;
+  const cudaError_t e = allow_smem(kern, smem);
+  return e != cudaSuccess ? e : launch_k(kern, dim3(cut.blocks, 3), LT_WALK_THREADS, smem, st, a[0], a[1], a[2], device_view(seqs), cut, limit, stall);
 }
 
 }  // namespace
 
-cudaError_t launch_lin_tc(const LinPass& p, const rom_ragged& seqs, LinCut cut, bool state_only, bool test_stall, cudaStream_t st) {
-  const bool k = p.dk > 64, v = p.dv > 64;
-  if (p.reverse)
-    return (k ? (v ? launch_shape<128, 128, true> : launch_shape<128, 64, true>) : (v ? launch_shape<64, 128, true> : launch_shape<64, 64, true>))(p, seqs, cut, state_only, test_stall, st);
-  return (k ? (v ? launch_shape<128, 128, false> : launch_shape<128, 64, false>) : (v ? launch_shape<64, 128, false> : launch_shape<64, 64, false>))(p, seqs, cut, state_only, test_stall, st);
+// By the model's d_k and d_v.
+cudaError_t launch_lin_states_tc(const LinPass* p, int n, int dk, int dv, const rom_ragged& seqs, const LinCut& cut, bool test_stall, cudaStream_t st) {
+  const uint32_t limit = test_stall ? WAIT_LIMIT_TEST : WAIT_LIMIT, stall = test_stall ? 16 : 0;
+  return (dk > 64 ? (dv > 64 ? launch_states_shape<128, 128> : launch_states_shape<128, 64>) : (dv > 64 ? launch_states_shape<64, 128> : launch_states_shape<64, 64>))(p, n, seqs, cut, limit, stall, st);
+}
+cudaError_t launch_lin_walks_tc(const LinPass* p, int n, int dk, int dv, const rom_ragged& seqs, const LinCut& cut, bool test_stall, cudaStream_t st) {
+  const uint32_t limit = test_stall ? WAIT_LIMIT_TEST : WAIT_LIMIT, stall = test_stall ? 16 : 0;
+  return (dk > 64 ? (dv > 64 ? launch_walks_shape<128, 128> : launch_walks_shape<128, 64>) : (dv > 64 ? launch_walks_shape<64, 128> : launch_walks_shape<64, 64>))(p, n, seqs, cut, limit, stall, st);
 }
 
 }  // namespace rom

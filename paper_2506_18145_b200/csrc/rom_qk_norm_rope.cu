@@ -100,11 +100,6 @@ __device__ __forceinline__ void load_weights(const float* w, const QkLane& at, f
     wb[e] = w ? make_float2(__ldg(w + at.ob + 2 * e), __ldg(w + at.ob + 2 * e + 1)) : both(1.0f);
   }
 }
-__device__ __forceinline__ void clear(float2 (&v)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = both(0.0f);
-}
-
 // What the lane multiplies a run's places with: y = x f + other g, other being the pair's second member, in the other run or (INTER: interleaved) beside it.  Where nothing is
 // turned g is 0.
 struct Factors { float2 fa[4], ga[4], fb[4], gb[4]; };

@@ -339,3 +339,61 @@ def test_stalled_call_is_reported(H, G, dk, dv, lens):
         pr.cfg = good
         again = pr.run()
         assert same_bits(ref[0], again[0]) and same_bits(ref[1], again[1]) and rb.rom_get_status(pr.ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_empty_sequences_alone(dtype):
+    """No rows at all: a resumed sequence keeps its state, another leaves zeros; backwards the gradient passes through."""
+    pr = Problem([0, 0, 0], 2, 1, 64, 64, dtype, seed=3, resume=[1, 0, 1], tail=4, backward=True)
+    o, s = pr.run()
+    dq, dk, dv, ds = pr.run_backward()
+    for i in range(3):
+        slot = int(pr.p.slots[i])
+        assert same_bits(s[slot], pr.s_in[slot]) if pr.p.resumes(i) else (s[slot] == 0).all()
+        assert same_bits(ds[slot], pr.ds_out[slot]) if pr.p.resumes(i) else (ds[slot] == 0).all()
+    for x in (o, dq, dk, dv):
+        assert (x == -7).all()
+    seqs = rb.make_ragged(0, pr.p.n_slots, torch.zeros(4, dtype=torch.int32, device="cuda"), *pr.p.dev[1:])
+    none, out = pr.q[:0], torch.full_like(pr.s_in, -7.0)
+    rb.rom_linattn_ragged(pr.cfg, seqs, none, none, pr.v[:0], pr.g, pr.s_in, out, pr.do[:0], pr.ws)
+    assert same_bits(out, s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 300])
+def test_many_short_sequences(n, dtype):
+    """Runs of many sequences: one, two and a few rows each, empty ones between, some longer; of more than 256 rows a sequence none."""
+    g = torch.Generator().manual_seed(n)
+    lens = [int(x) for x in torch.randint(0, 4, (n,), generator=g)]
+    lens[n // 3], lens[n // 2] = 200, 131
+    pr = Problem(lens, 3, 1, 72, 40, dtype, seed=n, backward=True)
+    check_forward(pr, *pr.run())
+    check_backward(pr, *pr.run_backward())
+    pool = pr.s_in.clone()
+    o, s = pr.run()
+    o2, _ = pr.run(s_in=pool, s_out=pool)
+    assert same_bits(o, o2) and all(same_bits(s[int(k)], pool[int(k)]) for k in pr.p.slots)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,lens", [(160, [300]), (150, [64, 900]), (40, [1000, 3, 2000]), (17, [4000])], ids=str)
+def test_head_counts_beside_the_blocks(H, lens, dtype):
+    """Whole heads on more blocks than the GPU holds, and runs that begin in one head and end in the next."""
+    pr = Problem(lens, H, H, 16, 16, dtype, seed=H, rates=[0.3 * 0.97 ** h for h in range(H)], backward=True)
+    check_forward(pr, *pr.run())
+    check_backward(pr, *pr.run_backward())
+
+
+def test_offsets_that_are_out_of_order_stay_in_bounds():
+    """What they yield is unspecified; rows of the buffers and slots behind the named ones are not touched, and nothing faults."""
+    H, d, rows = 2, 64, 700
+    cfg = rb.make_linattn_config(H, H, d, d, "bf16")
+    q, k, v = (torch.randn((rows, H * d), device="cuda").bfloat16() for _ in range(3))
+    g, pool = torch.full((H,), -0.01, device="cuda"), torch.zeros((4, H, d, d), device="cuda")
+    guarded = torch.full((rows + 64, H * d), -7.0, dtype=torch.bfloat16, device="cuda")
+    for start in ([0, 600, 200, 5000], [-40, 300, 300, 650], [699, 0, 10, 20]):
+        seqs = rb.make_ragged(rows, 3, torch.tensor(start, dtype=torch.int32, device="cuda"), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"))
+        ws = torch.zeros(rb.linattn_ragged_workspace_size(cfg, 3, rows), dtype=torch.uint8, device="cuda")
+        rb.rom_linattn_ragged(cfg, seqs, q, k, v, g, pool, pool, guarded[:rows], ws)
+        torch.cuda.synchronize()
+        assert (guarded[rows:] == -7).all() and (pool[3] == 0).all() and rb.rom_get_status(ws) == 0
