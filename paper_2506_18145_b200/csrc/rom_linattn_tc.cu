@@ -5,11 +5,13 @@
 //   S^T <- lambda^len S^T + V^T K~,  K~_j = ks lambda^{len-1-j} k_j      [dv x dk]     A = V^T, B = K~ (both MN-major)
 // (backwards: rows run the other way, j >= i, the exponents are counted from the chunk's other end.)
 //
-// Roundings: P and the S that a chunk meets are bf16 (half a step each, of separate parts of the sum); K~ is hi + lo, two bf16 numbers, in two matrix products, since
-// the state is an fp32 result that many chunks add up in.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
+// Roundings: P and the S that a chunk meets are bf16 (half a step each, of separate parts of the sum); K~ is the
+// sum of three bf16 numbers, in three matrix products: all 24 bits of the fp32 product, since the state is an fp32 result that many chunks add up in (two, rounded, left 2.5e-6
+// of its norm where fp32 sums leave 2e-7; the third costs 10 % of a walk: 16384 rows of 32 heads of 128 x 128 in 147 instead of 133 us).  Two where the state is no result but only
+// read as bf16 by dq or dk.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
 //
 // One CTA per SM walks one run of chunks.  640 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
-// width), warp 1 the matrix products, warps 4..11 turn scores into P and O1, O2 into output rows, warps 12..19 scale K in place (K~ hi; lo beside it), and keep S; two
+// width), warp 1 the matrix products, warps 4..11 turn scores into P and O1, O2 into output rows, warps 12..19 scale K in place (K~'s first part; the others beside it), and keep S; two
 // warps share each 32-lane quarter of tensor memory and take half of the columns each.  The scores' tensor memory is reused for P.
 //
 // Values that are not finite: a masked P is 0 by selection, but 0 * V is not 0 for a V of a later row that is not finite.  Rows whose O2 is not finite are summed
@@ -27,7 +29,7 @@ namespace {
 using bf16 = __nv_bfloat16;
 constexpr int LT_C = 128;                     // rows of a chunk
 constexpr int LT_BOX = 64 * LT_C * 2;         // bytes of one TMA box
-constexpr int LT_WALK_THREADS = 640, LT_STATE_THREADS = 320;
+constexpr int LT_WALK_THREADS = 640, LT_SCALERS = 16, LT_STATE_THREADS = 64 + 32 * LT_SCALERS;
 // Registers of the walk's threads: 640 x 96 at launch; the copies' and products' warps give theirs to those that make P and keep S: 128 x 48 + 256 x 104 + 256 x 112 =
 // 640 x 96.
 constexpr int LT_FEW = 48, LT_P = 104, LT_MANY = 112;
@@ -106,10 +108,15 @@ __device__ __forceinline__ float4 ld_state4(const float* p) {
   asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
   return v;
 }
-// Part of one row of K (16-byte pieces of a 128-byte row of one box, swizzled by the row) times w: hi in place, lo beside it; zeros where the row is not part of the
-// sum.  Some pieces at a time: one after the other, a piece's load, conversions and stores took 230 cycles.
-template <int AT_ONCE>
-__device__ __forceinline__ void scale_row(uint32_t khi, uint32_t klo, int row, float w, bool live, int piece0, int pieces) {
+// The upper halves of two fp32 numbers: bf16 numbers cut off, so that what is left of a number is exact, and 24 bits are three of them.
+__device__ __forceinline__ uint32_t uppers(float2 x) { return __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632); }
+__device__ __forceinline__ float2 less_upper(float2 x) {
+  return __ffma2_rn(make_float2(hi_of(__float_as_uint(x.x)), hi_of(__float_as_uint(x.y))), make_float2(-1.0f, -1.0f), x);      // (of an infinite number NaN: not finite either way)
+}
+// Part of one row of K (16-byte pieces of a 128-byte row of one box, swizzled by the row) times w: the first bf16 part in place, the second beside it, and the third where all of
+// the product's bits are asked for; zeros where the row is not part of the sum.  Some pieces at a time: one after the other, a piece's load, conversions and stores took 230 cycles.
+template <int AT_ONCE, bool THIRD>
+__device__ __forceinline__ void scale_row(uint32_t khi, uint32_t klo, uint32_t kll, int row, float w, bool live, int piece0, int pieces) {
   const float2 ww = make_float2(w, w);
 #pragma unroll 1
   for (int i = 0; i < pieces; i += AT_ONCE) {
@@ -122,16 +129,17 @@ __device__ __forceinline__ void scale_row(uint32_t khi, uint32_t klo, int row, f
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
       const uint32_t off = row * 128 + (((piece0 + i + u) ^ (row & 7)) << 4), in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-      uint32_t h[4], l[4];
+      uint32_t h[4], l[4], ll[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 a = make_float2(lo_of(in[e]), hi_of(in[e])), y = __fmul2_rn(a, ww);
-        h[e] = pack2(y.x, y.y);
-        const float2 rest = __ffma2_rn(a, ww, make_float2(-lo_of(h[e]), -hi_of(h[e])));      // (of an infinite product NaN: not finite either way)
-        l[e] = pack2(rest.x, rest.y);
+        const float2 y = __fmul2_rn(make_float2(lo_of(in[e]), hi_of(in[e])), ww), rest = less_upper(y);
+        h[e] = uppers(y);
+        if (THIRD) { l[e] = uppers(rest); ll[e] = uppers(less_upper(rest)); }
+        else l[e] = pack2(rest.x, rest.y);
       }
       sts128(khi + off, make_uint4(h[0], h[1], h[2], h[3]));
       sts128(klo + off, make_uint4(l[0], l[1], l[2], l[3]));
+      if (THIRD) sts128(kll + off, make_uint4(ll[0], ll[1], ll[2], ll[3]));
     }
   }
 }
@@ -162,12 +170,14 @@ __device__ __forceinline__ void store_rows(char* row_at, int64_t pitch, int rows
   for (int t = 0; t < N; ++t)
     if (piece_ok && t < rows) *reinterpret_cast<uint4*>(row_at + t * pitch) = make_uint4(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
 }
-// V^T K~: hi and lo, the first ks steps of 16 rows.
-template <int BOX>
-__device__ __forceinline__ void issue_state(uint32_t tmem_d, uint32_t v, uint32_t khi, uint32_t klo, uint32_t idesc, int ks, bool accumulate) {
-  const uint64_t a = desc_mn<BOX>(v), h = desc_mn<BOX>(khi), l = desc_mn<BOX>(klo);
-  for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), h + (uint64_t)(MN_KSTEP * k), idesc, accumulate || k > 0 ? 1u : 0u);
-  for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), l + (uint64_t)(MN_KSTEP * k), idesc, 1u);
+// V^T K~ of a chunk: the first ks steps of 16 rows, the smallest parts first (the accumulator drops what is below its last bit at every step).
+template <int BOX, bool THIRD>
+__device__ __forceinline__ void issue_state(uint32_t tmem_d, uint32_t v, uint32_t khi, uint32_t klo, uint32_t kll, uint32_t idesc, int ks) {
+  const uint64_t a = desc_mn<BOX>(v), h = desc_mn<BOX>(khi), l = desc_mn<BOX>(klo), ll = desc_mn<BOX>(kll);
+  if (THIRD)
+    for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), ll + (uint64_t)(MN_KSTEP * k), idesc, k > 0 ? 1u : 0u);
+  for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), l + (uint64_t)(MN_KSTEP * k), idesc, THIRD || k > 0 ? 1u : 0u);
+  for (int k = 0; k < ks; ++k) umma_bf16(tmem_d, a + (uint64_t)(MN_KSTEP * k), h + (uint64_t)(MN_KSTEP * k), idesc, 1u);
 }
 template <int BOXES>
 __device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int head, int row) {
@@ -222,12 +232,15 @@ __device__ __forceinline__ bool get_piece(const LinItem& it, const Ragged& q, bo
 // ------------------------------------------------------------------------------------------------------------------------------ the walk
 // A wait that gives up ends the waits of its warp, not its loop: the warps that meet at named barriers (a quarter's two, each role's eight) all come to every one of
 // them, and only the results are left out.
+__host__ __device__ constexpr int more(int a, int b) { return a > b ? a : b; }
 template <int KP, int VP>
 struct WalkShape {
   static constexpr int KB = KP / 64, VB = VP / 64;
   // stages, as many as 227 KB hold: a copy takes up to 2 us when memory is busy, a chunk of two heads' widths of 64 half of that
-  static constexpr int KVST = KP == 128 ? 2 : VP == 128 ? 3 : 4, QST = KP == 128 ? (VP == 128 ? 1 : 2) : KVST;
-  static constexpr int Q = 0, K = Q + QST * KB * LT_BOX, V = K + KVST * KB * LT_BOX, LO = V + KVST * VB * LT_BOX, S = LO + KB * LT_BOX, BYTES = S + KB * VP * 128;
+  // (Q, and at 128 x 128 V, with one stage: Q S and V^T K~ end well before their next operands are used, and these come from L2: no slower than two of V)
+  static constexpr int KST = KP == 128 ? 2 : VP == 128 ? 3 : 4, QST = KP == 128 ? 1 : VP == 128 ? 2 : 3, VST = KP == 128 && VP == 128 ? 1 : KST;
+  static constexpr int Q = 0, K = Q + QST * KB * LT_BOX, V = K + KST * KB * LT_BOX, LO = V + VST * VB * LT_BOX, LL = LO + KB * LT_BOX, S = LL + KB * LT_BOX, BYTES = S + KB * VP * 128;
+  static constexpr int BARS = 2 * (QST + KST + VST) + 8;
   static constexpr int SC = 0, O1 = 128, KV = O1 + VP, O2 = KV + KP;      // tensor-memory columns (P over the scores' first 64)
 };
 
@@ -275,15 +288,16 @@ __device__ __noinline__ void slow_rows(const LinPass& p, int head, uint32_t tadd
 }
 
 struct WalkArgs { CUtensorMap q, k, v; LinPass p; };
+template <int BARS>
 struct WalkShared {
   // powers of lambda: of the warps that make P (on the diagonal times p, behind 32 zeros), of those that keep S, with what each lost to fp32
   float p_lam[kLinPowers], p_diag[64], s_lam[kLinPowers], s_lo[kLinPowers];
-  unsigned long long bars[24];
+  unsigned long long bars[BARS];
   uint32_t tmem;
   int abort;
 };
-template <int KP, int VP, bool REV>
-__device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const uint32_t base, const Ragged& seqs, const LinCut& cut, uint32_t wait_limit, uint32_t stall) {
+template <int KP, int VP, bool REV, bool THIRD, int BARS>
+__device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh, const uint32_t base, const Ragged& seqs, const LinCut& cut, uint32_t wait_limit, uint32_t stall) {
   using W = WalkShape<KP, VP>;
   const LinPass& p = args.p;
   const CUtensorMap &tmap_q = args.q, &tmap_k = args.k, &tmap_v = args.v;
@@ -295,13 +309,17 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), run = blockIdx.x;
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
   // full: copies have landed; empty: the matrix products that read them are done; the others by name
+  constexpr int BK = 2 * W::QST, BV = BK + 2 * W::KST, B1 = BV + 2 * W::VST;
+  static_assert(W::BARS <= BARS, "barriers");
   auto q_full = [&](int s) { return bar(s); };
-  auto q_empty = [&](int s) { return bar(4 + s); };
-  auto kv_full = [&](int s) { return bar(8 + s); };
-  auto kv_empty = [&](int s) { return bar(12 + s); };
-  const uint32_t sc_full = bar(16), pv_full = bar(17), state_full = bar(18), drain = bar(19), p_ready = bar(20), k_ready = bar(21), s_ready = bar(22), o_free = bar(23);
+  auto q_empty = [&](int s) { return bar(W::QST + s); };
+  auto k_full = [&](int s) { return bar(BK + s); };
+  auto k_empty = [&](int s) { return bar(BK + W::KST + s); };
+  auto v_full = [&](int s) { return bar(BV + s); };
+  auto v_empty = [&](int s) { return bar(BV + W::VST + s); };
+  const uint32_t sc_full = bar(B1), pv_full = bar(B1 + 1), state_full = bar(B1 + 2), drain = bar(B1 + 3), p_ready = bar(B1 + 4), k_ready = bar(B1 + 5), s_ready = bar(B1 + 6), o_free = bar(B1 + 7);
   if (tid == 0) {
-    for (int i = 0; i < 24; ++i) mbar_init(bar(i), i >= 20 ? 8 : 1);
+    for (int i = 0; i < W::BARS; ++i) mbar_init(bar(i), i >= B1 + 4 ? 8 : 1);
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -334,24 +352,27 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
       const int head = it.head, s_first = first_piece(it, seqs);
       if (leader)
       for (int s = s_first; ok && get_piece<REV>(it, seqs, p.skip_single, s, x); ++s) {
-        if (!x.over) {                 // the state that the piece starts from, into L2 while the pieces before are walked
+        if (!x.over && x.r1 > x.r0) {  // the state that the piece starts from, into L2 while the pieces before are walked
           const float* from = lin_init_of(p, seqs, s, head);
           if (from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(p.dk * p.dv * sizeof(float))) : "memory");
         }
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
-          const int st = n % W::KVST, qs = n % W::QST;
+          const int ks = n % W::KST, qs = n % W::QST, vs = n % W::VST;
           if (n == 1) pdl_wait();      // (the first chunk's copies need not wait for the launch before, but no bounded wait may count its time)
-          if (!mbar_wait(kv_empty(st), (n / W::KVST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
-          mbar_expect_tx(kv_full(st), (W::KB + W::VB) * LT_BOX + stall);
-          load_tile<W::KB>(base + W::K + st * W::KB * LT_BOX, &tmap_k, kv_full(st), head / p.kdiv, row0);
-          load_tile<W::VB>(base + W::V + st * W::VB * LT_BOX, &tmap_v, kv_full(st), head / p.vdiv, row0);
+          if (!mbar_wait(k_empty(ks), (n / W::KST & 1) ^ 1, abort_flag, wait_limit)) { ok = false; break; }
+          mbar_expect_tx(k_full(ks), W::KB * LT_BOX + stall);
+          load_tile<W::KB>(base + W::K + ks * W::KB * LT_BOX, &tmap_k, k_full(ks), head / p.kdiv, row0);
           // one stage of Q: it is asked for when Q S of the chunk before is done, 4000 cycles from memory where the chunk has 2500 left; from L2 1500
           if (W::QST == 1) prefetch_tile<W::KB>(&tmap_q, head / p.qdiv, row0);
+          if (W::VST == 1) prefetch_tile<W::VB>(&tmap_v, head / p.vdiv, row0);
           if (!mbar_wait(q_empty(qs), (n / W::QST & 1) ^ 1, abort_flag, wait_limit)) { ++n; ok = false; break; }
           mbar_expect_tx(q_full(qs), W::KB * LT_BOX);
           load_tile<W::KB>(base + W::Q + qs * W::KB * LT_BOX, &tmap_q, q_full(qs), head / p.qdiv, row0);
+          if (!mbar_wait(v_empty(vs), (n / W::VST & 1) ^ 1, abort_flag, wait_limit)) { ++n; ok = false; break; }
+          mbar_expect_tx(v_full(vs), W::VB * LT_BOX);
+          load_tile<W::VB>(base + W::V + vs * W::VB * LT_BOX, &tmap_v, v_full(vs), head / p.vdiv, row0);
         }
       }
       __syncwarp();
@@ -359,10 +380,11 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
     if (leader) {
       if (!ok) latch(p, abort_flag, 51);
       if (*abort_flag)                 // the copies still in flight land (bounded) before the block ends
-        for (int i = 1; i <= W::KVST && i <= n; ++i) {
+        for (int i = 1; i <= W::KST && i <= n; ++i) {
           const int c = n - i;
-          for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(kv_full(c % W::KVST), c / W::KVST & 1); ++it) {}
+          for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(k_full(c % W::KST), c / W::KST & 1); ++it) {}
           for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(q_full(c % W::QST), c / W::QST & 1); ++it) {}
+          for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(v_full(c % W::VST), c / W::VST & 1); ++it) {}
         }
     }
     __syncwarp();
@@ -381,10 +403,10 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
         for (int m = 0, mm = x.chunks(); m < mm; ++m, ++n) {
           int row0, len;
           x.chunk<REV>(m, row0, len);
-          const int st = n % W::KVST, qs = n % W::QST, ks = (len + 15) / 16;
-          const uint32_t ph = n & 1, q = base + W::Q + qs * W::KB * LT_BOX, k = base + W::K + st * W::KB * LT_BOX, v = base + W::V + st * W::VB * LT_BOX;
+          const int st = n % W::KST, qs = n % W::QST, vs = n % W::VST, ks = (len + 15) / 16;
+          const uint32_t ph = n & 1, q = base + W::Q + qs * W::KB * LT_BOX, k = base + W::K + st * W::KB * LT_BOX, v = base + W::V + vs * W::VB * LT_BOX;
           // scores, once the P that lies over them has been used
-          if (!wait(kv_full(st), n / W::KVST & 1) || !wait(q_full(qs), n / W::QST & 1) || (n > 0 && !wait(pv_full, ph ^ 1))) break;
+          if (!wait(k_full(st), n / W::KST & 1) || !wait(q_full(qs), n / W::QST & 1) || (n > 0 && !wait(pv_full, ph ^ 1))) break;
           tc_fence_after();
 #pragma unroll
           for (int b = 0; b < W::KB; ++b)
@@ -402,13 +424,14 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
             for (int e = 0; e < 4; ++e)
               umma_bf16(tmem + W::O1, make_smem_desc(q + b * LT_BOX) + 2 * e, make_smem_desc(base + W::S + b * VP * 128) + 2 * e, d_o1, b + e > 0 ? 1u : 0u);
           umma_commit(q_empty(qs));
-          if (!wait(p_ready, ph) || !wait(k_ready, ph)) break;
+          if (!wait(v_full(vs), n / W::VST & 1) || !wait(p_ready, ph) || !wait(k_ready, ph)) break;
           tc_fence_after();
           for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 8 * e, desc_mn<LT_BOX>(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
           umma_commit(pv_full);
-          issue_state<LT_BOX>(tmem + W::KV, v, k, base + W::LO, d_kv, ks, false);
+          issue_state<LT_BOX, THIRD>(tmem + W::KV, v, k, base + W::LO, base + W::LL, d_kv, ks);
           umma_commit(state_full);
-          umma_commit(kv_empty(st));
+          umma_commit(k_empty(st));
+          umma_commit(v_empty(vs));
         }
       __syncwarp();
     }
@@ -590,7 +613,7 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
       if (from) {
         const int col = min(c, p.dv - 1);
         if (p.transposed) {
-          // rows of the memory are columns of S^T's rows: 32 rows x 16 columns at a time are read whole and change lanes through the (idle) space of K~'s low halves
+          // rows of the memory are columns of S^T's rows: 32 rows x 16 columns at a time are read whole and change lanes through the (idle) space of K~'s second part
           float4 v[KH / 4];
 #pragma unroll
           for (int g = 0; g < KH / 16; ++g)
@@ -628,15 +651,16 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared& sh, const
       for (int m = 0; m < mm; ++m, ++n) {
         int row0, len;
         x.chunk<REV>(m, row0, len);
-        const int st = n % W::KVST, early = m == 0 && !x.over && p.early ? 1 : 0, rows16 = (len + 15) / 16 * 16;
+        const int st = n % W::KST, vs = n % W::VST, early = m == 0 && !x.over && p.early ? 1 : 0, rows16 = (len + 15) / 16 * 16;
         const uint32_t ph = n & 1, k = base + W::K + st * W::KB * LT_BOX, box = KP == 128 ? half * LT_BOX : 0;
         // (the scores are made of this K: sc_full says that it has landed, but the copies' own barrier makes them visible)
-        ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit) && warp_wait(kv_full(st), n / W::KVST & 1, abort_flag, wait_limit);
+        ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit) && warp_wait(k_full(st), n / W::KST & 1, abort_flag, wait_limit);
+        if (rows16 > len) ok = ok && warp_wait(v_full(vs), n / W::VST & 1, abort_flag, wait_limit);
         if (c < rows16) {
           const bool live = c < len;
           const float w = live ? p.k_scale * lam[REV ? c : len - 1 - c] : 0.0f;
-          scale_row<KP == 128 ? 2 : 4>(k + box, base + W::LO + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
-          if (!live && half < W::VB) clear_row(base + W::V + (st * W::VB + half) * LT_BOX, c);
+          scale_row<KP == 128 ? 2 : 4, THIRD>(k + box, base + W::LO + box, base + W::LL + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
+          if (!live && half < W::VB) clear_row(base + W::V + (vs * W::VB + half) * LT_BOX, c);
         }
         fence_async();
         warp_arrive(k_ready);
@@ -686,8 +710,8 @@ template <int KP, int VP>
 __global__ void __launch_bounds__(LT_WALK_THREADS, 1)
 lin_walk_tc(const __grid_constant__ WalkArgs args, const Ragged seqs, const LinCut cut, uint32_t wait_limit, uint32_t stall) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(16) WalkShared sh;
-  walk<KP, VP, false>(args, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
+  __shared__ __align__(16) WalkShared<WalkShape<KP, VP>::BARS> sh;
+  walk<KP, VP, false, true>(args, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
 }
 // The backward's three: they read the same inputs and states and write different outputs, and a launch each would leave most SMs idle where sequences are few or short (two
 // sequences of one row, 8 heads: 37 us in three launches, most of it their latency).
@@ -696,29 +720,34 @@ __global__ void __launch_bounds__(LT_WALK_THREADS, 1)
 lin_walk3_tc(const __grid_constant__ WalkArgs dq, const __grid_constant__ WalkArgs dv, const __grid_constant__ WalkArgs dk, const Ragged seqs, const LinCut cut, uint32_t wait_limit,
              uint32_t stall) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(16) WalkShared sh;
+  __shared__ __align__(16) WalkShared<more(WalkShape<KP, VP>::BARS, WalkShape<VP, KP>::BARS)> sh;
   const uint32_t base = aligned_base(smem_raw);
-  if (blockIdx.y == 0) walk<KP, VP, true>(dv, sh, base, seqs, cut, wait_limit, stall);
-  else if (blockIdx.y == 1) walk<VP, KP, true>(dk, sh, base, seqs, cut, wait_limit, stall);
-  else walk<VP, KP, false>(dq, sh, base, seqs, cut, wait_limit, stall);
+  if (blockIdx.y == 0) walk<KP, VP, true, true>(dv, sh, base, seqs, cut, wait_limit, stall);
+  else if (blockIdx.y == 1) walk<VP, KP, true, false>(dk, sh, base, seqs, cut, wait_limit, stall);
+  else walk<VP, KP, false, false>(dq, sh, base, seqs, cut, wait_limit, stall);
 }
 
 // ------------------------------------------------------------------------------------------------------------------------------ launch 1: states at the cuts
 // sum over the rows between two cuts of the sequence that reaches over the far one, lambda^{distance to that cut} ks k_j v_j^T: every row's weight is known, so all of
-// them add up in tensor memory, in steps of 64 rows.  Warps 2..9 scale K, four threads to a row.
+// them add up in tensor memory, in steps of 64 rows: the first parts of K~ in one accumulator, the small ones in another, which the two products of V with K~'s first and second part
+// fill as one of twice the width (every step drops what is below the accumulator's last bit: in one accumulator for all of them the state was off by 1.2e-6, in two by 4e-7).  Sixteen
+// warps scale K, eight threads to a row (eight warps: 209.6 us for the whole call at 16384 rows of 32 heads of 128 x 128, sixteen: 207).  What bounds it: shared memory, 176 KB of
+// copies, operands and K~ a step of 128 x 128, 1400 cycles of the 2100 that a step takes; from DRAM it asks for 4 TB/s.
 template <int KP, int VP>
 struct StateShape {
   static constexpr int KB = KP / 64, VB = VP / 64, ROWS = 64, BOX = 64 * ROWS * 2;
-  static constexpr int STAGE = (2 * KB + VB) * BOX, LO = KB * BOX, V = 2 * KB * BOX;      // K (hi) | lo | V
+  static constexpr int STAGE = (3 * KB + VB) * BOX, LO = KB * BOX, LL = 2 * KB * BOX, V = 3 * KB * BOX;      // K (hi) | lo | the third part | V
   static constexpr int STAGES = 196608 / STAGE, BYTES = STAGES * STAGE + (VB == 1 ? BOX : 0);      // (see desc_mn: one box behind the last V)
 };
 constexpr int kLtMaxSmem = 232448 - 2048;      // what a block may ask for, less its static variables
+static_assert(sizeof(WalkShared<WalkShape<64, 128>::BARS>) <= 2048, "shared memory");
 static_assert(WalkShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && WalkShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && WalkShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
+static_assert(WalkShape<64, 64>::BYTES + (int)sizeof(WalkShared<WalkShape<64, 64>::BARS>) + 1024 <= 232448, "shared memory");
 static_assert(StateShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && StateShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && StateShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
 
 struct StateArgs { CUtensorMap k, v; LinPass p; };
 struct StateShared { unsigned long long bars[3 * 8 + 2]; uint32_t tmem; int abort; };
-template <int KP, int VP, bool REV>
+template <int KP, int VP, bool REV, bool THIRD>
 __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& sh, const uint32_t base, const Ragged& seqs, const LinCut& cut, uint32_t wait_limit, uint32_t stall) {
   using W = StateShape<KP, VP>;
   const LinPass& p = args.p;
@@ -741,7 +770,7 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
   auto scaled = [&](int i) { return smem_u32(&bars[16 + i]); };
   const uint32_t done = smem_u32(&bars[24]), drain = smem_u32(&bars[25]);
   if (tid == 0) {
-    for (int i = 0; i < 8; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); mbar_init(scaled(i), 8); }
+    for (int i = 0; i < 8; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); mbar_init(scaled(i), LT_SCALERS); }
     mbar_init(done, 1);
     mbar_init(drain, 1);
     abort_s = 0;
@@ -749,7 +778,7 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
     fence_async();
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)KP) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)(2 * KP)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -783,7 +812,11 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
         const uint32_t at = base + st * W::STAGE;
         if (!mbar_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
         tc_fence_after();
-        issue_state<W::BOX>(tmem, at + W::V, at, at + W::LO, lt_idesc(KP, true, true), (min(W::ROWS, r1 - r0 - W::ROWS * step(n)) + 15) / 16, n > 0);
+        const uint64_t a = desc_mn<W::BOX>(at + W::V), hl = desc_mn<W::BOX>(at), ll = desc_mn<W::BOX>(at + W::LL);
+        for (int k = 0, ks = (min(W::ROWS, r1 - r0 - W::ROWS * step(n)) + 15) / 16; k < ks; ++k) {
+          umma_bf16(tmem, a + (uint64_t)(MN_KSTEP * k), hl + (uint64_t)(MN_KSTEP * k), lt_idesc(2 * KP, true, true), n + k > 0 ? 1u : 0u);
+          if (THIRD) umma_bf16(tmem + KP, a + (uint64_t)(MN_KSTEP * k), ll + (uint64_t)(MN_KSTEP * k), lt_idesc(KP, true, true), 1u);
+        }
         umma_commit(empty(st));
         issued = true;
       }
@@ -796,7 +829,8 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
     }
     __syncwarp();
   } else {
-    const int half = (warp - 2) >> 2, quarter = warp & 3, j = quarter * 32 + lane, row = (tid - 64) & 63, part = (tid - 64) >> 6;
+    constexpr int PARTS = LT_SCALERS / 2, COLS = KP * 4 / LT_SCALERS;      // threads to a row of K; columns of a warp at the end
+    const int group = (warp - 2) >> 2, quarter = warp & 3, j = quarter * 32 + lane, row = (tid - 64) & 63, part = (tid - 64) >> 6;
     const double g2 = (double)__ldg(p.log_decay + head) * 1.4426950408889634;
     bool ok = true;
     for (int n = 0; n < chunks; ++n) {
@@ -808,8 +842,9 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
       if (!(ok = warp_wait(full(st), n / W::STAGES & 1, abort_flag, wait_limit))) break;
       if (row < rows16) {
         const bool live = row < len;
-        if (KP == 128) scale_row<4>(at + (part >> 1) * W::BOX, at + W::LO + (part >> 1) * W::BOX, row, w, live, 4 * (part & 1), 4);
-        else scale_row<2>(at, at + W::LO, row, w, live, 2 * part, 2);
+        constexpr int PIECES = KP / 8 / PARTS;
+        const uint32_t box = PIECES * part / 8 * W::BOX;
+        scale_row<PIECES, THIRD>(at + box, at + W::LO + box, at + W::LL + box, row, w, live, PIECES * part & 7, PIECES);
         if (!live && part < W::VB) clear_row(at + W::V + part * W::BOX, row);
       }
       fence_async();
@@ -819,14 +854,16 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
     if (ok && (ok = warp_wait(done, 0, abort_flag, wait_limit))) {
       tc_fence_after();
       float* to = p.cut_state + (size_t)blockIdx.x * ((size_t)p.dk * p.dv) + j;
-      for (int c = half * (KP / 2); c < (half + 1) * (KP / 2); c += 32) {
-        uint32_t r[32];
+      for (int c = group * COLS; c < (group + 1) * COLS; c += 16) {
+        uint32_t hi[16], lo[16];
         __syncwarp();
-        tmem_ld32_issue(tmem + ((uint32_t)(quarter * 32) << 16) + c, r);
-        tmem_ld_wait(r);
+        tmem_ld16_issue(tmem + ((uint32_t)(quarter * 32) << 16) + c, hi);
+        tmem_ld16_issue(tmem + ((uint32_t)(quarter * 32) << 16) + KP + c, lo);
+        tmem_ld16_wait(hi);
+        tmem_ld16_wait(lo);
 #pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (j < p.dv && c + e < p.dk) to[(size_t)(c + e) * p.dv] = __uint_as_float(r[e]);
+        for (int e = 0; e < 16; ++e)
+          if (j < p.dv && c + e < p.dk) to[(size_t)(c + e) * p.dv] = __uint_as_float(hi[e]) + __uint_as_float(lo[e]);
       }
     }
     if (!ok) latch(p, abort_flag, 57);
@@ -834,16 +871,16 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)KP) : "memory");
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * KP)) : "memory");
 }
-// blockIdx.y: the forward's states, the backward's.
-template <int KP, int VP>
+// blockIdx.y: the forward's states, the backward's.  WALKED: the first ones end in no result (the backward pass reads them), two parts do.
+template <int KP, int VP, bool WALKED>
 __global__ void __launch_bounds__(LT_STATE_THREADS, 1)
 lin_state_tc(const __grid_constant__ StateArgs fwd, const __grid_constant__ StateArgs rev, const Ragged seqs, const LinCut cut, uint32_t wait_limit, uint32_t stall) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) StateShared sh;
-  if (blockIdx.y == 0) cut_states<KP, VP, false>(fwd, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
-  else cut_states<KP, VP, true>(rev, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
+  if (blockIdx.y == 0) cut_states<KP, VP, false, !WALKED>(fwd, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
+  else cut_states<KP, VP, true, true>(rev, sh, aligned_base(smem_raw), seqs, cut, wait_limit, stall);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------------- host
@@ -866,7 +903,6 @@ bool make_walk(WalkArgs& a, const LinPass& p, const rom_ragged& seqs) {
 }
 template <typename K>
 cudaError_t allow_smem(K kern, int bytes) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); }
-constexpr int more(int a, int b) { return a > b ? a : b; }
 
 template <int KP, int VP>
 cudaError_t launch_states_shape(const LinPass* p, int n, const rom_ragged& seqs, const LinCut& cut, uint32_t limit, uint32_t stall, cudaStream_t st) {
@@ -877,7 +913,7 @@ cudaError_t launch_states_shape(const LinPass* p, int n, const rom_ragged& seqs,
     if (!make_tmap_heads(&a[i].k, p[i].k, seqs.rows, p[i].H / p[i].kdiv, p[i].dk, p[i].ldk, rows) || !make_tmap_heads(&a[i].v, p[i].v, seqs.rows, p[i].H / p[i].vdiv, p[i].dv, p[i].ldv, rows))
       return cudaErrorInvalidValue;
   }
-  auto kern = lin_state_tc<KP, VP>;
+  auto kern = n > 1 ? lin_state_tc<KP, VP, true> : lin_state_tc<KP, VP, false>;
   const cudaError_t e = allow_smem(kern, smem);
   if (e != cudaSuccess) return e;
   count_launch();
