@@ -399,9 +399,9 @@ ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_
  *   log_decay : [n_heads] fp32, finite and at most 0 (0: no decay; others are in bounds, their results unspecified);  a constant of the model: it has no gradient.
  *   State pools: [n_slots, n_heads, d_k, d_v] fp32, slots as in the serving calls above (rom_ragged; in place, or two that do not overlap).
  * Pitches: elements, at least the row's width and a multiple of 16 bytes.  log_decay needs the alignment of its elements, everything else 16 bytes.
- * States and sums are fp32.  In bf16 the scores (after their decay) and the state that a chunk of rows meets are rounded to bf16 as operands of the matrix
- * instructions; the keys that enter the state are the sum of three bf16 numbers, which are all of their bits (in the backward's states, which only dq and dk
- * meet, of two: 2^-16 of each).
+ * States and sums are fp32.  In bf16 the scores (after their decay) and the state that a chunk of rows meets are operands of the matrix instructions as the sum
+ * of two bf16 numbers (less than 2^-15 of each left out), and so are the keys in the backward's states, which only dq and dk meet; the keys that enter a state
+ * that is a result are the sum of three, which are all of their bits.
  * A value that is not finite shows in its own row and later ones of its sequence and head, in earlier rows never. */
 typedef struct {
   int32_t n_heads;            /* value heads, 1..1024: one state and one decay each                            */

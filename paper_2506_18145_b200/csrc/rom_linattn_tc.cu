@@ -5,10 +5,10 @@
 //   S^T <- lambda^len S^T + V^T K~,  K~_j = ks lambda^{len-1-j} k_j      [dv x dk]     A = V^T, B = K~ (both MN-major)
 // (backwards: rows run the other way, j >= i, the exponents are counted from the chunk's other end.)
 //
-// Roundings: P and the S that a chunk meets are bf16 (half a step each, of separate parts of the sum); K~ is the
-// sum of three bf16 numbers, in three matrix products: all 24 bits of the fp32 product, since the state is an fp32 result that many chunks add up in (two, rounded, left 2.5e-6
-// of its norm where fp32 sums leave 2e-7; the third costs 10 % of a walk: 16384 rows of 32 heads of 128 x 128 in 147 instead of 133 us).  Two where the state is no result but only
-// read as bf16 by dq or dk.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
+// Roundings: P and the S that a chunk meets are the sum of two bf16 numbers each, in two matrix products, which leaves out less than 2^-15 of a number: as one bf16 number each
+// they made outputs 2.35e-3 of their norm off 64 bits, where the outputs' own rounding makes 1.66e-3.  K~ is the sum of three bf16 numbers, in three matrix products: all 24 bits of
+// the fp32 product, since the state is an fp32 result that many chunks add up in (two, rounded, left 2.5e-6 of its norm where fp32 sums leave 2e-7; the third costs 10 % of a walk).
+// Two where the state is no result but only read in two parts by dq or dk.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
 //
 // One CTA per SM walks one run of chunks.  640 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
 // width), warp 1 the matrix products, warps 4..11 turn scores into P and O1, O2 into output rows, warps 12..19 scale K in place (K~'s first part; the others beside it), and keep S; two
@@ -112,6 +112,12 @@ __device__ __forceinline__ float4 ld_state4(const float* p) {
 __device__ __forceinline__ uint32_t uppers(float2 x) { return __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632); }
 __device__ __forceinline__ float2 less_upper(float2 x) {
   return __ffma2_rn(make_float2(hi_of(__float_as_uint(x.x)), hi_of(__float_as_uint(x.y))), make_float2(-1.0f, -1.0f), x);      // (of an infinite number NaN: not finite either way)
+}
+// Two numbers as the sums of two bf16 numbers each.
+__device__ __forceinline__ void halves(float2 x, uint32_t& first, uint32_t& second) {
+  const float2 rest = less_upper(x);
+  first = uppers(x);
+  second = pack2(rest.x, rest.y);
 }
 // Part of one row of K (16-byte pieces of a 128-byte row of one box, swizzled by the row) times w: the first bf16 part in place, the second beside it, and the third where all of
 // the product's bits are asked for; zeros where the row is not part of the sum.  Some pieces at a time: one after the other, a piece's load, conversions and stores took 230 cycles.
@@ -230,7 +236,7 @@ __device__ __forceinline__ bool get_piece(const LinItem& it, const Ragged& q, bo
 }
 
 // ------------------------------------------------------------------------------------------------------------------------------ the walk
-// A wait that gives up ends the waits of its warp, not its loop: the warps that meet at named barriers (a quarter's two, each role's eight) all come to every one of
+// A wait that gives up ends the waits of its warp, not its loop: the warps that meet at named barriers (each role's eight) all come to every one of
 // them, and only the results are left out.
 __host__ __device__ constexpr int more(int a, int b) { return a > b ? a : b; }
 template <int KP, int VP>
@@ -238,10 +244,13 @@ struct WalkShape {
   static constexpr int KB = KP / 64, VB = VP / 64;
   // stages, as many as 227 KB hold: a copy takes up to 2 us when memory is busy, a chunk of two heads' widths of 64 half of that
   // (Q, and at 128 x 128 V, with one stage: Q S and V^T K~ end well before their next operands are used, and these come from L2: no slower than two of V)
-  static constexpr int KST = KP == 128 ? 2 : VP == 128 ? 3 : 4, QST = KP == 128 ? 1 : VP == 128 ? 2 : 3, VST = KP == 128 && VP == 128 ? 1 : KST;
-  static constexpr int Q = 0, K = Q + QST * KB * LT_BOX, V = K + KST * KB * LT_BOX, LO = V + VST * VB * LT_BOX, LL = LO + KB * LT_BOX, S = LL + KB * LT_BOX, BYTES = S + KB * VP * 128;
-  static constexpr int BARS = 2 * (QST + KST + VST) + 8;
-  static constexpr int SC = 0, O1 = 128, KV = O1 + VP, O2 = KV + KP;      // tensor-memory columns (P over the scores' first 64)
+  static constexpr int KST = KP == 128 ? 2 : VP == 128 ? 3 : 4, QST = KP == 128 || VP == 128 ? 1 : 2, VST = KP == 128 && VP == 128 ? 1 : KST;
+  static constexpr int Q = 0, K = Q + QST * KB * LT_BOX, V = K + KST * KB * LT_BOX, LO = V + VST * VB * LT_BOX, LL = LO + KB * LT_BOX, S = LL + KB * LT_BOX, S_BYTES = KB * VP * 128;
+  // the second part of S; at 128 x 128 it has no room of its own, and lies where K~'s third part comes once Q S has read it
+  static constexpr bool S2_IN_LL = KP == 128 && VP == 128;
+  static constexpr int S2 = S2_IN_LL ? LL : S + S_BYTES, BYTES = S + (S2_IN_LL ? 1 : 2) * S_BYTES;
+  static constexpr int BARS = 2 * (QST + KST + VST) + 9;
+  static constexpr int SC = 0, O1 = 128, KV = O1 + VP, O2 = KV + KP;      // tensor-memory columns (P over the scores: of every 16 columns the first parts in 8, the second in 8)
 };
 
 // Rows of O2 that are not finite, summed again over their own and earlier rows, where what the state gives is finite (else the result is not, either way: a value that is not
@@ -270,7 +279,7 @@ __device__ __noinline__ void slow_rows(const LinPass& p, int head, uint32_t tadd
       float s = 0.0f;
 #pragma unroll 1
       for (int d = 0; d < p.dk; ++d) s = fmaf(to_f32(qi[d]), to_f32(kj[d]), s);
-      const float w = to_f32(__float2bfloat16_rn(s * (p.p_scale * lam[REV ? j - i : i - j])));
+      const float w = s * (p.p_scale * lam[REV ? j - i : i - j]);
       const bf16* vj = static_cast<const bf16*>(p.v) + (int64_t)(row0 + j) * p.ldv + (head / p.vdiv) * p.dv + c0;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -317,9 +326,10 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
   auto k_empty = [&](int s) { return bar(BK + W::KST + s); };
   auto v_full = [&](int s) { return bar(BV + s); };
   auto v_empty = [&](int s) { return bar(BV + W::VST + s); };
-  const uint32_t sc_full = bar(B1), pv_full = bar(B1 + 1), state_full = bar(B1 + 2), drain = bar(B1 + 3), p_ready = bar(B1 + 4), k_ready = bar(B1 + 5), s_ready = bar(B1 + 6), o_free = bar(B1 + 7);
+  const uint32_t sc_full = bar(B1), pv_full = bar(B1 + 1), state_full = bar(B1 + 2), drain = bar(B1 + 3), p_ready = bar(B1 + 4), k_ready = bar(B1 + 5), s_ready = bar(B1 + 6), o_free = bar(B1 + 7), s2_read = bar(B1 + 8);
+  constexpr bool S2_LEAVES = W::S2_IN_LL && THIRD;      // K~'s third part waits for Q S to have read S's second
   if (tid == 0) {
-    for (int i = 0; i < W::BARS; ++i) mbar_init(bar(i), i >= B1 + 4 ? 8 : 1);
+    for (int i = 0; i < W::BARS; ++i) mbar_init(bar(i), i >= B1 + 4 && i < B1 + 8 ? 8 : 1);
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -422,12 +432,22 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
           for (int b = 0; b < W::KB; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              umma_bf16(tmem + W::O1, make_smem_desc(q + b * LT_BOX) + 2 * e, make_smem_desc(base + W::S + b * VP * 128) + 2 * e, d_o1, b + e > 0 ? 1u : 0u);
+              umma_bf16(tmem + W::O1, make_smem_desc(q + b * LT_BOX) + 2 * e, make_smem_desc(base + W::S2 + b * VP * 128) + 2 * e, d_o1, b + e > 0 ? 1u : 0u);
+          if (S2_LEAVES) umma_commit(s2_read);
+#pragma unroll
+          for (int b = 0; b < W::KB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              umma_bf16(tmem + W::O1, make_smem_desc(q + b * LT_BOX) + 2 * e, make_smem_desc(base + W::S + b * VP * 128) + 2 * e, d_o1, 1u);
           umma_commit(q_empty(qs));
-          if (!wait(v_full(vs), n / W::VST & 1) || !wait(p_ready, ph) || !wait(k_ready, ph)) break;
+          // P V while K~ is made, but where that clears rows of V
+          if (!wait(v_full(vs), n / W::VST & 1) || !wait(p_ready, ph) || ((len & 15) != 0 && !wait(k_ready, ph))) break;
           tc_fence_after();
-          for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 8 * e, desc_mn<LT_BOX>(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
+          for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 16 * e + 8, desc_mn<LT_BOX>(v) + (uint64_t)(MN_KSTEP * e), d_o2, e > 0 ? 1u : 0u);
+          for (int e = 0; e < ks; ++e) umma_bf16_ta(tmem + W::O2, tmem + W::SC + 16 * e, desc_mn<LT_BOX>(v) + (uint64_t)(MN_KSTEP * e), d_o2, 1u);
           umma_commit(pv_full);
+          if (!wait(k_ready, ph)) break;
+          tc_fence_after();
           issue_state<LT_BOX, THIRD>(tmem + W::KV, v, k, base + W::LO, base + W::LL, d_kv, ks);
           umma_commit(state_full);
           umma_commit(k_empty(st));
@@ -466,54 +486,56 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
         int row0, len;
         x.chunk<REV>(m, row0, len);
         const uint32_t ph = n & 1;
-        const int early = m == 0 && !x.over && p.early ? 1 : 0, blocks = (len + 31) / 32;
+        const int early = m == 0 && !x.over && p.early ? 1 : 0;
         ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit);
         tc_fence_after();
-        // blocks half and half + 2 of 32 columns; P lies over the scores, so both warps of the quarter have read theirs before either writes
-        uint32_t w[2][16];
+        // The quarter's two warps take every other 16 columns, and put P's first and second parts in the same columns, 8 each.  (Loops that are not unrolled, here, in the outputs and
+        // over K's pieces: the roles' code together is more than the instruction cache holds, and unrolled 16384 rows of 32 heads of 128 took 232 us instead of 215, prompts with heads
+        // of 64 120 instead of 98.)
+#pragma unroll 1
+        for (int b = half; b < (len + 15) / 16; b += 2) {
+          uint32_t w[16];
+          const int gap = 16 * b - 32 * quarter;      // of the columns from the quarter's first row
+          if (REV ? gap < 0 : gap > 16) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int b = half + 2 * t;
-          if (b >= blocks || (REV ? b < quarter : b > quarter)) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) w[t][e] = 0;
-            continue;
-          }
-          uint32_t r[32];
-          tmem_ld32_issue(lanes + W::SC + 32 * b, r);
-          tmem_ld_wait(r);
-          // A masked score is times 0; where it is not finite, the row is summed again below.  In the last chunk, whose other rows are not the sequence's, they are
-          // selected 0: forwards they are ahead of the diagonal, backwards in the last blocks.  (A pass of its own: tests among the loads of the powers left each to wait for
-          // its own, 75 cycles a place.)
-          if (len < LT_C && (REV ? 32 * b + 32 > len : b == quarter)) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (REV ? 32 * b + e >= len : e > lane) r[e] = 0;
-          }
-          if (b == quarter) {
-            const float* l = p_diag + 32 + (REV ? -lane : lane);
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 y = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), REV ? make_float2(l[e], l[e + 1]) : make_float2(l[-e], l[-e - 1]));
-              w[t][e / 2] = pack2(y.x, y.y);
-            }
+            for (int e = 0; e < 16; ++e) w[e] = 0;
           } else {
-            // lambda^{i-j} = lambda^{i - last of the block} lambda^{last - j}
-            const float g = p.p_scale * lam[REV ? 32 * b - i : i - 32 * b - 31];
+            uint32_t r[16];
+            tmem_ld16_issue(lanes + W::SC + 16 * b, r);
+            tmem_ld16_wait(r);
+            const bool diagonal = REV ? gap <= 16 : gap >= 0;
+            // A masked score is times 0; where it is not finite, the row is summed again below.  In the last chunk, whose other rows are not the sequence's, they are
+            // selected 0: forwards they are ahead of the diagonal, backwards in the last columns.
+            if (len < LT_C && (REV ? 16 * b + 16 > len : diagonal)) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 u = *reinterpret_cast<const float4*>(lam + (REV ? e : 28 - e));
-              const float2 u0 = REV ? make_float2(u.x, u.y) : make_float2(u.w, u.z), u1 = REV ? make_float2(u.z, u.w) : make_float2(u.y, u.x);
-              const float2 p0 = __fmul2_rn(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), __fmul2_rn(u0, make_float2(g, g)));
-              const float2 p1 = __fmul2_rn(make_float2(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), __fmul2_rn(u1, make_float2(g, g)));
-              w[t][e / 2] = pack2(p0.x, p0.y);
-              w[t][e / 2 + 1] = pack2(p1.x, p1.y);
+              for (int e = 0; e < 16; ++e)
+                if (REV ? 16 * b + e >= len : gap + e > lane) r[e] = 0;
             }
+            // lambda^{i-j} in steps of eight places, lambda^{i - last of the eight} lambda^{last - j}.  On the diagonal the row's own eight have powers of their own, zeros behind it.
+            float g[2];
+            float2 d[4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              g[k] = diagonal ? p_diag[32 + (REV ? gap + 8 * k - lane : lane - gap - 8 * k - 7)] : p.p_scale * lam[REV ? 16 * b - i + 8 * k : i - 16 * b - 8 * k - 7];
+            if (diagonal) {
+              const float* l = p_diag + 32 + (REV ? -(lane & 7) : lane & 7);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) d[e] = REV ? make_float2(l[2 * e], l[2 * e + 1]) : make_float2(l[-2 * e], l[-2 * e - 1]);
+            }
+            const float4 u0 = *reinterpret_cast<const float4*>(lam), u1 = *reinterpret_cast<const float4*>(lam + 4);
+            const float2 u[4] = {REV ? make_float2(u0.x, u0.y) : make_float2(u1.w, u1.z), REV ? make_float2(u0.z, u0.w) : make_float2(u1.y, u1.x),
+                                 REV ? make_float2(u1.x, u1.y) : make_float2(u0.w, u0.z), REV ? make_float2(u1.z, u1.w) : make_float2(u0.y, u0.x)};
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float2 f = __fmul2_rn(u[e], make_float2(g[k], g[k]));
+                if (diagonal && gap + 8 * k == (lane & 24)) f = d[e];
+                halves(__fmul2_rn(make_float2(__uint_as_float(r[8 * k + 2 * e]), __uint_as_float(r[8 * k + 2 * e + 1])), f), w[4 * k + e], w[8 + 4 * k + e]);
+              }
           }
+          tmem_st16(lanes + W::SC + 16 * b, w);
         }
-        asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
-        tmem_st16(lanes + W::SC + 16 * half, w[0]);
-        if (half + 2 < blocks) tmem_st16(lanes + W::SC + 16 * (half + 2), w[1]);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         warp_arrive(p_ready);
@@ -522,7 +544,7 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
         const bool mine = i < len;
         const float f = p.inter_scale * lam[REV ? max(len - i - early, 0) : i + 1 - early];
         float2 odd = make_float2(0.0f, 0.0f);
-        constexpr int PC = VP / 16;    // 16-byte pieces of a warp's columns in bf16
+        constexpr int PC = 4;
         const int c_from = half * (VP / 2), c_to = min(p.dv, c_from + VP / 2), first = quarter * 32 + lane / PC * PC, rows = ok ? len - first : 0;      // (rows that the lane stores)
         const int first8 = quarter * 32 + (lane & 24), rows8 = ok ? len - first8 : 0;
         // 16 columns: f O1 + O2, noting what is not finite
@@ -554,16 +576,18 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
             const int col = c + 4 * (lane & 7);
             store_rows<8>(reinterpret_cast<char*>(static_cast<float*>(p.out) + (int64_t)(row0 + first8) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 4, rows8, col < p.dv, w, lane);
           }
-        } else if (c_from < c_to) {
+        } else
+#pragma unroll 1
+        for (int c1 = c_from; c1 < c_to; c1 += 32) {
           uint32_t w[4 * PC];
 #pragma unroll
           for (int u = 0; u < PC / 2; ++u) {
             float2 o[8];
-            columns(c_from + 16 * u, o);
+            columns(c1 + 16 * u, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[8 * u + e] = pack2(o[e].x, o[e].y);
           }
-          const int col = c_from + 8 * (lane & (PC - 1));
+          const int col = c1 + 8 * (lane & (PC - 1));
           store_rows<PC>(reinterpret_cast<char*>(out + (int64_t)(row0 + first) * p.ldo + (int64_t)head * p.dv + col), p.ldo * 2, rows, col < p.dv, w, lane);
         }
         const bool again = ok && mine && !(odd.x == 0.0f && odd.y == 0.0f);
@@ -585,12 +609,18 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
     pdl_wait();
     pdl_trigger();                     // (behind the block's tensor memory: the successor takes its own before it waits)
     bool ok = true;
-    auto write_s = [&]() {      // bf16 rows of S^T, K-major
-      if (c < VP)
-#pragma unroll
-        for (int a = 0; a < KH; a += 8)
-          sts128(base + W::S + (KP == 128 ? half : 0) * VP * 128 + c * 128 + ((((KP == 128 ? 0 : 4 * half) + a / 8) ^ (c & 7)) << 4),
-                 make_uint4(pack2(S[a], S[a + 1]), pack2(S[a + 2], S[a + 3]), pack2(S[a + 4], S[a + 5]), pack2(S[a + 6], S[a + 7])));
+    // Eight numbers of S^T's row c, K-major, in two parts.
+    auto write_8 = [&](int a, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7) {
+      const uint32_t off = (KP == 128 ? half : 0) * VP * 128 + c * 128 + ((((KP == 128 ? 0 : 4 * half) + a / 8) ^ (c & 7)) << 4);
+      uint4 h, l;
+      halves(make_float2(x0, x1), h.x, l.x);
+      halves(make_float2(x2, x3), h.y, l.y);
+      halves(make_float2(x4, x5), h.z, l.z);
+      halves(make_float2(x6, x7), h.w, l.w);
+      sts128(base + W::S + off, h);
+      sts128(base + W::S2 + off, l);
+    };
+    auto wrote_s = [&]() {
       fence_async();
       warp_arrive(s_ready);
     };
@@ -647,7 +677,12 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
 #pragma unroll
       for (int a = 0; a < KH; ++a)
         if (!mine || a0 + a >= p.dk) S[a] = 0.0f;
-      if (mm > 0) write_s();
+      if (mm > 0) {
+        if (c < VP)
+#pragma unroll
+          for (int a = 0; a < KH; a += 8) write_8(a, S[a], S[a + 1], S[a + 2], S[a + 3], S[a + 4], S[a + 5], S[a + 6], S[a + 7]);
+        wrote_s();
+      }
       for (int m = 0; m < mm; ++m, ++n) {
         int row0, len;
         x.chunk<REV>(m, row0, len);
@@ -656,10 +691,11 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
         // (the scores are made of this K: sc_full says that it has landed, but the copies' own barrier makes them visible)
         ok = ok && warp_wait(sc_full, ph, abort_flag, wait_limit) && warp_wait(k_full(st), n / W::KST & 1, abort_flag, wait_limit);
         if (rows16 > len) ok = ok && warp_wait(v_full(vs), n / W::VST & 1, abort_flag, wait_limit);
+        if (S2_LEAVES) ok = ok && warp_wait(s2_read, ph, abort_flag, wait_limit);
         if (c < rows16) {
           const bool live = c < len;
           const float w = live ? p.k_scale * lam[REV ? c : len - 1 - c] : 0.0f;
-          scale_row<KP == 128 ? 2 : 4, THIRD>(k + box, base + W::LO + box, base + W::LL + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
+          scale_row<2, THIRD>(k + box, base + W::LO + box, base + W::LL + box, c, w, live, KP == 128 ? 0 : 4 * half, KP == 128 ? 8 : 4);
           if (!live && half < W::VB) clear_row(base + W::V + (vs * W::VB + half) * LT_BOX, c);
         }
         fence_async();
@@ -679,9 +715,12 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
             S[a + e] = v.x;
             S[a + e + 1] = v.y;
           }
+          if (c < VP && m + 1 < mm)      // (here and not behind the loop: all of S's parts at once are more registers than there are)
+#pragma unroll
+            for (int e = 0; e < 16; e += 8) write_8(a + e, S[a + e], S[a + e + 1], S[a + e + 2], S[a + e + 3], S[a + e + 4], S[a + e + 5], S[a + e + 6], S[a + e + 7]);
         }
         tc_fence_before();
-        if (m + 1 < mm) write_s();
+        if (m + 1 < mm) wrote_s();
       }
       if (ok && p.last && slot >= 0 && x.ends && c < p.dv) {
         const bool none = p.init_all && !seqs.resumes(s);

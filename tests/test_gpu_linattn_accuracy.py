@@ -1,0 +1,85 @@
+"""Linear attention in bf16 against closed forms in 64 bits, to what its arithmetic leaves beside the rounding of the results themselves.
+
+A result is one rounding of a number x that lies within `slack` of the exact one: rounding is monotone, so it lies between the rounded ends of [exact - slack, exact + slack]."""
+import pytest
+import torch
+
+from paper_2506_18145_b200 import binding as rb
+
+import linattn_testlib as T
+from linattn_testlib import Problem
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(2, 2, 16, 64), (4, 2, 64, 64), (2, 1, 128, 128), (2, 2, 128, 40), (3, 3, 24, 128)]
+# Operands are sums of two bf16 numbers: the first, cut off, leaves less than 2^-7 of a number, of which the second loses half a step, 2^-8.
+PARTS = 2.0 ** -15
+STEP = 2.0 ** -23      # what a sum in the matrix instructions may lose a term, of the sum of its terms' sizes
+
+
+def one_rounding(got, ref, slack, what):
+    got, ref = got.double().reshape(ref.shape), ref.double()
+    low, high = (ref - slack).to(torch.bfloat16).double(), (ref + slack).to(torch.bfloat16).double()
+    wrong = ~((got >= low) & (got <= high))
+    assert not wrong.any(), f"{what}: {int(wrong.sum())} of {wrong.numel()} are no rounding of the result, the first off by {float((got - ref)[wrong][0]):.3g} where {float(slack[wrong][0]):.3g} is left"
+
+
+def by_heads(x, rows, n):
+    return x[rows].reshape(x[rows].shape[0], n, -1)
+
+
+@pytest.mark.parametrize("H,G,dk,dv", SHAPES)
+@pytest.mark.parametrize("n", [1, 16, 37, 128])
+def test_scores_keep_their_bits(n, H, G, dk, dv):
+    """One chunk from a state of zeros: only scores, decayed, times values."""
+    pr = Problem([n], H, G, dk, dv, "bf16", seed=n, lead=1, tail=2, resume=[0], backward=True)
+    rows, q, k, v, do, S0, _ = pr.sequence(0)
+    o, _ = pr.run(s_out=None)
+    q_, k_, v_ = T._share(q, H), T._share(k, H), v.transpose(0, 1)
+    D = T._decays(pr.g.double(), n)[0]
+    P, Psize = abs(pr.scale) * (q_ @ k_.transpose(1, 2)).abs() * D, abs(pr.scale) * (q_.abs() @ k_.abs().transpose(1, 2)) * D
+    ref, _ = T.forward(q, k, v, pr.g.double(), S0, pr.scale)
+    slack = (PARTS * P + (dk + n + 8) * STEP * Psize) @ v_.abs()
+    one_rounding(by_heads(o, rows, H), ref, slack.transpose(0, 1), "o")
+    dq, dk_, dv_, _ = pr.run_backward(ds_out=None, ds_in=None, s_in=None)
+    do_ = do.transpose(0, 1)
+    A, Asize = abs(pr.scale) * (do_ @ v_.transpose(1, 2)).abs() * D, abs(pr.scale) * (do_.abs() @ v_.abs().transpose(1, 2)) * D
+    left, right = PARTS * A + (dv + n + 8 + H // G) * STEP * Asize, PARTS * P + (dk + n + 8) * STEP * Psize
+    ref = T.backward(do, q, k, v, pr.g.double(), S0, torch.zeros_like(S0), pr.scale)
+    back = lambda x: x.transpose(0, 1).reshape(n, G, H // G, x.shape[2]).sum(2)  # noqa: E731
+    one_rounding(by_heads(dq, rows, G), ref[0], back(left @ k_.abs()), "dq")
+    one_rounding(by_heads(dk_, rows, G), ref[1], back(left.transpose(1, 2) @ q_.abs()), "dk")
+    one_rounding(by_heads(dv_, rows, H), ref[2], (right.transpose(1, 2) @ do_.abs()).transpose(0, 1), "dv")
+
+
+@pytest.mark.parametrize("H,G,dk,dv", SHAPES)
+@pytest.mark.parametrize("n", [1, 33, 128, 300])
+def test_the_state_keeps_its_bits(n, H, G, dk, dv):
+    """Keys (or queries, or values) of zeros: the scores are zero, and every result is a product with the state that came in, decayed."""
+    chunks = n / 128 + 1
+    pr = Problem([n], H, G, dk, dv, "bf16", seed=n, tail=3, resume=[1], rates=[0.02 * 0.5 ** h for h in range(H)], backward=True)
+    pr.k.zero_()
+    rows, q, k, v, do, S0, dS = pr.sequence(0)
+    ref, _ = T.forward(q, k, v, pr.g.double(), S0, pr.scale)
+    size, _ = T.forward(q.abs(), k, v, pr.g.double(), S0.abs(), abs(pr.scale))
+    unit = PARTS + (dk + 8 + 3 * chunks) * STEP
+    one_rounding(by_heads(pr.run(s_out=None)[0], rows, H), ref, unit * size, "o")
+
+    gen = torch.Generator().manual_seed(n)
+    pr.k.copy_(torch.randn(pr.k.shape, generator=gen))
+    pr.q.zero_()      # dk = v R^T, dv = k R: of ds_out alone
+    rows, q, k, v, do, S0, dS = pr.sequence(0)
+    got = pr.run_backward()
+    ref = T.backward(do, q, k, v, pr.g.double(), S0, dS, pr.scale)
+    size = T.backward(do.abs(), q, k.abs(), v.abs(), pr.g.double(), S0.abs(), dS.abs(), abs(pr.scale))
+    unit = PARTS + (max(dk, dv) + H // G + 8 + 3 * chunks) * STEP
+    one_rounding(by_heads(got[1], rows, G), ref[1], unit * size[1], "dk")
+    one_rounding(by_heads(got[2], rows, H), ref[2], unit * size[2], "dv")
+
+    pr.q.copy_(torch.randn(pr.q.shape, generator=gen))
+    pr.v.zero_()      # dq = dout S^T: of s_in alone
+    rows, q, k, v, do, S0, dS = pr.sequence(0)
+    got = pr.run_backward()
+    ref = T.backward(do, q, k, v, pr.g.double(), S0, dS, pr.scale)
+    size = T.backward(do.abs(), q.abs(), k.abs(), v, pr.g.double(), S0.abs(), dS.abs(), abs(pr.scale))
+    one_rounding(by_heads(got[0], rows, G), ref[0], unit * size[0], "dq")
