@@ -401,7 +401,8 @@ ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_
  * Pitches: elements, at least the row's width and a multiple of 16 bytes.  log_decay needs the alignment of its elements, everything else 16 bytes.
  * States and sums are fp32.  In bf16 the scores (after their decay) and the state that a chunk of rows meets are operands of the matrix instructions as the sum
  * of two bf16 numbers (less than 2^-15 of each left out), and so are the keys in the backward's states, which only dq and dk meet; the keys that enter a state
- * that is a result are the sum of three, which are all of their bits.
+ * that is a result are the sum of three, which are all of their bits.  A sum in the matrix instructions, which drop what is below its last bit, moves to fp32
+ * registers after 512 rows at most, so that a state's error does not grow with its sequence (6e-7 of its norm measured, without decay).
  * A value that is not finite shows in its own row and later ones of its sequence and head, in earlier rows never. */
 typedef struct {
   int32_t n_heads;            /* value heads, 1..1024: one state and one decay each                            */

@@ -767,10 +767,12 @@ lin_walk3_tc(const __grid_constant__ WalkArgs dq, const __grid_constant__ WalkAr
 }
 
 // ------------------------------------------------------------------------------------------------------------------------------ launch 1: states at the cuts
-// sum over the rows between two cuts of the sequence that reaches over the far one, lambda^{distance to that cut} ks k_j v_j^T: every row's weight is known, so all of
-// them add up in tensor memory, in steps of 64 rows: the first parts of K~ in one accumulator, the small ones in another, which the two products of V with K~'s first and second part
-// fill as one of twice the width (every step drops what is below the accumulator's last bit: in one accumulator for all of them the state was off by 1.2e-6, in two by 4e-7).  Sixteen
-// warps scale K, eight threads to a row (eight warps: 209.6 us for the whole call at 16384 rows of 32 heads of 128 x 128, sixteen: 207).  What bounds it: shared memory, 176 KB of
+// sum over the rows between two cuts of the sequence that reaches over the far one, lambda^{distance to that cut} ks k_j v_j^T: every row's weight is known, so they
+// add up in tensor memory, in steps of 64 rows: the first parts of K~ in one accumulator, the small ones in another, which the two products of V with K~'s first and second part
+// fill as one of twice the width (in one accumulator for all of them the state was off by three times as much).  Every product of 16 rows drops what is below the accumulator's last bit,
+// which is the same way each time: the error of one sum grows with its rows.  After 512 rows the sum moves to fp32 registers, which round to nearest, while the next 512 add up in
+// another pair (16384 rows of 32 heads without decay, in
+// one sum of 4096 rows: the last state 3.8e-6 of its norm off, 131072 rows 3.2e-5; so 4.4e-7 and 5.6e-7, for 3 us of 217 of the call at 16384 rows of 32 heads of 128).  Sixteen warps scale K, eight threads to a row (eight warps: 209.6 us for the whole call at 16384 rows of 32 heads of 128 x 128, sixteen: 207).  What bounds it: shared memory, 176 KB of
 // copies, operands and K~ a step of 128 x 128, 1400 cycles of the 2100 that a step takes; from DRAM it asks for 4 TB/s.
 template <int KP, int VP>
 struct StateShape {
@@ -785,7 +787,8 @@ static_assert(WalkShape<64, 64>::BYTES + (int)sizeof(WalkShared<WalkShape<64, 64
 static_assert(StateShape<128, 128>::BYTES + 1024 <= kLtMaxSmem && StateShape<128, 64>::BYTES + 1024 <= kLtMaxSmem && StateShape<64, 128>::BYTES + 1024 <= kLtMaxSmem, "shared memory");
 
 struct StateArgs { CUtensorMap k, v; LinPass p; };
-struct StateShared { unsigned long long bars[3 * 8 + 2]; uint32_t tmem; int abort; };
+constexpr int LT_FOLD = 8;                    // steps of 64 rows in one sum
+struct StateShared { unsigned long long bars[3 * 8 + 3]; uint32_t tmem; int abort; };
 template <int KP, int VP, bool REV, bool THIRD>
 __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& sh, const uint32_t base, const Ragged& seqs, const LinCut& cut, uint32_t wait_limit, uint32_t stall) {
   using W = StateShape<KP, VP>;
@@ -807,17 +810,19 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
   auto full = [&](int i) { return smem_u32(&bars[i]); };
   auto empty = [&](int i) { return smem_u32(&bars[8 + i]); };
   auto scaled = [&](int i) { return smem_u32(&bars[16 + i]); };
-  const uint32_t done = smem_u32(&bars[24]), drain = smem_u32(&bars[25]);
+  auto done = [&](int sum) { return smem_u32(&bars[24 + (sum & 1)]); };
+  const uint32_t drain = smem_u32(&bars[26]);
   if (tid == 0) {
     for (int i = 0; i < 8; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); mbar_init(scaled(i), LT_SCALERS); }
-    mbar_init(done, 1);
+    mbar_init(done(0), 1);
+    mbar_init(done(1), 1);
     mbar_init(drain, 1);
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)(2 * KP)) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)(4 * KP)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -851,16 +856,17 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
         const uint32_t at = base + st * W::STAGE;
         if (!mbar_wait(scaled(st), n / W::STAGES & 1, abort_flag, wait_limit)) { ok = false; break; }
         tc_fence_after();
+        const uint32_t sum = tmem + (n / LT_FOLD & 1) * 2 * KP;
         const uint64_t a = desc_mn<W::BOX>(at + W::V), hl = desc_mn<W::BOX>(at), ll = desc_mn<W::BOX>(at + W::LL);
         for (int k = 0, ks = (min(W::ROWS, r1 - r0 - W::ROWS * step(n)) + 15) / 16; k < ks; ++k) {
-          umma_bf16(tmem, a + (uint64_t)(MN_KSTEP * k), hl + (uint64_t)(MN_KSTEP * k), lt_idesc(2 * KP, true, true), n + k > 0 ? 1u : 0u);
-          if (THIRD) umma_bf16(tmem + KP, a + (uint64_t)(MN_KSTEP * k), ll + (uint64_t)(MN_KSTEP * k), lt_idesc(KP, true, true), 1u);
+          umma_bf16(sum, a + (uint64_t)(MN_KSTEP * k), hl + (uint64_t)(MN_KSTEP * k), lt_idesc(2 * KP, true, true), n % LT_FOLD + k > 0 ? 1u : 0u);
+          if (THIRD) umma_bf16(sum + KP, a + (uint64_t)(MN_KSTEP * k), ll + (uint64_t)(MN_KSTEP * k), lt_idesc(KP, true, true), 1u);
         }
         umma_commit(empty(st));
+        if (n % LT_FOLD == LT_FOLD - 1 || n == chunks - 1) umma_commit(done(n / LT_FOLD));
         issued = true;
       }
-      if (ok) umma_commit(done);
-      else latch(p, abort_flag, 56);
+      if (!ok) latch(p, abort_flag, 56);
       if (*abort_flag && issued) {
         umma_commit(drain);
         for (uint32_t it = 0; it < wait_limit >> 2 && !mbar_try_wait(drain, 0); ++it) {}
@@ -872,13 +878,36 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
     const int group = (warp - 2) >> 2, quarter = warp & 3, j = quarter * 32 + lane, row = (tid - 64) & 63, part = (tid - 64) >> 6;
     const double g2 = (double)__ldg(p.log_decay + head) * 1.4426950408889634;
     bool ok = true;
-    for (int n = 0; n < chunks; ++n) {
+    float total[COLS];
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) total[e] = 0.0f;
+    auto fold = [&](int sum) {
+      if (!(ok = ok && warp_wait(done(sum), sum >> 1 & 1, abort_flag, wait_limit))) return;
+      tc_fence_after();
+      const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (sum & 1) * 2 * KP + group * COLS;
+#pragma unroll
+      for (int c = 0; c < COLS; c += 16) {
+        uint32_t hi[16], lo[16];
+        __syncwarp();
+        tmem_ld16_issue(from + c, hi);
+        tmem_ld16_issue(from + KP + c, lo);
+        tmem_ld16_wait(hi);
+        tmem_ld16_wait(lo);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) total[c + e] += __uint_as_float(hi[e]) + __uint_as_float(lo[e]);
+      }
+      tc_fence_before();
+    };
+    int folded = 0;
+    for (int n = 0; n < chunks && ok; ++n) {
+      // the sum before, two steps late: its products are done.  (The pair is used again only once the warps have scaled a later step's keys.)
+      if (n % LT_FOLD == 2 && n > LT_FOLD) fold(folded++);
       const int st = n % W::STAGES, row0 = r0 + W::ROWS * step(n), len = min(W::ROWS, r1 - row0), rows16 = (len + 15) / 16 * 16;
       const uint32_t at = base + st * W::STAGE;
       // lambda^{distance}: the exponent in 64 bits, its fraction alone through fp32
       const double t = fmax(g2 * max(REV ? row0 + row - r0 : r1 - 1 - row0 - row, 0), -400.0), whole = rint(t);
       const float w = p.k_scale * ldexpf(exp2f((float)(t - whole)), (int)whole);
-      if (!(ok = warp_wait(full(st), n / W::STAGES & 1, abort_flag, wait_limit))) break;
+      if (!(ok = ok && warp_wait(full(st), n / W::STAGES & 1, abort_flag, wait_limit))) break;
       if (row < rows16) {
         const bool live = row < len;
         constexpr int PIECES = KP / 8 / PARTS;
@@ -890,27 +919,19 @@ __device__ __forceinline__ void cut_states(const StateArgs& args, StateShared& s
       warp_arrive(scaled(st));
     }
     pdl_wait();
-    if (ok && (ok = warp_wait(done, 0, abort_flag, wait_limit))) {
-      tc_fence_after();
+    while (folded <= (chunks - 1) / LT_FOLD) fold(folded++);
+    if (ok && j < p.dv) {
       float* to = p.cut_state + (size_t)blockIdx.x * ((size_t)p.dk * p.dv) + j;
-      for (int c = group * COLS; c < (group + 1) * COLS; c += 16) {
-        uint32_t hi[16], lo[16];
-        __syncwarp();
-        tmem_ld16_issue(tmem + ((uint32_t)(quarter * 32) << 16) + c, hi);
-        tmem_ld16_issue(tmem + ((uint32_t)(quarter * 32) << 16) + KP + c, lo);
-        tmem_ld16_wait(hi);
-        tmem_ld16_wait(lo);
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (j < p.dv && c + e < p.dk) to[(size_t)(c + e) * p.dv] = __uint_as_float(hi[e]) + __uint_as_float(lo[e]);
-      }
+      for (int e = 0; e < COLS; ++e)
+        if (group * COLS + e < p.dk) to[(size_t)(group * COLS + e) * p.dv] = total[e];
     }
     if (!ok) latch(p, abort_flag, 57);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * KP)) : "memory");
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(4 * KP)) : "memory");
 }
 // blockIdx.y: the forward's states, the backward's.  WALKED: the first ones end in no result (the backward pass reads them), two parts do.
 template <int KP, int VP, bool WALKED>

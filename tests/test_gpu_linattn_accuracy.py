@@ -83,3 +83,34 @@ def test_the_state_keeps_its_bits(n, H, G, dk, dv):
     ref = T.backward(do, q, k, v, pr.g.double(), S0, dS, pr.scale)
     size = T.backward(do.abs(), q.abs(), k.abs(), v, pr.g.double(), S0.abs(), dS.abs(), abs(pr.scale))
     one_rounding(by_heads(got[0], rows, G), ref[0], unit * size[0], "dq")
+
+
+def weighted(x, y, g, exponent):
+    """sum_t lambda^exponent_t x_t y_t^T for every head, [H, dx, dy]; x, y [n, H, d]."""
+    w = torch.exp(g[:, None] * exponent)      # [H, n]
+    return torch.stack([(x[:, h] * w[h][:, None]).T @ y[:, h] for h in range(x.shape[1])])
+
+
+@pytest.mark.parametrize("n,d", [(16384, 16), (131072, 16), (16384, 128)])
+def test_long_sums_lose_no_more_than_short_ones(n, d):
+    """One sequence of many heads, thousands of rows from cut to cut, hardly any decay: the last state and the gradient of the first one, which are sums over all rows.
+
+    `near` allows 2^-19 of the norm, what 32 sums in the matrix instructions lose at most before they move to registers; how many rows there are does not matter."""
+    H = 32
+    pr = Problem([n], H, H, d, d, "bf16", seed=3, resume=[1], rates=[[0.0, 2.0 ** -11, 1e-5, 2.0 ** -7][h % 4] for h in range(H)], backward=True)
+    g, slot = pr.g.double(), int(pr.p.slots[0])
+    at = torch.arange(n, dtype=torch.float64, device="cuda")
+    full = torch.exp(g * n)[:, None, None]
+    _, s = pr.run()
+    cut = lambda x: x.double().view(n, H, d)  # noqa: E731
+    es = T.units(n, d, True)[1]
+    S = weighted(cut(pr.k), cut(pr.v), g, n - 1 - at) + full * pr.s_in[slot].double()
+    size = weighted(cut(pr.k).abs(), cut(pr.v).abs(), g, n - 1 - at) + full * pr.s_in[slot].double().abs()
+    for h in range(4):      # (each rate of its own: the sums without decay are the largest)
+        T.near(s[slot][h::4], S[h::4], size[h::4], es, "f32", f"state, rate {float(-pr.g[h]):.2g}")
+    *_, ds = pr.run_backward()
+    R = pr.scale * weighted(cut(pr.q), cut(pr.do), g, at + 1) + full * pr.ds_out[slot].double()
+    size = pr.scale * weighted(cut(pr.q).abs(), cut(pr.do).abs(), g, at + 1) + full * pr.ds_out[slot].double().abs()
+    for h in range(4):
+        T.near(ds[slot][h::4], R[h::4], size[h::4], es, "f32", f"gradient of the state, rate {float(-pr.g[h]):.2g}")
+    assert rb.rom_get_status(pr.ws) == 0
