@@ -429,7 +429,7 @@ ROM_API int rom_linattn_step(const rom_linattn_config *cfg, int32_t B, const voi
 /* Backward of rom_linattn_ragged on the same sequences and inputs: given dout = dLoss/do and ds_out = dLoss/d(s_out) (NULL: zeros),
  *   dq_t = scale * S_t dout_t,   R_t = lambda R_{t+1} + scale * q_t dout_t^T  (+ ds_out at a sequence's last row),   dk_t = R_t v_t,   dv_t = R_t^T k_t,
  * dq and dk summed over the value heads that share them, and ds_in = lambda R at a sequence's first row (of an empty one: ds_out), zeros for a sequence that
- * started from zeros.  The states are recomputed, not kept by the forward.
+ * started from zeros (without s_in: all of them, whatever `resume` says).  The states are recomputed, not kept by the forward.
  *   dout : [rows, n_heads, d_v] contiguous;  dq, dk : [rows, n_qk_heads, d_k] contiguous;  dv : [rows, n_heads, d_v], pitch lddv;  all dtype, rows outside the
  *   sequences are left as they are;  ds_in (NULL: not produced): [n_slots, n_heads, d_k, d_v] fp32, slots that no sequence names are left as they are; does not
  *   overlap ds_out or s_in.  No output is an input.  Sums are taken in a fixed order: results are the same from run to run.

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) lin_walk_simt(const __grid_const
         else load_state(lin_init_of(p, seqs, s, head));
         if (!empty) walk(r0, r1, !over);
         if (p.last && slot >= 0 && (empty || (p.reverse ? st >= a : en <= b)))
-          store_state(p.last + ((size_t)slot * p.H + head) * state, p.init_all && !seqs.resumes(s) ? 0.0f : !empty && p.early ? lam[1] : 1.0f);
+          store_state(p.last + ((size_t)slot * p.H + head) * state, lin_leaves_zeros(p, seqs, s) ? 0.0f : !empty && p.early ? lam[1] : 1.0f);
       }
     }
   }
@@ -655,6 +655,7 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   dv_walk.q = k; dv_walk.k = q; dv_walk.v = dout; dv_walk.ldq = ldk; dv_walk.ldk = ldq; dv_walk.ldv = ld_do;
   dv_walk.qdiv = dv_walk.kdiv = share; dv_walk.vdiv = 1; dv_walk.dk = c.d_k; dv_walk.dv = c.d_v;
   dv_walk.inter_scale = 1.0f; dv_walk.k_scale = c.scale; dv_walk.reverse = true; dv_walk.init = ds_out; dv_walk.init_all = true; dv_walk.early = true; dv_walk.last = ds_in;
+  dv_walk.none_resumes = !s_in;
   dv_walk.cut_state = reinterpret_cast<float*>(W + lay.cut_b);
   dv_walk.out = dv; dv_walk.ldo = lddv;
   // dq on S, dk on R, both transposed

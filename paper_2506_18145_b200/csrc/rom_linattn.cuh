@@ -31,7 +31,8 @@ struct LinPass {
   const float* init;               // pool of the states that sequences start from, or null
   bool init_all;                   // every sequence starts from it (else: those that resume)
   bool early;                      // it meets the first row undecayed, and the state left at the end is decayed once more
-  float* last;                     // pool of the states left at the end (a sequence that does not resume leaves zeros when init_all), or null
+  float* last;                     // pool of the states left at the end (when init_all, a sequence that started from zeros leaves zeros), or null
+  bool none_resumes;               // every sequence started from zeros, whatever its flag says
   const float* powers;             // [H][2][kLinPowers]
   float* cut_state;                // [cuts, state]: launch 1 writes, launch 2 chains in place, launch 3 reads; [i - 1] belongs to the cut before run i
   float* init_copy;                // [cuts, state] or null: initial states of sequences that start in run i - 1 and reach over the cut before run i (pools in place)
@@ -129,6 +130,8 @@ __device__ __forceinline__ bool lin_cut_rows(const LinCut& c, int i, bool revers
   }
   return r1 > r0;
 }
+// Whether sequence s leaves zeros at its end instead of the state.
+__device__ __forceinline__ bool lin_leaves_zeros(const LinPass& p, const Ragged& seqs, int s) { return p.init_all && (p.none_resumes || !seqs.resumes(s)); }
 __device__ __forceinline__ const float* lin_init_of(const LinPass& p, const Ragged& seqs, int s, int head) {
   const int slot = seqs.slot_of(s);
   if (!p.init || slot < 0 || !(p.init_all || seqs.resumes(s))) return nullptr;

@@ -723,7 +723,7 @@ __device__ __forceinline__ void walk(const WalkArgs& args, WalkShared<BARS>& sh,
         if (m + 1 < mm) wrote_s();
       }
       if (ok && p.last && slot >= 0 && x.ends && c < p.dv) {
-        const bool none = p.init_all && !seqs.resumes(s);
+        const bool none = lin_leaves_zeros(p, seqs, s);
         const float f = mm > 0 && p.early ? lam[1] : 1.0f;
         float* to = p.last + ((size_t)slot * p.H + head) * state + c;
 #pragma unroll
