@@ -266,7 +266,8 @@ constexpr int CHAIN_THREADS = 128;
 __global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(const __grid_constant__ LinJobs jobs, Ragged seqs, LinCut cut) {
   const LinPass& p = jobs.p[blockIdx.z];
   __shared__ int how[kLinMaxBlocks];            // at the head's cuts: -3 nobody reaches over it; -2 the state comes over a cut; else a sequence starts here: its state's slot, or -1
-  __shared__ float weight[kLinMaxBlocks];       // of the state at the cut before, or of the sequence's initial state
+  // of the state at the cut before, or of the sequence's initial state, in two floats: cuts are as many rows apart, and the rounding of one float would be the same at each of them
+  __shared__ float weight[kLinMaxBlocks], weight_lo[kLinMaxBlocks];
   const int head = blockIdx.y;
   const double g = (double)__ldg(p.log_decay + head);
   const long long u0 = (long long)head * cut.per_head, u1 = u0 + cut.per_head;
@@ -281,14 +282,15 @@ __global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(const __grid_constant
   for (int j = threadIdx.x; j < n; j += CHAIN_THREADS) {
     const int r = row_of(j), s = lin_spanning_1(seqs, r), far = row_of(p.reverse ? j + 1 : j - 1);
     int h = -3;
-    float w = 0.0f;
+    double w = 0.0;
     if (s >= 0) {
       const int away = p.reverse ? seqs.end_of(s) - r : r - seqs.start_of(s), seg = p.reverse ? far - r : r - far, slot = seqs.slot_of(s);
       h = away > seg ? -2 : p.init && (p.init_all || seqs.resumes(s)) ? slot : -1;
-      w = (float)exp(g * (h == -2 ? seg : away - (p.early ? 1 : 0)));
+      w = exp(g * (h == -2 ? seg : away - (p.early ? 1 : 0)));
     }
     how[j] = h;
-    weight[j] = w;
+    weight[j] = (float)w;
+    weight_lo[j] = (float)(w - (double)(float)w);
   }
   pdl_sync();                           // (the tables above come from inputs, which are older than launch 1)
   __syncthreads();
@@ -309,12 +311,13 @@ __global__ void __launch_bounds__(CHAIN_THREADS) lin_chain(const __grid_constant
       if (i0 + u >= n) break;
       const int j = p.reverse ? n - 1 - (i0 + u) : i0 + u, h = how[j];
       if (h == -3) continue;
-      const float w = weight[j];
+      const float w = weight[j], wl = weight_lo[j];
       if (h >= 0) {
         x = init[u];
         if (p.init_copy) *reinterpret_cast<float4*>(p.init_copy + (size_t)(first + j - 1) * state + e) = x;
       }
-      x = h != -1 ? make_float4(fmaf(w, x.x, add[u].x), fmaf(w, x.y, add[u].y), fmaf(w, x.z, add[u].z), fmaf(w, x.w, add[u].w)) : add[u];
+      x = h != -1 ? make_float4(fmaf(w, x.x, fmaf(wl, x.x, add[u].x)), fmaf(w, x.y, fmaf(wl, x.y, add[u].y)), fmaf(w, x.z, fmaf(wl, x.z, add[u].z)), fmaf(w, x.w, fmaf(wl, x.w, add[u].w)))
+                  : add[u];
       *reinterpret_cast<float4*>(p.cut_state + (size_t)(first + j - 1) * state + e) = x;
     }
   }

@@ -114,3 +114,22 @@ def test_long_sums_lose_no_more_than_short_ones(n, d):
     for h in range(4):
         T.near(ds[slot][h::4], R[h::4], size[h::4], es, "f32", f"gradient of the state, rate {float(-pr.g[h]):.2g}")
     assert rb.rom_get_status(pr.ws) == 0
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 148 * 256 - 128), ("f32", 296 * 256 - 32)])
+def test_a_slow_decay_over_every_cut(dtype, n):
+    """One head, cut as often as it can be, 256 rows from cut to cut, and a decay whose power of 256 lies half way between two floats: nothing but the first state, decayed.
+
+    A cut rounds each number once, 2^-24 of it at most and independent: at 296 cuts sqrt(296 / 3) 2^-24 = 2^-20.7 of the norm.  (One float for the power would be 2^-25 off at each cut,
+    the same way: 296 2^-25 = 2^-16.8.)"""
+    pr = Problem([n], 1, 1, 16, 16, dtype, seed=5, resume=[1], rates=[1.1230999916733708e-05], backward=True)
+    slot, full = int(pr.p.slots[0]), torch.exp(pr.g.double()[0] * n)
+    pr.k.zero_()
+    s = pr.run()[1][slot].double()
+    ref = full * pr.s_in[slot].double()
+    assert (s - ref).norm() <= 2.0 ** -20 * ref.norm()
+    pr.k.fill_(1.0)
+    pr.q.zero_()
+    ds = pr.run_backward()[3][slot].double()
+    ref = full * pr.ds_out[slot].double()
+    assert (ds - ref).norm() <= 2.0 ** -20 * ref.norm()
