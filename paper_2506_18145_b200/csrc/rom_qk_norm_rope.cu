@@ -68,15 +68,18 @@ struct QkLane {
     if (!has_b) ob = oa;
   }
 };
+// 1 / 2 pi, rounded to 64 bits, and what that left
+constexpr double INV_2PI = 0.15915494309189535, INV_2PI_LO = -9.839338337591243e-18;
 // cos and sin of rows [row0, row0 + n) of a block, [n][rot / 2].
 __device__ __forceinline__ void block_angles(const QkArgs& p, int row0, int n, float2* cs) {
   const int half = p.rot / 2;
   for (int i = threadIdx.x; i < n * half; i += QK_THREADS) {
     const int r = i / half, e = i - r * half;
-    double t = (double)__ldg(p.pos + row0 + r) * 0.15915494309189535 * (double)__ldg(p.inv_freq + e);
-    t -= rint(t);
+    // the product's 55 bits and 1 / 2 pi as two numbers each: with one, an angle of 2^31 was 4e-7 off, eight units of fp32
+    const double pos = (double)__ldg(p.pos + row0 + r), freq = (double)__ldg(p.inv_freq + e), a = pos * freq, a_lo = fma(pos, freq, -a);
+    const double t = a * INV_2PI, t_lo = fma(a, INV_2PI, -t) + fma(a, INV_2PI_LO, a_lo * INV_2PI);
     float s, c;
-    sincospif(2.0f * (float)t, &s, &c);
+    sincospif(2.0f * (float)((t - rint(t)) + t_lo), &s, &c);
     cs[i] = make_float2(c, s);
   }
 }

@@ -1,6 +1,12 @@
-"""Linear attention with a decay per head: what its documentation says of starts from zeros, of values that are not finite, of cuts."""
+"""Linear attention with a decay per head, and the rotation of its queries and keys: what their documentation says of starts from zeros, of values that are not finite, of far
+positions."""
+import math
+from fractions import Fraction
+
 import pytest
 import torch
+
+from paper_2506_18145_b200 import binding as rb
 
 import linattn_testlib as T
 from linattn_testlib import Problem
@@ -24,3 +30,31 @@ def test_without_initial_states_every_sequence_started_from_zeros(H, lens, dtype
         assert same_bits(a, b)
     for s in slots:
         assert (ds[s] == 0).all() and (ds_want[s] == 0).all()
+
+
+def turns(pos, freq):
+    """pos * freq in turns of a circle, less the whole ones, in rational arithmetic (pi to 60 places)."""
+    two_pi = 2 * Fraction(3141592653589793238462643383279502884197169399375105820974944, 10 ** 60)
+    t = Fraction(pos) * Fraction(freq) / two_pi
+    return float(t - round(t))
+
+
+@pytest.mark.parametrize("far", [5000, 2 ** 24, 2 ** 31 - 300])
+def test_angles_of_far_positions_are_those_of_the_exact_product(far):
+    """One in the first place of every pair, zero in the second: the pair's angle after the rotation is the position's.
+
+    In units of 2^-24: the turn as a float, half a step in [1/4, 1/2] 2^-26 times 2 pi: 1.6; sine and cosine, an ulp each, 1.5 together; product, sum and root of each, 2: 5.1."""
+    rows, d = 200, 128
+    cfg = rb.make_qk_config(1, 1, d, d, "f32")
+    x = torch.zeros((rows, d), device="cuda")
+    x[:, :d // 2] = 1.0
+    pos = torch.arange(far, far + rows, dtype=torch.int64).to(torch.int32)
+    freq = (10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) / 640)).float()      # (slowly falling: most of the angles are large)
+    q, k = torch.empty_like(x), torch.empty_like(x)
+    rb.rom_qk_norm_rope(cfg, x, x.clone(), None, None, pos.cuda(), freq.cuda(), q, k)
+    y = q.double().cpu()
+    got = torch.atan2(y[:, d // 2:], y[:, :d // 2]) / (2 * math.pi)
+    want = torch.tensor([[turns(p, f) for f in freq.tolist()] for p in pos.tolist()], dtype=torch.float64)
+    off = got - want
+    off = (off - torch.round(off)).abs() * 2 * math.pi
+    assert float(off.max()) <= 5.1 * 2.0 ** -24, f"{float(off.max()) * 2 ** 24:.2f} units"
