@@ -133,3 +133,54 @@ def test_a_slow_decay_over_every_cut(dtype, n):
     ds = pr.run_backward()[3][slot].double()
     ref = full * pr.ds_out[slot].double()
     assert (ds - ref).norm() <= 2.0 ** -20 * ref.norm()
+
+
+def on_places(got, ref, size, unit, store, places, what):
+    """`near`, elementwise, at the places that a value which is not finite does not reach."""
+    got, ref, tol = got.double()[places], ref[places], (unit * size * (1 + T.HALF_STEP[store]) + T.HALF_STEP[store] * ref.abs())[places] + 1e-37
+    assert torch.isfinite(got).all(), f"{what}: not finite at {int((~torch.isfinite(got)).sum())} places"
+    assert float(((got - ref).abs() / tol).max()) <= 1.0, f"{what}: {float(((got - ref).abs() / tol).max()):.2f} times the bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,dk,dv", [(4, 4, 64, 64), (4, 2, 128, 72), (6, 1, 40, 128)])
+@pytest.mark.parametrize("which,bad", [("v", float("nan")), ("v", float("inf")), ("k", float("-inf")), ("q", float("nan")), ("do", float("inf")), ("do", float("nan"))])
+@pytest.mark.parametrize("at", [173, 255])
+def test_rows_beside_one_that_is_not_finite_keep_their_bits(at, which, bad, H, G, dk, dv, dtype):
+    """One value of one row, in the middle or at the end of a chunk: what it does not reach is as exact as without it."""
+    n, head = 400, 1
+    pr = Problem([n, 150], H, G, dk, dv, dtype, seed=7, resume=[1, 0], backward=True)
+    group = head * G // H
+    place = 5
+    x = getattr(pr, which)
+    x[at, (head * dv if which in ("v", "do") else group * dk) + place] = 0.0
+    rows, q, k, v, do, S0, dS = pr.sequence(0)
+    ref, _ = T.forward(q, k, v, pr.g.double(), S0, pr.scale)
+    size, _ = T.forward(q.abs(), k.abs(), v.abs(), pr.g.double(), S0.abs(), abs(pr.scale))
+    gref = T.backward(do, q, k, v, pr.g.double(), S0, dS, pr.scale)
+    gsize = T.backward(do.abs(), q.abs(), k.abs(), v.abs(), pr.g.double(), S0.abs(), dS.abs(), abs(pr.scale))
+    x[at, (head * dv if which in ("v", "do") else group * dk) + place] = bad
+
+    row = torch.arange(n, device="cuda")[:, None, None]
+    heads = torch.arange(H, device="cuda")[None, :, None]
+    shared = heads * G // H == group              # value heads that read the group's q and k
+    groups = torch.arange(G, device="cuda")[None, :, None] == group
+    cv, ck = torch.arange(dv, device="cuda")[None, None, :] == place, torch.arange(dk, device="cuda")[None, None, :] == place
+    every_v, every_k = torch.ones_like(cv), torch.ones_like(ck)
+    none = torch.zeros((1, 1, 1), dtype=torch.bool, device="cuda")
+    mine = heads == head
+    reached = {      # o, dq, dk, dv: rows from or up to it, one column or all
+        "q": ((row == at) & shared & every_v, none, (row <= at) & groups & ck, (row <= at) & shared & every_v),
+        "k": ((row >= at) & shared & every_v, (row >= at) & groups & ck, none, (row == at) & shared & every_v),
+        "v": ((row >= at) & mine & cv, (row >= at) & groups & every_k, (row == at) & groups & every_k, none),
+        "do": (none, (row == at) & groups & every_k, (row <= at) & groups & every_k, (row <= at) & mine & cv)}[which]
+    parts = 2 * PARTS if dtype == "bf16" else 0.0
+    unit = T.units(n, max(dk, dv) + H // G, False)[0] + parts
+    o, _ = pr.run()
+    dq, dk_, dv_, _ = pr.run_backward()
+    for name, got, r, s, where in (("o", by_heads(o, rows, H), ref, size, reached[0]), ("dq", by_heads(dq, rows, G), gref[0], gsize[0], reached[1]),
+                                   ("dk", by_heads(dk_, rows, G), gref[1], gsize[1], reached[2]), ("dv", by_heads(dv_, rows, H), gref[2], gsize[2], reached[3])):
+        where = where.expand(r.shape)
+        on_places(got, r, s, unit, dtype, ~where, name)
+        assert not torch.isfinite(got.float()[where]).any(), f"{name}: finite where it cannot be"
+    assert rb.rom_get_status(pr.ws) == 0
