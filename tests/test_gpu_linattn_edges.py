@@ -58,3 +58,65 @@ def test_angles_of_far_positions_are_those_of_the_exact_product(far):
     off = got - want
     off = (off - torch.round(off)).abs() * 2 * math.pi
     assert float(off.max()) <= 5.1 * 2.0 ** -24, f"{float(off.max()) * 2 ** 24:.2f} units"
+
+
+def test_rows_beyond_32_bits_of_elements():
+    """One sequence behind 2^31 elements of v and of the results; what lies ahead of it belongs to nobody, and is neither read nor written."""
+    H, G, d, n, lead = 32, 16, 128, 200, 1 << 19
+    rows = lead + n
+    cfg = rb.make_linattn_config(H, G, d, d, "bf16")
+    gen = torch.Generator().manual_seed(2)
+
+    def tall(width):
+        x = torch.empty((rows, width), dtype=torch.bfloat16, device="cuda")
+        x[lead:] = torch.randn((n, width), generator=gen).bfloat16().cuda()
+        return x
+
+    q, k, v, do = tall(G * d), tall(G * d), tall(H * d), tall(H * d)
+    g = (-torch.logspace(-0.5, -3, H)).cuda()
+    start = torch.tensor([lead, rows], dtype=torch.int32, device="cuda")
+    seqs = rb.make_ragged(rows, 1, start)
+    ws = torch.empty(rb.linattn_backward_workspace_size(cfg, 1, rows), dtype=torch.uint8, device="cuda")
+    o, dq, dk, dv = tall(H * d), tall(G * d), tall(G * d), tall(H * d)
+    for x in (o, dq, dk, dv):
+        x[:300], x[lead - 300:lead] = -7.0, -7.0
+    s_out, ds_in = torch.empty((1, H, d, d), device="cuda"), torch.empty((1, H, d, d), device="cuda")
+    rb.rom_linattn_ragged(cfg, seqs, q, k, v, g, None, s_out, o, ws)
+    rb.rom_linattn_backward(cfg, seqs, do, q, k, v, g, None, None, dq, dk, dv, ds_in, ws)
+    assert rb.rom_get_status(ws) == 0
+    x = lambda t, m: t[lead:].double().view(n, m, d)  # noqa: E731
+    zero = torch.zeros((H, d, d), dtype=torch.float64, device="cuda")
+    scale = float(torch.tensor(cfg.scale, dtype=torch.float32))
+    ref, S = T.forward(x(q, G), x(k, G), x(v, H), g.double(), zero, scale)
+    size, Ssize = T.forward(x(q, G).abs(), x(k, G).abs(), x(v, H).abs(), g.double(), zero, scale)
+    eo, es = T.units(n, d + 2, True)
+    T.near(x(o, H), ref, size, eo, "bf16", "o")
+    T.near(s_out[0], S, Ssize, es, "f32", "state")
+    gref = T.backward(x(do, H), x(q, G), x(k, G), x(v, H), g.double(), zero, zero, scale)
+    gsize = T.backward(x(do, H).abs(), x(q, G).abs(), x(k, G).abs(), x(v, H).abs(), g.double(), zero, zero, scale)
+    for name, got, m, i in (("dq", dq, G, 0), ("dk", dk, G, 1), ("dv", dv, H, 2)):
+        T.near(x(got, m), gref[i], gsize[i], eo, "bf16", name)
+    assert (ds_in == 0).all()
+    for y in (o, dq, dk, dv):
+        assert (y[:300] == -7).all() and (y[lead - 300:lead] == -7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_calls_at_once(dtype):
+    """Two streams, a workspace each: what each call gives is what it gives alone."""
+    problems = [Problem([900, 333, 1, 64], 4, 2, 128, 64, dtype, seed=8, backward=True), Problem([2500], 2, 2, 128, 128, dtype, seed=9, backward=True)]
+    alone = [[*p.run(), *p.run_backward()] for p in problems]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in problems]
+    for _ in range(3):
+        got = []
+        for p, st in zip(problems, streams):
+            st.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(st):
+                got.append([*p.run(), *p.run_backward()])
+        torch.cuda.synchronize()
+        for a, b in zip(alone, got):
+            for x, y in zip(a, b):
+                assert same_bits(x, y)
+    for p in problems:
+        assert rb.rom_get_status(p.ws) == 0
