@@ -442,16 +442,16 @@ int most_runs(const rom_linattn_config& c, int n_seq, int rows) {      // with c
   const long long n = (long long)c.n_heads * units_per_head(s, n_seq, rows) / s.least;
   return (int)(n < 1 ? 1 : n < s.blocks ? n : s.blocks);
 }
-LinCut cut_rows(const rom_linattn_config& c, int n_seq, int rows) {
+LinCut cut_rows(const rom_linattn_config& c, int n_seq, int rows, bool backward) {
   const LinSlots s = slots_of(c);
   LinCut cut{s.chunk, s.start, units_per_head(s, n_seq, rows), c.n_heads, 0, false};
   cut.units = (long long)c.n_heads * cut.per_head;
   // A run inside one head starts once, and heads that are cut at the same rows read memory side by side: a whole number of runs a head, where that leaves no more than a
-  // fifth of the blocks out (8 sequences, 16384 rows, 32 heads of 128, backward: 503 us with 128 runs, 527 with 148; 23 prompts of 8186 rows, 32 heads of 64: 99 and 105; one
-  // prompt of 16384 rows, 32 heads of 128: 207 and 194, but its last state, most of it then the sums of launch 1 in tensor memory, 1.6e-6 of its norm off instead of 4e-7).
+  // fifth of the blocks out, for the backward (8 sequences, 16384 rows, 32 heads of 128: 503 us with 128 runs, 527 with 148) and for heads of 64, whose starts cost as much as
+  // several chunks (23 prompts of 8186 rows, 32 heads: 99 and 105).  Elsewhere every block has a run (one prompt of 16384 rows, 32 heads of 128: 207 with 128, 194 with 148).
   int n = most_runs(c, n_seq, rows);
   const int aligned = n / c.n_heads * c.n_heads;
-  if (aligned * 5 >= n * 4) n = aligned;
+  if ((backward || (c.d_k <= 64 && c.d_v <= 64)) && aligned * 5 >= n * 4) n = aligned;
   const double whole = (double)((c.n_heads + s.blocks - 1) / s.blocks) * cut.per_head, even = 1.6 * (double)cut.units / n + 6.0;
   if (even < whole) { cut.blocks = n; cut.inside = true; }
   return cut;
@@ -567,7 +567,7 @@ int rom_linattn_ragged(const rom_linattn_config* cfg, const rom_ragged* seqs, co
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
-  const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows);
+  const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows, false);
   LinPass p{};
   p.q = q; p.k = k; p.v = v; p.ldq = ldq; p.ldk = ldk; p.ldv = ldv;
   p.qdiv = p.kdiv = c.n_heads / c.n_qk_heads; p.vdiv = 1;
@@ -642,7 +642,7 @@ int rom_linattn_backward(const rom_linattn_config* cfg, const rom_ragged* seqs, 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LaunchCounter::count = 0;
   char* W = static_cast<char*>(ws);
-  const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows);
+  const LinCut cut = cut_rows(c, seqs->n_seq, seqs->rows, true);
   const int share = c.n_heads / c.n_qk_heads;
   float *part_q = share > 1 ? reinterpret_cast<float*>(W + lay.part_q) : nullptr, *part_k = share > 1 ? reinterpret_cast<float*>(W + lay.part_k) : nullptr;
   float* powers = reinterpret_cast<float*>(W + lay.powers);
