@@ -392,7 +392,8 @@ ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_
 
 /* ------------------------------------------------------------------------------------------------------------------------------
  * Linear attention with a decay for each head: the linear recurrence of Section 3.1 with a matrix state per head instead of d_state numbers per
- * channel (Section 5.2: other linear recurrent architectures).  Per value head h,
+ * channel, and a decay that is the head's alone.  (The architectures that Section 5.2 names, Mamba2 and Gated DeltaNet, decay by the token: they are not
+ * this.)  Per value head h,
  *   S_t = lambda_h S_{t-1} + k_t v_t^T   [d_k, d_v],     o_t = scale * q_t S_t,     lambda_h = exp(log_decay[h]).
  * Value head h uses head h / (n_heads / n_qk_heads) of q and k.  Values wider than d_v = 128 are several heads that share q and k and their decay.
  *   q, k : [rows, n_qk_heads, d_k] dtype, pitches ldq, ldk;   v : [rows, n_heads, d_v] dtype, pitch ldv;   o : [rows, n_heads, d_v] dtype, contiguous;
@@ -403,7 +404,7 @@ ROM_API int rom_ffn_moe_step(const rom_config *cfg, int32_t d_ff, const void *W_
  * of two bf16 numbers (less than 2^-15 of each left out), and so are the keys in the backward's states, which only dq and dk meet; the keys that enter a state
  * that is a result are the sum of three, which are all of their bits.  A sum in the matrix instructions, which drop what is below its last bit, moves to fp32
  * registers after 512 rows at most, so that a state's error does not grow with its sequence (6e-7 of its norm measured, without decay).
- * A value that is not finite shows in its own row and later ones of its sequence and head, in earlier rows never. */
+ * A value that is not finite shows in its own row and later ones of its sequence and head, as infinity or NaN, in earlier rows never. */
 typedef struct {
   int32_t n_heads;            /* value heads, 1..1024: one state and one decay each                            */
   int32_t n_qk_heads;         /* heads of q and k, a divisor of n_heads                                        */

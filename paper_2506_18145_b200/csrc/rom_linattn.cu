@@ -447,8 +447,8 @@ LinCut cut_rows(const rom_linattn_config& c, int n_seq, int rows, bool backward)
   LinCut cut{s.chunk, s.start, units_per_head(s, n_seq, rows), c.n_heads, 0, false};
   cut.units = (long long)c.n_heads * cut.per_head;
   // A run inside one head starts once, and heads that are cut at the same rows read memory side by side: a whole number of runs a head, where that leaves no more than a
-  // fifth of the blocks out, for the backward (8 sequences, 16384 rows, 32 heads of 128: 503 us with 128 runs, 527 with 148) and for heads of 64, whose starts cost as much as
-  // several chunks (23 prompts of 8186 rows, 32 heads: 99 and 105).  Elsewhere every block has a run (one prompt of 16384 rows, 32 heads of 128: 207 with 128, 194 with 148).
+  // fifth of the blocks out, for the backward (8 sequences, 16384 rows, 32 heads of 128: 565 us with 128 runs, 586 with 148) and for heads of 64, whose starts cost as much as
+  // several chunks (23 prompts of 8186 rows, 32 heads: 100 and 109).  Elsewhere every block has a run (32 heads of 128, one prompt of 16384 rows: 221 with 128, 213 with 148; 12 of 8192: 130 and 123).
   int n = most_runs(c, n_seq, rows);
   const int aligned = n / c.n_heads * c.n_heads;
   if ((backward || (c.d_k <= 64 && c.d_v <= 64)) && aligned * 5 >= n * 4) n = aligned;
@@ -482,8 +482,8 @@ int lin_ws_size(const rom_linattn_config* c, int32_t n_seq, int32_t rows, size_t
 }
 
 // Sequences of one row (continuous batching) in a launch of their own, where they may be many: fewer than 256 rows a sequence on average.  A walk takes 3 to 5 us for each of a
-// run's in turn (256 sequences of 1200 rows, 32 heads of 128 bf16: 512 us a call, with this launch 324; 64 of 300, 8 heads of 64: 37.5 and 34.5); with few of them the launch costs its
-// 2 us (37 of 531 rows, 8 heads of 64 fp32: 46 and 48).
+// run's in turn (256 sequences of 1200 rows, 32 heads of 128 bf16: 485 us a call, with this launch 320; 64 of 300, 8 heads of 64: 37.3 and 35); with few of them the launch costs its
+// 2 us (37 of 531 rows, 8 heads of 64 fp32: 46 and 47.3).
 bool singles_apart(const rom_linattn_config& c, const rom_ragged& seqs) {
   return seqs.n_seq > 1 && (long long)seqs.rows < 256LL * seqs.n_seq && (long long)seqs.n_seq * c.n_heads * ((c.d_v + STEP_COLS - 1) / STEP_COLS) <= INT32_MAX;
 }

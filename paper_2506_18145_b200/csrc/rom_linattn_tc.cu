@@ -7,7 +7,8 @@
 //
 // Roundings: P and the S that a chunk meets are the sum of two bf16 numbers each, in two matrix products, which leaves out less than 2^-15 of a number: as one bf16 number each
 // they made outputs 2.35e-3 of their norm off 64 bits, where the outputs' own rounding makes 1.66e-3.  K~ is the sum of three bf16 numbers, in three matrix products: all 24 bits of
-// the fp32 product, since the state is an fp32 result that many chunks add up in (two, rounded, left 2.5e-6 of its norm where fp32 sums leave 2e-7; the third costs 10 % of a walk).
+// the fp32 product, since the state is an fp32 result that many chunks add up in (two left 4.9e-6 of its norm where fp32 sums leave 2e-7; 16384 rows of 32 heads of
+// 128 take 211 us with three, 199 with two).
 // Two where the state is no result but only read in two parts by dq or dk.  S itself stays in fp32 registers, one column of S^T's rows per thread; lambda^128 is two floats.
 //
 // One CTA per SM walks one run of chunks.  640 threads: warp 0 issues the copies (TMA boxes of 64 columns x 128 rows, zeros beyond a head's
@@ -771,9 +772,9 @@ lin_walk3_tc(const __grid_constant__ WalkArgs dq, const __grid_constant__ WalkAr
 // add up in tensor memory, in steps of 64 rows: the first parts of K~ in one accumulator, the small ones in another, which the two products of V with K~'s first and second part
 // fill as one of twice the width (in one accumulator for all of them the state was off by three times as much).  Every product of 16 rows drops what is below the accumulator's last bit,
 // which is the same way each time: the error of one sum grows with its rows.  After 512 rows the sum moves to fp32 registers, which round to nearest, while the next 512 add up in
-// another pair (16384 rows of 32 heads without decay, in
-// one sum of 4096 rows: the last state 3.8e-6 of its norm off, 131072 rows 3.2e-5; so 4.4e-7 and 5.6e-7, for 3 us of 217 of the call at 16384 rows of 32 heads of 128).  Sixteen warps scale K, eight threads to a row (eight warps: 209.6 us for the whole call at 16384 rows of 32 heads of 128 x 128, sixteen: 207).  What bounds it: shared memory, 176 KB of
-// copies, operands and K~ a step of 128 x 128, 1400 cycles of the 2100 that a step takes; from DRAM it asks for 4 TB/s.
+// another pair (32 heads without decay, runs of 4096 rows in one sum: the last state 3.8e-6 of its norm off, of 32768 rows 3.2e-5; so 4.4e-7 and 5.6e-7, for 3 us of a call of 217).
+// Sixteen warps scale K, eight threads to a row (eight warps are as fast).  What bounds it: shared memory, 176 KB of copies, operands and K~ a step of 128 x 128, 1400 cycles of the
+// 2000 that a step takes (the tensor pipe is busy for 41 % of them); from DRAM it asks for 4 TB/s.
 template <int KP, int VP>
 struct StateShape {
   static constexpr int KB = KP / 64, VB = VP / 64, ROWS = 64, BOX = 64 * ROWS * 2;

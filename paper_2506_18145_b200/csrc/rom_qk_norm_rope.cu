@@ -1,7 +1,7 @@
 // RMS norm of every head of q and k and its rotation by the row's position, in one pass, and the backward of both.
 //
 // Eight lanes (fewer or more by the head's width) own a head of one row: each holds two runs of eight places, the two halves of eight pairs in the rotated part,
-// sixteen adjacent places behind it.  The angle pos * inv_freq is formed in 64 bits and reduced to a turn before it is rounded: an fp32 product is off by 0.06 at a position
+// sixteen adjacent places behind it.  The angle pos * inv_freq is formed in two numbers of 64 bits and reduced to a turn before it is rounded: an fp32 product is off by 0.06 at a position
 // of a million.  A block takes the sines and cosines of its rows once, into shared memory; a group of lanes folds them and the weights into two factors a place for the
 // heads of a row that it works on, with several heads' loads in flight.
 //
