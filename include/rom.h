@@ -448,6 +448,7 @@ ROM_API int rom_linattn_backward(const rom_linattn_config *cfg, const rom_ragged
  *   input (same address and pitch), otherwise no output overlaps an input;
  *   w_q, w_k : [d_head] fp32, or NULL (ones);  pos : [rows] int32;  inv_freq : [rot_dim/2] fp32 (both NULL when rot_dim is 0).
  * The angle is the exact product of the two, reduced before it is rounded: positions up to 2^31 keep fp32 accuracy.  Norm and rotation are fp32, rounded once.
+ * A value that is not finite may show in every place of its head in its row (and of its kind's dw in the backward), in no other row or head.
  * Pitches as above; w, pos and inv_freq need the alignment of their elements, everything else 16 bytes.                  */
 typedef struct {
   int32_t n_q_heads, n_k_heads;   /* 1..1024                                                      */

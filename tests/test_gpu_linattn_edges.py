@@ -120,3 +120,32 @@ def test_two_calls_at_once(dtype):
                 assert same_bits(x, y)
     for p in problems:
         assert rb.rom_get_status(p.ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot,interleaved", [(128, 128, False), (96, 48, True), (40, 16, False)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_norm_of_a_value_that_is_not_finite_stays_in_its_head_and_row(bad, d, rot, interleaved, dtype):
+    rows, nq, nk = 37, 5, 2
+    gen = torch.Generator().manual_seed(d)
+    cfg = rb.make_qk_config(nq, nk, d, rot, dtype, interleaved=interleaved)
+    new = lambda n: torch.randn((rows, n * d), generator=gen).to(T.TORCH[dtype]).cuda()  # noqa: E731
+    q, k, gq, gk, w = new(nq), new(nk), new(nq), new(nk), torch.rand(d, generator=gen).cuda()
+    pos, freq = torch.arange(rows, dtype=torch.int32, device="cuda"), torch.rand(rot // 2, generator=gen).cuda()
+    ws = torch.empty(rb.qk_norm_rope_backward_workspace_size(cfg, rows), dtype=torch.uint8, device="cuda")
+
+    def both():
+        y = [torch.empty_like(q), torch.empty_like(k)]
+        rb.rom_qk_norm_rope(cfg, q, k, w, w, pos, freq, *y)
+        dx, dw = [torch.empty_like(q), torch.empty_like(k)], [torch.empty(d, device="cuda"), torch.empty(d, device="cuda")]
+        rb.rom_qk_norm_rope_backward(cfg, gq, gk, q, k, w, w, pos, freq, *dx, *dw, ws)
+        return y, dx, dw
+
+    (y, dx, dw) = both()
+    q[20, 3 * d + d - 1] = bad
+    (y2, dx2, dw2) = both()
+    assert same_bits(y[1], y2[1]) and same_bits(dx[1], dx2[1]) and same_bits(dw[1], dw2[1])
+    for a, b in ((y[0], y2[0]), (dx[0], dx2[0])):
+        other = torch.ones((rows, nq), dtype=torch.bool, device="cuda")
+        other[20, 3] = False
+        assert same_bits(a.view(rows, nq, d)[other], b.view(rows, nq, d)[other]) and not torch.isfinite(b.view(rows, nq, d)[20, 3, d - 1].float())
